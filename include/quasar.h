@@ -45,7 +45,8 @@ typedef enum quasar_status {
     QUASAR_ERR_HIP = 6         /* the HIP runtime reported an error at launch */
 } quasar_status;
 
-typedef enum quasar_dtype { QUASAR_F32 = 0, QUASAR_BF16 = 1 } quasar_dtype;
+/* QUASAR_E4M3 (8-bit floating point, largest finite value 448): pages of a paged cache only. */
+typedef enum quasar_dtype { QUASAR_F32 = 0, QUASAR_BF16 = 1, QUASAR_E4M3 = 2 } quasar_dtype;
 
 /* Contraction variant used by quasar_w8_linear (for A/B measurements). */
 typedef enum quasar_path {
@@ -513,6 +514,89 @@ size_t quasar_attention_workspace_bytes(int64_t M, int64_t n_q_heads, int64_t n_
 int quasar_verify_attention(const uint16_t *q, int64_t M, int64_t ldq, int64_t n_q_heads, int64_t n_kv_heads,
                             const void *kv_cache, int64_t max_len, int64_t L_total,
                             uint16_t *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
+ * ---- A batch of sequences over a paged key/value cache (Sec. 3.1: the positions of a step are verified in one forward pass;
+ * here of several sequences at once, and of their prompts; the attention is the target model's own, as above: grouped-query,
+ * causal, head dimension 128) ----
+ *
+ * Pages.  A page holds page_len positions (32, 64, 128, 256, 512 or 1024) of every kv head.  The pool of a cache is ONE device buffer of
+ * quasar_paged_cache_bytes, 16-byte aligned, [layer][page][kv head][page_len / 32][keys | values][32 x 128], each block of 32 positions in
+ * matrix-core operand order:
+ *   QUASAR_BF16   keys   [p / 16][d / 32][d % 32 / 8][p % 16][d % 8],   values [d / 16][p % 16 / 4][d % 16][p / 16][p % 4]
+ *   QUASAR_E4M3   keys   [p / 16][d / 64][d % 32 / 8][p % 16][d / 32 % 2][d % 8],
+ *                 values [d / 32][p % 16 / 4][d % 16][d / 16 % 2][p / 16][p % 4]            (p = position % 32)
+ * An e4m3 code stands for code * scale of its kv head: k_scale, v_scale are device [n_kv_heads] fp32, > 0, or NULL for 1 (NULL for bf16
+ * pages); choosing them is not part of this library.  The pool need not be initialised.
+ *
+ * Books, all device int32, never read by the host, so that a step whose accepted lengths only the device knows goes on without
+ * waiting, and may be captured into a graph:
+ *   table    [n_seqs, max_pages], row stride table_ld >= max_pages: the pages of a sequence, one for each page_len positions; -1 none
+ *   lengths  [n_seqs]: cached positions L, the new rows of a call not counted; 0 <= L <= 2^24
+ *   refs     [n_pages]: rows of the table that hold a page; 0 = free (start with all 0).  A caller that keeps a page beyond its
+ *            sequences (a common prompt) adds one
+ *   row_start [n_seqs + 1]: rows row_start[s] .. row_start[s + 1] - 1 of the packed tensors are the new tokens of sequence s, at positions
+ *            lengths[s] onwards; not decreasing; sequences may have none.  Rows ahead of the first and behind the last sequence are left as
+ *            they were
+ * 1 <= n_seqs <= 1024, max_pages * page_len <= 2^24, n_pages <= 2^20.  Books that break these rules (a page id or row beyond its buffer, a
+ * length beyond the table) give unspecified values, but nothing outside the buffers is read or written: positions without a page are
+ * not visible and are not written, sequences whose rows do not fit have none.
+ * Order of a step: quasar_pages_reserve, then per layer quasar_paged_prepare and quasar_paged_attention (quasar_prompt_attention), then
+ * the caller adds the accepted tokens to lengths.
+ */
+size_t quasar_paged_cache_bytes(int64_t n_layers, int64_t n_kv_heads, int64_t n_pages, int64_t page_len, int kv_dtype);   /* 0 on invalid arguments */
+
+/* quasar_attn_prepare for the packed rows of a batch: qkv [T, (n_q_heads + 2 n_kv_heads) * 128] bf16 (16-byte aligned, ld a multiple
+ * of 8), q_out [T, n_q_heads * 128] (likewise).  `pages`: the layer's part of the pool.  Queries and keys are normalised and rotated
+ * with the roundings of quasar_attn_prepare; e4m3 pages take e4m3( clamp( that bf16 value / scale, -448, 448 ) ), an fp32 division,
+ * to nearest even.  The pages must be there (quasar_pages_reserve) and held by no other sequence. */
+int quasar_paged_prepare(const uint16_t *qkv, int64_t T, int64_t ld, int64_t n_q_heads, int64_t n_kv_heads, const int32_t *row_start,
+                         int64_t n_seqs, const uint16_t *q_gamma, const uint16_t *k_gamma, float eps, float rope_theta, uint16_t *q_out,
+                         int64_t ldq, void *pages, int64_t n_pages, int64_t page_len, int kv_dtype, const float *k_scale, const float *v_scale,
+                         const int32_t *table, int64_t table_ld, int64_t max_pages, const int32_t *lengths, void *hip_stream);
+
+/* quasar_verify_attention for a batch: row i of sequence s sees positions 0 .. lengths[s] + i; rows that see nothing give 0.  For the new
+ * tokens of a step: at most max_new <= 32 a sequence (a sequence with more has rows beyond that left as they were), and
+ * max_new * n_q_heads / n_kv_heads <= 1024.  Work is shared by cached positions, not by sequences: ragged lengths cost no more than even ones.
+ * workspace: quasar_paged_attention_workspace_bytes.  q 16-byte, out 8-byte aligned; ldq a multiple of 8, ldo of 4.  Two launches. */
+size_t quasar_paged_attention_workspace_bytes(int64_t max_new, int64_t n_q_heads, int64_t n_kv_heads);   /* 0 on invalid arguments */
+int quasar_paged_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n_q_heads, int64_t n_kv_heads, const int32_t *row_start,
+                           int64_t n_seqs, int64_t max_new, const void *pages, int64_t n_pages, int64_t page_len, int kv_dtype,
+                           const float *k_scale, const float *v_scale, const int32_t *table, int64_t table_ld, int64_t max_pages,
+                           const int32_t *lengths, uint16_t *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/* The same attention for whole prompts, or chunks of them behind what is cached: any number of rows a sequence
+ * (T * n_q_heads / n_kv_heads <= 2^26), one launch. */
+int quasar_prompt_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n_q_heads, int64_t n_kv_heads, const int32_t *row_start,
+                            int64_t n_seqs, const void *pages, int64_t n_pages, int64_t page_len, int kv_dtype, const float *k_scale,
+                            const float *v_scale, const int32_t *table, int64_t table_ld, int64_t max_pages, const int32_t *lengths,
+                            uint16_t *out, int64_t ldo, void *hip_stream);
+
+/*
+ * The books.  Each result is determined by the arguments alone: of the free pages (refs 0) the lowest are taken first, in the order of
+ * sequences and, within one, of positions.  workspace: quasar_pages_workspace_bytes (scratch).
+ *
+ * quasar_pages_reserve  pages for positions lengths[s] .. lengths[s] + n_new[s] - 1 of every sequence (n_new[s] <= 0: nothing asked).  Columns of
+ *   the table from lengths[s] / page_len on that are -1 get free pages.  If the first of them already holds positions (lengths[s] not a multiple
+ *   of page_len) and its page is held elsewhere too, it is replaced by a copy, of all layers, of the blocks of 32 positions that hold any:
+ *   the holders that write in this call take copies in order, and the last holder keeps the page.  (Pages without positions are never
+ *   shared: quasar_pages_fork shares none.)  out_status[s]: 1, or 0 for a sequence that is left as it was, because its row of the table is
+ *   too short, or because it is the first that finds too few free pages, or is behind that one.  Two launches.
+ * quasar_pages_fork     a gather over the rows of the table: sequence s becomes sequence parent[s] as it was before the call, cut to keep[s] positions
+ *   (keep may be NULL: not cut; fewer than 0 count as 0), with the pages that hold positions and no others.  parent[s] = s keeps (or cuts) it,
+ *   another one forks or moves it, -1 (or anything that is no row) frees it.  refs follow.  No page is copied.  Two launches.
+ * quasar_pages_compact  with n pages in use (refs > 0), the i-th in use at n and beyond moves, in all layers, to the i-th free page below n; table
+ *   and refs follow; out_to [n_pages] says where each page went (pages that did not move: themselves).  Two launches.
+ */
+size_t quasar_pages_workspace_bytes(int64_t n_seqs, int64_t n_pages);   /* 0 on invalid arguments */
+int quasar_pages_reserve(int32_t *table, int64_t table_ld, int64_t n_seqs, int64_t max_pages, const int32_t *lengths, const int32_t *n_new,
+                         int32_t *refs, int64_t n_pages, int64_t page_len, int32_t *out_status, void *pool, int64_t n_layers,
+                         int64_t n_kv_heads, int kv_dtype, void *workspace, size_t workspace_bytes, void *hip_stream);
+int quasar_pages_fork(int32_t *table, int64_t table_ld, int64_t n_seqs, int64_t max_pages, int32_t *lengths, const int32_t *parent,
+                      const int32_t *keep, int32_t *refs, int64_t n_pages, int64_t page_len, void *hip_stream);
+int quasar_pages_compact(int32_t *table, int64_t table_ld, int64_t n_seqs, int64_t max_pages, int32_t *refs, int64_t n_pages,
+                         int64_t page_len, int32_t *out_to, void *pool, int64_t n_layers, int64_t n_kv_heads, int kv_dtype,
+                         void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
  * ---- Prompt-lookup n-gram drafter (Sec. 2: drafts by n-gram matching against the context;

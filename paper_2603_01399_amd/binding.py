@@ -15,7 +15,7 @@ import torch  # imported first so that the library binds to the HIP runtime torc
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libquasar.so")
 
-F32, BF16 = 0, 1
+F32, BF16, E4M3 = 0, 1, 2
 PATH_AUTO, PATH_VALU, PATH_MFMA = 0, 1, 2
 
 # every symbol declared in include/quasar.h
@@ -39,6 +39,8 @@ EXPORTS = (
     "quasar_w8_gateup_workspace_bytes", "quasar_w8_gateup_swiglu_split",
     "quasar_kv_cache_bytes", "quasar_kv_cache_fill", "quasar_attn_prepare", "quasar_attention_workspace_bytes",
     "quasar_verify_attention",
+    "quasar_paged_cache_bytes", "quasar_paged_prepare", "quasar_paged_attention_workspace_bytes", "quasar_paged_attention",
+    "quasar_prompt_attention", "quasar_pages_workspace_bytes", "quasar_pages_reserve", "quasar_pages_fork", "quasar_pages_compact",
 )
 
 
@@ -134,6 +136,19 @@ def _load() -> ctypes.CDLL:
     lib.quasar_attention_workspace_bytes.argtypes = [i64, i64, i64, i64]
     lib.quasar_attention_workspace_bytes.restype = sz
     lib.quasar_verify_attention.argtypes = [vp, i64, i64, i64, i64, vp, i64, i64, vp, i64, vp, sz, vp]
+    lib.quasar_paged_cache_bytes.argtypes = [i64, i64, i64, i64, ci]
+    lib.quasar_paged_cache_bytes.restype = sz
+    paged = [vp, i64, i64, ci, vp, vp, vp, i64, i64, vp]          # pages, n_pages, page_len, dtype, scales, table, table_ld, max_pages, lengths
+    lib.quasar_paged_prepare.argtypes = [vp, i64, i64, i64, i64, vp, i64, vp, vp, ctypes.c_float, ctypes.c_float, vp, i64, *paged, vp]
+    lib.quasar_paged_attention_workspace_bytes.argtypes = [i64, i64, i64]
+    lib.quasar_paged_attention_workspace_bytes.restype = sz
+    lib.quasar_paged_attention.argtypes = [vp, i64, i64, i64, i64, vp, i64, i64, *paged, vp, i64, vp, sz, vp]
+    lib.quasar_prompt_attention.argtypes = [vp, i64, i64, i64, i64, vp, i64, *paged, vp, i64, vp]
+    lib.quasar_pages_workspace_bytes.argtypes = [i64, i64]
+    lib.quasar_pages_workspace_bytes.restype = sz
+    lib.quasar_pages_reserve.argtypes = [vp, i64, i64, i64, vp, vp, vp, i64, i64, vp, vp, i64, i64, ci, vp, sz, vp]
+    lib.quasar_pages_fork.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, i64, i64, vp]
+    lib.quasar_pages_compact.argtypes = [vp, i64, i64, i64, vp, i64, i64, vp, vp, i64, i64, ci, vp, sz, vp]
     lib.quasar_drafter_create.argtypes = [ci, ci, i64]
     lib.quasar_drafter_create.restype = vp
     lib.quasar_drafter_destroy.argtypes = [vp]
@@ -630,6 +645,176 @@ def verify_attention(q: torch.Tensor, n_q_heads: int, cache: KvCache, L_total: i
            _lib.quasar_verify_attention(_ptr(q), M, q.stride(0), n_q_heads, cache.n_kv_heads, _ptr(cache.buf),
                                         cache.max_len, L_total, _ptr(out), out.stride(0), _ptr(workspace),
                                         workspace.nbytes, _stream()))
+    return out
+
+
+class PagedKvCache:
+    """Key/value cache of a batch of sequences in pages (head dimension 128): the pool of all layers and the books.
+
+    Everything is device memory, and the methods wait for nothing: `refs` [n_pages], `lengths` [max_seqs] and `table`
+    [max_seqs, max_pages] (int32) are the caller's to read and, for lengths, to advance after a step
+    (cache.lengths += accepted).  dtype: torch.bfloat16, or torch.float8_e4m3fn with k_scale, v_scale [n_layers, n_kv_heads] fp32 (or
+    None for 1).  pool, books: the buffers, where the caller has them (books: refs | lengths | table in one int32 tensor).
+    """
+
+    def __init__(self, n_layers: int, n_kv_heads: int, n_pages: int, *, page_len: int = 64, max_seqs: int = 1, max_pages: int = None,
+                 dtype: torch.dtype = torch.bfloat16, k_scale: torch.Tensor = None, v_scale: torch.Tensor = None, device="cuda",
+                 pool: torch.Tensor = None, books: torch.Tensor = None):
+        code = {torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}.get(dtype)
+        if code is None:
+            raise TypeError("dtype must be torch.bfloat16 or torch.float8_e4m3fn")
+        max_pages = n_pages if max_pages is None else max_pages
+        if not _lib.quasar_paged_cache_bytes(n_layers, n_kv_heads, n_pages, page_len, code) or not _lib.quasar_pages_workspace_bytes(max_seqs, n_pages) \
+                or max_pages < 1 or max_pages * page_len > 1 << 24:
+            raise ValueError("invalid cache shape")
+        shape, n_books = (n_layers, n_pages, n_kv_heads, page_len // 32, 2, 32 * 128), n_pages + max_seqs + max_seqs * max_pages
+        if pool is None:
+            pool = torch.empty(shape, dtype=dtype, device=device)
+        elif _dev(pool, "pool", dtype).shape != shape or not pool.is_contiguous():
+            raise ValueError(f"pool must be a contiguous tensor of shape {shape}")
+        if books is None:
+            books = torch.zeros(n_books, dtype=torch.int32, device=pool.device)
+            books[n_pages + max_seqs:] = -1
+        elif _dev(books, "books", torch.int32).numel() != n_books or not books.is_contiguous() or books.device != pool.device:
+            raise ValueError(f"books must be a contiguous tensor of {n_books} elements beside the pool")
+        for name, scale in (("k_scale", k_scale), ("v_scale", v_scale)):
+            if scale is None:
+                continue
+            _dev(scale, name, torch.float32)
+            if code != E4M3 or scale.shape != (n_layers, n_kv_heads) or not scale.is_contiguous() or scale.device != pool.device:
+                raise ValueError(f"{name} must be a contiguous [n_layers, n_kv_heads] tensor, of a cache of 8-bit pages")
+        self.n_layers, self.n_kv_heads, self.n_pages, self.page_len = n_layers, n_kv_heads, n_pages, page_len
+        self.max_seqs, self.max_pages, self.dtype, self.k_scale, self.v_scale, self.pool, self.books = max_seqs, max_pages, dtype, k_scale, v_scale, pool, books
+        self.refs = books[:n_pages]
+        self.lengths = books[n_pages:n_pages + max_seqs]
+        self.table = books[n_pages + max_seqs:].view(max_seqs, max_pages)
+        # what the calls pass on: addresses and sizes of buffers that this object holds
+        self._code = code
+        self._refs, self._lengths, self._table = self.refs.data_ptr(), self.lengths.data_ptr(), self.table.data_ptr()
+        self._layer_bytes = pool.nbytes // n_layers
+        self._workspace_bytes = _lib.quasar_pages_workspace_bytes(max_seqs, n_pages)
+
+    def _layer(self, layer: int):
+        if not 0 <= layer < self.n_layers:
+            raise ValueError(f"layer must be in 0 .. {self.n_layers - 1}")
+        at = 4 * self.n_kv_heads * layer
+        return (self.pool.data_ptr() + layer * self._layer_bytes, self.n_pages, self.page_len, self._code,
+                None if self.k_scale is None else self.k_scale.data_ptr() + at, None if self.v_scale is None else self.v_scale.data_ptr() + at,
+                self._table, self.max_pages, self.max_pages, self._lengths)
+
+    def _per_sequence(self, t, name):
+        _dev(t, name, torch.int32)
+        if t.shape != (self.max_seqs,) or not t.is_contiguous():
+            raise ValueError(f"{name} must be a contiguous [max_seqs] vector")
+        _beside(t, name, self.pool)
+        return t.data_ptr()
+
+    def reserve(self, n_new: torch.Tensor) -> torch.Tensor:
+        """Pages for n_new [max_seqs] further positions of each sequence; a shared last page is replaced by a copy.
+        -> int32 [max_seqs]: 1, or 0 for a sequence that found too few pages and is as it was."""
+        new = self._per_sequence(n_new, "n_new")
+        status = torch.empty(self.max_seqs, dtype=torch.int32, device=self.pool.device)
+        ws = torch.empty(self._workspace_bytes, dtype=torch.uint8, device=self.pool.device)
+        _check("quasar_pages_reserve",
+               _lib.quasar_pages_reserve(self._table, self.max_pages, self.max_seqs, self.max_pages, self._lengths, new, self._refs, self.n_pages,
+                                         self.page_len, status.data_ptr(), self.pool.data_ptr(), self.n_layers, self.n_kv_heads, self._code,
+                                         ws.data_ptr(), self._workspace_bytes, _stream()))
+        return status
+
+    def fork(self, parent: torch.Tensor, keep: torch.Tensor = None) -> None:
+        """Sequence s becomes sequence parent[s] as it was, cut to keep[s] positions (None: not cut); parent -1 frees it."""
+        _check("quasar_pages_fork",
+               _lib.quasar_pages_fork(self._table, self.max_pages, self.max_seqs, self.max_pages, self._lengths, self._per_sequence(parent, "parent"),
+                                      None if keep is None else self._per_sequence(keep, "keep"), self._refs, self.n_pages, self.page_len,
+                                      _stream()))
+
+    def compact(self) -> torch.Tensor:
+        """Moves the pages in use together at the beginning of the pool.  -> int32 [n_pages]: where each page went."""
+        _beside(self.books, "the cache", self.pool)
+        to = torch.empty(self.n_pages, dtype=torch.int32, device=self.pool.device)
+        ws = torch.empty(self._workspace_bytes, dtype=torch.uint8, device=self.pool.device)
+        _check("quasar_pages_compact",
+               _lib.quasar_pages_compact(self._table, self.max_pages, self.max_seqs, self.max_pages, self._refs, self.n_pages, self.page_len,
+                                         to.data_ptr(), self.pool.data_ptr(), self.n_layers, self.n_kv_heads, self._code, ws.data_ptr(),
+                                         self._workspace_bytes, _stream()))
+        return to
+
+
+def _beside(t, name, pool):
+    """The launch goes to the current device and its current stream: everything a call touches is there."""
+    if t.device != pool.device or pool.device.index != _current_device():
+        raise ValueError(f"{name} and the cache must be on the current device")
+
+
+def _rows_of(x, width, name, cache):
+    _dev(x, name, torch.bfloat16)
+    if x.dim() != 2 or x.shape[1] != width or (x.stride(1) != 1 and x.shape[1] != 1):
+        raise ValueError(f"{name} must be [rows, {width}] with a contiguous last dimension")
+    _beside(x, name, cache.pool)
+    # (torch gives a tensor of one row any stride)
+    return x.shape[0], x.stride(0) if x.shape[0] > 1 else width
+
+
+def _row_start_of(row_start, cache):
+    _dev(row_start, "row_start", torch.int32)
+    if row_start.dim() != 1 or not 2 <= row_start.numel() <= cache.max_seqs + 1 or not row_start.is_contiguous():
+        raise ValueError("row_start must be a contiguous vector of at most max_seqs + 1 elements")
+    _beside(row_start, "row_start", cache.pool)
+    return row_start.data_ptr(), row_start.numel() - 1
+
+
+def _output_like(out, rows, width, cache, name):
+    if out is None:
+        return torch.empty((rows, width), dtype=torch.bfloat16, device=cache.pool.device), width
+    n, ld = _rows_of(out, width, name, cache)
+    if n != rows:
+        raise ValueError(f"{name} must have {rows} rows")
+    return out, ld
+
+
+def paged_prepare(qkv: torch.Tensor, n_q_heads: int, cache: PagedKvCache, layer: int, row_start: torch.Tensor, q_gamma: torch.Tensor,
+                  k_gamma: torch.Tensor, eps: float = 1e-6, rope_theta: float = 1.0e6, q_out: torch.Tensor = None) -> torch.Tensor:
+    """attn_prepare for the packed rows of a batch: row_start [sequences + 1], positions from cache.lengths on."""
+    rows, ld = _rows_of(qkv, (n_q_heads + 2 * cache.n_kv_heads) * 128, "qkv", cache)
+    starts, n_seqs = _row_start_of(row_start, cache)
+    for name, gamma in (("q_gamma", q_gamma), ("k_gamma", k_gamma)):
+        _gamma_arg(gamma, 128) if gamma is not None else _dev(gamma, name)
+        _beside(gamma, name, cache.pool)
+    q_out, ldq = _output_like(q_out, rows, n_q_heads * 128, cache, "q_out")
+    if rows:
+        _check("quasar_paged_prepare",
+               _lib.quasar_paged_prepare(qkv.data_ptr(), rows, ld, n_q_heads, cache.n_kv_heads, starts, n_seqs, q_gamma.data_ptr(), k_gamma.data_ptr(),
+                                         eps, rope_theta, q_out.data_ptr(), ldq, *cache._layer(layer), _stream()))
+    return q_out
+
+
+def paged_attention(q: torch.Tensor, n_q_heads: int, cache: PagedKvCache, layer: int, row_start: torch.Tensor, max_new: int,
+                    workspace: torch.Tensor = None, out: torch.Tensor = None) -> torch.Tensor:
+    """Attention of the new tokens of a step, at most max_new (1 .. 32) a sequence, over their sequences' pages."""
+    rows, ldq = _rows_of(q, n_q_heads * 128, "q", cache)
+    starts, n_seqs = _row_start_of(row_start, cache)
+    out, ldo = _output_like(out, rows, n_q_heads * 128, cache, "out")
+    if workspace is None:
+        workspace = torch.empty(max(_lib.quasar_paged_attention_workspace_bytes(max_new, n_q_heads, cache.n_kv_heads), 16), dtype=torch.uint8, device=q.device)
+    else:
+        _beside(_dev(workspace, "workspace"), "workspace", cache.pool)
+    if rows:
+        _check("quasar_paged_attention",
+               _lib.quasar_paged_attention(q.data_ptr(), rows, ldq, n_q_heads, cache.n_kv_heads, starts, n_seqs, max_new, *cache._layer(layer),
+                                           out.data_ptr(), ldo, workspace.data_ptr(), workspace.nbytes, _stream()))
+    return out
+
+
+def prompt_attention(q: torch.Tensor, n_q_heads: int, cache: PagedKvCache, layer: int, row_start: torch.Tensor,
+                     out: torch.Tensor = None) -> torch.Tensor:
+    """Causal attention of whole prompts, or of chunks behind what is cached: any number of rows a sequence."""
+    rows, ldq = _rows_of(q, n_q_heads * 128, "q", cache)
+    starts, n_seqs = _row_start_of(row_start, cache)
+    out, ldo = _output_like(out, rows, n_q_heads * 128, cache, "out")
+    if rows:
+        _check("quasar_prompt_attention",
+               _lib.quasar_prompt_attention(q.data_ptr(), rows, ldq, n_q_heads, cache.n_kv_heads, starts, n_seqs, *cache._layer(layer),
+                                            out.data_ptr(), ldo, _stream()))
     return out
 
 

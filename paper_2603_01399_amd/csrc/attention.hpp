@@ -19,13 +19,9 @@
 // one partial (max, sum, output) per split; attention_merge_kernel combines the splits.
 #pragma once
 
-#include "quasar_device.hpp"
+#include "kv_layout.hpp"
 
 namespace quasar {
-
-constexpr int kHeadDim = 128;
-constexpr int kKvBlock = 32;                 // positions per cache block
-constexpr int kKvBlockBytes = 8192;          // 32 positions x 128 d x 2 B
 
 struct AttnParams {
     const uint16_t *q;        // [M, Hq * 128] bf16 (normalised, rotated)
@@ -40,16 +36,6 @@ struct AttnParams {
     int row0;                 // first query row (m * G + g) of this launch; group z has rows row0 + 16 NQT z .. + 16 NQT - 1
     float scale_log2;         // log2(e) / sqrt(128)
 };
-
-__device__ __forceinline__ long long k_cache_index(int pos_in_block, int d) {
-    const int sub = pos_in_block >> 4, p = pos_in_block & 15;
-    return ((((long long)sub * 4 + (d >> 5)) * 4 + ((d & 31) >> 3)) * 16 + p) * 8 + (d & 7);
-}
-__device__ __forceinline__ long long v_cache_index(int pos_in_block, int d) {
-    const int o = pos_in_block & 15;
-    const int g4 = o >> 2, slot = (o & 3) + ((pos_in_block >> 4) << 2);
-    return ((((long long)(d >> 4)) * 4 + g4) * 16 + (d & 15)) * 8 + slot;
-}
 
 // ---------------------------------------------------------------------------------------------
 // Per head of the fused q/k/v projection output: RMSNorm over the head, rotary embedding at the
