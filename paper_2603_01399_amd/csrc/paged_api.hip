@@ -128,13 +128,13 @@ int launch_step(const PagedAttnParams &p, const StepShape &a, hipStream_t st) {
     }
 }
 
-template <int KV, int NT>
+template <int KV, int NW>
 int launch_prompt(const PromptParams &p, hipStream_t st) {
-    constexpr auto kern = prompt_attention_kernel<KV, NT>;
+    constexpr auto kern = prompt_attention_kernel<KV, NW>;
     if (!large_lds<kern>()) return QUASAR_ERR_HIP;
-    const long long rows = (long long)p.c.T * p.c.G, tiles = rows / (32 * NT * kPromptWaves) + p.c.n_seqs;   // (at most a ragged one a sequence)
-    const int lds = 2 * kPromptStepBytes + (kMaxSeqs + 1 + kPromptWaves + 4) * 4;
-    hipLaunchKernelGGL(kern, dim3((unsigned int)(tiles * p.c.Hkv)), dim3(kPromptWaves * 64), lds, st, p);
+    const long long rows = (long long)p.c.T * p.c.G, tiles = rows / (32 * NW) + p.c.n_seqs;   // (at most a ragged one a sequence)
+    const int lds = 2 * kPromptStepBytes + (kMaxSeqs + 1 + NW + 4) * 4;
+    hipLaunchKernelGGL(kern, dim3((unsigned int)(tiles * p.c.Hkv)), dim3(NW * 64), lds, st, p);
     return launched();
 }
 
@@ -235,7 +235,7 @@ int quasar_prompt_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n
     p.q = q; p.out = out; p.ldq = ldq; p.ldo = ldo;
     p.scale_log2 = kScaleLog2;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    return kv_type(kv_dtype) == KV_BF16 ? launch_prompt<KV_BF16, 2>(p, st) : launch_prompt<KV_E4M3, 2>(p, st);
+    return kv_type(kv_dtype) == KV_BF16 ? launch_prompt<KV_BF16, 8>(p, st) : launch_prompt<KV_E4M3, 8>(p, st);
 }
 
 size_t quasar_pages_workspace_bytes(int64_t n_seqs, int64_t n_pages) {
