@@ -116,6 +116,7 @@ __global__ __launch_bounds__(NW * 64) void prompt_attention_kernel(const PromptP
     int ids = -1, ids_at = -64;                                  // pages of steps ids_at .. + 63, one a lane
     u32x4 code[NL];
     auto request = [&](int step) {
+        const int stage = step & 1;
         if (step >= ids_at + 64 || ids_at < 0) {
             ids_at = step;
             const int b = 2 * (step + lane) + my_blk;
@@ -123,10 +124,10 @@ __global__ __launch_bounds__(NW * 64) void prompt_attention_kernel(const PromptP
         }
         const int page = __builtin_amdgcn_readlane(ids, step - ids_at);
         const bool good = page_exists(page, c.n_pages);
-        if (my_at == 0 && lane == 0) there[2 * (step & 1) + my_blk] = good;
+        if (my_at == 0 && lane == 0) there[2 * stage + my_blk] = good;
         const unsigned char *from = head + (good ? page : 0) * page_step + ((2 * step + my_blk) & in_page) * (2 * BB);
         if constexpr (KV == KV_BF16) {
-            const unsigned int to = lds_address_of(lds) + (step & 1) * kPromptStepBytes + w * PART;
+            const unsigned int to = lds_address_of(lds) + stage * kPromptStepBytes + w * PART;
 #pragma unroll
             for (int i = 0; i < NL; ++i) load_to_lds_16(reinterpret_cast<unsigned long long>(from) + 1024 * i, 16 * lane, to + 1024 * i);
         } else {
@@ -135,11 +136,11 @@ __global__ __launch_bounds__(NW * 64) void prompt_attention_kernel(const PromptP
         }
     };
     // what request() asked for is in LDS afterwards (for this wave; the others' behind a barrier)
-    auto settle = [&](int step) {
+    auto settle = [&](int stage) {
         if constexpr (KV == KV_BF16) {
             asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         } else {
-            u32x4 *to = reinterpret_cast<u32x4 *>(lds + (step & 1) * kPromptStepBytes + w * 2 * PART) + lane;
+            u32x4 *to = reinterpret_cast<u32x4 *>(lds + stage * kPromptStepBytes + w * 2 * PART) + lane;
 #pragma unroll
             for (int i = 0; i < NL; ++i) {
                 to[64 * (2 * i)] = e4m3x8_to_bf16(code[i].x, code[i].y);
@@ -158,8 +159,8 @@ __global__ __launch_bounds__(NW * 64) void prompt_attention_kernel(const PromptP
     const int k_lane = (((col >> 3) & 1) * 16 * 16 + ((col >> 4) * 8 + (col & 7)) + 16 * hi) * 16;   // [sub 2][kstep 4][g4 4][p 16] of 16 bytes
     const int v_lane = ((col >> 4) * 64 + (col & 15) + 16 * hi) * 16;                             // [dt 8][g4 4][dd 16] of 16 bytes
 
-    // the 64 positions of a step; edge: some are hidden from some row, or are nobody's
-    auto attend = [&](auto edge, int step, bool there0, bool there1) {
+    // the 64 positions of a step; edge: some are hidden from some row, or are nobody's; between(): called while the scores are computed
+    auto attend = [&](auto edge, int step, bool there0, bool there1, auto between) {
         constexpr bool EDGE = decltype(edge)::value;
         const unsigned char *buf = lds + (step & 1) * kPromptStepBytes;
         const int pos0 = step * kPromptStep;
@@ -185,6 +186,12 @@ __global__ __launch_bounds__(NW * 64) void prompt_attention_kernel(const PromptP
                     if (16 * ((i >> 2) & 1) + 8 * (i >> 3) + (i & 3) > left) sc[blk][i] = -__builtin_inff();
             }
         }
+        between();                                               // (dozens of scalar instructions: while the products are under way)
+        u32x4 v0[2][4];                                          // the first values, ahead of the softmax: its exponentials cover the way
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt) v0[t][dt] = *reinterpret_cast<const u32x4 *>(buf + kKvBlockBytes + v_lane + dt * 2048 + t * 512);
         float mx = larger(sc[0][0], sc[1][0]);
 #pragma unroll
         for (int i = 1; i < 16; ++i) mx = larger(mx, larger(sc[0][i], sc[1][i]));
@@ -217,7 +224,7 @@ __global__ __launch_bounds__(NW * 64) void prompt_attention_kernel(const PromptP
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int dt = 0; dt < 4; ++dt) {
-                    u32x4 va = *reinterpret_cast<const u32x4 *>(buf + (2 * blk + 1) * kKvBlockBytes + v_lane + dt * 2048 + t * 512);
+                    u32x4 va = blk == 0 ? v0[t][dt] : *reinterpret_cast<const u32x4 *>(buf + (2 * blk + 1) * kKvBlockBytes + v_lane + dt * 2048 + t * 512);
                     if constexpr (EDGE) {
                         // positions that no row sees hold whatever the page held: they must not reach the product (0 x NaN)
                         const int end = (blk ? there1 : there0) ? last_pos - pos0 - 32 * blk - 4 * (2 * t + hi) : -1;
@@ -230,29 +237,30 @@ __global__ __launch_bounds__(NW * 64) void prompt_attention_kernel(const PromptP
                     oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, va), __builtin_bit_cast(bf16x8, pb[blk][t]), oacc[dt], 0, 0, 0);
                 }
     };
-    if (steps > 0) request(0);
-    // the steps that every row sees whole, then the others (and all from the first that lacks a page on): two loops, since the outputs'
-    // registers would be copied once a step where the two ways met
+    // The steps that every row sees whole, then the others (and all from the first that lacks a page on): two loops, since the outputs'
+    // registers would be copied once a step where the two ways met.
     const int whole = min((first_pos + 1) / kPromptStep, steps);
     int step = 0;
     bool settled = false;
-    for (; step < whole; ++step) {
-        settle(step);
-        __syncthreads();
+    auto arrive = [&] {
+        settle(step & 1);
+        lds_barrier();
+    };
+    auto request_next = [&] {
+        if (step + 1 < steps) request(step + 1);
+    };
+    if (steps > 0) request(0);
+    for (; step < whole; step = step + 1) {
+        arrive();
         settled = !(there[2 * (step & 1)] && there[2 * (step & 1) + 1]);
         if (settled) break;
-        if (step + 1 < steps) request(step + 1);
-        attend(std::false_type{}, step, true, true);
+        attend(std::false_type{}, step, true, true, request_next);
     }
-    for (; step < steps; ++step) {
-        if (!settled) {
-            settle(step);
-            __syncthreads();
-        }
+    for (; step < steps; step = step + 1) {
+        if (!settled) arrive();
         settled = false;
         const bool there0 = there[2 * (step & 1)], there1 = there[2 * (step & 1) + 1];
-        if (step + 1 < steps) request(step + 1);
-        attend(std::true_type{}, step, there0, there1);
+        attend(std::true_type{}, step, there0, there1, request_next);
     }
     float sum = lrow + __shfl_xor(lrow, 32, 64);
     const float inv = sum > 0.f ? __fdiv_rn(vs, sum) : 0.f;      // a row that sees nothing: zeros
