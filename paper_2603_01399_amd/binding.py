@@ -40,7 +40,7 @@ EXPORTS = (
     "quasar_kv_cache_bytes", "quasar_kv_cache_fill", "quasar_attn_prepare", "quasar_attention_workspace_bytes",
     "quasar_verify_attention",
     "quasar_paged_cache_bytes", "quasar_paged_prepare", "quasar_paged_attention_workspace_bytes", "quasar_paged_attention",
-    "quasar_prompt_attention", "quasar_pages_workspace_bytes", "quasar_pages_reserve", "quasar_pages_fork", "quasar_pages_compact",
+    "quasar_prompt_attention_workspace_bytes", "quasar_prompt_attention", "quasar_pages_workspace_bytes", "quasar_pages_reserve", "quasar_pages_fork", "quasar_pages_compact",
 )
 
 
@@ -143,7 +143,9 @@ def _load() -> ctypes.CDLL:
     lib.quasar_paged_attention_workspace_bytes.argtypes = [i64, i64, i64]
     lib.quasar_paged_attention_workspace_bytes.restype = sz
     lib.quasar_paged_attention.argtypes = [vp, i64, i64, i64, i64, vp, i64, i64, *paged, vp, i64, vp, sz, vp]
-    lib.quasar_prompt_attention.argtypes = [vp, i64, i64, i64, i64, vp, i64, *paged, vp, i64, vp]
+    lib.quasar_prompt_attention_workspace_bytes.argtypes = [i64, i64, i64, i64]
+    lib.quasar_prompt_attention_workspace_bytes.restype = sz
+    lib.quasar_prompt_attention.argtypes = [vp, i64, i64, i64, i64, vp, i64, *paged, vp, i64, vp, sz, vp]
     lib.quasar_pages_workspace_bytes.argtypes = [i64, i64]
     lib.quasar_pages_workspace_bytes.restype = sz
     lib.quasar_pages_reserve.argtypes = [vp, i64, i64, i64, vp, vp, vp, i64, i64, vp, vp, i64, i64, ci, vp, sz, vp]
@@ -812,9 +814,10 @@ def prompt_attention(q: torch.Tensor, n_q_heads: int, cache: PagedKvCache, layer
     starts, n_seqs = _row_start_of(row_start, cache)
     out, ldo = _output_like(out, rows, n_q_heads * 128, cache, "out")
     if rows:
+        ws, need = _scratch(_lib.quasar_prompt_attention_workspace_bytes(rows, n_q_heads, cache.n_kv_heads, n_seqs), q.device)
         _check("quasar_prompt_attention",
                _lib.quasar_prompt_attention(q.data_ptr(), rows, ldq, n_q_heads, cache.n_kv_heads, starts, n_seqs, *cache._layer(layer),
-                                            out.data_ptr(), ldo, _stream()))
+                                            out.data_ptr(), ldo, _ptr(ws), need, _stream()))
     return out
 
 

@@ -88,6 +88,7 @@ int check_cache(const CacheArgs &a, PagedParams &p) {
     p.block_shift = block_shift_of(a.page_len);
     return QUASAR_OK;
 }
+constexpr int kFlatRounds = 1, kFlatPositions = 1024;
 constexpr float kScaleLog2 = 1.4426950408889634f / 11.313708498984761f;      // log2(e) / sqrt(128)
 
 // ---- attention of a step: workers of a kv head, query tiles and groups of 64 rows
@@ -99,7 +100,7 @@ bool step_shape(int64_t max_new, int64_t Hq, int64_t Hkv, StepShape &a) {
     a.NQT = R >= 64 ? 4 : (int)((R + 15) / 16);
     a.groups = (int)((R + 63) / 64);
     const int64_t per = (int64_t)compute_units() / (Hkv * a.groups);         // one workgroup per compute unit in total
-    a.workers = (int)(per < 1 ? 1 : per);
+    a.workers = (int)(per < 1 ? 1 : per > kMaxWorkers ? kMaxWorkers : per);
     const size_t slots = (size_t)a.groups * Hkv * 2 * a.workers * a.NQT;
     a.part_o = slots * 8 * 64 * 16;
     a.part_ml = slots * 16 * 2 * 4;
@@ -115,7 +116,7 @@ int launch_step(const PagedAttnParams &p, const StepShape &a, hipStream_t st) {
     hipLaunchKernelGGL(kern, dim3((unsigned int)a.workers, (unsigned int)p.c.Hkv, (unsigned int)a.groups), dim3(kPagedWaves * 64), lds, st, p);
     if (const int e = launched()) return e;
     if (a.workers == 1) return QUASAR_OK;                                    // (every sequence is finished by its one worker)
-    hipLaunchKernelGGL(paged_merge_kernel, dim3((unsigned int)a.workers, (unsigned int)p.c.Hkv, (unsigned int)(a.groups * NQT * 8)), dim3(512), 0, st, p, NQT);
+    hipLaunchKernelGGL(paged_merge_kernel, dim3((unsigned int)(2 * compute_units()), (unsigned int)a.groups), dim3(512), 0, st, p, NQT);
     return launched();
 }
 template <int KV>
@@ -128,13 +129,35 @@ int launch_step(const PagedAttnParams &p, const StepShape &a, hipStream_t st) {
     }
 }
 
-template <int KV, int NW>
-int launch_prompt(const PromptParams &p, hipStream_t st) {
-    constexpr auto kern = prompt_attention_kernel<KV, NW>;
+// ---- attention of prompts: workgroups of a kv head where tiles are shared
+struct PromptShape { int64_t tiles; int workers; size_t part_o, part_ml, pieces; };
+PromptShape prompt_shape(int64_t T, int64_t Hq, int64_t Hkv, int64_t n_seqs) {
+    PromptShape a{};
+    a.tiles = T * (Hq / Hkv) / (32 * kPromptWaves) + n_seqs;                 // (at most a ragged one a sequence)
+    const int64_t per = 2 * (int64_t)compute_units() / Hkv;
+    if (a.tiles > kMaxFlatTiles || a.tiles >= kFlatRounds * per) return a;
+    a.workers = (int)(per < 1 ? 1 : per > kMaxWorkers ? kMaxWorkers : per);
+    const size_t parts = (size_t)Hkv * 2 * a.workers * kPromptWaves;
+    a.part_o = parts * 16 * 64 * 16;
+    a.part_ml = parts * 64 * 8;
+    a.pieces = (size_t)a.workers * 16;
+    return a;
+}
+
+template <int KV>
+int launch_prompt(const PromptParams &p, const PromptShape &a, hipStream_t st) {
+    const int lds = 2 * kPromptStepBytes + (kMaxSeqs + kPromptWaves + 4) * 4;
+    if (!p.workers) {
+        constexpr auto kern = prompt_attention_kernel<KV, false>;
+        if (!large_lds<kern>()) return QUASAR_ERR_HIP;
+        hipLaunchKernelGGL(kern, dim3((unsigned int)(a.tiles * p.c.Hkv)), dim3(kPromptWaves * 64), lds, st, p);
+        return launched();
+    }
+    constexpr auto kern = prompt_attention_kernel<KV, true>;
     if (!large_lds<kern>()) return QUASAR_ERR_HIP;
-    const long long rows = (long long)p.c.T * p.c.G, tiles = rows / (32 * NW) + p.c.n_seqs;   // (at most a ragged one a sequence)
-    const int lds = 2 * kPromptStepBytes + (kMaxSeqs + 1 + NW + 4) * 4;
-    hipLaunchKernelGGL(kern, dim3((unsigned int)(tiles * p.c.Hkv)), dim3(NW * 64), lds, st, p);
+    hipLaunchKernelGGL(kern, dim3((unsigned int)(p.workers * p.c.Hkv)), dim3(kPromptWaves * 64), lds + kMaxFlatTiles * 4, st, p);
+    if (const int e = launched()) return e;
+    hipLaunchKernelGGL(prompt_merge_kernel, dim3((unsigned int)(4 * compute_units())), dim3(256), 0, st, p);
     return launched();
 }
 
@@ -221,21 +244,34 @@ int quasar_paged_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n_
     return kv_type(kv_dtype) == KV_BF16 ? launch_step<KV_BF16>(p, shape, st) : launch_step<KV_E4M3>(p, shape, st);
 }
 
+size_t quasar_prompt_attention_workspace_bytes(int64_t T, int64_t n_q_heads, int64_t n_kv_heads, int64_t n_seqs) {
+    if (T < 1 || T > kMaxPositions || check_heads(n_q_heads, n_kv_heads) || n_seqs < 1 || n_seqs > kMaxSeqs) return 0;
+    const PromptShape a = prompt_shape(T, n_q_heads, n_kv_heads, n_seqs);
+    return a.part_o + a.part_ml + a.pieces;
+}
+
 int quasar_prompt_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n_q_heads, int64_t n_kv_heads, const int32_t *row_start,
                             int64_t n_seqs, const void *pages, int64_t n_pages, int64_t page_len, int kv_dtype, const float *k_scale,
                             const float *v_scale, const int32_t *table, int64_t table_ld, int64_t max_pages, const int32_t *lengths,
-                            uint16_t *out, int64_t ldo, void *hip_stream) {
+                            uint16_t *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *hip_stream) {
     if (!q || !out) return QUASAR_ERR_NULL;
     PromptParams p{};
     const CacheArgs a{T, n_q_heads, n_kv_heads, pages, n_pages, page_len, kv_dtype, k_scale, v_scale, table, table_ld, n_seqs, max_pages, lengths, row_start};
     if (const int e = check_cache(a, p.c)) return e;
     if (T * (n_q_heads / n_kv_heads) > (1 << 26)) return QUASAR_ERR_SHAPE;       // (the tiles of all sequences are counted in 32 bits)
     if (ldq < n_q_heads * kHeadDim || ldo < n_q_heads * kHeadDim || ldq % 8 || ldo % 4) return QUASAR_ERR_SHAPE;
-    if (!aligned(q, 16) || !aligned(out, 8)) return QUASAR_ERR_ALIGN;
+    if (!aligned(q, 16) || !aligned(out, 8) || !aligned(workspace, 16)) return QUASAR_ERR_ALIGN;
     p.q = q; p.out = out; p.ldq = ldq; p.ldo = ldo;
     p.scale_log2 = kScaleLog2;
+    const PromptShape shape = prompt_shape(T, n_q_heads, n_kv_heads, n_seqs);
+    if (workspace && shape.workers && workspace_bytes >= shape.part_o + shape.part_ml + shape.pieces && max_pages * page_len > kFlatPositions) {
+        p.workers = shape.workers;
+        p.part_o = static_cast<f32x4 *>(workspace);
+        p.part_ml = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace) + shape.part_o);
+        p.pieces = reinterpret_cast<int *>(static_cast<unsigned char *>(workspace) + shape.part_o + shape.part_ml);
+    }
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    return kv_type(kv_dtype) == KV_BF16 ? launch_prompt<KV_BF16, 8>(p, st) : launch_prompt<KV_E4M3, 8>(p, st);
+    return kv_type(kv_dtype) == KV_BF16 ? launch_prompt<KV_BF16>(p, shape, st) : launch_prompt<KV_E4M3>(p, shape, st);
 }
 
 size_t quasar_pages_workspace_bytes(int64_t n_seqs, int64_t n_pages) {

@@ -26,6 +26,7 @@ struct PagedAttnParams {
 };
 
 constexpr int kPagedWaves = 4;
+constexpr int kMaxWorkers = 512;             // of a kv head
 
 // Prefix sums of the sequences' blocks into lds[0 .. n_seqs] (exclusive; the total at the end).  `row_group`: sequences without
 // rows in this group of 64 have none.
@@ -314,77 +315,96 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
     }
 }
 
-// Joins the pieces of the sequences that several workers share.  One workgroup per (worker in whose piece such a sequence begins,
-// kv head, 16-row tile, 16-d tile); its 8 waves share the pieces.
+// The workers in whose pieces a shared sequence (or tile) begins, in order, into list; how many.  records: of each worker `words` ints, the
+// first of them < 0 where none begins.
+__device__ __forceinline__ int shared_pieces(const int *records, int words, int workers, int *list) {
+    const int lane = threadIdx.x & 63;
+    int n = 0;
+    for (int i = 0; i < workers; i += 64) {
+        const bool begins = i + lane < workers && records[(i + lane) * words] >= 0;
+        const unsigned long long mask = __builtin_amdgcn_ballot_w64(begins);
+        if (begins && threadIdx.x < 64) list[n + __popcll(mask & ((1ull << lane) - 1))] = i + lane;
+        n += __popcll(mask);
+    }
+    __syncthreads();
+    return n;
+}
+
+// Joins the pieces of the sequences that several workers share, for one group of 64 rows (blockIdx.y).  A unit is 16 rows and 16 d of a kv
+// head of such a sequence: the eight waves of a workgroup share its pieces, four of them requested at a time, and meet in LDS.  The
+// workgroups walk the units: one for every worker, head and unit were up to 8192, nearly all with nothing to do (24 us where this takes XX).
 __global__ __launch_bounds__(512) void paged_merge_kernel(const PagedAttnParams p, int NQT) {
     __shared__ float smax[8][16];
     __shared__ float slsum[8][16];
     __shared__ f32x4 sacc[8][64];
+    __shared__ int list[kMaxWorkers];
     const PagedParams &c = p.c;
-    const int worker = blockIdx.x, h = blockIdx.y;
-    const int dt = blockIdx.z & 7, qt = (blockIdx.z >> 3) % NQT, z = (blockIdx.z >> 3) / NQT;
-    const int *piece = p.pieces + ((long long)z * p.workers + worker) * 4;
-    const int s = piece[0], last = piece[1], first_slot = piece[2];
-    if (s < 0) return;
-    const SeqSpan a = seq_span(c, s);
-    const int n = a.n < p.max_new ? a.n : p.max_new, R = n * c.G;
-    if (64 * z + 16 * qt >= R) return;
+    const int z = blockIdx.y;
+    const int *records = p.pieces + (long long)z * p.workers * 4;
+    const int units = shared_pieces(records, 4, p.workers, list) * c.Hkv * NQT * 8;
     const int sg = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int g4 = lane >> 4, col = lane & 15;
-    const int r = 64 * z + 16 * qt + col;
-    const int count = last - worker + 1;
-    float mw = -__builtin_inff(), lsum = 0.f;
-    f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-    for (int i0 = sg; i0 < count; i0 += 32) {
-        f32x4 o[4];
-        u32x2 ml[4];
+    for (int u = blockIdx.x; u < units; u += gridDim.x) {
+        const int dt = u & 7, qt = (u >> 3) % NQT, h = (u >> 3) / NQT % c.Hkv, worker = list[(u >> 3) / NQT / c.Hkv];
+        const int s = records[worker * 4], last = records[worker * 4 + 1], first_slot = records[worker * 4 + 2];
+        const SeqSpan a = seq_span(c, s);
+        const int n = a.n < p.max_new ? a.n : p.max_new, R = n * c.G;
+        if (64 * z + 16 * qt >= R) continue;
+        const int r = 64 * z + 16 * qt + col;
+        const int count = last - worker + 1;
+        float mw = -__builtin_inff(), lsum = 0.f;
+        f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+        for (int k0 = sg; k0 < count; k0 += 32) {
+            f32x4 o[4];
+            u32x2 ml[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int k = min(i0 + 8 * i, count - 1);
-            const int slot = flat_part_slot(worker, first_slot, k);
-            const long long pb = (((long long)z * c.Hkv + h) * (2 * p.workers) + slot) * NQT + qt;
-            ml[i] = reinterpret_cast<const u32x2 *>(p.part_ml)[pb * 16 + col];
-            o[i] = p.part_o[(pb * 8 + dt) * 64 + lane];
-        }
-        float m_new = mw;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i0 + 8 * i < count) m_new = fmaxf(m_new, __uint_as_float(ml[i].x));
-        const float m_use = m_new == -__builtin_inff() ? 0.f : m_new;            // nothing visible in these pieces
-        const float keep = exp2f(mw - m_use);
-        acc *= keep;
-        lsum *= keep;
-        mw = m_new;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (i0 + 8 * i < count) {
-                const float f = exp2f(__uint_as_float(ml[i].x) - m_use);
-                lsum += f * __uint_as_float(ml[i].y);
-                acc += o[i] * f;
+            for (int i = 0; i < 4; ++i) {
+                const int slot = flat_part_slot(worker, first_slot, min(k0 + 8 * i, count - 1));
+                const long long pb = (((long long)z * c.Hkv + h) * (2 * p.workers) + slot) * NQT + qt;
+                ml[i] = reinterpret_cast<const u32x2 *>(p.part_ml)[pb * 16 + col];
+                o[i] = p.part_o[(pb * 8 + dt) * 64 + lane];
             }
+            float m_new = mw;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (k0 + 8 * i < count) m_new = fmaxf(m_new, __uint_as_float(ml[i].x));
+            const float m_use = m_new == -__builtin_inff() ? 0.f : m_new;        // nothing visible in these pieces
+            const float keep = exp2f(mw - m_use);
+            acc *= keep;
+            lsum *= keep;
+            mw = m_new;
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (k0 + 8 * i < count) {
+                    const float f = exp2f(__uint_as_float(ml[i].x) - m_use);
+                    lsum += f * __uint_as_float(ml[i].y);
+                    acc += o[i] * f;
+                }
         }
-    }
-    sacc[sg][lane] = acc;
-    if (g4 == 0) { smax[sg][col] = mw; slsum[sg][col] = lsum; }
-    __syncthreads();
-    if (sg != 0 || r >= R) return;
-    float mstar = smax[0][col];
+        sacc[sg][lane] = acc;
+        if (g4 == 0) { smax[sg][col] = mw; slsum[sg][col] = lsum; }
+        __syncthreads();
+        if (sg == 0 && r < R) {
+            float mstar = smax[0][col];
 #pragma unroll
-    for (int i = 1; i < 8; ++i) mstar = fmaxf(mstar, smax[i][col]);
-    const float m_use = mstar == -__builtin_inff() ? 0.f : mstar;
-    acc = f32x4{0.f, 0.f, 0.f, 0.f};
-    lsum = 0.f;
+            for (int i = 1; i < 8; ++i) mstar = fmaxf(mstar, smax[i][col]);
+            const float m_use = mstar == -__builtin_inff() ? 0.f : mstar;
+            acc = f32x4{0.f, 0.f, 0.f, 0.f};
+            lsum = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const float f = exp2f(smax[i][col] - m_use);
-        acc += sacc[i][lane] * f;
-        lsum += slsum[i][col] * f;
+            for (int i = 0; i < 8; ++i) {
+                const float f = exp2f(smax[i][col] - m_use);
+                acc += sacc[i][lane] * f;
+                lsum += slsum[i][col] * f;
+            }
+            const float vs = c.v_scale ? c.v_scale[h] : 1.0f;
+            const float inv = lsum > 0.f ? __fdiv_rn(vs, lsum) : 0.f;
+            const int m = r / c.G, g = r % c.G;
+            const u32x2 o = {float2_to_bf16_pair(acc.x * inv, acc.y * inv), float2_to_bf16_pair(acc.z * inv, acc.w * inv)};
+            *reinterpret_cast<u32x2 *>(p.out + (a.row0 + m) * p.ldo + ((long long)h * c.G + g) * kHeadDim + 16 * dt + 4 * g4) = o;
+        }
+        __syncthreads();
     }
-    const float vs = c.v_scale ? c.v_scale[h] : 1.0f;
-    const float inv = lsum > 0.f ? __fdiv_rn(vs, lsum) : 0.f;
-    const int m = r / c.G, g = r % c.G;
-    const u32x2 o = {float2_to_bf16_pair(acc.x * inv, acc.y * inv), float2_to_bf16_pair(acc.z * inv, acc.w * inv)};
-    *reinterpret_cast<u32x2 *>(p.out + (a.row0 + m) * p.ldo + ((long long)h * c.G + g) * kHeadDim + 16 * dt + 4 * g4) = o;
 }
 
 }  // namespace quasar

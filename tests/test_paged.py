@@ -190,12 +190,12 @@ def test_paged_attention_refuses(lib, change, status):
 
 
 @pytest.mark.parametrize("change,status", BAD_PAGED + [(dict(x=None), NULL), (dict(out=None), NULL), (dict(ldq=4088), SHAPE), (dict(ldo=4098), SHAPE),
-                                                       (dict(T=1 << 24, hq=64), SHAPE), (dict(x=ODD_ADDRESS), ALIGN), (dict(out=ODD_ADDRESS), ALIGN)])
+                                                       (dict(T=1 << 24, hq=64), SHAPE), (dict(x=ODD_ADDRESS), ALIGN), (dict(out=ODD_ADDRESS), ALIGN), (dict(ws=ODD_ADDRESS), ALIGN)])
 def test_prompt_attention_refuses(lib, change, status):
-    c = dict(PAGED, x=A, T=5, ldq=8192, hq=32, hk=8, row_start=A, n_seqs=2, out=A, ldo=8192) | change
+    c = dict(PAGED, x=A, T=5, ldq=8192, hq=32, hk=8, row_start=A, n_seqs=2, out=A, ldo=8192, ws=None) | change
     if status == SHAPE and "ldq" in change:
         c["hq"] = 64
-    assert lib.quasar_prompt_attention(c["x"], c["T"], c["ldq"], c["hq"], c["hk"], c["row_start"], c["n_seqs"], *paged_args(c), c["out"], c["ldo"], None) == status
+    assert lib.quasar_prompt_attention(c["x"], c["T"], c["ldq"], c["hq"], c["hk"], c["row_start"], c["n_seqs"], *paged_args(c), c["out"], c["ldo"], c["ws"], 1 << 30, None) == status
 
 
 BOOKS = dict(table=A, table_ld=4, n_seqs=2, max_pages=4, lengths=A, other=A, refs=A, n_pages=10, page_len=64, out=A, pool=A, layers=2, hk=8, kv=1, ws=A, room=1 << 30)
