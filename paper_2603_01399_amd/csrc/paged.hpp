@@ -73,6 +73,27 @@ __device__ __forceinline__ u32x4 e4m3x8_to_bf16(unsigned int lo, unsigned int hi
     return r;
 }
 
+// ---- softmax in the 32 x 32 x 16 products' layout: a lane owns a query column, lanes l and l ^ 32 share it
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+// Scores may pass the running maximum by this much (in powers of two) before sums and outputs are scaled down: p up to 2^8 costs neither
+// product nor sum any precision.
+constexpr float kLazyMax = 8.f;
+
+// The maximum that hands a NaN on: one instruction, also of three operands (fmaxf has every operand made quiet first).
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+
+// the larger of lanes l and l ^ 32
+__device__ __forceinline__ float max_halves(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return larger(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+// sum + both bf16 of a pair, in fp32: sums are taken of the rounded weights, so that the weights that are applied sum to one
+__device__ __forceinline__ float add_bf16_pair(unsigned int pair, float sum) {
+    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3F803F80u), sum, false);
+}
+
 // ---------------------------------------------------------------------------------------------
 // Append: per head of a new row RMSNorm and rotary embedding (queries and keys), queries to q_out, keys and values to the
 // page of the row's position.

@@ -91,15 +91,18 @@ int check_cache(const CacheArgs &a, PagedParams &p) {
 constexpr int kFlatRounds = 1, kFlatPositions = 1024;
 constexpr float kScaleLog2 = 1.4426950408889634f / 11.313708498984761f;      // log2(e) / sqrt(128)
 
-// ---- attention of a step: workers of a kv head, query tiles and groups of 64 rows
-struct StepShape { int NQT, groups, workers; size_t part_o, part_ml, pieces; };
-bool step_shape(int64_t max_new, int64_t Hq, int64_t Hkv, StepShape &a) {
+// ---- attention of a step: workers of a kv head, query tiles and groups of rows.  Up to 16 rows of a sequence and kv head take the 16 x 16
+// products; more take the 32 x 32 ones, but bf16 pages up to 32 rows: 16 sequences of 8 tokens over up to 4000 positions, 32 / 8 heads
+// 45.2 us narrow and 61 wide, 8-bit pages 36.4 and 30.4; 8 of 16 tokens over 8000 in bf16 65.7 (four narrow tiles) and 55.8.
+struct StepShape { int NQT, groups, workers; bool wide; size_t part_o, part_ml, pieces; };
+bool step_shape(int64_t max_new, int64_t Hq, int64_t Hkv, int kv, StepShape &a) {
     if (max_new < 1 || max_new > 32 || check_heads(Hq, Hkv)) return false;
     const int64_t R = max_new * (Hq / Hkv);
     if (R > 1024) return false;
-    a.NQT = R >= 64 ? 4 : (int)((R + 15) / 16);
-    a.groups = (int)((R + 63) / 64);
-    const int64_t per = (int64_t)compute_units() / (Hkv * a.groups);         // one workgroup per compute unit in total
+    a.NQT = R <= 16 ? 1 : R <= 32 ? 2 : R <= 64 ? 4 : 8;
+    a.wide = a.NQT > 2 || (a.NQT == 2 && kv == KV_E4M3);
+    a.groups = (int)((R + 16 * a.NQT - 1) / (16 * a.NQT));
+    const int64_t per = (a.wide ? 2 : 1) * (int64_t)compute_units() / (Hkv * a.groups);      // as many workgroups as are on the GPU at once
     a.workers = (int)(per < 1 ? 1 : per > kMaxWorkers ? kMaxWorkers : per);
     const size_t slots = (size_t)a.groups * Hkv * 2 * a.workers * a.NQT;
     a.part_o = slots * 8 * 64 * 16;
@@ -108,25 +111,26 @@ bool step_shape(int64_t max_new, int64_t Hq, int64_t Hkv, StepShape &a) {
     return true;
 }
 
-template <int KV, int NQT>
-int launch_step(const PagedAttnParams &p, const StepShape &a, hipStream_t st) {
-    constexpr auto kern = paged_attention_kernel<KV, NQT>;
-    if (!large_lds<kern>()) return QUASAR_ERR_HIP;
-    const int lds = kPagedWaves * NQT * (8 * 64 * 16 + 16 * 2 * 4) + (kPagedWaves + p.c.n_seqs + 1) * 4;
-    hipLaunchKernelGGL(kern, dim3((unsigned int)a.workers, (unsigned int)p.c.Hkv, (unsigned int)a.groups), dim3(kPagedWaves * 64), lds, st, p);
+template <auto Kernel>
+int launch_step(const PagedAttnParams &p, const StepShape &a, int lds, hipStream_t st) {
+    if (!large_lds<Kernel>()) return QUASAR_ERR_HIP;
+    hipLaunchKernelGGL(Kernel, dim3((unsigned int)a.workers, (unsigned int)p.c.Hkv, (unsigned int)a.groups), dim3(kPagedWaves * 64),
+                       lds + (kPagedWaves + p.c.n_seqs + 1) * 4, st, p);
     if (const int e = launched()) return e;
     if (a.workers == 1) return QUASAR_OK;                                    // (every sequence is finished by its one worker)
-    hipLaunchKernelGGL(paged_merge_kernel, dim3((unsigned int)(2 * compute_units()), (unsigned int)a.groups), dim3(512), 0, st, p, NQT);
+    hipLaunchKernelGGL(paged_merge_kernel, dim3((unsigned int)(2 * compute_units()), (unsigned int)a.groups), dim3(512), 0, st, p, a.NQT);
     return launched();
 }
 template <int KV>
-int launch_step(const PagedAttnParams &p, const StepShape &a, hipStream_t st) {
-    switch (a.NQT) {
-        case 1: return launch_step<KV, 1>(p, a, st);
-        case 2: return launch_step<KV, 2>(p, a, st);
-        case 3: return launch_step<KV, 3>(p, a, st);
-        default: return launch_step<KV, 4>(p, a, st);
-    }
+int launch_step(PagedAttnParams &p, const StepShape &a, hipStream_t st) {
+    p.group_rows = 16 * a.NQT;
+    constexpr auto narrow = [](int nqt) { return kPagedWaves * nqt * (8 * 64 * 16 + 16 * 2 * 4); };
+    constexpr auto wide = [](int rw) { return rw * (kPagedWaves / rw - 1) * (16 * 64 * 16 + 64 * 8); };
+    if (a.NQT == 1) return launch_step<paged_attention_kernel<KV, 1>>(p, a, narrow(1), st);
+    if (a.NQT == 4) return launch_step<paged_attention_wide_kernel<KV, 2>>(p, a, wide(2), st);
+    if (a.NQT == 8) return launch_step<paged_attention_wide_kernel<KV, 4>>(p, a, wide(4), st);
+    if constexpr (KV == KV_BF16) return launch_step<paged_attention_kernel<KV, 2>>(p, a, narrow(2), st);
+    else return launch_step<paged_attention_wide_kernel<KV, 1>>(p, a, wide(1), st);
 }
 
 // ---- attention of prompts: workgroups of a kv head where tiles are shared
@@ -216,8 +220,10 @@ int quasar_paged_prepare(const uint16_t *qkv, int64_t T, int64_t ld, int64_t n_q
 }
 
 size_t quasar_paged_attention_workspace_bytes(int64_t max_new, int64_t n_q_heads, int64_t n_kv_heads) {
-    StepShape a{};
-    return step_shape(max_new, n_q_heads, n_kv_heads, a) ? a.part_o + a.part_ml + a.pieces : 0;
+    StepShape a{}, b{};
+    if (!step_shape(max_new, n_q_heads, n_kv_heads, KV_BF16, a) || !step_shape(max_new, n_q_heads, n_kv_heads, KV_E4M3, b)) return 0;
+    const size_t x = a.part_o + a.part_ml + a.pieces, y = b.part_o + b.part_ml + b.pieces;
+    return x > y ? x : y;
 }
 
 int quasar_paged_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n_q_heads, int64_t n_kv_heads, const int32_t *row_start,
@@ -229,10 +235,10 @@ int quasar_paged_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n_
     const CacheArgs a{T, n_q_heads, n_kv_heads, pages, n_pages, page_len, kv_dtype, k_scale, v_scale, table, table_ld, n_seqs, max_pages, lengths, row_start};
     if (const int e = check_cache(a, p.c)) return e;
     StepShape shape{};
-    if (!step_shape(max_new, n_q_heads, n_kv_heads, shape)) return QUASAR_ERR_SHAPE;
+    if (!step_shape(max_new, n_q_heads, n_kv_heads, kv_type(kv_dtype), shape)) return QUASAR_ERR_SHAPE;
     if (ldq < n_q_heads * kHeadDim || ldo < n_q_heads * kHeadDim || ldq % 8 || ldo % 4) return QUASAR_ERR_SHAPE;
     if (!aligned(q, 16) || !aligned(out, 8)) return QUASAR_ERR_ALIGN;
-    if (!workspace || workspace_bytes < shape.part_o + shape.part_ml + shape.pieces) return QUASAR_ERR_WORKSPACE;
+    if (!workspace || workspace_bytes < quasar_paged_attention_workspace_bytes(max_new, n_q_heads, n_kv_heads)) return QUASAR_ERR_WORKSPACE;
     if (!aligned(workspace, 16)) return QUASAR_ERR_ALIGN;
     p.q = q; p.out = out; p.ldq = ldq; p.ldo = ldo;
     p.part_o = static_cast<f32x4 *>(workspace);

@@ -37,7 +37,6 @@ struct PromptTile {
     SeqSpan a;
 };
 
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 template <int ROWS>
 __device__ __forceinline__ PromptTile prompt_tile(const PagedParams &c, const int *prefix, int f) {
     PromptTile t;
@@ -84,18 +83,6 @@ __device__ __forceinline__ int prefix_sums(int n, int *out, int *wave_sums, V v)
 }
 constexpr int kPromptStep = 64;                          // positions in LDS at a time
 constexpr int kPromptStepBytes = kPromptStep / kKvBlock * 2 * kKvBlockBytes;   // 32 KB: two blocks, keys and values
-// Scores may pass the running maximum by this much (in powers of two) before sums and outputs are scaled down: p up to 2^8 costs neither
-// product nor sum any precision.
-constexpr float kLazyMax = 8.f;
-
-// The maximum that hands a NaN on: one instruction, also of three operands (fmaxf has every operand made quiet first).
-__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
-
-// the larger of lanes l and l ^ 32
-__device__ __forceinline__ float max_halves(float x) {
-    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-    return larger(__uint_as_float(r[0]), __uint_as_float(r[1]));
-}
 
 // FLAT: the steps of all tiles as one line, in equal pieces for `workers` workgroups of a kv head (as the blocks of a step's sequences,
 // paged_attention.hpp), for launches whose tiles would leave compute units idle; else a workgroup a tile, the last ones, which see most,
@@ -263,9 +250,7 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
                 const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[blk][2 * i + 1], scale_log2, mc));
                 const unsigned int pk = float2_to_bf16_pair(e0, e1);
                 pb[blk][i >> 2][i & 3] = pk;
-                // the sum of the rounded values, so that the weights that are applied sum to one
-                typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-                lrow = __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pk), __builtin_bit_cast(bf16x2, 0x3F803F80u), lrow, false);
+                lrow = add_bf16_pair(pk, lrow);
             }
 #pragma unroll
         for (int blk = 0; blk < 2; ++blk)

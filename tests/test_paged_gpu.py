@@ -50,6 +50,15 @@ def test_attention_of_a_step(qb, kv, page, hq, hk, lengths, news):
     close(bf16_to_host(qb.paged_attention(b.q(), hq, b.cache, 0, b.row_start, max(news))), b)
 
 
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+@pytest.mark.parametrize("group,new", [(1, 1), (1, 16), (1, 17), (1, 32), (3, 5), (3, 11), (5, 7), (8, 8), (8, 9), (2, 32), (7, 10), (8, 16), (8, 17), (16, 32), (32, 32)])
+def test_attention_of_any_number_of_rows(qb, kv, group, new):
+    """Rows of a sequence and kv head around every form's border, over lengths that one worker and that many take."""
+    say("rows", kv, group, new)
+    b = Batch(qb, kv, 64, 2 * group, 2, [1500, 31, 4, 0, 700], [new, 1, max(new - 1, 0), new, 0], seed=200 + group + new)
+    close(bf16_to_host(qb.paged_attention(b.q(), 2 * group, b.cache, 0, b.row_start, new)), b)
+
+
 PROMPT = STEP[:9] + STEP[10:16] + [
     ("bf16", 64, 4, 1, [0], [64]), ("bf16", 64, 4, 4, [0], [1]), ("bf16", 64, 8, 2, [0], [65]), ("bf16", 32, 8, 2, [0, 0, 0], [130, 0, 257]),
     ("bf16", 64, 5, 1, [0, 40], [300, 77]), ("bf16", 128, 2, 2, [1000, 0], [200, 700]), ("e4m3", 64, 8, 2, [0, 100], [129, 311]),
