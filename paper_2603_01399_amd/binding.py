@@ -196,7 +196,9 @@ from . import _fastcall as _fast  # noqa: E402
 
 _NATIVE_ENTRIES = ("quasar_w8_linear", "quasar_bf16_linear", "quasar_w8a8_linear_split", "quasar_w4_linear_split", "quasar_w4_packed_bytes",
                    "quasar_w8a8_workspace_bytes", "quasar_w4_workspace_bytes", "quasar_w8_linear_fused_split",
-                   "quasar_w8_gateup_swiglu_split", "quasar_w8_fused_workspace_bytes", "quasar_w8_gateup_workspace_bytes")
+                   "quasar_w8_gateup_swiglu_split", "quasar_w8_fused_workspace_bytes", "quasar_w8_gateup_workspace_bytes",
+                   "quasar_paged_prepare", "quasar_paged_attention", "quasar_paged_attention_workspace_bytes", "quasar_prompt_attention",
+                   "quasar_prompt_attention_workspace_bytes", "quasar_pages_reserve", "quasar_pages_fork", "quasar_pages_compact")
 
 
 def _native_addresses(lib):
@@ -695,6 +697,10 @@ class PagedKvCache:
         self._refs, self._lengths, self._table = self.refs.data_ptr(), self.lengths.data_ptr(), self.table.data_ptr()
         self._layer_bytes = pool.nbytes // n_layers
         self._workspace_bytes = _lib.quasar_pages_workspace_bytes(max_seqs, n_pages)
+        # the ordinary calls take this handle to the native side
+        self._handle = _fast.paged_cache(n_layers, n_kv_heads, n_pages, page_len, max_seqs, max_pages, code, self._layer_bytes, self._workspace_bytes,
+                                         pool.device.index, pool.data_ptr(), self._refs, self._lengths, self._table,
+                                         0 if k_scale is None else k_scale.data_ptr(), 0 if v_scale is None else v_scale.data_ptr())
 
     def _layer(self, layer: int):
         if not 0 <= layer < self.n_layers:
@@ -714,6 +720,9 @@ class PagedKvCache:
     def reserve(self, n_new: torch.Tensor) -> torch.Tensor:
         """Pages for n_new [max_seqs] further positions of each sequence; a shared last page is replaced by a copy.
         -> int32 [max_seqs]: 1, or 0 for a sequence that found too few pages and is as it was."""
+        done = _fast.pages_reserve(self._handle, n_new)
+        if type(done) is not int or done > 0:
+            return _checked("quasar_pages_reserve", done)
         new = self._per_sequence(n_new, "n_new")
         status = torch.empty(self.max_seqs, dtype=torch.int32, device=self.pool.device)
         ws = torch.empty(self._workspace_bytes, dtype=torch.uint8, device=self.pool.device)
@@ -725,6 +734,9 @@ class PagedKvCache:
 
     def fork(self, parent: torch.Tensor, keep: torch.Tensor = None) -> None:
         """Sequence s becomes sequence parent[s] as it was, cut to keep[s] positions (None: not cut); parent -1 frees it."""
+        status = _fast.pages_fork(self._handle, parent, keep)
+        if status >= 0:
+            return _check("quasar_pages_fork", status)
         _check("quasar_pages_fork",
                _lib.quasar_pages_fork(self._table, self.max_pages, self.max_seqs, self.max_pages, self._lengths, self._per_sequence(parent, "parent"),
                                       None if keep is None else self._per_sequence(keep, "keep"), self._refs, self.n_pages, self.page_len,
@@ -732,6 +744,9 @@ class PagedKvCache:
 
     def compact(self) -> torch.Tensor:
         """Moves the pages in use together at the beginning of the pool.  -> int32 [n_pages]: where each page went."""
+        done = _fast.pages_compact(self._handle)
+        if type(done) is not int or done > 0:
+            return _checked("quasar_pages_compact", done)
         _beside(self.books, "the cache", self.pool)
         to = torch.empty(self.n_pages, dtype=torch.int32, device=self.pool.device)
         ws = torch.empty(self._workspace_bytes, dtype=torch.uint8, device=self.pool.device)
@@ -740,6 +755,13 @@ class PagedKvCache:
                                          to.data_ptr(), self.pool.data_ptr(), self.n_layers, self.n_kv_heads, self._code, ws.data_ptr(),
                                          self._workspace_bytes, _stream()))
         return to
+
+
+def _checked(fn, done):
+    """What a call on a cache's handle gave: the tensor, or the status of one that failed."""
+    if type(done) is int:
+        _check(fn, done)
+    return done
 
 
 def _beside(t, name, pool):
@@ -777,6 +799,9 @@ def _output_like(out, rows, width, cache, name):
 def paged_prepare(qkv: torch.Tensor, n_q_heads: int, cache: PagedKvCache, layer: int, row_start: torch.Tensor, q_gamma: torch.Tensor,
                   k_gamma: torch.Tensor, eps: float = 1e-6, rope_theta: float = 1.0e6, q_out: torch.Tensor = None) -> torch.Tensor:
     """attn_prepare for the packed rows of a batch: row_start [sequences + 1], positions from cache.lengths on."""
+    done = _fast.paged_prepare(cache._handle, qkv, n_q_heads, layer, row_start, q_gamma, k_gamma, eps, rope_theta, q_out)
+    if type(done) is not int or done > 0:
+        return _checked("quasar_paged_prepare", done)
     rows, ld = _rows_of(qkv, (n_q_heads + 2 * cache.n_kv_heads) * 128, "qkv", cache)
     starts, n_seqs = _row_start_of(row_start, cache)
     for name, gamma in (("q_gamma", q_gamma), ("k_gamma", k_gamma)):
@@ -793,6 +818,9 @@ def paged_prepare(qkv: torch.Tensor, n_q_heads: int, cache: PagedKvCache, layer:
 def paged_attention(q: torch.Tensor, n_q_heads: int, cache: PagedKvCache, layer: int, row_start: torch.Tensor, max_new: int,
                     workspace: torch.Tensor = None, out: torch.Tensor = None) -> torch.Tensor:
     """Attention of the new tokens of a step, at most max_new (1 .. 32) a sequence, over their sequences' pages."""
+    done = _fast.paged_attention(cache._handle, q, n_q_heads, layer, row_start, max_new, workspace, out)
+    if type(done) is not int or done > 0:
+        return _checked("quasar_paged_attention", done)
     rows, ldq = _rows_of(q, n_q_heads * 128, "q", cache)
     starts, n_seqs = _row_start_of(row_start, cache)
     out, ldo = _output_like(out, rows, n_q_heads * 128, cache, "out")
@@ -810,6 +838,9 @@ def paged_attention(q: torch.Tensor, n_q_heads: int, cache: PagedKvCache, layer:
 def prompt_attention(q: torch.Tensor, n_q_heads: int, cache: PagedKvCache, layer: int, row_start: torch.Tensor,
                      out: torch.Tensor = None) -> torch.Tensor:
     """Causal attention of whole prompts, or of chunks behind what is cached: any number of rows a sequence."""
+    done = _fast.prompt_attention(cache._handle, q, n_q_heads, layer, row_start, out)
+    if type(done) is not int or done > 0:
+        return _checked("quasar_prompt_attention", done)
     rows, ldq = _rows_of(q, n_q_heads * 128, "q", cache)
     starts, n_seqs = _row_start_of(row_start, cache)
     out, ldo = _output_like(out, rows, n_q_heads * 128, cache, "out")

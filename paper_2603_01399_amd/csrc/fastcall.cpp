@@ -1,5 +1,5 @@
-// The linears' and fused linears' argument marshalling in native code: what binding.py does for an ordinary call - plain CUDA tensors, an output
-// given - without its Python and ctypes steps.  Scratch that a call uses comes from torch's allocator, on the stream of the call.
+// The argument marshalling of the linears, the fused linears and the paged cache in native code: what binding.py does for an ordinary call - plain CUDA tensors, of a
+// linear with an output given - without its Python and ctypes steps.  Scratch that a call uses comes from torch's allocator, on the stream of the call.
 //
 // Every function returns the status of the C entry point it calls, or -1 for "not an ordinary call": binding.py then goes its
 // own way, which raises what is to be raised.  Nothing is kept from one call for the next.
@@ -10,11 +10,14 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <ATen/ops/empty.h>
 #include <c10/core/Allocator.h>
 #include <c10/util/Exception.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cstdint>
+#include <new>
+#include <type_traits>
 
 #include "../../include/quasar.h"
 #include "unlocked.hpp"
@@ -36,6 +39,14 @@ decltype(&quasar_w8_linear_fused_split) p_w8_linear_fused;
 decltype(&quasar_w8_gateup_swiglu_split) p_w8_gateup_swiglu;
 decltype(&quasar_w8_fused_workspace_bytes) p_w8_fused_workspace_bytes;
 decltype(&quasar_w8_gateup_workspace_bytes) p_w8_gateup_workspace_bytes;
+decltype(&quasar_paged_prepare) p_paged_prepare;
+decltype(&quasar_paged_attention) p_paged_attention;
+decltype(&quasar_paged_attention_workspace_bytes) p_paged_attention_workspace_bytes;
+decltype(&quasar_prompt_attention) p_prompt_attention;
+decltype(&quasar_prompt_attention_workspace_bytes) p_prompt_attention_workspace_bytes;
+decltype(&quasar_pages_reserve) p_pages_reserve;
+decltype(&quasar_pages_fork) p_pages_fork;
+decltype(&quasar_pages_compact) p_pages_compact;
 PyObject *g_device, *g_stream;
 
 struct NotOrdinary {};
@@ -225,22 +236,243 @@ PyObject *w8_gateup_swiglu(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
-// (addresses of the eleven entry points, current device, current raw stream)
+// ---- the paged cache: calls on a handle, which answer with the tensor that they return in Python, else with the status or -1
+
+// What PagedKvCache holds; its tensors live as long as that object, which holds this.
+struct PagedCache {
+    long long n_layers, n_kv_heads, n_pages, page_len, max_seqs, max_pages, code, layer_bytes, workspace_bytes, device;
+    unsigned long long pool, refs, lengths, table, k_scale, v_scale;
+};
+constexpr const char *kCacheName = "quasar.PagedCache";
+
+// (the members of PagedCache in order)
+PyObject *paged_cache(PyObject *, PyObject *args) {
+    PagedCache c;
+    if (!PyArg_ParseTuple(args, "LLLLLLLLLLKKKKKK", &c.n_layers, &c.n_kv_heads, &c.n_pages, &c.page_len, &c.max_seqs, &c.max_pages, &c.code, &c.layer_bytes,
+                          &c.workspace_bytes, &c.device, &c.pool, &c.refs, &c.lengths, &c.table, &c.k_scale, &c.v_scale))
+        return nullptr;
+    auto *held = new (std::nothrow) PagedCache(c);
+    if (!held) return PyErr_NoMemory();
+    PyObject *o = PyCapsule_New(held, kCacheName, [](PyObject *o) { delete static_cast<PagedCache *>(PyCapsule_GetPointer(o, kCacheName)); });
+    if (!o) delete held;
+    return o;
+}
+template <class T> T *address(unsigned long long a) { return reinterpret_cast<T *>(static_cast<uintptr_t>(a)); }
+
+// A handle and, on its device, which is the current one, what a call is given.
+struct PagedCall {
+    const PagedCache *c;
+    explicit PagedCall(PyObject *o) {
+        if (!PyCapsule_IsValid(o, kCacheName)) throw NotOrdinary{};
+        c = static_cast<const PagedCache *>(PyCapsule_GetPointer(o, kCacheName));
+        PyObject *dev = PyObject_CallNoArgs(g_device);
+        const long now = dev ? PyLong_AsLong(dev) : -1;
+        Py_XDECREF(dev);
+        if (now != c->device) throw NotOrdinary{};
+    }
+    const at::Tensor &tensor(PyObject *o, at::ScalarType type) const {
+        const at::Tensor &t = cuda_tensor(o, type);
+        if (t.device().index() != c->device) throw NotOrdinary{};
+        return t;
+    }
+    const at::Tensor &rows(PyObject *o, int64_t width) const {
+        const at::Tensor &t = tensor(o, at::kBFloat16);
+        if (t.dim() != 2 || t.size(0) < 1 || t.size(1) != width || t.stride(1) != 1) throw NotOrdinary{};
+        return t;
+    }
+    const int32_t *per_sequence(PyObject *o) const {
+        const at::Tensor &t = tensor(o, at::kInt);
+        if (t.dim() != 1 || t.size(0) != c->max_seqs || !t.is_contiguous()) throw NotOrdinary{};
+        return static_cast<const int32_t *>(t.data_ptr());
+    }
+    int64_t layer(PyObject *o) const {
+        const int64_t v = integer(o);
+        if (v < 0 || v >= c->n_layers) throw NotOrdinary{};
+        return v;
+    }
+    const float *scale(unsigned long long at, int64_t layer) const { return at ? address<const float>(at) + layer * c->n_kv_heads : nullptr; }
+    at::Tensor fresh(at::IntArrayRef shape, at::ScalarType type) const {
+        return at::empty(shape, at::TensorOptions().dtype(type).device(at::kCUDA, static_cast<c10::DeviceIndex>(c->device)));
+    }
+};
+int64_t ld_of(const at::Tensor &t) { return t.size(0) > 1 ? t.stride(0) : t.size(1); }   // (torch gives a tensor of one row any stride)
+uint16_t *bits(const at::Tensor &t) { return static_cast<uint16_t *>(t.data_ptr()); }
+struct RowStart {
+    const int32_t *p;
+    int64_t n_seqs;
+    RowStart(const PagedCall &call, PyObject *o) {
+        const at::Tensor &t = call.tensor(o, at::kInt);
+        if (t.dim() != 1 || t.size(0) < 2 || t.size(0) > call.c->max_seqs + 1 || !t.is_contiguous()) throw NotOrdinary{};
+        p = static_cast<const int32_t *>(t.data_ptr());
+        n_seqs = t.size(0) - 1;
+    }
+};
+// the tensor that a call writes, new where none is given
+at::Tensor output(const PagedCall &call, PyObject *o, int64_t rows, int64_t width) {
+    if (o == Py_None) return call.fresh({rows, width}, at::kBFloat16);
+    const at::Tensor &t = call.rows(o, width);
+    if (t.size(0) != rows) throw NotOrdinary{};
+    return t;
+}
+// body(out) -> status; the answer is out where that is 0
+template <typename Body>
+PyObject *tensor_of(Py_ssize_t got, Py_ssize_t want, Body body) {
+    at::Tensor out;
+    long status = -1;
+    try {
+        if (got == want) status = body(out);
+        if (status == 0) {
+            PyObject *o = THPVariable_Wrap(std::move(out));
+            if (o) return o;
+            status = -1;
+        }
+    } catch (...) {
+        status = -1;
+    }
+    if (PyErr_Occurred()) PyErr_Clear();
+    return PyLong_FromLong(status);
+}
+c10::DataPtr scratch_of(size_t bytes) { return c10::GetAllocator(c10::DeviceType::CUDA)->allocate(bytes); }
+int64_t heads_of(PyObject *o) {
+    const int64_t n = integer(o);
+    if (n < 1 || n > 1 << 20) throw NotOrdinary{};
+    return n;
+}
+
+// (handle, qkv, n_q_heads, layer, row_start, q_gamma, k_gamma, eps, rope_theta, q_out)
+PyObject *paged_prepare(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return tensor_of(n, 10, [&](at::Tensor &out) {
+        const PagedCall p(a[0]);
+        const PagedCache &c = *p.c;
+        const int64_t hq = heads_of(a[2]), layer = p.layer(a[3]);
+        const at::Tensor &x = p.rows(a[1], (hq + 2 * c.n_kv_heads) * 128);
+        const RowStart starts(p, a[4]);
+        const uint16_t *gamma[2];
+        for (int i = 0; i < 2; ++i) {
+            const at::Tensor &g = p.tensor(a[5 + i], at::kBFloat16);
+            if (g.numel() != 128 || !g.is_contiguous()) throw NotOrdinary{};
+            gamma[i] = bits(g);
+        }
+        const float eps = real(a[7]), theta = real(a[8]);
+        out = output(p, a[9], x.size(0), hq * 128);
+        return call(p_paged_prepare, bits(x), x.size(0), ld_of(x), hq, c.n_kv_heads, starts.p, starts.n_seqs, gamma[0], gamma[1], eps, theta, bits(out), ld_of(out),
+                    address<void>(c.pool + layer * c.layer_bytes), c.n_pages, c.page_len, (int)c.code, p.scale(c.k_scale, layer), p.scale(c.v_scale, layer),
+                    address<const int32_t>(c.table), c.max_pages, c.max_pages, address<const int32_t>(c.lengths), current_stream());
+    });
+}
+
+// (handle, q, n_q_heads, layer, row_start, max_new, workspace, out)
+PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return tensor_of(n, 8, [&](at::Tensor &out) {
+        const PagedCall p(a[0]);
+        const PagedCache &c = *p.c;
+        const int64_t hq = heads_of(a[2]), layer = p.layer(a[3]), max_new = integer(a[5]);
+        const at::Tensor &q = p.rows(a[1], hq * 128);
+        const RowStart starts(p, a[4]);
+        out = output(p, a[7], q.size(0), hq * 128);
+        void *ws, *stream = current_stream();
+        size_t bytes;
+        c10::DataPtr scratch;
+        if (a[6] == Py_None) {
+            bytes = p_paged_attention_workspace_bytes(max_new, hq, c.n_kv_heads);
+            if (!bytes) throw NotOrdinary{};
+            scratch = scratch_of(bytes);
+            ws = scratch.get();
+        } else {
+            const at::Tensor &t = any_tensor(a[6]);
+            if (!t.is_cuda() || t.device().index() != c.device) throw NotOrdinary{};
+            ws = t.data_ptr();
+            bytes = t.nbytes();
+        }
+        return call(p_paged_attention, bits(q), q.size(0), ld_of(q), hq, c.n_kv_heads, starts.p, starts.n_seqs, max_new, address<const void>(c.pool + layer * c.layer_bytes),
+                    c.n_pages, c.page_len, (int)c.code, p.scale(c.k_scale, layer), p.scale(c.v_scale, layer), address<const int32_t>(c.table), c.max_pages, c.max_pages,
+                    address<const int32_t>(c.lengths), bits(out), ld_of(out), ws, bytes, stream);
+    });
+}
+
+// (handle, q, n_q_heads, layer, row_start, out)
+PyObject *prompt_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return tensor_of(n, 6, [&](at::Tensor &out) {
+        const PagedCall p(a[0]);
+        const PagedCache &c = *p.c;
+        const int64_t hq = heads_of(a[2]), layer = p.layer(a[3]);
+        const at::Tensor &q = p.rows(a[1], hq * 128);
+        const RowStart starts(p, a[4]);
+        out = output(p, a[5], q.size(0), hq * 128);
+        return call_with_scratch(p_prompt_attention, p_prompt_attention_workspace_bytes(q.size(0), hq, c.n_kv_heads, starts.n_seqs), current_stream(), bits(q), q.size(0),
+                                 ld_of(q), hq, c.n_kv_heads, starts.p, starts.n_seqs, address<const void>(c.pool + layer * c.layer_bytes), c.n_pages, c.page_len, (int)c.code,
+                                 p.scale(c.k_scale, layer), p.scale(c.v_scale, layer), address<const int32_t>(c.table), c.max_pages, c.max_pages,
+                                 address<const int32_t>(c.lengths), bits(out), ld_of(out));
+    });
+}
+
+// (handle, n_new)
+PyObject *pages_reserve(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return tensor_of(n, 2, [&](at::Tensor &out) {
+        const PagedCall p(a[0]);
+        const PagedCache &c = *p.c;
+        const int32_t *n_new = p.per_sequence(a[1]);
+        out = p.fresh({c.max_seqs}, at::kInt);
+        const c10::DataPtr scratch = scratch_of(c.workspace_bytes);
+        return call(p_pages_reserve, address<int32_t>(c.table), c.max_pages, c.max_seqs, c.max_pages, address<const int32_t>(c.lengths), n_new, address<int32_t>(c.refs),
+                    c.n_pages, c.page_len, static_cast<int32_t *>(out.data_ptr()), address<void>(c.pool), c.n_layers, c.n_kv_heads, (int)c.code, scratch.get(),
+                    (size_t)c.workspace_bytes, current_stream());
+    });
+}
+
+// (handle, parent, keep)
+PyObject *pages_fork(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return status_of(n, 3, [&] {
+        const PagedCall p(a[0]);
+        const PagedCache &c = *p.c;
+        return call(p_pages_fork, address<int32_t>(c.table), c.max_pages, c.max_seqs, c.max_pages, address<int32_t>(c.lengths), p.per_sequence(a[1]),
+                    a[2] == Py_None ? nullptr : p.per_sequence(a[2]), address<int32_t>(c.refs), c.n_pages, c.page_len, current_stream());
+    });
+}
+
+// (handle)
+PyObject *pages_compact(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return tensor_of(n, 1, [&](at::Tensor &out) {
+        const PagedCall p(a[0]);
+        const PagedCache &c = *p.c;
+        out = p.fresh({c.n_pages}, at::kInt);
+        const c10::DataPtr scratch = scratch_of(c.workspace_bytes);
+        return call(p_pages_compact, address<int32_t>(c.table), c.max_pages, c.max_seqs, c.max_pages, address<int32_t>(c.refs), c.n_pages, c.page_len,
+                    static_cast<int32_t *>(out.data_ptr()), address<void>(c.pool), c.n_layers, c.n_kv_heads, (int)c.code, scratch.get(), (size_t)c.workspace_bytes,
+                    current_stream());
+    });
+}
+
+// every entry point, in the order of binding.py's _NATIVE_ENTRIES
+template <typename Each> void each_entry(Each each) {
+    each(p_w8_linear); each(p_bf16_linear); each(p_w8a8_linear); each(p_w4_linear); each(p_w4_packed_bytes); each(p_w8a8_workspace_bytes);
+    each(p_w4_workspace_bytes); each(p_w8_linear_fused); each(p_w8_gateup_swiglu); each(p_w8_fused_workspace_bytes); each(p_w8_gateup_workspace_bytes);
+    each(p_paged_prepare); each(p_paged_attention); each(p_paged_attention_workspace_bytes); each(p_prompt_attention); each(p_prompt_attention_workspace_bytes);
+    each(p_pages_reserve); each(p_pages_fork); each(p_pages_compact);
+}
+Py_ssize_t entries() {
+    Py_ssize_t n = 0;
+    each_entry([&](auto &) { ++n; });
+    return n;
+}
+
+// (addresses of the entry points, current device, current raw stream)
 PyObject *bind(PyObject *, PyObject *args) {
-    unsigned long long f[11];
-    PyObject *device, *stream;
-    if (!PyArg_ParseTuple(args, "(KKKKKKKKKKK)OO", &f[0], &f[1], &f[2], &f[3], &f[4], &f[5], &f[6], &f[7], &f[8], &f[9], &f[10], &device, &stream)) return nullptr;
-    p_w8_linear = reinterpret_cast<decltype(p_w8_linear)>(f[0]);
-    p_bf16_linear = reinterpret_cast<decltype(p_bf16_linear)>(f[1]);
-    p_w8a8_linear = reinterpret_cast<decltype(p_w8a8_linear)>(f[2]);
-    p_w4_linear = reinterpret_cast<decltype(p_w4_linear)>(f[3]);
-    p_w4_packed_bytes = reinterpret_cast<decltype(p_w4_packed_bytes)>(f[4]);
-    p_w8a8_workspace_bytes = reinterpret_cast<decltype(p_w8a8_workspace_bytes)>(f[5]);
-    p_w4_workspace_bytes = reinterpret_cast<decltype(p_w4_workspace_bytes)>(f[6]);
-    p_w8_linear_fused = reinterpret_cast<decltype(p_w8_linear_fused)>(f[7]);
-    p_w8_gateup_swiglu = reinterpret_cast<decltype(p_w8_gateup_swiglu)>(f[8]);
-    p_w8_fused_workspace_bytes = reinterpret_cast<decltype(p_w8_fused_workspace_bytes)>(f[9]);
-    p_w8_gateup_workspace_bytes = reinterpret_cast<decltype(p_w8_gateup_workspace_bytes)>(f[10]);
+    PyObject *addresses, *device, *stream;
+    if (!PyArg_ParseTuple(args, "O!OO", &PyTuple_Type, &addresses, &device, &stream)) return nullptr;
+    if (PyTuple_GET_SIZE(addresses) != entries()) {
+        PyErr_SetString(PyExc_TypeError, "as many addresses as entry points");
+        return nullptr;
+    }
+    for (Py_ssize_t i = 0; i < entries(); ++i)
+        if (!PyLong_Check(PyTuple_GET_ITEM(addresses, i)) || (PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(addresses, i)), PyErr_Occurred())) {
+            if (!PyErr_Occurred()) PyErr_SetString(PyExc_TypeError, "addresses are integers");
+            return nullptr;
+        }
+    Py_ssize_t i = 0;
+    each_entry([&](auto &entry) {
+        entry = reinterpret_cast<std::decay_t<decltype(entry)>>(static_cast<uintptr_t>(PyLong_AsUnsignedLongLong(PyTuple_GET_ITEM(addresses, i++))));
+    });
     Py_INCREF(device);
     Py_INCREF(stream);
     Py_XSETREF(g_device, device);
@@ -250,15 +482,18 @@ PyObject *bind(PyObject *, PyObject *args) {
 
 // the addresses that bind() was given
 PyObject *bound(PyObject *, PyObject *) {
-    auto at = [](auto *entry) { return static_cast<unsigned long long>(reinterpret_cast<uintptr_t>(entry)); };
-    return Py_BuildValue("(KKKKKKKKKKK)", at(p_w8_linear), at(p_bf16_linear), at(p_w8a8_linear), at(p_w4_linear), at(p_w4_packed_bytes),
-                         at(p_w8a8_workspace_bytes), at(p_w4_workspace_bytes), at(p_w8_linear_fused), at(p_w8_gateup_swiglu),
-                         at(p_w8_fused_workspace_bytes), at(p_w8_gateup_workspace_bytes));
+    PyObject *t = PyTuple_New(entries());
+    if (!t) return nullptr;
+    Py_ssize_t i = 0;
+    each_entry([&](auto &entry) { PyTuple_SET_ITEM(t, i++, PyLong_FromUnsignedLongLong(static_cast<unsigned long long>(reinterpret_cast<uintptr_t>(entry)))); });
+    return t;
 }
 
 #define FAST(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {FAST(w8_linear), FAST(bf16_linear), FAST(w8a8_linear), FAST(w4_linear),
                          FAST(w8_linear_fused), FAST(w8_gateup_swiglu),
+                         FAST(paged_prepare), FAST(paged_attention), FAST(prompt_attention), FAST(pages_reserve), FAST(pages_fork), FAST(pages_compact),
+                         {"paged_cache", paged_cache, METH_VARARGS, nullptr},
                          {"bind", bind, METH_VARARGS, nullptr}, {"bound", bound, METH_NOARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

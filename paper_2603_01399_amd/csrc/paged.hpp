@@ -46,6 +46,33 @@ __device__ __forceinline__ int seq_of_row(const PagedParams &p, int t, int lane)
     return s < p.n_seqs ? s : -1;
 }
 
+// Exclusive prefix sums of v(0 .. n - 1) into out[0 .. n - 1]; the sum for all threads of the workgroup.
+template <int NW, class V>
+__device__ __forceinline__ int prefix_sums(int n, int *out, int *wave_sums, V v) {
+    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+    int carry = 0;
+    for (int i0 = 0; i0 < n; i0 += 64 * NW) {
+        const int i = i0 + tid, mine = i < n ? v(i) : 0;
+        int sum = mine;
+#pragma unroll
+        for (int off = 1; off < 64; off <<= 1) {
+            const int up = __shfl_up(sum, off, 64);
+            if (lane >= off) sum += up;
+        }
+        if (lane == 63) wave_sums[w] = sum;
+        __syncthreads();
+        int before = carry;
+#pragma unroll
+        for (int k = 0; k < NW; ++k) {
+            before += k < w ? wave_sums[k] : 0;
+            carry += wave_sums[k];
+        }
+        if (i < n) out[i] = before + sum - mine;
+        __syncthreads();
+    }
+    return carry;
+}
+
 template <int KV> __device__ __forceinline__ int k_page_index(int pib, int d) {
     if constexpr (KV == KV_BF16) return (int)k_cache_index(pib, d);
     return (((((pib >> 4) * 2 + (d >> 6)) * 4 + ((d & 31) >> 3)) * 16 + (pib & 15)) * 2 + ((d >> 5) & 1)) * 8 + (d & 7);
@@ -108,8 +135,52 @@ struct PrepareParams {
     int parts;                // waves that share a row's heads
 };
 
-// One wave takes four heads at a time, 16 lanes of 16 bytes each: lane 16 h + j holds d = 8 j .. 8 j + 7, its rotary partner
-// (d +- 64) is lane j ^ 8.
+// What a lane does with its eight elements of a head, d = 8 j .. 8 j + 7, of lanes 16 h + j: the norm with its two roundings to bf16, then the
+// rotation; the rotary partner (d +- 64) is lane j ^ 8.  sinv is negative in the first half (x1 cos - x2 sin).
+__device__ __forceinline__ u32x4 norm_and_rotate(const u32x4 raw, const u32x4 graw, float eps, const float (&cosv)[8], const float (&sinv)[8]) {
+    float x[8], o[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[2 * e] = __uint_as_float(raw[e] << 16);
+        x[2 * e + 1] = __uint_as_float(raw[e] & 0xFFFF0000u);
+    }
+    float ss = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ss += x[e] * x[e];
+#pragma unroll
+    for (int off = 8; off >= 1; off >>= 1) ss += __shfl_xor(ss, off, 64);
+    const float r = __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(ss, (float)kHeadDim) + eps));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const unsigned int n = float2_to_bf16_pair(x[2 * e] * r, x[2 * e + 1] * r);
+        const unsigned int g = float2_to_bf16_pair(__uint_as_float(n << 16) * __uint_as_float(graw[e] << 16),
+                                                   __uint_as_float(n & 0xFFFF0000u) * __uint_as_float(graw[e] & 0xFFFF0000u));
+        const unsigned int other = __shfl_xor(g, 8, 64);
+        o[2 * e] = __uint_as_float(g << 16) * cosv[2 * e] + __uint_as_float(other << 16) * sinv[2 * e];
+        o[2 * e + 1] = __uint_as_float(g & 0xFFFF0000u) * cosv[2 * e + 1] + __uint_as_float(other & 0xFFFF0000u) * sinv[2 * e + 1];
+    }
+    return u32x4{float2_to_bf16_pair(o[0], o[1]), float2_to_bf16_pair(o[2], o[3]), float2_to_bf16_pair(o[4], o[5]), float2_to_bf16_pair(o[6], o[7])};
+}
+
+// eight bf16 -> eight codes of value / scale
+__device__ __forceinline__ u32x2 e4m3_codes(const u32x4 v, float scale) {
+    float f[8];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        f[2 * e] = __fdiv_rn(__uint_as_float(v[e] << 16), scale);
+        f[2 * e + 1] = __fdiv_rn(__uint_as_float(v[e] & 0xFFFF0000u), scale);
+    }
+    return u32x2{floats_to_e4m3x4(f[0], f[1], f[2], f[3]), floats_to_e4m3x4(f[4], f[5], f[6], f[7])};
+}
+
+// theta^(-2 i / 128) / 2 pi: an angle in turns, reduced in double by rotation(): positions reach tens of thousands of radians
+__device__ __forceinline__ double turns_per_position(double log2_theta, int i) { return exp2(-(2.0 * i / kHeadDim) * log2_theta) * 0.15915494309189535; }
+__device__ __forceinline__ void rotation(int pos, double per_position, float &sn, float &cs) {
+    const double turns = (double)pos * per_position;
+    sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cs);
+}
+
+// For few rows a sequence: a wave takes four heads of a row at a time, 16 lanes of 16 bytes each.
 template <int KV>
 __global__ __launch_bounds__(256) void paged_prepare_kernel(const PrepareParams p) {
     const PagedParams &c = p.c;
@@ -122,17 +193,15 @@ __global__ __launch_bounds__(256) void paged_prepare_kernel(const PrepareParams 
     const SeqSpan sp = seq_span(c, s);
     if (t < sp.row0 || t >= sp.row0 + sp.n) return;
     const int pos = sp.len + t - sp.row0;
-    // the angle in turns, reduced in double: positions reach tens of thousands of radians
     const int j = lane & 15;
-    const double turns = (double)pos * exp2(-(2.0 * lane / kHeadDim) * p.log2_theta) * 0.15915494309189535;
     float sn, cs;
-    sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cs);
+    rotation(pos, turns_per_position(p.log2_theta, lane), sn, cs);
     float cosv[8], sinv[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) {
         cosv[e] = __shfl(cs, 8 * (j & 7) + e, 64);
         sinv[e] = __shfl(sn, 8 * (j & 7) + e, 64);
-        if (j < 8) sinv[e] = -sinv[e];                       // first half: x1 cos - x2 sin
+        if (j < 8) sinv[e] = -sinv[e];
     }
     const int blk = pos / kKvBlock, pib = pos % kKvBlock, col = blk >> c.block_shift;
     const int page = col < c.columns ? c.table[s * c.table_ld + col] : -1;
@@ -145,33 +214,11 @@ __global__ __launch_bounds__(256) void paged_prepare_kernel(const PrepareParams 
         const bool live = h < heads;
         u32x4 raw = {0u, 0u, 0u, 0u};
         if (live) raw = *reinterpret_cast<const u32x4 *>(p.qkv + t * p.ld + (long long)h * kHeadDim + 8 * j);
-        float x[8], o[8];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            x[2 * e] = __uint_as_float(raw[e] << 16);
-            x[2 * e + 1] = __uint_as_float(raw[e] & 0xFFFF0000u);
-        }
-        float ss = 0.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) ss += x[e] * x[e];
-#pragma unroll
-        for (int off = 8; off >= 1; off >>= 1) ss += __shfl_xor(ss, off, 64);
-        const float r = __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(ss, (float)kHeadDim) + p.eps));
         const u32x4 graw = *reinterpret_cast<const u32x4 *>((h < c.Hq ? p.q_gamma : p.k_gamma) + 8 * j);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const float g = e & 1 ? __uint_as_float(graw[e >> 1] & 0xFFFF0000u) : __uint_as_float(graw[e >> 1] << 16);
-            const float n = bf16_bits_to_float(float_to_bf16_bits(bf16_bits_to_float(float_to_bf16_bits(x[e] * r)) * g));
-            const float other = __shfl_xor(n, 8, 64);
-            o[e] = n * cosv[e] + other * sinv[e];
-        }
+        const u32x4 turned = norm_and_rotate(raw, graw, p.eps, cosv, sinv);      // (all lanes: it exchanges)
         if (!live) continue;
         const bool value = h >= c.Hq + c.Hkv;
-        u32x4 rounded = raw;                                    // (values are stored as they are)
-        if (!value) {
-#pragma unroll
-            for (int e = 0; e < 4; ++e) rounded[e] = float2_to_bf16_pair(o[2 * e], o[2 * e + 1]);
-        }
+        const u32x4 rounded = value ? raw : turned;                              // (values are stored as they are)
         if (h < c.Hq) {
             *reinterpret_cast<u32x4 *>(p.q_out + t * p.ldq + (long long)h * kHeadDim + 8 * j) = rounded;
             continue;
@@ -189,14 +236,7 @@ __global__ __launch_bounds__(256) void paged_prepare_kernel(const PrepareParams 
             }
         } else {
             const float *scale = value ? c.v_scale : c.k_scale;
-            const float sc = scale ? scale[hk] : 1.0f;
-            float f[8];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                f[2 * e] = __fdiv_rn(__uint_as_float(rounded[e] << 16), sc);
-                f[2 * e + 1] = __fdiv_rn(__uint_as_float(rounded[e] & 0xFFFF0000u), sc);
-            }
-            const u32x2 codes = {floats_to_e4m3x4(f[0], f[1], f[2], f[3]), floats_to_e4m3x4(f[4], f[5], f[6], f[7])};
+            const u32x2 codes = e4m3_codes(rounded, scale ? scale[hk] : 1.0f);
             if (!value) {
                 *reinterpret_cast<u32x2 *>(dst + k_page_index<KV>(pib, 8 * j)) = codes;
             } else {
@@ -204,6 +244,120 @@ __global__ __launch_bounds__(256) void paged_prepare_kernel(const PrepareParams 
                 for (int e = 0; e < 8; ++e) dst[v_page_index<KV>(pib, 8 * j + e)] = (unsigned char)(codes[e >> 2] >> (8 * (e & 3)));
             }
         }
+    }
+}
+
+// For many rows a sequence: a workgroup takes the new rows of one block of 32 positions and kPrepareHeads heads.  The rotations of
+// the block are computed once, in LDS; a value head goes through LDS too, since its 16-byte units hold eight positions of one d: written
+// one by one they cost 2 bytes of every 16 a store.
+constexpr int kPrepareHeads = 8;
+
+template <int KV>
+__global__ __launch_bounds__(256) void paged_prepare_block_kernel(const PrepareParams p) {
+    constexpr int BB = kv_block_bytes<KV>, STRIDE = kHeadDim + 8;                // (of a row of the values in LDS)
+    __shared__ float2 turned[kKvBlock][kHeadDim / 2];
+    __shared__ __align__(16) uint16_t rows[2][kKvBlock][STRIDE];
+    __shared__ int prefix[kMaxSeqs];
+    __shared__ int wave_sums[4];
+    const PagedParams &c = p.c;
+    const int tid = threadIdx.x, lane = tid & 63, j = tid & 15, r0 = tid >> 4;
+    const double per_position = turns_per_position(p.log2_theta, lane);
+
+    auto blocks_with_rows = [&](int s) {
+        const SeqSpan a = seq_span(c, s);
+        return a.n ? (a.len + a.n - 1) / kKvBlock - a.len / kKvBlock + 1 : 0;
+    };
+    const int units = prefix_sums<4>(c.n_seqs, prefix, wave_sums, blocks_with_rows);
+    const int u = blockIdx.x;
+    if (u >= units) return;
+    int s = 0;
+    for (int up = c.n_seqs; up - s > 1;) {
+        const int mid = (s + up) >> 1;
+        if (prefix[mid] <= u) s = mid; else up = mid;
+    }
+    const SeqSpan a = seq_span(c, s);
+    const int blk = a.len / kKvBlock + u - prefix[s], pos0 = blk * kKvBlock, column = blk >> c.block_shift;
+    const int lo = a.len - pos0, hi = a.len + a.n - pos0;                        // rows lo .. hi - 1 of the block are new
+    const int page = column < c.columns ? c.table[s * c.table_ld + column] : -1;
+    const bool stored = page_exists(page, c.n_pages);
+    const long long base = stored ? ((((long long)page * c.Hkv) << c.block_shift) + (blk & ((1 << c.block_shift) - 1))) * (2 * BB) : 0;
+    const long long head_step = (long long)(2 * BB) << c.block_shift;
+    const int h0 = blockIdx.y * kPrepareHeads, h1 = min(h0 + kPrepareHeads, c.Hq + 2 * c.Hkv);
+    auto is_new = [&](int r) { return r >= lo && r < hi; };
+    auto row_of = [&](int r) { return (long long)(a.row0 + pos0 + r - a.len); };
+    auto load = [&](int h, int i) {
+        const int r = r0 + 16 * i;
+        return is_new(r) ? *reinterpret_cast<const u32x4 *>(p.qkv + row_of(r) * p.ld + (long long)h * kHeadDim + 8 * j) : u32x4{0u, 0u, 0u, 0u};
+    };
+    u32x4 x[2] = {load(h0, 0), load(h0, 1)};
+    float cosv[2][8], sinv[2][8];
+    if (h0 < c.Hq + c.Hkv) {
+        for (int r = tid >> 6; r < kKvBlock; r += 4) {
+            float sn, cs;
+            rotation(pos0 + r, per_position, sn, cs);
+            turned[r][lane] = float2{cs, sn};
+        }
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float2 v = turned[r0 + 16 * i][8 * (j & 7) + e];
+                cosv[i][e] = v.x;
+                sinv[i][e] = j < 8 ? -v.y : v.y;
+            }
+    }
+    for (int h = h0; h < h1; ++h) {
+        u32x4 next[2];
+        if (h + 1 < h1) { next[0] = load(h + 1, 0); next[1] = load(h + 1, 1); }
+        if (h < c.Hq + c.Hkv) {
+            const u32x4 graw = *reinterpret_cast<const u32x4 *>((h < c.Hq ? p.q_gamma : p.k_gamma) + 8 * j);
+            const float sc = KV == KV_E4M3 && h >= c.Hq && c.k_scale ? c.k_scale[h - c.Hq] : 1.0f;
+            unsigned char *dst = c.pages + base + (h - c.Hq) * head_step;
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const int r = r0 + 16 * i;
+                const u32x4 o = norm_and_rotate(x[i], graw, p.eps, cosv[i], sinv[i]);
+                if (!is_new(r)) continue;
+                if (h < c.Hq) *reinterpret_cast<u32x4 *>(p.q_out + row_of(r) * p.ldq + (long long)h * kHeadDim + 8 * j) = o;
+                else if (!stored) continue;
+                else if constexpr (KV == KV_BF16) *reinterpret_cast<u32x4 *>(dst + 2 * k_page_index<KV>(r, 8 * j)) = o;
+                else *reinterpret_cast<u32x2 *>(dst + k_page_index<KV>(r, 8 * j)) = e4m3_codes(o, sc);
+            }
+        } else {
+            const int hk = h - c.Hq - c.Hkv, buf = h & 1;                        // (two buffers: a barrier a head is enough)
+#pragma unroll
+            for (int i = 0; i < 2; ++i) *reinterpret_cast<u32x4 *>(&rows[buf][r0 + 16 * i][8 * j]) = x[i];
+            __syncthreads();
+            const float sc = KV == KV_E4M3 && c.v_scale ? c.v_scale[hk] : 1.0f;
+            unsigned char *dst = c.pages + base + hk * head_step + BB;
+            if (stored)
+                for (int i = 0; i < 2; ++i) {
+                    // unit (d, g4): positions 4 g4 .. + 3 and 16 + 4 g4 .. + 3 of one d
+                    const int at = tid + 256 * i, d = (at >> 6) * 16 + (at & 15), g4 = (at >> 4) & 3;
+                    u32x4 v;
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int pos = 4 * g4 + 2 * (k & 1) + 16 * (k >> 1);
+                        v[k] = rows[buf][pos][d] | (unsigned int)rows[buf][pos + 1][d] << 16;
+                    }
+                    const u32x2 codes = KV == KV_E4M3 ? e4m3_codes(v, sc) : u32x2{0u, 0u};
+                    unsigned char *to = dst + (KV == KV_E4M3 ? 1 : 2) * v_page_index<KV>(4 * g4, d);
+                    if (lo <= 0 && hi >= kKvBlock) {
+                        if constexpr (KV == KV_BF16) *reinterpret_cast<u32x4 *>(to) = v;
+                        else *reinterpret_cast<u32x2 *>(to) = codes;
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 8; ++k) {
+                            if (!is_new(4 * g4 + (k & 3) + 16 * (k >> 2))) continue;
+                            if constexpr (KV == KV_BF16) *reinterpret_cast<uint16_t *>(to + 2 * k) = (uint16_t)(v[k >> 1] >> (16 * (k & 1)));
+                            else to[k] = (unsigned char)(codes[k >> 2] >> (8 * (k & 3)));
+                        }
+                    }
+                }
+        }
+        x[0] = next[0];
+        x[1] = next[1];
     }
 }
 

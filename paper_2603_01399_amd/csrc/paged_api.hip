@@ -88,6 +88,7 @@ int check_cache(const CacheArgs &a, PagedParams &p) {
     p.block_shift = block_shift_of(a.page_len);
     return QUASAR_OK;
 }
+constexpr int kBlockRows = 16;
 constexpr int kFlatRounds = 1, kFlatPositions = 1024;
 constexpr float kScaleLog2 = 1.4426950408889634f / 11.313708498984761f;      // log2(e) / sqrt(128)
 
@@ -208,12 +209,19 @@ int quasar_paged_prepare(const uint16_t *qkv, int64_t T, int64_t ld, int64_t n_q
     p.qkv = qkv; p.q_gamma = q_gamma; p.k_gamma = k_gamma; p.q_out = q_out;
     p.ld = ld; p.ldq = ldq; p.eps = eps;
     p.log2_theta = std::log2((double)rope_theta);
-    const int64_t quads = (n_q_heads + 2 * n_kv_heads + 3) / 4;
+    hipStream_t st = static_cast<hipStream_t>(hip_stream);
+    const int64_t heads = n_q_heads + 2 * n_kv_heads;
+    if (T >= kBlockRows * n_seqs) {
+        const dim3 grid((unsigned int)(T / kKvBlock + 2 * n_seqs), (unsigned int)((heads + kPrepareHeads - 1) / kPrepareHeads));   // (two ragged blocks a sequence)
+        if (kv_type(kv_dtype) == KV_BF16) hipLaunchKernelGGL(paged_prepare_block_kernel<KV_BF16>, grid, dim3(256), 0, st, p);
+        else hipLaunchKernelGGL(paged_prepare_block_kernel<KV_E4M3>, grid, dim3(256), 0, st, p);
+        return launched();
+    }
+    const int64_t quads = (heads + 3) / 4;
     int64_t parts = 4096 / T;
     parts = parts < 1 ? 1 : parts > quads ? quads : parts;
     p.parts = (int)parts;
     const dim3 grid((unsigned int)((T * parts + 3) / 4));
-    hipStream_t st = static_cast<hipStream_t>(hip_stream);
     if (kv_type(kv_dtype) == KV_BF16) hipLaunchKernelGGL(paged_prepare_kernel<KV_BF16>, grid, dim3(256), 0, st, p);
     else hipLaunchKernelGGL(paged_prepare_kernel<KV_E4M3>, grid, dim3(256), 0, st, p);
     return launched();

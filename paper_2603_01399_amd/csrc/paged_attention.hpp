@@ -34,36 +34,14 @@ constexpr int kMaxWorkers = 512;             // of a kv head
 // Prefix sums of the sequences' blocks into lds[0 .. n_seqs] (exclusive; the total at the end).  `row_group`: sequences without
 // rows in this group have none.
 __device__ __forceinline__ int scan_blocks(const PagedAttnParams &p, int row_group, int *lds, int *wave_sums) {
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    int carry = 0;
-    for (int s0 = 0; s0 < p.c.n_seqs; s0 += 64 * kPagedWaves) {
-        const int s = s0 + tid;
-        int nb = 0;
-        if (s < p.c.n_seqs) {
-            const SeqSpan a = seq_span(p.c, s);
-            const int n = a.n < p.max_new ? a.n : p.max_new;
-            if (n * p.c.G > p.group_rows * row_group) nb = blocks_of(p.c, a.len + n);
-        }
-        int sum = nb;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const int up = __shfl_up(sum, off, 64);
-            if (lane >= off) sum += up;
-        }
-        if (lane == 63) wave_sums[w] = sum;
-        __syncthreads();
-        int before = carry;
-#pragma unroll
-        for (int i = 0; i < kPagedWaves; ++i) {
-            before += i < w ? wave_sums[i] : 0;
-            carry += wave_sums[i];
-        }
-        if (s < p.c.n_seqs) lds[s] = before + sum - nb;
-        __syncthreads();
-    }
-    if (tid == 0) lds[p.c.n_seqs] = carry;
+    const int total = prefix_sums<kPagedWaves>(p.c.n_seqs, lds, wave_sums, [&](int s) {
+        const SeqSpan a = seq_span(p.c, s);
+        const int n = a.n < p.max_new ? a.n : p.max_new;
+        return n * p.c.G > p.group_rows * row_group ? blocks_of(p.c, a.len + n) : 0;
+    });
+    if (threadIdx.x == 0) lds[p.c.n_seqs] = total;
     __syncthreads();
-    return carry;
+    return total;
 }
 
 template <int KV, int NQT>

@@ -55,32 +55,6 @@ __device__ __forceinline__ PromptTile prompt_tile(const PagedParams &c, const in
     return t;
 }
 
-// Exclusive prefix sums of v(0 .. n - 1) into out[0 .. n - 1]; the sum for all threads of the workgroup.
-template <int NW, class V>
-__device__ __forceinline__ int prefix_sums(int n, int *out, int *wave_sums, V v) {
-    const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-    int carry = 0;
-    for (int i0 = 0; i0 < n; i0 += 64 * NW) {
-        const int i = i0 + tid, mine = i < n ? v(i) : 0;
-        int sum = mine;
-#pragma unroll
-        for (int off = 1; off < 64; off <<= 1) {
-            const int up = __shfl_up(sum, off, 64);
-            if (lane >= off) sum += up;
-        }
-        if (lane == 63) wave_sums[w] = sum;
-        __syncthreads();
-        int before = carry;
-#pragma unroll
-        for (int k = 0; k < NW; ++k) {
-            before += k < w ? wave_sums[k] : 0;
-            carry += wave_sums[k];
-        }
-        if (i < n) out[i] = before + sum - mine;
-        __syncthreads();
-    }
-    return carry;
-}
 constexpr int kPromptStep = 64;                          // positions in LDS at a time
 constexpr int kPromptStepBytes = kPromptStep / kKvBlock * 2 * kKvBlockBytes;   // 32 KB: two blocks, keys and values
 

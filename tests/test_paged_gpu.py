@@ -493,12 +493,53 @@ def test_another_device_is_refused(qb, monkeypatch):
     """Launches go to the current device: tensors of another one are refused (here: another device is made current in name)."""
     say("other device")
     b = Batch(qb, "bf16", 32, 4, 2, [30], [2], seed=90)
+    q, n, g, qkv = b.q(), i32_to_dev([1]), torch.ones(D, dtype=torch.bfloat16, device="cuda"), torch.zeros((2, 8 * D), dtype=torch.bfloat16, device="cuda")
+    addresses = qb._native_addresses(qb.lib())
     monkeypatch.setattr(qb, "_current_device", lambda: 1)
-    n = i32_to_dev([1])
-    for call in (lambda: qb.paged_attention(b.q(), 4, b.cache, 0, b.row_start, 2), lambda: qb.prompt_attention(b.q(), 4, b.cache, 0, b.row_start),
-                 lambda: b.cache.reserve(n), lambda: b.cache.fork(n), lambda: b.cache.compact()):
-        with pytest.raises(ValueError, match="current device"):
-            call()
+    qb._fast.bind(addresses, lambda: 1, qb._current_raw_stream)
+    try:
+        for call in (lambda: qb.paged_attention(q, 4, b.cache, 0, b.row_start, 2), lambda: qb.prompt_attention(q, 4, b.cache, 0, b.row_start),
+                     lambda: qb.paged_prepare(qkv, 4, b.cache, 0, b.row_start, g, g), lambda: b.cache.reserve(n), lambda: b.cache.fork(n), lambda: b.cache.compact()):
+            with pytest.raises(ValueError, match="current device"):
+                call()
+    finally:
+        monkeypatch.undo()
+        qb._fast.bind(addresses, qb._current_device, qb._current_raw_stream)
+
+
+def test_native_and_python_marshalling_give_the_same(qb, monkeypatch):
+    """Every call on a handle answers as the Python path does: same bits, same output tensors, the same errors of the library."""
+    say("marshalling")
+    b = Batch(qb, "e4m3", 32, 4, 2, [30, 3, 100], [2, 1, 2], seed=92, layers=2, layer=1)
+    g = torch.ones(D, dtype=torch.bfloat16, device="cuda")
+    qkv = bf16_to_dev(rnd_bits((5, 8 * D), 93))
+    out, ws = torch.empty((5, 4 * D), dtype=torch.bfloat16, device="cuda"), torch.empty(qb.lib().quasar_paged_attention_workspace_bytes(2, 4, 2), dtype=torch.uint8, device="cuda")
+    n_new, parent, keep = i32_to_dev([2, 40, 0]), i32_to_dev([1, 1, -1]), i32_to_dev([2, 9, 9])
+    saved, pool = b.cache.books.clone(), b.cache.pool.view(torch.uint8).clone()
+
+    def calls():
+        b.cache.books.copy_(saved)
+        b.cache.pool.view(torch.uint8).copy_(pool)
+        q = qb.paged_prepare(qkv, 4, b.cache, 1, b.row_start, g, g, eps=1e-5, rope_theta=1e4)
+        assert qb.paged_prepare(qkv, 4, b.cache, 1, b.row_start, g, g, q_out=out) is out
+        got = [q, out.clone(), qb.paged_attention(q, 4, b.cache, 1, b.row_start, 2), qb.prompt_attention(q, 4, b.cache, 1, b.row_start)]
+        assert qb.paged_attention(q, 4, b.cache, 1, b.row_start, 2, workspace=ws, out=out) is out
+        got.append(out.clone())
+        assert qb.prompt_attention(q[:1], 4, b.cache, 0, i32_to_dev([0, 1]), out=out[:1]).shape == (1, 4 * D)
+        got += [out.clone(), b.cache.reserve(n_new), b.cache.books.clone()]
+        assert b.cache.fork(parent, keep) is None
+        got += [b.cache.books.clone(), b.cache.compact(), b.cache.books.clone(), b.cache.pool.view(torch.uint8).clone()]
+        for bad in (lambda: qb.paged_attention(q, 4, b.cache, 1, b.row_start, 33), lambda: qb.paged_prepare(qkv, 4, b.cache, 1, b.row_start, g, g, eps=2.0),
+                    lambda: qb.paged_attention(q, 4, b.cache, 1, b.row_start, 2, workspace=ws[:64])):
+            with pytest.raises(qb.QuasarError):
+                bad()
+        return [t.view(torch.int16) if t.dtype == torch.bfloat16 else t for t in got]
+
+    native = calls()
+    for name in ("paged_prepare", "paged_attention", "prompt_attention", "pages_reserve", "pages_fork", "pages_compact"):
+        monkeypatch.setattr(qb._fast, name, lambda *a: -1)
+    for x, y in zip(native, calls()):
+        assert torch.equal(x, y)
 
 
 def test_refusals_of_the_binding(qb):
