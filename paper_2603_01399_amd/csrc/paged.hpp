@@ -132,7 +132,7 @@ struct PrepareParams {
     long long ld, ldq;
     float eps;
     double log2_theta;
-    int parts;                // waves that share a row's heads
+    int parts;                // waves that share a row's heads; heads of a workgroup in the block form
 };
 
 // What a lane does with its eight elements of a head, d = 8 j .. 8 j + 7, of lanes 16 h + j: the norm with its two roundings to bf16, then the
@@ -247,11 +247,9 @@ __global__ __launch_bounds__(256) void paged_prepare_kernel(const PrepareParams 
     }
 }
 
-// For many rows a sequence: a workgroup takes the new rows of one block of 32 positions and kPrepareHeads heads.  The rotations of
+// For many rows a sequence: a workgroup takes the new rows of one block of 32 positions and p.parts heads.  The rotations of
 // the block are computed once, in LDS; a value head goes through LDS too, since its 16-byte units hold eight positions of one d: written
 // one by one they cost 2 bytes of every 16 a store.
-constexpr int kPrepareHeads = 8;
-
 template <int KV>
 __global__ __launch_bounds__(256) void paged_prepare_block_kernel(const PrepareParams p) {
     constexpr int BB = kv_block_bytes<KV>, STRIDE = kHeadDim + 8;                // (of a row of the values in LDS)
@@ -282,7 +280,7 @@ __global__ __launch_bounds__(256) void paged_prepare_block_kernel(const PrepareP
     const bool stored = page_exists(page, c.n_pages);
     const long long base = stored ? ((((long long)page * c.Hkv) << c.block_shift) + (blk & ((1 << c.block_shift) - 1))) * (2 * BB) : 0;
     const long long head_step = (long long)(2 * BB) << c.block_shift;
-    const int h0 = blockIdx.y * kPrepareHeads, h1 = min(h0 + kPrepareHeads, c.Hq + 2 * c.Hkv);
+    const int h0 = blockIdx.y * p.parts, h1 = min(h0 + p.parts, c.Hq + 2 * c.Hkv);
     auto is_new = [&](int r) { return r >= lo && r < hi; };
     auto row_of = [&](int r) { return (long long)(a.row0 + pos0 + r - a.len); };
     auto load = [&](int h, int i) {
