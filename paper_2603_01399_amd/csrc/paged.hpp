@@ -31,9 +31,14 @@ struct PagedParams {
     long long table_ld;
     int T, n_seqs, n_pages, columns, Hkv, Hq, G;
     int block_shift;          // log2 of the blocks of a page
+    int max_new;              // rows of a sequence that the call takes
 };
 
-__device__ __forceinline__ SeqSpan seq_span(const PagedParams &p, int s) { return span_of(p.row_start[s], p.row_start[s + 1], p.lengths[s], p.T); }
+__device__ __forceinline__ SeqSpan seq_span(const PagedParams &p, int s) {
+    SeqSpan a = span_of(p.row_start[s], p.row_start[s + 1], p.lengths[s], p.T);
+    a.n = a.n < p.max_new ? a.n : p.max_new;
+    return a;
+}
 __device__ __forceinline__ int blocks_of(const PagedParams &p, int total) { return blocks_reached(total, p.columns, p.block_shift); }
 
 // Sequence of packed row t (-1 behind the last one): how many sequences end at or before it.
@@ -115,10 +120,40 @@ __device__ __forceinline__ float max_halves(float x) {
     return larger(__uint_as_float(r[0]), __uint_as_float(r[1]));
 }
 
-// sum + both bf16 of a pair, in fp32: sums are taken of the rounded weights, so that the weights that are applied sum to one
-__device__ __forceinline__ float add_bf16_pair(unsigned int pair, float sum) {
-    typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-    return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3F803F80u), sum, false);
+// Weights and values meet in the second product in 16 bits.  bf16 pages: bf16, the weights rounded to 8 significant bits.  e4m3 pages: fp16, which
+// holds their values exactly and the weights to 11 bits; weights are scaled by 2^7 there, so that with kLazyMax they end at 2^15 and what
+// is lost below the smallest fp16, 2^-24, is 2^-31 of the largest.  (Sums carry the same factor: it cancels.)
+template <int KV> constexpr float kWeightShift = KV == KV_E4M3 ? 7.f : 0.f;
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+template <int KV> __device__ __forceinline__ unsigned int weight_pair(float lo, float hi) {
+    if constexpr (KV == KV_BF16) return float2_to_bf16_pair(lo, hi);
+    else return __builtin_bit_cast(unsigned int, __builtin_convertvector(f32x2{lo, hi}, f16x2));
+}
+// sum + both weights of a pair, in fp32: sums are taken of the rounded weights, so that the weights that are applied sum to one
+template <int KV> __device__ __forceinline__ float add_pair(unsigned int pair, float sum) {
+    if constexpr (KV == KV_BF16) return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, pair), __builtin_bit_cast(bf16x2, 0x3F803F80u), sum, false);
+    else return __builtin_amdgcn_fdot2(__builtin_bit_cast(f16x2, pair), f16x2{(_Float16)1.0f, (_Float16)1.0f}, sum, false);
+}
+// eight e4m3 codes -> eight fp16, exactly
+__device__ __forceinline__ u32x4 e4m3x8_to_f16(unsigned int lo, unsigned int hi) {
+    u32x4 r;
+    r.x = __builtin_bit_cast(unsigned int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false));
+    r.y = __builtin_bit_cast(unsigned int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true));
+    r.z = __builtin_bit_cast(unsigned int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false));
+    r.w = __builtin_bit_cast(unsigned int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true));
+    return r;
+}
+template <int KV> __device__ __forceinline__ f32x16 values_times_weights(const u32x4 v, const u32x4 w, const f32x16 acc) {
+    if constexpr (KV == KV_BF16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, w), acc, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, w), acc, 0, 0, 0);
+}
+template <int KV> __device__ __forceinline__ f32x4 values_times_weights(const u32x4 v, const u32x4 w, const f32x4 acc) {
+    if constexpr (KV == KV_BF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, w), acc, 0, 0, 0);
+    else return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, w), acc, 0, 0, 0);
 }
 
 // ---------------------------------------------------------------------------------------------

@@ -86,86 +86,98 @@ int check_cache(const CacheArgs &a, PagedParams &p) {
     p.T = (int)a.T; p.n_seqs = (int)a.n_seqs; p.n_pages = (int)a.n_pages; p.columns = (int)a.max_pages;
     p.Hkv = (int)a.Hkv; p.Hq = (int)a.Hq; p.G = (int)(a.Hq / a.Hkv);
     p.block_shift = block_shift_of(a.page_len);
+    p.max_new = kMaxPositions;
     return QUASAR_OK;
 }
 // New rows a sequence, on average, from which the append goes block by block: 40 sequences of up to 90 rows of 32 / 8 heads in 8-bit pages
 // 22.4 us row by row and 24 to 31 by blocks, 11 of up to 1531 88 and 57.
 constexpr int kBlockRows = 64;
-constexpr int kFlatRounds = 1, kFlatPositions = 1024;
+constexpr int kStepLeast = 2, kPromptLeast = 4;
+constexpr int kFlatPositions = 1024;
 constexpr float kScaleLog2 = 1.4426950408889634f / 11.313708498984761f;      // log2(e) / sqrt(128)
 
-// ---- attention of a step: workers of a kv head, query tiles and groups of rows.  Up to 16 rows of a sequence and kv head take the 16 x 16
-// products; more take the 32 x 32 ones, but bf16 pages up to 32 rows: 16 sequences of 8 tokens over up to 4000 positions, 32 / 8 heads
-// 45.2 us narrow and 61 wide, 8-bit pages 36.4 and 30.4; 8 of 16 tokens over 8000 in bf16 65.7 (four narrow tiles) and 55.8.
-struct StepShape { int NQT, groups, workers; bool wide; size_t part_o, part_ml, pieces; };
-bool step_shape(int64_t max_new, int64_t Hq, int64_t Hkv, int kv, StepShape &a) {
+// ---- what the attention calls share of a launch: workgroups of a kv head, and the room for what they leave of shared sequences or tiles
+struct FlatShape {
+    int64_t tiles;            // of rows, at most (prompts)
+    int workers;              // 0: nothing is shared
+    size_t part_o, part_ml, pieces;
+    size_t bytes() const { return part_o + part_ml + pieces; }
+    void room(int64_t wanted, int64_t parts_each /* 16-byte-a-lane parts of a slot */, int64_t stats_each /* bytes */, int64_t Hkv) {
+        workers = (int)(wanted < 1 ? 1 : wanted > kMaxWorkers ? kMaxWorkers : wanted);
+        const size_t slots = (size_t)Hkv * 2 * workers;
+        part_o = slots * parts_each * 64 * 16;
+        part_ml = slots * stats_each;
+        pieces = (size_t)workers * 16;
+    }
+};
+
+// ---- attention of a step.  Up to 32 rows of a sequence and kv head take the 16 x 16 products, more the kernel of prompts, whose tiles have 64
+// or 128 rows: 16 sequences of 8 tokens over up to 4000 positions, 32 / 8 heads (32 rows), 44.5 us in tiles of 16 and 61 in tiles of 32; 8
+// of 16 tokens over 8000 (64 rows) 65.7 and 48.5.
+struct StepShape {
+    int NQT;                  // 16-row tiles; 0: the kernel of prompts with PW
+    int PW;
+    FlatShape flat;
+};
+bool step_shape(int64_t max_new, int64_t Hq, int64_t Hkv, int64_t n_seqs, StepShape &a) {
     if (max_new < 1 || max_new > 32 || check_heads(Hq, Hkv)) return false;
-    const int64_t R = max_new * (Hq / Hkv);
+    const int64_t R = max_new * (Hq / Hkv), cus = compute_units();
     if (R > 1024) return false;
-    a.NQT = R <= 16 ? 1 : R <= 32 ? 2 : R <= 64 ? 4 : 8;
-    a.wide = a.NQT > 2 || (a.NQT == 2 && kv == KV_E4M3);
-    a.groups = (int)((R + 16 * a.NQT - 1) / (16 * a.NQT));
-    const int64_t per = (a.wide ? 2 : 1) * (int64_t)compute_units() / (Hkv * a.groups);      // as many workgroups as are on the GPU at once
-    a.workers = (int)(per < 1 ? 1 : per > kMaxWorkers ? kMaxWorkers : per);
-    const size_t slots = (size_t)a.groups * Hkv * 2 * a.workers * a.NQT;
-    a.part_o = slots * 8 * 64 * 16;
-    a.part_ml = slots * 16 * 2 * 4;
-    a.pieces = (size_t)a.groups * a.workers * 16;
+    a = StepShape{};
+    a.NQT = R <= 16 ? 1 : R <= 32 ? 2 : 0;
+    if (a.NQT) {
+        a.flat.room(cus / Hkv, a.NQT * 8, a.NQT * 16 * 8, Hkv);
+        return true;
+    }
+    a.PW = R <= 64 ? 2 : 1;
+    const int rw = kPromptWaves / a.PW;
+    a.flat.tiles = n_seqs * ((R + 32 * rw - 1) / (32 * rw));
+    if (a.flat.tiles <= kMaxFlatTiles) a.flat.room(2 * cus / Hkv, rw * 16, rw * 64 * 8, Hkv);
     return true;
 }
 
-template <auto Kernel>
-int launch_step(const PagedAttnParams &p, const StepShape &a, int lds, hipStream_t st) {
+template <auto Kernel, class Params>
+int launch_attention(unsigned int workgroups_x, unsigned int workgroups_y, int lds, hipStream_t st, const Params &p) {
     if (!large_lds<Kernel>()) return QUASAR_ERR_HIP;
-    hipLaunchKernelGGL(Kernel, dim3((unsigned int)a.workers, (unsigned int)p.c.Hkv, (unsigned int)a.groups), dim3(kPagedWaves * 64),
-                       lds + (kPagedWaves + p.c.n_seqs + 1) * 4, st, p);
-    if (const int e = launched()) return e;
-    if (a.workers == 1) return QUASAR_OK;                                    // (every sequence is finished by its one worker)
-    hipLaunchKernelGGL(paged_merge_kernel, dim3((unsigned int)(2 * compute_units()), (unsigned int)a.groups), dim3(512), 0, st, p, a.NQT);
+    hipLaunchKernelGGL(Kernel, dim3(workgroups_x, workgroups_y), dim3(kPromptWaves * 64), lds, st, p);
     return launched();
 }
 template <int KV>
-int launch_step(PagedAttnParams &p, const StepShape &a, hipStream_t st) {
-    p.group_rows = 16 * a.NQT;
-    constexpr auto narrow = [](int nqt) { return kPagedWaves * nqt * (8 * 64 * 16 + 16 * 2 * 4); };
-    constexpr auto wide = [](int rw) { return rw * (kPagedWaves / rw - 1) * (16 * 64 * 16 + 64 * 8); };
-    if (a.NQT == 1) return launch_step<paged_attention_kernel<KV, 1>>(p, a, narrow(1), st);
-    if (a.NQT == 4) return launch_step<paged_attention_wide_kernel<KV, 2>>(p, a, wide(2), st);
-    if (a.NQT == 8) return launch_step<paged_attention_wide_kernel<KV, 4>>(p, a, wide(4), st);
-    if constexpr (KV == KV_BF16) return launch_step<paged_attention_kernel<KV, 2>>(p, a, narrow(2), st);
-    else return launch_step<paged_attention_wide_kernel<KV, 1>>(p, a, wide(1), st);
+int launch_step(const PagedAttnParams &p, int NQT, hipStream_t st) {
+    const int lds = kPagedWaves * NQT * (8 * 64 * 16 + 16 * 2 * 4) + (kPagedWaves + 4 * (p.c.n_seqs + 1)) * 4;
+    const int e = NQT == 1 ? launch_attention<paged_attention_kernel<KV, 1>>(p.workers, p.c.Hkv, lds, st, p)
+                           : launch_attention<paged_attention_kernel<KV, 2>>(p.workers, p.c.Hkv, lds, st, p);
+    if (e || p.workers == 1) return e;                                       // (one worker finishes every sequence)
+    hipLaunchKernelGGL(paged_merge_kernel, dim3((unsigned int)(2 * compute_units())), dim3(512), 0, st, p, NQT);
+    return launched();
 }
 
-// ---- attention of prompts: workgroups of a kv head where tiles are shared
-struct PromptShape { int64_t tiles; int workers; size_t part_o, part_ml, pieces; };
-PromptShape prompt_shape(int64_t T, int64_t Hq, int64_t Hkv, int64_t n_seqs) {
-    PromptShape a{};
+// ---- attention of prompts: tiles of 128 rows, shared where they would leave compute units idle
+FlatShape prompt_shape(int64_t T, int64_t Hq, int64_t Hkv, int64_t n_seqs) {
+    FlatShape a{};
     a.tiles = T * (Hq / Hkv) / (32 * kPromptWaves) + n_seqs;                 // (at most a ragged one a sequence)
     const int64_t per = 2 * (int64_t)compute_units() / Hkv;
-    if (a.tiles > kMaxFlatTiles || a.tiles >= kFlatRounds * per) return a;
-    a.workers = (int)(per < 1 ? 1 : per > kMaxWorkers ? kMaxWorkers : per);
-    const size_t parts = (size_t)Hkv * 2 * a.workers * kPromptWaves;
-    a.part_o = parts * 16 * 64 * 16;
-    a.part_ml = parts * 64 * 8;
-    a.pieces = (size_t)a.workers * 16;
+    if (a.tiles <= kMaxFlatTiles && a.tiles < per) a.room(per, kPromptWaves * 16, kPromptWaves * 64 * 8, Hkv);
     return a;
 }
-
 template <int KV>
-int launch_prompt(const PromptParams &p, const PromptShape &a, hipStream_t st) {
-    const int lds = 2 * kPromptStepBytes + (kMaxSeqs + kPromptWaves + 4) * 4;
-    if (!p.workers) {
-        constexpr auto kern = prompt_attention_kernel<KV, false>;
-        if (!large_lds<kern>()) return QUASAR_ERR_HIP;
-        hipLaunchKernelGGL(kern, dim3((unsigned int)(a.tiles * p.c.Hkv)), dim3(kPromptWaves * 64), lds, st, p);
-        return launched();
-    }
-    constexpr auto kern = prompt_attention_kernel<KV, true>;
-    if (!large_lds<kern>()) return QUASAR_ERR_HIP;
-    hipLaunchKernelGGL(kern, dim3((unsigned int)(p.workers * p.c.Hkv)), dim3(kPromptWaves * 64), lds + kMaxFlatTiles * 4, st, p);
-    if (const int e = launched()) return e;
-    hipLaunchKernelGGL(prompt_merge_kernel, dim3((unsigned int)(4 * compute_units())), dim3(256), 0, st, p);
+int launch_prompt(const PromptParams &p, int64_t tiles, int PW, hipStream_t st) {
+    const int lds = 2 * kPromptStepBytes + (kMaxSeqs + kPromptWaves + 8) * 4;
+    if (!p.workers) return launch_attention<prompt_attention_kernel<KV, false, 1>>((unsigned int)(tiles * p.c.Hkv), 1, lds, st, p);
+    const unsigned int n = (unsigned int)(p.workers * p.c.Hkv);
+    const int e = PW == 1 ? launch_attention<prompt_attention_kernel<KV, true, 1>>(n, 1, lds + kMaxFlatTiles * 4, st, p)
+                          : launch_attention<prompt_attention_kernel<KV, true, 2>>(n, 1, lds + kMaxFlatTiles * 4, st, p);
+    if (e || p.workers == 1) return e;
+    hipLaunchKernelGGL(prompt_merge_kernel, dim3((unsigned int)(4 * compute_units())), dim3(256), 0, st, p, kPromptWaves / PW);
     return launched();
+}
+
+// The workspace's parts, in the parameters of either kernel.
+template <class Params> void lay_out(Params &p, const FlatShape &a, void *workspace) {
+    p.workers = a.workers;
+    p.part_o = static_cast<f32x4 *>(workspace);
+    p.part_ml = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace) + a.part_o);
+    p.pieces = reinterpret_cast<int *>(static_cast<unsigned char *>(workspace) + a.part_o + a.part_ml);
 }
 
 BooksParams books(int32_t *table, int64_t table_ld, int64_t n_seqs, int64_t max_pages, int32_t *lengths, int32_t *refs, int64_t n_pages, int64_t page_len) {
@@ -236,10 +248,8 @@ int quasar_paged_prepare(const uint16_t *qkv, int64_t T, int64_t ld, int64_t n_q
 }
 
 size_t quasar_paged_attention_workspace_bytes(int64_t max_new, int64_t n_q_heads, int64_t n_kv_heads) {
-    StepShape a{}, b{};
-    if (!step_shape(max_new, n_q_heads, n_kv_heads, KV_BF16, a) || !step_shape(max_new, n_q_heads, n_kv_heads, KV_E4M3, b)) return 0;
-    const size_t x = a.part_o + a.part_ml + a.pieces, y = b.part_o + b.part_ml + b.pieces;
-    return x > y ? x : y;
+    StepShape a{};
+    return step_shape(max_new, n_q_heads, n_kv_heads, 1, a) ? a.flat.bytes() : 0;
 }
 
 int quasar_paged_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n_q_heads, int64_t n_kv_heads, const int32_t *row_start,
@@ -247,29 +257,38 @@ int quasar_paged_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n_
                            const float *k_scale, const float *v_scale, const int32_t *table, int64_t table_ld, int64_t max_pages,
                            const int32_t *lengths, uint16_t *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *hip_stream) {
     if (!q || !out) return QUASAR_ERR_NULL;
-    PagedAttnParams p{};
+    PagedParams c{};
     const CacheArgs a{T, n_q_heads, n_kv_heads, pages, n_pages, page_len, kv_dtype, k_scale, v_scale, table, table_ld, n_seqs, max_pages, lengths, row_start};
-    if (const int e = check_cache(a, p.c)) return e;
+    if (const int e = check_cache(a, c)) return e;
+    const int kv = kv_type(kv_dtype);
     StepShape shape{};
-    if (!step_shape(max_new, n_q_heads, n_kv_heads, kv_type(kv_dtype), shape)) return QUASAR_ERR_SHAPE;
+    if (!step_shape(max_new, n_q_heads, n_kv_heads, n_seqs, shape)) return QUASAR_ERR_SHAPE;
     if (ldq < n_q_heads * kHeadDim || ldo < n_q_heads * kHeadDim || ldq % 8 || ldo % 4) return QUASAR_ERR_SHAPE;
     if (!aligned(q, 16) || !aligned(out, 8)) return QUASAR_ERR_ALIGN;
     if (!workspace || workspace_bytes < quasar_paged_attention_workspace_bytes(max_new, n_q_heads, n_kv_heads)) return QUASAR_ERR_WORKSPACE;
     if (!aligned(workspace, 16)) return QUASAR_ERR_ALIGN;
-    p.q = q; p.out = out; p.ldq = ldq; p.ldo = ldo;
-    p.part_o = static_cast<f32x4 *>(workspace);
-    p.part_ml = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace) + shape.part_o);
-    p.pieces = reinterpret_cast<int *>(static_cast<unsigned char *>(workspace) + shape.part_o + shape.part_ml);
-    p.workers = shape.workers; p.max_new = (int)max_new;
-    p.scale_log2 = kScaleLog2;
+    c.max_new = (int)max_new;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    return kv_type(kv_dtype) == KV_BF16 ? launch_step<KV_BF16>(p, shape, st) : launch_step<KV_E4M3>(p, shape, st);
+    if (shape.NQT) {
+        PagedAttnParams p{};
+        p.c = c;
+        p.q = q; p.out = out; p.ldq = ldq; p.ldo = ldo;
+        p.scale_log2 = kScaleLog2;
+        lay_out(p, shape.flat, workspace);
+        return kv == KV_BF16 ? launch_step<KV_BF16>(p, shape.NQT, st) : launch_step<KV_E4M3>(p, shape.NQT, st);
+    }
+    PromptParams p{};
+    p.c = c;
+    p.q = q; p.out = out; p.ldq = ldq; p.ldo = ldo;
+    p.scale_log2 = kScaleLog2;
+    p.least = kStepLeast;
+    if (shape.flat.workers) lay_out(p, shape.flat, workspace);
+    return kv == KV_BF16 ? launch_prompt<KV_BF16>(p, shape.flat.tiles, shape.PW, st) : launch_prompt<KV_E4M3>(p, shape.flat.tiles, shape.PW, st);
 }
 
 size_t quasar_prompt_attention_workspace_bytes(int64_t T, int64_t n_q_heads, int64_t n_kv_heads, int64_t n_seqs) {
     if (T < 1 || T > kMaxPositions || check_heads(n_q_heads, n_kv_heads) || n_seqs < 1 || n_seqs > kMaxSeqs) return 0;
-    const PromptShape a = prompt_shape(T, n_q_heads, n_kv_heads, n_seqs);
-    return a.part_o + a.part_ml + a.pieces;
+    return prompt_shape(T, n_q_heads, n_kv_heads, n_seqs).bytes();
 }
 
 int quasar_prompt_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n_q_heads, int64_t n_kv_heads, const int32_t *row_start,
@@ -285,15 +304,11 @@ int quasar_prompt_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n
     if (!aligned(q, 16) || !aligned(out, 8) || !aligned(workspace, 16)) return QUASAR_ERR_ALIGN;
     p.q = q; p.out = out; p.ldq = ldq; p.ldo = ldo;
     p.scale_log2 = kScaleLog2;
-    const PromptShape shape = prompt_shape(T, n_q_heads, n_kv_heads, n_seqs);
-    if (workspace && shape.workers && workspace_bytes >= shape.part_o + shape.part_ml + shape.pieces && max_pages * page_len > kFlatPositions) {
-        p.workers = shape.workers;
-        p.part_o = static_cast<f32x4 *>(workspace);
-        p.part_ml = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace) + shape.part_o);
-        p.pieces = reinterpret_cast<int *>(static_cast<unsigned char *>(workspace) + shape.part_o + shape.part_ml);
-    }
+    p.least = kPromptLeast;
+    const FlatShape shape = prompt_shape(T, n_q_heads, n_kv_heads, n_seqs);
+    if (workspace && shape.workers && workspace_bytes >= shape.bytes() && max_pages * page_len > kFlatPositions) lay_out(p, shape, workspace);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    return kv_type(kv_dtype) == KV_BF16 ? launch_prompt<KV_BF16>(p, shape, st) : launch_prompt<KV_E4M3>(p, shape, st);
+    return kv_type(kv_dtype) == KV_BF16 ? launch_prompt<KV_BF16>(p, shape.tiles, 1, st) : launch_prompt<KV_E4M3>(p, shape.tiles, 1, st);
 }
 
 size_t quasar_pages_workspace_bytes(int64_t n_seqs, int64_t n_pages) {

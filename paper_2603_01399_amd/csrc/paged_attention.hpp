@@ -1,4 +1,5 @@
-// Attention of the new tokens of a step - one, or a draft of up to 32, per sequence - over a paged key/value cache (gfx950).
+// Attention of the new tokens of a step - one, or a short draft, per sequence - over a paged key/value cache (gfx950): up to 32 rows
+// m * G + g of a sequence and kv head; more go the way of prompts (prompt_attention.hpp).
 //
 // The arithmetic is that of verify_attention_kernel: S^T = K Q^T and O^T = V^T P^T, a lane owning one query column.  What differs is the
 // work split.  The lengths are on the device and as ragged as the traffic, so a grid over sequences leaves the card to the longest
@@ -20,29 +21,15 @@ struct PagedAttnParams {
     const uint16_t *q;        // [T, Hq * 128] bf16
     uint16_t *out;
     long long ldq, ldo;
-    f32x4 *part_o;            // [group of rows][Hkv][2 workers][NQT][8][64]
-    float *part_ml;           // [group of rows][Hkv][2 workers][NQT][16][2]
-    int *pieces;              // [group of rows][workers][4]: sequence that begins here and goes on (-1: none), last worker, slot
-    int workers, max_new;
-    int group_rows;           // rows m * G + g of a group: 16 NQT or 32 RW
+    f32x4 *part_o;            // [Hkv][2 workers][NQT][8][64]
+    float *part_ml;           // [Hkv][2 workers][NQT][16][2]
+    int *pieces;              // [workers][4]: sequence that begins here and goes on (-1: none), last worker, slot
+    int workers;
     float scale_log2;         // log2(e) / sqrt(128)
 };
 
 constexpr int kPagedWaves = 4;
 constexpr int kMaxWorkers = 512;             // of a kv head
-
-// Prefix sums of the sequences' blocks into lds[0 .. n_seqs] (exclusive; the total at the end).  `row_group`: sequences without
-// rows in this group have none.
-__device__ __forceinline__ int scan_blocks(const PagedAttnParams &p, int row_group, int *lds, int *wave_sums) {
-    const int total = prefix_sums<kPagedWaves>(p.c.n_seqs, lds, wave_sums, [&](int s) {
-        const SeqSpan a = seq_span(p.c, s);
-        const int n = a.n < p.max_new ? a.n : p.max_new;
-        return n * p.c.G > p.group_rows * row_group ? blocks_of(p.c, a.len + n) : 0;
-    });
-    if (threadIdx.x == 0) lds[p.c.n_seqs] = total;
-    __syncthreads();
-    return total;
-}
 
 template <int KV, int NQT>
 __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const PagedAttnParams p) {
@@ -52,17 +39,24 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
     float *lml = reinterpret_cast<float *>(lds + NW * NQT * 8 * 64 * 16);        // [NW][NQT][16][2]
     int *wave_sums = reinterpret_cast<int *>(lml + NW * NQT * 16 * 2);
     int *prefix = wave_sums + NW;                                                // [n_seqs + 1]
+    SeqSpan *spans = reinterpret_cast<SeqSpan *>(prefix + p.c.n_seqs + 1);       // [n_seqs]: read once, not again from memory
     const PagedParams &c = p.c;
     const int tid = threadIdx.x, lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int g4 = lane >> 4, col = lane & 15;
-    const int h = blockIdx.y, worker = blockIdx.x, z = blockIdx.z;
+    const int h = blockIdx.y, worker = blockIdx.x;
 
-    const int total = scan_blocks(p, z, prefix, wave_sums);
+    const int total = prefix_sums<NW>(c.n_seqs, prefix, wave_sums, [&](int s) {
+        const SeqSpan a = seq_span(c, s);
+        spans[s] = a;
+        return a.n ? blocks_of(c, a.len + a.n) : 0;
+    });
+    if (tid == 0) prefix[c.n_seqs] = total;
+    __syncthreads();
     const FlatShare mine = flat_share(total, p.workers, NW, worker);             // (a block for each wave)
     int f = mine.begin;
     const int f_end = mine.end;
-    int *piece = p.pieces + ((long long)z * p.workers + worker) * 4;
+    int *piece = p.pieces + worker * 4;
     int goes_on = -1, last_worker = 0, first_slot = 0;
     // first sequence of the piece: the last one that begins at or before f (those without blocks are skipped by the search)
     int s = 0;
@@ -81,8 +75,8 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
     for (; f < f_end; ++s) {
         const int s_begin = prefix[s], s_end = prefix[s + 1];
         if (s_end <= f) continue;
-        const SeqSpan a = seq_span(c, s);
-        const int n = a.n < p.max_new ? a.n : p.max_new, R = n * c.G, row0 = p.group_rows * z;
+        const SeqSpan a = spans[s];
+        const int n = a.n, R = n * c.G;
         const int b0 = f - s_begin, b1 = (s_end < f_end ? s_end : f_end) - s_begin;
         const int32_t *pages_of = c.table + s * c.table_ld;
 
@@ -91,7 +85,7 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
         int limit[NQT];                       // last visible position of this lane's query column
 #pragma unroll
         for (int qt = 0; qt < NQT; ++qt) {
-            const int r = row0 + 16 * qt + col;
+            const int r = 16 * qt + col;
             const int m = r < R ? r / c.G : n - 1, g = r < R ? r % c.G : 0;
             limit[qt] = a.len + m;
 #pragma unroll
@@ -128,7 +122,7 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
         auto v_operand = [&](int dt) {
             if constexpr (KV == KV_BF16) return vc[dt];
             const u32x4 v = vc[dt >> 1];
-            return dt & 1 ? e4m3x8_to_bf16(v.z, v.w) : e4m3x8_to_bf16(v.x, v.y);
+            return dt & 1 ? e4m3x8_to_f16(v.z, v.w) : e4m3x8_to_f16(v.x, v.y);
         };
         // `there`: the table names a page of the cache for the block; else its positions count as hidden
         auto process = [&](int b, bool there) {
@@ -173,18 +167,17 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
                 mx = fmaxf(mx, __shfl_xor(mx, 16, 64));
                 mx = fmaxf(mx, __shfl_xor(mx, 32, 64));
                 const float m_new = fmaxf(mrow[qt], mx);
-                const float mc = m_new == -__builtin_inff() ? 0.f : -m_new * scale_log2;          // nothing visible yet
+                const float mc = m_new == -__builtin_inff() ? 0.f : -m_new * scale_log2;                                      // nothing visible yet
+                const float ms = mc + kWeightShift<KV>;
                 alpha[qt] = __builtin_amdgcn_exp2f(__builtin_fmaf(mrow[qt], scale_log2, mc));   // 0 while mrow is -inf
                 mrow[qt] = m_new;
                 float psum = 0.f;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[qt][i >> 1][2 * (i & 1)], scale_log2, mc));
-                    const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[qt][i >> 1][2 * (i & 1) + 1], scale_log2, mc));
-                    // bf16 in the second product, and the same rounded values in the sum, so that the weights that are applied sum to one
-                    const unsigned int pk = float2_to_bf16_pair(e0, e1);
-                    pb16[qt][i] = pk;
-                    psum += __uint_as_float(pk << 16) + __uint_as_float(pk & 0xFFFF0000u);
+                    const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[qt][i >> 1][2 * (i & 1)], scale_log2, ms));
+                    const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[qt][i >> 1][2 * (i & 1) + 1], scale_log2, ms));
+                    pb16[qt][i] = weight_pair<KV>(e0, e1);
+                    psum = add_pair<KV>(pb16[qt][i], psum);
                 }
                 lrow[qt] = lrow[qt] * alpha[qt] + psum;
                 moved |= alpha[qt] != 1.0f;
@@ -206,7 +199,7 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
                 }
 #pragma unroll
                 for (int qt = 0; qt < NQT; ++qt)
-                    oacc[dt][qt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, pb16[qt]), oacc[dt][qt], 0, 0, 0);
+                    oacc[dt][qt] = values_times_weights<KV>(v, pb16[qt], oacc[dt][qt]);
             }
         };
         // a wave's blocks are b0 + w, b0 + w + NW, ...; 64 of their page ids are fetched at a time, one a lane
@@ -247,7 +240,7 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
         __syncthreads();
         const bool whole = b0 == 0 && b1 == s_end - s_begin;
         const int slot = flat_slot(mine, worker, s_begin);
-        const long long pbase = (((long long)z * c.Hkv + h) * (2 * p.workers) + slot) * NQT;
+        const long long pbase = ((long long)h * (2 * p.workers) + slot) * NQT;
         if (!whole && b0 == 0) {
             goes_on = s;
             last_worker = (s_end - 1) / mine.share;
@@ -263,7 +256,7 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
                 fac[ww] = exp2f(lml[((ww * NQT + qt) * 16 + col) * 2] - m_use);
                 lsum += fac[ww] * lml[((ww * NQT + qt) * 16 + col) * 2 + 1];
             }
-            const int r = row0 + 16 * qt + col;
+            const int r = 16 * qt + col;
             const float inv = lsum > 0.f ? __fdiv_rn(vs, lsum) : 0.f;            // a row that sees nothing: zeros
             for (int dt = w; dt < 8; dt += NW) {
                 f32x4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -291,247 +284,6 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
     }
 }
 
-// The same for more than 32 rows of a sequence and kv head: 32 x 32 x 16 products as in prompt_attention.hpp (same order of positions and
-// scores), without LDS.  RW waves take 32 rows each and read the same blocks, at about the same time, so that all but the first find
-// them in the L1; the 4 / RW of them that have the same rows take blocks in turn and join at the end.
-template <int KV, int RW>
-__global__ __launch_bounds__(kPagedWaves * 64, 2) void paged_attention_wide_kernel(const PagedAttnParams p) {
-    constexpr int PW = kPagedWaves / RW, BB = kv_block_bytes<KV>, NL = BB / 1024, NQT = 2 * RW;
-    extern __shared__ __align__(16) unsigned char lds[];
-    f32x4 *lo = reinterpret_cast<f32x4 *>(lds);                                  // [RW][PW - 1][16][64]
-    u32x2 *lml = reinterpret_cast<u32x2 *>(lds + RW * (PW - 1) * 16 * 64 * 16);  // [RW][PW - 1][64]
-    int *wave_sums = reinterpret_cast<int *>(lml + RW * (PW - 1) * 64);
-    int *prefix = wave_sums + kPagedWaves;                                       // [n_seqs + 1]
-    const PagedParams &c = p.c;
-    const int tid = threadIdx.x, lane = tid & 63;
-    const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int rw = w % RW, pw = w / RW;
-    const int hi = lane >> 5, col = lane & 31;
-    const int h = blockIdx.y, worker = blockIdx.x, z = blockIdx.z;
-
-    const int total = scan_blocks(p, z, prefix, wave_sums);
-    const FlatShare mine = flat_share(total, p.workers, kPagedWaves, worker);
-    int f = mine.begin;
-    const int f_end = mine.end;
-    int *piece = p.pieces + ((long long)z * p.workers + worker) * 4;
-    int goes_on = -1, last_worker = 0, first_slot = 0;
-    int s = 0;
-    if (f < f_end) {
-        int up = c.n_seqs;
-        while (up - s > 1) {
-            const int mid = (s + up) >> 1;
-            if (prefix[mid] <= f) s = mid; else up = mid;
-        }
-    }
-    const float ks = c.k_scale ? c.k_scale[h] : 1.0f, vs = c.v_scale ? c.v_scale[h] : 1.0f;
-    const float scale_log2 = p.scale_log2 * ks;
-    const long long head_step = (long long)(2 * BB) << c.block_shift, page_step = head_step * c.Hkv;
-    const int in_page = (1 << c.block_shift) - 1;
-    // this lane's 16 bytes of a block: bf16 operands as prompt_attention.hpp reads them from LDS; 8-bit ones in pairs of neighbouring
-    // ksteps of 32 (keys) and of 16-d tiles (values)
-    const int k_lane = KV == KV_BF16 ? (((col >> 3) & 1) * 256 + (col >> 4) * 8 + (col & 7) + 16 * hi) * 16
-                                     : (((col >> 3) & 1) * 128 + (col >> 4) * 8 + (col & 7) + 16 * hi) * 16;
-    const int v_lane = KV == KV_BF16 ? ((col >> 4) * 64 + (col & 15) + 16 * hi) * 16 : ((col & 15) + 16 * hi) * 16 + (col >> 4) * 8;
-
-    for (; f < f_end; ++s) {
-        const int s_begin = prefix[s], s_end = prefix[s + 1];
-        if (s_end <= f) continue;
-        const SeqSpan a = seq_span(c, s);
-        const int n = a.n < p.max_new ? a.n : p.max_new, R = n * c.G;
-        const int b0 = f - s_begin, b1 = (s_end < f_end ? s_end : f_end) - s_begin;
-        const int32_t *pages_of = c.table + s * c.table_ld;
-        const int my_row = p.group_rows * z + 32 * rw + col, row = my_row < R ? my_row : R - 1;   // (rows behind the last one repeat it)
-        const int token = row / c.G, limit = a.len + token;
-        const long long head_at = ((long long)h * c.G + row % c.G) * kHeadDim;
-        bf16x8 qb[8];
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-            qb[k] = __builtin_bit_cast(bf16x8, *reinterpret_cast<const u32x4 *>(p.q + (a.row0 + token) * p.ldq + head_at + 16 * k + 8 * hi));
-        f32x16 oacc[4];
-        float mrow = -__builtin_inff(), lrow = 0.f;
-#pragma unroll
-        for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-            for (int i = 0; i < 16; ++i) oacc[dt][i] = 0.f;
-
-        u32x4 kc[NL], vc[NL];
-        auto block_at = [&](int b, int page) {
-            return c.pages + (page_exists(page, c.n_pages) ? page : 0) * page_step + h * head_step + (b & in_page) * (2 * BB);
-        };
-        // bf16: an operand a load (ksteps of 16 d; [dt of 32][t]); e4m3: 16 bytes of the keys hold two ksteps, 8 of the values an operand
-        auto load_keys = [&](const unsigned char *from) {
-#pragma unroll
-            for (int i = 0; i < NL; ++i)
-                kc[i] = *reinterpret_cast<const u32x4 *>(from + k_lane + (KV == KV_BF16 ? i * 512 : (i >> 1) * 1024 + (i & 1) * 512));
-        };
-        auto load_values = [&](const unsigned char *from) {
-            from += BB + v_lane;
-            if constexpr (KV == KV_BF16) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) vc[i] = *reinterpret_cast<const u32x4 *>(from + (i >> 1) * 2048 + (i & 1) * 512);
-            } else {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const u32x2 t0 = *reinterpret_cast<const u32x2 *>(from + i * 1024), t1 = *reinterpret_cast<const u32x2 *>(from + i * 1024 + 512);
-                    vc[i] = u32x4{t0.x, t0.y, t1.x, t1.y};
-                }
-            }
-        };
-        auto process = [&](auto edge, auto more, int b, bool there, const unsigned char *next) {
-            constexpr bool EDGE = decltype(edge)::value;         // some position is hidden from some row, or nobody's
-            const int pos0 = b * kKvBlock;
-            f32x16 sc;
-#pragma unroll
-            for (int i = 0; i < 16; ++i) sc[i] = 0.f;
-#pragma unroll
-            for (int k = 0; k < 8; ++k) {
-                // kstep k of 16: octets 2 k + hi of the row; e4m3: octet o of 16 lies in load (o / 8, o % 4 / 2), half o / 4 % 2
-                u32x4 ka;
-                if constexpr (KV == KV_BF16) ka = kc[k];
-                else {
-                    const u32x4 v = kc[(k >> 2) * 2 + (k & 1)];
-                    ka = (k >> 1) & 1 ? e4m3x8_to_bf16(v.z, v.w) : e4m3x8_to_bf16(v.x, v.y);
-                }
-                sc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, ka), qb[k], sc, 0, 0, 0);
-            }
-            __builtin_amdgcn_sched_barrier(0);                           // (into the registers that the products have read: no earlier)
-            if constexpr (decltype(more)::value) load_keys(next);
-            __builtin_amdgcn_sched_barrier(0);
-            if constexpr (EDGE) {
-                const int left = there ? limit - pos0 - 4 * hi : -1;
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (16 * ((i >> 2) & 1) + 8 * (i >> 3) + (i & 3) > left) sc[i] = -__builtin_inff();
-            }
-            float mx = sc[0];
-#pragma unroll
-            for (int i = 1; i < 16; ++i) mx = larger(mx, sc[i]);
-            mx = max_halves(mx);
-            if (__builtin_amdgcn_ballot_w64((mx - mrow) * scale_log2 > kLazyMax) != 0ull) {
-                const float m_new = larger(mrow, mx);
-                const float alpha = m_new == -__builtin_inff() ? 1.f : __builtin_amdgcn_exp2f((mrow - m_new) * scale_log2);
-                mrow = m_new;
-                lrow *= alpha;
-#pragma unroll
-                for (int dt = 0; dt < 4; ++dt) oacc[dt] *= alpha;
-            }
-            const float mc = mrow == -__builtin_inff() ? 0.f : -mrow * scale_log2;
-            u32x4 pb[2];
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[2 * i], scale_log2, mc));
-                const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[2 * i + 1], scale_log2, mc));
-                const unsigned int pk = float2_to_bf16_pair(e0, e1);
-                pb[i >> 2][i & 3] = pk;
-                lrow = add_bf16_pair(pk, lrow);
-            }
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-#pragma unroll
-                for (int dt = 0; dt < 4; ++dt) {
-                    u32x4 va;
-                    if constexpr (KV == KV_BF16) va = vc[2 * dt + t];
-                    else va = t ? e4m3x8_to_bf16(vc[dt].z, vc[dt].w) : e4m3x8_to_bf16(vc[dt].x, vc[dt].y);
-                    if constexpr (EDGE) {
-                        // positions behind the sequence hold whatever the page held: they must not reach the product (0 x NaN)
-                        const int end = there ? a.len + n - 1 - pos0 - 4 * (2 * t + hi) : -1;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const int at = 16 * (j >> 1) + 2 * (j & 1);
-                            va[j] &= (at <= end ? 0x0000FFFFu : 0u) | (at + 1 <= end ? 0xFFFF0000u : 0u);
-                        }
-                    }
-                    oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, va), __builtin_bit_cast(bf16x8, pb[t]), oacc[dt], 0, 0, 0);
-                }
-            __builtin_amdgcn_sched_barrier(0);
-            if constexpr (decltype(more)::value) load_values(next);
-            __builtin_amdgcn_sched_barrier(0);
-        };
-        for (int bs = b0 + pw; bs < b1; bs += 64 * PW) {
-            const int ahead = bs + PW * lane;
-            int id = -1;
-            if (ahead < b1) id = pages_of[ahead >> c.block_shift];
-            const int cnt = min(64, (b1 - bs + PW - 1) / PW);
-            auto page_at = [&](int i) { return __builtin_amdgcn_readlane(id, i); };
-            auto good = [&](int i) { return page_exists(page_at(i), c.n_pages); };
-            auto from = [&](int i) { return block_at(bs + PW * i, page_at(i)); };
-            // blocks that every row sees whole, then the others (and all from the first without a page on); the last one requests none
-            const int whole = min(cnt - 1, ((a.len + 1) / kKvBlock - bs + PW - 1) / PW);       // (may be negative)
-            int i = 0;
-            load_keys(from(0));
-            load_values(from(0));
-            for (; i < whole && good(i); ++i) process(std::false_type{}, std::true_type{}, bs + PW * i, true, from(i + 1));
-            for (; i + 1 < cnt; ++i) process(std::true_type{}, std::true_type{}, bs + PW * i, good(i), from(i + 1));
-            process(std::true_type{}, std::false_type{}, bs + PW * i, good(i), nullptr);
-        }
-        mrow *= scale_log2;
-        float lsum = lrow + __shfl_xor(lrow, 32, 64);
-        if constexpr (PW > 1) {
-            if (pw) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    lo[((rw * (PW - 1) + pw - 1) * 16 + i) * 64 + lane] = f32x4{oacc[i >> 2][4 * (i & 3)], oacc[i >> 2][4 * (i & 3) + 1], oacc[i >> 2][4 * (i & 3) + 2], oacc[i >> 2][4 * (i & 3) + 3]};
-                lml[(rw * (PW - 1) + pw - 1) * 64 + lane] = u32x2{__float_as_uint(mrow), __float_as_uint(lsum)};
-            }
-            __syncthreads();
-        }
-        const bool whole = b0 == 0 && b1 == s_end - s_begin;
-        const int slot = flat_slot(mine, worker, s_begin);
-        if (!whole && b0 == 0) {
-            goes_on = s;
-            last_worker = (s_end - 1) / mine.share;
-            first_slot = slot;
-        }
-        if (pw == 0) {
-            for (int k = 0; k < PW - 1; ++k) {
-                const u32x2 ml = lml[(rw * (PW - 1) + k) * 64 + lane];
-                const float m_new = fmaxf(mrow, __uint_as_float(ml.x)), m_use = m_new == -__builtin_inff() ? 0.f : m_new;
-                const float keep = exp2f(mrow - m_use), fac = exp2f(__uint_as_float(ml.x) - m_use);
-                lsum = lsum * keep + fac * __uint_as_float(ml.y);
-                mrow = m_new;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const f32x4 o = lo[((rw * (PW - 1) + k) * 16 + i) * 64 + lane];
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) oacc[i >> 2][4 * (i & 3) + j] = oacc[i >> 2][4 * (i & 3) + j] * keep + o[j] * fac;
-                }
-            }
-            if (!whole) {
-                // in the order of the 16 x 16 kernel: [16-row tile][16-d tile][d / 4, row]
-                const long long pbase = (((long long)z * c.Hkv + h) * (2 * p.workers) + slot) * NQT + 2 * rw + (col >> 4);
-#pragma unroll
-                for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        p.part_o[(pbase * 8 + 2 * dt + (i >> 1)) * 64 + (2 * (i & 1) + hi) * 16 + (col & 15)] =
-                            f32x4{oacc[dt][4 * i], oacc[dt][4 * i + 1], oacc[dt][4 * i + 2], oacc[dt][4 * i + 3]};
-                if (hi == 0) {
-                    p.part_ml[(pbase * 16 + (col & 15)) * 2 + 0] = mrow;
-                    p.part_ml[(pbase * 16 + (col & 15)) * 2 + 1] = lsum;
-                }
-            } else if (my_row < R) {
-                const float inv = lsum > 0.f ? __fdiv_rn(vs, lsum) : 0.f;        // a row that sees nothing: zeros
-                uint16_t *to = p.out + (a.row0 + token) * p.ldo + head_at + 4 * hi;
-#pragma unroll
-                for (int dt = 0; dt < 4; ++dt)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const u32x2 o = {float2_to_bf16_pair(oacc[dt][4 * i] * inv, oacc[dt][4 * i + 1] * inv),
-                                         float2_to_bf16_pair(oacc[dt][4 * i + 2] * inv, oacc[dt][4 * i + 3] * inv)};
-                        *reinterpret_cast<u32x2 *>(to + 32 * dt + 8 * i) = o;
-                    }
-            }
-        }
-        if constexpr (PW > 1) __syncthreads();                                   // (the next sequence's join reuses the LDS)
-        f = s_begin + b1;
-    }
-    if (h == 0 && tid == 0) {
-        piece[0] = goes_on;
-        piece[1] = last_worker;
-        piece[2] = first_slot;
-    }
-}
-
 // The workers in whose pieces a shared sequence (or tile) begins, in order, into list; how many.  records: of each worker `words` ints, the
 // first of them < 0 where none begins.
 __device__ __forceinline__ int shared_pieces(const int *records, int words, int workers, int *list) {
@@ -547,7 +299,7 @@ __device__ __forceinline__ int shared_pieces(const int *records, int words, int 
     return n;
 }
 
-// Joins the pieces of the sequences that several workers share, for one group of rows (blockIdx.y).  A unit is 16 rows and 16 d of a kv
+// Joins the pieces of the sequences that several workers share.  A unit is 16 rows and 16 d of a kv
 // head of such a sequence: the eight waves of a workgroup share its pieces, four of them requested at a time, and meet in LDS.  The
 // workgroups walk the units: one for every worker, head and unit were up to 8192, nearly all with nothing to do (24 us where this takes 6).
 __global__ __launch_bounds__(512) void paged_merge_kernel(const PagedAttnParams p, int NQT) {
@@ -556,8 +308,7 @@ __global__ __launch_bounds__(512) void paged_merge_kernel(const PagedAttnParams 
     __shared__ f32x4 sacc[8][64];
     __shared__ int list[kMaxWorkers];
     const PagedParams &c = p.c;
-    const int z = blockIdx.y;
-    const int *records = p.pieces + (long long)z * p.workers * 4;
+    const int *records = p.pieces;
     const int units = shared_pieces(records, 4, p.workers, list) * c.Hkv * NQT * 8;
     const int sg = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const int g4 = lane >> 4, col = lane & 15;
@@ -565,9 +316,8 @@ __global__ __launch_bounds__(512) void paged_merge_kernel(const PagedAttnParams 
         const int dt = u & 7, qt = (u >> 3) % NQT, h = (u >> 3) / NQT % c.Hkv, worker = list[(u >> 3) / NQT / c.Hkv];
         const int s = records[worker * 4], last = records[worker * 4 + 1], first_slot = records[worker * 4 + 2];
         const SeqSpan a = seq_span(c, s);
-        const int n = a.n < p.max_new ? a.n : p.max_new, R = n * c.G;
-        if (p.group_rows * z + 16 * qt >= R) continue;
-        const int r = p.group_rows * z + 16 * qt + col;
+        const int R = a.n * c.G, r = 16 * qt + col;
+        if (16 * qt >= R) continue;
         const int count = last - worker + 1;
         float mw = -__builtin_inff(), lsum = 0.f;
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
@@ -577,7 +327,7 @@ __global__ __launch_bounds__(512) void paged_merge_kernel(const PagedAttnParams 
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
                 const int slot = flat_part_slot(worker, first_slot, min(k0 + 8 * i, count - 1));
-                const long long pb = (((long long)z * c.Hkv + h) * (2 * p.workers) + slot) * NQT + qt;
+                const long long pb = ((long long)h * (2 * p.workers) + slot) * NQT + qt;
                 ml[i] = reinterpret_cast<const u32x2 *>(p.part_ml)[pb * 16 + col];
                 o[i] = p.part_o[(pb * 8 + dt) * 64 + lane];
             }

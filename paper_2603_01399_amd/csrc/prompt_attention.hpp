@@ -1,8 +1,9 @@
-// Causal attention of whole prompts, or chunks of them, over a paged key/value cache (gfx950): many rows per sequence.
+// Causal attention of whole prompts, or chunks of them, over a paged key/value cache (gfx950): many rows per sequence, or the more than
+// 32 rows of a draft.
 //
 // Rows are r = m * G + g: the G query heads of a key/value head side by side, so that a tile of rows covers few tokens
-// (a narrow causal edge) and shares every key and value it loads.  A workgroup of NW waves takes 32 * NW rows of one kv head; the
-// waves share tiles of 64 positions in LDS, loaded straight from the pages, two tiles in turn.
+// (a narrow causal edge) and shares every key and value it loads.  A workgroup of four waves takes 128 (or 64) rows of one kv
+// head; the waves share steps of 64 positions in LDS, loaded straight from the pages, two steps in turn.
 //
 // S^T = K Q^T and O^T = V^T P^T in 32 x 32 x 16 products: a lane owns one query column.  The
 // rows of K are permuted, row 16 t + 8 c + 4 h + b of the product being position 16 c + 8 t + 4 h + b, which makes the scores that a lane
@@ -20,16 +21,15 @@ struct PromptParams {
     const uint16_t *q;        // [T, Hq * 128] bf16
     uint16_t *out;
     long long ldq, ldo;
-    f32x4 *part_o;            // FLAT: [Hkv][2 workers][NW][16][64], what workers leave of a tile that they share
-    float *part_ml;           // [Hkv][2 workers][NW][64][2]
+    f32x4 *part_o;            // FLAT: [Hkv][2 workers][32 rows of a tile][16][64], what workers leave of a tile that they share
+    float *part_ml;           // [Hkv][2 workers][32 rows of a tile][64][2]
     int *pieces;              // [workers][4]: sequence of the tile that begins with a worker and goes on (-1: none), its first row, last worker, slot
-    int workers;
+    int workers, least;       // steps that a worker takes at least
     float scale_log2;         // log2(e) / sqrt(128)
 };
 
-constexpr int kPromptWaves = 4;                          // 128 rows a workgroup, two workgroups a compute unit
+constexpr int kPromptWaves = 4;                          // of a workgroup, two workgroups a compute unit
 constexpr int kMaxFlatTiles = 2048;                      // of a launch that shares tiles: their prefix sums live in LDS
-constexpr int kFlatLeast = 4;                            // steps that a worker takes at least
 
 // A tile of rows: its sequence, its first row there, and what its rows see.
 struct PromptTile {
@@ -37,7 +37,8 @@ struct PromptTile {
     SeqSpan a;
 };
 
-template <int ROWS>
+// UNIFORM: f is the same for the wave, and so is what it finds (LDS does not say so).
+template <int ROWS, bool UNIFORM>
 __device__ __forceinline__ PromptTile prompt_tile(const PagedParams &c, const int *prefix, int f) {
     PromptTile t;
     int s = 0, up = c.n_seqs;
@@ -45,10 +46,10 @@ __device__ __forceinline__ PromptTile prompt_tile(const PagedParams &c, const in
         const int mid = (s + up) >> 1;
         if (prefix[mid] <= f) s = mid; else up = mid;
     }
-    t.s = s;
+    t.s = s = UNIFORM ? __builtin_amdgcn_readfirstlane(s) : s;
     t.a = seq_span(c, s);
     t.R = t.a.n * c.G;
-    t.tile0 = (f - prefix[s]) * ROWS;
+    t.tile0 = (f - (UNIFORM ? __builtin_amdgcn_readfirstlane(prefix[s]) : prefix[s])) * ROWS;
     t.first_pos = t.a.len + t.tile0 / c.G;                       // positions up to here are visible to every row of the tile
     t.last_pos = t.a.len + (min(t.tile0 + ROWS, t.R) - 1) / c.G;
     t.steps = (blocks_of(c, t.last_pos + 1) + 1) / 2;
@@ -61,51 +62,59 @@ constexpr int kPromptStepBytes = kPromptStep / kKvBlock * 2 * kKvBlockBytes;   /
 // FLAT: the steps of all tiles as one line, in equal pieces for `workers` workgroups of a kv head (as the blocks of a step's sequences,
 // paged_attention.hpp), for launches whose tiles would leave compute units idle; else a workgroup a tile, the last ones, which see most,
 // first.
-template <int KV, bool FLAT>
+// PW: waves that share rows.  1: four times 32 rows, each wave over both blocks of a step.  2: twice 32 rows, each wave over one of the
+// blocks, joined at the end: for up to 64 rows a sequence, where half of four times 32 would be nobody's.
+// 8-bit pages.  PW = 1: widened on the way into LDS, once for all waves.  PW = 2, where memory bounds: in LDS as they are, four steps of half the
+// size, so that three are under way, and widened by each wave that reads them.
+template <int KV, bool FLAT, int PW>
 __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(const PromptParams p) {
-    constexpr int NW = kPromptWaves, ROWS = 32 * NW;
-    extern __shared__ __align__(16) unsigned char lds[];         // [2 steps][2 blocks][keys | values][8192], then the prefix sums
+    constexpr int NW = kPromptWaves, RW = NW / PW, ROWS = 32 * RW, NB = 2 / PW;  // row groups; blocks of a step for a wave
+    constexpr bool RAW = KV == KV_E4M3 && PW == 2, DIRECT = KV == KV_BF16 || RAW;
+    constexpr int STAGES = RAW ? 4 : 2, STAGE_BYTES = 2 * kPromptStepBytes / STAGES;         // steps in use and under way
+    extern __shared__ __align__(16) unsigned char lds[];         // [STAGES steps][2 blocks][keys | values], then the prefix sums
     int *prefix = reinterpret_cast<int *>(lds + 2 * kPromptStepBytes);   // tiles ahead of a sequence
     int *wave_sums = prefix + kMaxSeqs;
-    int *there = wave_sums + NW;                                 // [step parity][block]: the block has a page
-    int *line = there + 4;                                       // FLAT: steps ahead of a tile
+    int *there = wave_sums + NW;                                 // [step & (STAGES - 1)][block]: the block has a page
+    int *line = there + 2 * STAGES;                                       // FLAT: steps ahead of a tile
     const PagedParams &c = p.c;
     const int tid = threadIdx.x, lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int rw = w % RW, pw = w / RW;
     const int hi = lane >> 5, col = lane & 31;
     const int h = blockIdx.x % c.Hkv, worker = blockIdx.x / c.Hkv;
     const float ks = c.k_scale ? c.k_scale[h] : 1.0f, vs = c.v_scale ? c.v_scale[h] : 1.0f;
     const float scale_log2 = p.scale_log2 * ks;
 
     int tiles = prefix_sums<NW>(c.n_seqs, prefix, wave_sums, [&](int s) { return (int)(((long long)seq_span(c, s).n * c.G + ROWS - 1) / ROWS); });
-    int tile = tiles - 1 - worker, at = 0, end = 0;              // FLAT: steps at .. end - 1 of the line
+    int tile = __builtin_amdgcn_readfirstlane(tiles - 1 - worker), at = 0, end = 0;              // FLAT: steps at .. end - 1 of the line
     FlatShare mine{};
     int goes_on = -1, goes_on_at = 0, last_worker = 0, first_slot = 0;
     if constexpr (FLAT) {
         tiles = min(tiles, kMaxFlatTiles);                       // (more only where the rows' starts do not fit the tensor)
-        const int total = prefix_sums<NW>(tiles, line, wave_sums, [&](int f) { return prompt_tile<ROWS>(c, prefix, f).steps; });
-        mine = flat_share(total, p.workers, kFlatLeast, worker);
-        at = mine.begin;
-        end = mine.end;
+        const int total = prefix_sums<NW>(tiles, line, wave_sums, [&](int f) { return prompt_tile<ROWS, false>(c, prefix, f).steps; });
+        mine = flat_share(total, p.workers, p.least, worker);
+        at = __builtin_amdgcn_readfirstlane(mine.begin);
+        end = __builtin_amdgcn_readfirstlane(mine.end);
         tile = 0;
         for (int up = tiles; up - tile > 1;) {
             const int mid = (tile + up) >> 1;
             if (line[mid] <= at) tile = mid; else up = mid;
         }
+        tile = __builtin_amdgcn_readfirstlane(tile);
     }
     for (; FLAT ? at < end : tile >= 0; tile = FLAT ? tile + 1 : -1) {
-    const PromptTile pt = prompt_tile<ROWS>(c, prefix, tile);
+    const PromptTile pt = prompt_tile<ROWS, true>(c, prefix, tile);
     const SeqSpan a = pt.a;
     const int R = pt.R, tile0 = pt.tile0, first_pos = pt.first_pos, last_pos = pt.last_pos, s = pt.s;
     const int nblk = blocks_of(c, last_pos + 1);
     int step0 = 0, steps = pt.steps;                             // the piece's part of the tile's steps
     if constexpr (FLAT) {
-        step0 = at - line[tile];
+        step0 = at - __builtin_amdgcn_readfirstlane(line[tile]);
         steps = min(pt.steps, step0 + end - at);
         at += steps - step0;
         lds_barrier();                                           // (the last tile's values may still be read)
     }
-    const int my_row = tile0 + w * 32 + col;
+    const int my_row = tile0 + rw * 32 + col;
     const int row = min(my_row, R - 1);                          // (rows behind the last one repeat it and are not stored)
     const int token = row / c.G;
     const int limit = a.len + token;                             // last visible position of the lane's column
@@ -117,7 +126,7 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
 
     // ---- staging: the waves share the keys and values of the two blocks of a step in equal parts
     constexpr int BB = kv_block_bytes<KV>, PART = 4 * BB / NW, NL = PART / 1024;   // bytes and 16-byte loads a lane of a wave
-    static_assert(PART <= BB && NL >= 1, "a wave's part lies in one block's keys or values");
+    static_assert(PART == BB, "a wave's part is one block's keys or values");
     const int my_blk = w / (NW / 2), my_at = w * PART - my_blk * 2 * BB;         // (keys, then values, of a block are contiguous)
     const long long head_step = (long long)(2 * BB) << c.block_shift, page_step = head_step * c.Hkv;
     const int in_page = (1 << c.block_shift) - 1;
@@ -126,7 +135,6 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
     int ids = -1, ids_at = -64;                                  // pages of steps ids_at .. + 63, one a lane
     u32x4 code[NL];
     auto request = [&](int step) {
-        const int stage = step & 1;
         if (step >= ids_at + 64 || ids_at < 0) {
             ids_at = step;
             const int b = 2 * (step + lane) + my_blk;
@@ -134,27 +142,35 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
         }
         const int page = __builtin_amdgcn_readlane(ids, step - ids_at);
         const bool good = page_exists(page, c.n_pages);
-        if (my_at == 0 && lane == 0) there[2 * stage + my_blk] = good;
+        if (my_at == 0 && lane == 0) there[2 * (step & (STAGES - 1)) + my_blk] = good;
         const unsigned char *from = head + (good ? page : 0) * page_step + ((2 * step + my_blk) & in_page) * (2 * BB);
-        if constexpr (KV == KV_BF16) {
-            const unsigned int to = lds_address_of(lds) + stage * kPromptStepBytes + w * PART;
+        if constexpr (DIRECT) {
+            // (scalar registers, which the load takes; the compiler may have them in vector ones)
+            const unsigned int to = __builtin_amdgcn_readfirstlane(lds_address_of(lds) + (step & (STAGES - 1)) * STAGE_BYTES + w * PART);
+            const unsigned long long from64 = reinterpret_cast<unsigned long long>(from);
+            const unsigned long long at = (unsigned long long)(unsigned int)__builtin_amdgcn_readfirstlane((int)(from64 >> 32)) << 32 |
+                                          (unsigned int)__builtin_amdgcn_readfirstlane((int)from64);
 #pragma unroll
-            for (int i = 0; i < NL; ++i) load_to_lds_16(reinterpret_cast<unsigned long long>(from) + 1024 * i, 16 * lane, to + 1024 * i);
+            for (int i = 0; i < NL; ++i) load_to_lds_16(at + 1024 * i, 16 * lane, to + 1024 * i);
         } else {
 #pragma unroll
             for (int i = 0; i < NL; ++i) code[i] = reinterpret_cast<const u32x4 *>(from)[64 * i + lane];
         }
     };
-    // what request() asked for is in LDS afterwards (for this wave; the others' behind a barrier)
-    auto settle = [&](int stage) {
-        if constexpr (KV == KV_BF16) {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    // what request() asked for is in LDS afterwards (for this wave; the others' behind a barrier); `behind`: steps requested since
+    auto settle = [&](int step, int behind) {
+        if constexpr (DIRECT) {
+            // (loads arrive in order: those of later steps may be under way)
+            if (STAGES > 2 && behind >= 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NL) : "memory");
+            else if (STAGES > 2 && behind == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NL) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         } else {
-            u32x4 *to = reinterpret_cast<u32x4 *>(lds + stage * kPromptStepBytes + w * 2 * PART) + lane;
+            u32x4 *to = reinterpret_cast<u32x4 *>(lds + (step & (STAGES - 1)) * STAGE_BYTES + w * 2 * PART) + lane;
 #pragma unroll
             for (int i = 0; i < NL; ++i) {
-                to[64 * (2 * i)] = e4m3x8_to_bf16(code[i].x, code[i].y);
-                to[64 * (2 * i + 1)] = e4m3x8_to_bf16(code[i].z, code[i].w);
+                // (a wave's part is keys or values)
+                to[64 * (2 * i)] = my_at ? e4m3x8_to_f16(code[i].x, code[i].y) : e4m3x8_to_bf16(code[i].x, code[i].y);
+                to[64 * (2 * i + 1)] = my_at ? e4m3x8_to_f16(code[i].z, code[i].w) : e4m3x8_to_bf16(code[i].z, code[i].w);
             }
         }
     };
@@ -165,35 +181,49 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
     for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
         for (int i = 0; i < 16; ++i) oacc[dt][i] = 0.f;
-    // this lane's place in a block: row col of the keys, d = col of the values
-    const int k_lane = (((col >> 3) & 1) * 16 * 16 + ((col >> 4) * 8 + (col & 7)) + 16 * hi) * 16;   // [sub 2][kstep 4][g4 4][p 16] of 16 bytes
-    const int v_lane = ((col >> 4) * 64 + (col & 15) + 16 * hi) * 16;                             // [dt 8][g4 4][dd 16] of 16 bytes
+    // this lane's place in a block: row col of the keys, d = col of the values.  8-bit: 16 bytes of the keys hold two operands (ksteps of 32),
+    // 8 of the values one
+    constexpr int LB = RAW ? BB : kKvBlockBytes;                 // keys or values of a block in LDS
+    const int k_lane = (((col >> 3) & 1) * (LB / 32) + (col >> 4) * 8 + (col & 7) + 16 * hi) * 16;
+    const int v_lane = RAW ? ((col & 15) + 16 * hi) * 16 + (col >> 4) * 8 : ((col >> 4) * 64 + (col & 15) + 16 * hi) * 16;
+    auto keys = [&](const unsigned char *at, int k) {            // operand k of 8
+        if constexpr (!RAW) return *reinterpret_cast<const u32x4 *>(at + k_lane + k * 512);
+        const u32x2 v = *reinterpret_cast<const u32x2 *>(at + k_lane + (k >> 2) * 1024 + (k & 1) * 512 + ((k >> 1) & 1) * 8);
+        return e4m3x8_to_bf16(v.x, v.y);
+    };
+    auto values = [&](const unsigned char *at, int dt, int t) {  // (RAW: the codes, in the first half)
+        if constexpr (!RAW) return *reinterpret_cast<const u32x4 *>(at + v_lane + dt * 2048 + t * 512);
+        const u32x2 v = *reinterpret_cast<const u32x2 *>(at + v_lane + dt * 1024 + t * 512);
+        return u32x4{v.x, v.y, 0u, 0u};
+    };
 
-    // the 64 positions of a step; edge: some are hidden from some row, or are nobody's; between(): called while the scores are computed
+    // the wave's blocks of a step; edge: some are hidden from some row, or are nobody's; between(): called while the scores are computed
     auto attend = [&](auto edge, int step, bool there0, bool there1, auto between) {
         constexpr bool EDGE = decltype(edge)::value;
-        const unsigned char *buf = lds + (step & 1) * kPromptStepBytes;
+        const unsigned char *buf = lds + (step & (STAGES - 1)) * STAGE_BYTES;
         const int pos0 = step * kPromptStep;
-        f32x16 sc[2];
+        auto block = [&](int b) { return PW == 1 ? b : pw; };    // the wave's b-th block
+        auto has_page = [&](int b) { return block(b) ? there1 : there0; };
+        f32x16 sc[NB];
 #pragma unroll
-        for (int blk = 0; blk < 2; ++blk)
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
-            for (int i = 0; i < 16; ++i) sc[blk][i] = 0.f;
+            for (int i = 0; i < 16; ++i) sc[b][i] = 0.f;
 #pragma unroll
         for (int k = 0; k < 8; ++k)
 #pragma unroll
-            for (int blk = 0; blk < 2; ++blk) {
-                const bf16x8 ka = *reinterpret_cast<const bf16x8 *>(buf + blk * 2 * kKvBlockBytes + k_lane + k * 512);
-                sc[blk] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qb[k], sc[blk], 0, 0, 0);
+            for (int b = 0; b < NB; ++b) {
+                const bf16x8 ka = __builtin_bit_cast(bf16x8, keys(buf + block(b) * 2 * LB, k));
+                sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qb[k], sc[b], 0, 0, 0);
             }
         if constexpr (EDGE) {
 #pragma unroll
-            for (int blk = 0; blk < 2; ++blk) {
+            for (int b = 0; b < NB; ++b) {
                 // register 4 (2 t + c) + b: position 16 c + 8 t + 4 hi + b
-                const int left = (blk ? there1 : there0) ? limit - pos0 - 32 * blk - 4 * hi : -1;
+                const int left = has_page(b) ? limit - pos0 - 32 * block(b) - 4 * hi : -1;
 #pragma unroll
                 for (int i = 0; i < 16; ++i)
-                    if (16 * ((i >> 2) & 1) + 8 * (i >> 3) + (i & 3) > left) sc[blk][i] = -__builtin_inff();
+                    if (16 * ((i >> 2) & 1) + 8 * (i >> 3) + (i & 3) > left) sc[b][i] = -__builtin_inff();
             }
         }
         between();                                               // (dozens of scalar instructions: while the products are under way)
@@ -201,10 +231,10 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int dt = 0; dt < 4; ++dt) v0[t][dt] = *reinterpret_cast<const u32x4 *>(buf + kKvBlockBytes + v_lane + dt * 2048 + t * 512);
-        float mx = larger(sc[0][0], sc[1][0]);
+            for (int dt = 0; dt < 4; ++dt) v0[t][dt] = values(buf + (2 * block(0) + 1) * LB, dt, t);
+        float mx = larger(sc[0][0], sc[NB - 1][0]);
 #pragma unroll
-        for (int i = 1; i < 16; ++i) mx = larger(mx, larger(sc[0][i], sc[1][i]));
+        for (int i = 1; i < 16; ++i) mx = larger(mx, larger(sc[0][i], sc[NB - 1][i]));
         mx = max_halves(mx);
         if (__builtin_amdgcn_ballot_w64((mx - mrow) * scale_log2 > kLazyMax) != 0ull) {          // (the first visible score, too)
             const float m_new = larger(mrow, mx);
@@ -214,35 +244,36 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
 #pragma unroll
             for (int dt = 0; dt < 4; ++dt) oacc[dt] *= alpha;
         }
-        const float mc = mrow == -__builtin_inff() ? 0.f : -mrow * scale_log2;
-        u32x4 pb[2][2];
+        const float mc = kWeightShift<KV> + (mrow == -__builtin_inff() ? 0.f : -mrow * scale_log2);
+        u32x4 pb[NB][2];
 #pragma unroll
-        for (int blk = 0; blk < 2; ++blk)
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[blk][2 * i], scale_log2, mc));
-                const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[blk][2 * i + 1], scale_log2, mc));
-                const unsigned int pk = float2_to_bf16_pair(e0, e1);
-                pb[blk][i >> 2][i & 3] = pk;
-                lrow = add_bf16_pair(pk, lrow);
+                const float e0 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][2 * i], scale_log2, mc));
+                const float e1 = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[b][2 * i + 1], scale_log2, mc));
+                const unsigned int pk = weight_pair<KV>(e0, e1);
+                pb[b][i >> 2][i & 3] = pk;
+                lrow = add_pair<KV>(pk, lrow);
             }
 #pragma unroll
-        for (int blk = 0; blk < 2; ++blk)
+        for (int b = 0; b < NB; ++b)
 #pragma unroll
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int dt = 0; dt < 4; ++dt) {
-                    u32x4 va = blk == 0 ? v0[t][dt] : *reinterpret_cast<const u32x4 *>(buf + (2 * blk + 1) * kKvBlockBytes + v_lane + dt * 2048 + t * 512);
+                    u32x4 va = b == 0 ? v0[t][dt] : values(buf + (2 * block(b) + 1) * LB, dt, t);
+                    if constexpr (RAW) va = e4m3x8_to_f16(va.x, va.y);
                     if constexpr (EDGE) {
                         // positions that no row sees hold whatever the page held: they must not reach the product (0 x NaN)
-                        const int end = (blk ? there1 : there0) ? last_pos - pos0 - 32 * blk - 4 * (2 * t + hi) : -1;
+                        const int end = has_page(b) ? last_pos - pos0 - 32 * block(b) - 4 * (2 * t + hi) : -1;
 #pragma unroll
                         for (int j = 0; j < 4; ++j) {
                             const int at = 16 * (j >> 1) + 2 * (j & 1);
                             va[j] &= (at <= end ? 0x0000FFFFu : 0u) | (at + 1 <= end ? 0xFFFF0000u : 0u);
                         }
                     }
-                    oacc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, va), __builtin_bit_cast(bf16x8, pb[blk][t]), oacc[dt], 0, 0, 0);
+                    oacc[dt] = values_times_weights<KV>(va, pb[b][t], oacc[dt]);
                 }
     };
     // The steps that every row sees whole, then the others (and all from the first that lacks a page on): two loops, since the outputs'
@@ -251,34 +282,63 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
     int step = step0;
     bool settled = false;
     auto arrive = [&] {
-        settle(step & 1);
+        settle(step, steps - 1 - step);
         lds_barrier();
     };
     auto request_next = [&] {
-        if (step + 1 < steps) request(step + 1);
+        if (step + STAGES - 1 < steps) request(step + STAGES - 1);
     };
-    if (step < steps) request(step);
+    auto has = [&](int blk) { return __builtin_amdgcn_readfirstlane(there[2 * (step & (STAGES - 1)) + blk]) != 0; };
+    for (int i = 0; i < STAGES - 1; ++i)
+        if (step + i < steps) request(step + i);
     for (; step < whole; step = step + 1) {
         arrive();
-        settled = !(there[2 * (step & 1)] && there[2 * (step & 1) + 1]);
+        settled = !(has(0) && has(1));
         if (settled) break;
         attend(std::false_type{}, step, true, true, request_next);
     }
     for (; step < steps; step = step + 1) {
         if (!settled) arrive();
         settled = false;
-        const bool there0 = there[2 * (step & 1)], there1 = there[2 * (step & 1) + 1];
-        attend(std::true_type{}, step, there0, there1, request_next);
+        attend(std::true_type{}, step, has(0), has(1), request_next);
+    }
+    if constexpr (PW > 1) {
+        // waves that share rows: the second leaves its part in LDS (in the place of the steps), the first takes it in
+        f32x4 *lo = reinterpret_cast<f32x4 *>(lds);              // [RW][16][64]
+        u32x2 *lml = reinterpret_cast<u32x2 *>(lds + RW * 16 * 64 * 16);
+        lds_barrier();
+        if (pw) {
+#pragma unroll
+            for (int i = 0; i < 16; ++i)
+                lo[(rw * 16 + i) * 64 + lane] = f32x4{oacc[i >> 2][4 * (i & 3)], oacc[i >> 2][4 * (i & 3) + 1], oacc[i >> 2][4 * (i & 3) + 2], oacc[i >> 2][4 * (i & 3) + 3]};
+            lml[rw * 64 + lane] = u32x2{__float_as_uint(mrow), __float_as_uint(lrow)};
+        }
+        lds_barrier();
+        if (!pw) {
+            const u32x2 ml = lml[rw * 64 + lane];
+            const float m_new = fmaxf(mrow, __uint_as_float(ml.x)), m_use = m_new == -__builtin_inff() ? 0.f : m_new;
+            const float keep = __builtin_amdgcn_exp2f((mrow - m_use) * scale_log2), fac = __builtin_amdgcn_exp2f((__uint_as_float(ml.x) - m_use) * scale_log2);
+            lrow = lrow * keep + fac * __uint_as_float(ml.y);
+            mrow = m_new;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const f32x4 o = lo[(rw * 16 + i) * 64 + lane];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) oacc[i >> 2][4 * (i & 3) + j] = oacc[i >> 2][4 * (i & 3) + j] * keep + o[j] * fac;
+            }
+        }
     }
     if (FLAT && (step0 > 0 || steps < pt.steps)) {
         const int slot = flat_slot(mine, worker, line[tile]);
-        const long long part = ((long long)h * 2 * p.workers + slot) * NW + w;
+        const long long part = ((long long)h * 2 * p.workers + slot) * RW + rw;
+        if (pw == 0) {
 #pragma unroll
-        for (int dt = 0; dt < 4; ++dt)
+            for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-                p.part_o[(part * 16 + 4 * dt + i) * 64 + lane] = f32x4{oacc[dt][4 * i], oacc[dt][4 * i + 1], oacc[dt][4 * i + 2], oacc[dt][4 * i + 3]};
-        *reinterpret_cast<u32x2 *>(p.part_ml + (part * 64 + lane) * 2) = u32x2{__float_as_uint(mrow * scale_log2), __float_as_uint(lrow)};
+                for (int i = 0; i < 4; ++i)
+                    p.part_o[(part * 16 + 4 * dt + i) * 64 + lane] = f32x4{oacc[dt][4 * i], oacc[dt][4 * i + 1], oacc[dt][4 * i + 2], oacc[dt][4 * i + 3]};
+            *reinterpret_cast<u32x2 *>(p.part_ml + (part * 64 + lane) * 2) = u32x2{__float_as_uint(mrow * scale_log2), __float_as_uint(lrow)};
+        }
         if (step0 == 0) {
             goes_on = s;
             goes_on_at = tile0;
@@ -289,7 +349,7 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
     }
     float sum = lrow + __shfl_xor(lrow, 32, 64);
     const float inv = sum > 0.f ? __fdiv_rn(vs, sum) : 0.f;      // a row that sees nothing: zeros
-    if (my_row < R) {
+    if (pw == 0 && my_row < R) {
         uint16_t *to = p.out + (a.row0 + token) * p.ldo + head_at + 4 * hi;
 #pragma unroll
         for (int dt = 0; dt < 4; ++dt)
@@ -312,16 +372,15 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
 
 // Joins the parts of the tiles that several workers share.  A unit is 32 rows (a wave's) and 32 d of a kv head of such a tile: the four waves
 // of a workgroup share its parts, four of them requested at a time, and meet in LDS; the workgroups walk the units.
-__global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptParams p) {
-    constexpr int NW = kPromptWaves;
+__global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptParams p, int RW /* 32 rows of a tile */) {
     __shared__ f32x4 sacc[3][4][64];
     __shared__ u32x2 sml[3][64];
     __shared__ int list[kMaxWorkers];
     const PagedParams &c = p.c;
-    const int units = shared_pieces(p.pieces, 4, p.workers, list) * c.Hkv * NW * 4;
+    const int units = shared_pieces(p.pieces, 4, p.workers, list) * c.Hkv * RW * 4;
     const int lane = threadIdx.x & 63, sg = threadIdx.x >> 6, hi = lane >> 5, col = lane & 31;
     for (int u = blockIdx.x; u < units; u += gridDim.x) {
-        const int dt = u & 3, w = (u >> 2) % NW, h = (u >> 2) / NW % c.Hkv, worker = list[(u >> 2) / NW / c.Hkv];
+        const int dt = u & 3, w = (u >> 2) % RW, h = (u >> 2) / RW % c.Hkv, worker = list[(u >> 2) / RW / c.Hkv];
         const int *piece = p.pieces + worker * 4;
         const int s = piece[0], row = piece[1] + w * 32 + col, count = piece[2] - worker + 1, first_slot = piece[3];
         const SeqSpan a = seq_span(c, s);
@@ -345,7 +404,7 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptParams p)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int slot = flat_part_slot(worker, first_slot, min(k0 + 4 * j, count - 1));
-                const long long part = ((long long)h * 2 * p.workers + slot) * NW + w;
+                const long long part = ((long long)h * 2 * p.workers + slot) * RW + w;
                 ml[j] = *reinterpret_cast<const u32x2 *>(p.part_ml + (part * 64 + lane) * 2);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) o[j][i] = p.part_o[(part * 16 + 4 * dt + i) * 64 + lane];
