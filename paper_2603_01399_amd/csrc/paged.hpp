@@ -147,6 +147,30 @@ __device__ __forceinline__ u32x4 e4m3x8_to_f16(unsigned int lo, unsigned int hi)
     r.w = __builtin_bit_cast(unsigned int, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true));
     return r;
 }
+// A value that is not finite, at a position that some rows of a product see and others do not, would reach those others as 0 x inf: it is
+// taken out of the product, and the rows that see it get a NaN for their sum.
+template <int KV> __device__ __forceinline__ unsigned int nonfinite_halves(unsigned int x) {      // bits 15 and 31
+    return KV == KV_BF16 ? ((x & 0x7F807F80u) + 0x00800080u) & 0x80008000u : ((x & 0x7C007C00u) + 0x04000400u) & 0x80008000u;
+}
+template <int KV> __device__ __forceinline__ bool any_nonfinite(const u32x4 v) {                  // of the wave
+    const unsigned int bad = nonfinite_halves<KV>(v.x) | nonfinite_halves<KV>(v.y) | nonfinite_halves<KV>(v.z) | nonfinite_halves<KV>(v.w);
+    return __builtin_amdgcn_ballot_w64(bad != 0) != 0ull;
+}
+// Clears them; the first position that had one, of the wave.  `first`: of the lane's slot 0; slots 4 .. 7 are 16 further on.
+template <int KV> __device__ __forceinline__ int drop_nonfinite(u32x4 &v, int first) {
+    int at = kMaxPositions * 2;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const unsigned int bad = nonfinite_halves<KV>(v[j]);
+        const int pos = first + 16 * (j >> 1) + 2 * (j & 1);
+        if (bad & 0x80000000u) { v[j] &= 0x0000FFFFu; at = min(at, pos + 1); }
+        if (bad & 0x00008000u) { v[j] &= 0xFFFF0000u; at = min(at, pos); }
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) at = min(at, __shfl_xor(at, off, 64));
+    return at;
+}
+
 template <int KV> __device__ __forceinline__ f32x16 values_times_weights(const u32x4 v, const u32x4 w, const f32x16 acc) {
     if constexpr (KV == KV_BF16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, w), acc, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, w), acc, 0, 0, 0);

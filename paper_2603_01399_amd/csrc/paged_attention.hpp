@@ -32,7 +32,7 @@ constexpr int kPagedWaves = 4;
 constexpr int kMaxWorkers = 512;             // of a kv head
 
 template <int KV, int NQT>
-__global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const PagedAttnParams p) {
+__global__ __launch_bounds__(kPagedWaves * 64, NQT == 1 ? 2 : 1) void paged_attention_kernel(const PagedAttnParams p) {
     constexpr int NW = kPagedWaves, BB = kv_block_bytes<KV>, NL = BB / 1024;     // 16-byte loads of a lane per block
     extern __shared__ __align__(16) unsigned char lds[];
     f32x4 *lo = reinterpret_cast<f32x4 *>(lds);                                  // [NW][NQT][8][64]
@@ -196,6 +196,12 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
                     v.y &= keep[1];
                     v.z &= keep[2];
                     v.w &= keep[3];
+                    if (n > 1 && any_nonfinite<KV>(v)) {
+                        const int first = drop_nonfinite<KV>(v, pos0 + 4 * g4);
+#pragma unroll
+                        for (int qt = 0; qt < NQT; ++qt)
+                            if (limit[qt] >= first) lrow[qt] = __builtin_nanf("");
+                    }
                 }
 #pragma unroll
                 for (int qt = 0; qt < NQT; ++qt)
@@ -257,7 +263,7 @@ __global__ __launch_bounds__(kPagedWaves * 64) void paged_attention_kernel(const
                 lsum += fac[ww] * lml[((ww * NQT + qt) * 16 + col) * 2 + 1];
             }
             const int r = 16 * qt + col;
-            const float inv = lsum > 0.f ? __fdiv_rn(vs, lsum) : 0.f;            // a row that sees nothing: zeros
+            const float inv = lsum == 0.f ? 0.f : __fdiv_rn(vs, lsum);            // a row that sees nothing: zeros
             for (int dt = w; dt < 8; dt += NW) {
                 f32x4 acc = {0.f, 0.f, 0.f, 0.f};
                 for (int ww = 0; ww < NW; ++ww) acc += lo[((ww * NQT + qt) * 8 + dt) * 64 + lane] * fac[ww];
@@ -365,7 +371,7 @@ __global__ __launch_bounds__(512) void paged_merge_kernel(const PagedAttnParams 
                 lsum += slsum[i][col] * f;
             }
             const float vs = c.v_scale ? c.v_scale[h] : 1.0f;
-            const float inv = lsum > 0.f ? __fdiv_rn(vs, lsum) : 0.f;
+            const float inv = lsum == 0.f ? 0.f : __fdiv_rn(vs, lsum);
             const int m = r / c.G, g = r % c.G;
             const u32x2 o = {float2_to_bf16_pair(acc.x * inv, acc.y * inv), float2_to_bf16_pair(acc.z * inv, acc.w * inv)};
             *reinterpret_cast<u32x2 *>(p.out + (a.row0 + m) * p.ldo + ((long long)h * c.G + g) * kHeadDim + 16 * dt + 4 * g4) = o;

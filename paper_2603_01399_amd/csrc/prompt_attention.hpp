@@ -272,6 +272,10 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
                             const int at = 16 * (j >> 1) + 2 * (j & 1);
                             va[j] &= (at <= end ? 0x0000FFFFu : 0u) | (at + 1 <= end ? 0xFFFF0000u : 0u);
                         }
+                        if (any_nonfinite<KV>(va)) {
+                            const int first = drop_nonfinite<KV>(va, pos0 + 32 * block(b) + 4 * (2 * t + hi));
+                            if (limit >= first) lrow = __builtin_nanf("");
+                        }
                     }
                     oacc[dt] = values_times_weights<KV>(va, pb[b][t], oacc[dt]);
                 }
@@ -348,7 +352,7 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
         continue;
     }
     float sum = lrow + __shfl_xor(lrow, 32, 64);
-    const float inv = sum > 0.f ? __fdiv_rn(vs, sum) : 0.f;      // a row that sees nothing: zeros
+    const float inv = sum == 0.f ? 0.f : __fdiv_rn(vs, sum);      // a row that sees nothing: zeros
     if (pw == 0 && my_row < R) {
         uint16_t *to = p.out + (a.row0 + token) * p.ldo + head_at + 4 * hi;
 #pragma unroll
@@ -426,7 +430,7 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptParams p,
             }
             const float sum = l + __shfl_xor(l, 32, 64);
             const float vs = c.v_scale ? c.v_scale[h] : 1.0f;
-            const float inv = sum > 0.f ? __fdiv_rn(vs, sum) : 0.f;
+            const float inv = sum == 0.f ? 0.f : __fdiv_rn(vs, sum);
             if (row < a.n * c.G) {
                 uint16_t *to = p.out + (a.row0 + row / c.G) * p.ldo + ((long long)h * c.G + row % c.G) * kHeadDim + 32 * dt + 4 * hi;
 #pragma unroll

@@ -111,6 +111,35 @@ def test_positions_without_a_page_are_not_visible(qb, call, kv):
     assert (np.abs(got - want) <= tol)[np.r_[0:4, 8:10]].all()
 
 
+@pytest.mark.parametrize("kv,bad", [("bf16", np.inf), ("bf16", -np.inf), ("bf16", np.nan), ("e4m3", np.nan)])
+@pytest.mark.parametrize("call,hq,news", [(c, *x) for c in ("paged", "prompt") for x in ((2, [6, 1]), (8, [5, 3]), (20, [8, 2]))] + [("prompt", 8, [40, 7])])
+def test_what_is_not_finite_reaches_the_rows_that_see_it_alone(qb, call, kv, bad, hq, news):
+    """A key and a value that are not finite, at new positions: rows behind them get no finite value for the head; rows before them and
+    other sequences and heads are as near the oracle as ever.  (Not their bits: 32 rows move the maximum that their weights are taken
+    against together, and another one rounds the weights elsewhere.)"""
+    say("not finite", call, kv, bad, hq, news)
+    b = Batch(qb, kv, 64, hq, 2, [90, 33], news, seed=300 + hq)
+    fn = lambda: (qb.paged_attention(b.q(), hq, b.cache, 0, b.row_start, max(news)) if call == "paged" else qb.prompt_attention(b.q(), hq, b.cache, 0, b.row_start))
+    want, tol = b.expected()
+    places, raw = pg.block_places(kv), b.cache.pool[0].view(torch.int16 if kv == "bf16" else torch.uint8)
+    bits = int(ref.f32_to_bf16_bits(np.array([bad], np.float32)).view(np.int16)[0]) if kv == "bf16" else 0x7F
+    for half in (0, 1):
+        keep = raw.clone()
+        pos = 90 + 3                                       # row 3 of the first sequence
+        raw[int(b.table[0, pos // 64]), 1, pos % 64 // 32, half, int(places[half][pos % 32, 17])] = bits
+        got = fn().view(b.rows, hq, D)
+        raw.copy_(keep)
+        same = torch.ones((b.rows, hq), dtype=torch.bool, device="cuda")
+        same[3:news[0], hq // 2:] = False
+        same = same.cpu().numpy()
+        assert (np.abs(got.double().cpu().numpy() - want)[same] <= tol[same]).all()
+        seen = got[3:news[0], hq // 2:].float()
+        if half == 1:                                      # (a score of -inf is a weight of 0: no fault of the output)
+            assert not torch.isfinite(seen).all(dim=2).any()
+        elif not np.isinf(bad):
+            assert not torch.isfinite(seen).all(dim=2).any()
+
+
 @pytest.mark.parametrize("call", ["paged", "prompt"])
 def test_books_that_do_not_fit(qb, call):
     """Lengths beyond the table end with it, rows beyond the tensor or below 0 are nobody's, more than max_new rows are left."""
