@@ -64,18 +64,17 @@ constexpr int kPromptStepBytes = kPromptStep / kKvBlock * 2 * kKvBlockBytes;   /
 // first.
 // PW: waves that share rows.  1: four times 32 rows, each wave over both blocks of a step.  2: twice 32 rows, each wave over one of the
 // blocks, joined at the end: for up to 64 rows a sequence, where half of four times 32 would be nobody's.
-// 8-bit pages.  PW = 1: widened on the way into LDS, once for all waves.  PW = 2, where memory bounds: in LDS as they are, four steps of half the
-// size, so that three are under way, and widened by each wave that reads them.
+// 8-bit pages are widened on the way into LDS, once for all waves.  (In LDS as they are, four steps of half the size with three under way, and
+// widened by each wave that reads them, 2 x 8 tokens of 64 / 8 heads over 100003 positions take 75.7 us, and 76.6 so.)
 template <int KV, bool FLAT, int PW>
 __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(const PromptParams p) {
     constexpr int NW = kPromptWaves, RW = NW / PW, ROWS = 32 * RW, NB = 2 / PW;  // row groups; blocks of a step for a wave
-    constexpr bool RAW = KV == KV_E4M3 && PW == 2, DIRECT = KV == KV_BF16 || RAW;
-    constexpr int STAGES = RAW ? 4 : 2, STAGE_BYTES = 2 * kPromptStepBytes / STAGES;         // steps in use and under way
-    extern __shared__ __align__(16) unsigned char lds[];         // [STAGES steps][2 blocks][keys | values], then the prefix sums
+    constexpr bool DIRECT = KV == KV_BF16;                       // from memory into LDS
+    extern __shared__ __align__(16) unsigned char lds[];         // [2 steps][2 blocks][keys | values][8192], then the prefix sums
     int *prefix = reinterpret_cast<int *>(lds + 2 * kPromptStepBytes);   // tiles ahead of a sequence
     int *wave_sums = prefix + kMaxSeqs;
-    int *there = wave_sums + NW;                                 // [step & (STAGES - 1)][block]: the block has a page
-    int *line = there + 2 * STAGES;                                       // FLAT: steps ahead of a tile
+    int *there = wave_sums + NW;                                 // [step & 3][block]: the block has a page
+    int *line = there + 8;                                       // FLAT: steps ahead of a tile
     const PagedParams &c = p.c;
     const int tid = threadIdx.x, lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -142,11 +141,11 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
         }
         const int page = __builtin_amdgcn_readlane(ids, step - ids_at);
         const bool good = page_exists(page, c.n_pages);
-        if (my_at == 0 && lane == 0) there[2 * (step & (STAGES - 1)) + my_blk] = good;
+        if (my_at == 0 && lane == 0) there[2 * (step & 3) + my_blk] = good;
         const unsigned char *from = head + (good ? page : 0) * page_step + ((2 * step + my_blk) & in_page) * (2 * BB);
         if constexpr (DIRECT) {
             // (scalar registers, which the load takes; the compiler may have them in vector ones)
-            const unsigned int to = __builtin_amdgcn_readfirstlane(lds_address_of(lds) + (step & (STAGES - 1)) * STAGE_BYTES + w * PART);
+            const unsigned int to = __builtin_amdgcn_readfirstlane(lds_address_of(lds) + (step & 1) * kPromptStepBytes + w * PART);
             const unsigned long long from64 = reinterpret_cast<unsigned long long>(from);
             const unsigned long long at = (unsigned long long)(unsigned int)__builtin_amdgcn_readfirstlane((int)(from64 >> 32)) << 32 |
                                           (unsigned int)__builtin_amdgcn_readfirstlane((int)from64);
@@ -157,15 +156,12 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
             for (int i = 0; i < NL; ++i) code[i] = reinterpret_cast<const u32x4 *>(from)[64 * i + lane];
         }
     };
-    // what request() asked for is in LDS afterwards (for this wave; the others' behind a barrier); `behind`: steps requested since
-    auto settle = [&](int step, int behind) {
+    // what request() asked for is in LDS afterwards (for this wave; the others' behind a barrier)
+    auto settle = [&](int step) {
         if constexpr (DIRECT) {
-            // (loads arrive in order: those of later steps may be under way)
-            if (STAGES > 2 && behind >= 2) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(2 * NL) : "memory");
-            else if (STAGES > 2 && behind == 1) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(NL) : "memory");
-            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
         } else {
-            u32x4 *to = reinterpret_cast<u32x4 *>(lds + (step & (STAGES - 1)) * STAGE_BYTES + w * 2 * PART) + lane;
+            u32x4 *to = reinterpret_cast<u32x4 *>(lds + (step & 1) * kPromptStepBytes + w * 2 * PART) + lane;
 #pragma unroll
             for (int i = 0; i < NL; ++i) {
                 // (a wave's part is keys or values)
@@ -181,26 +177,16 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
     for (int dt = 0; dt < 4; ++dt)
 #pragma unroll
         for (int i = 0; i < 16; ++i) oacc[dt][i] = 0.f;
-    // this lane's place in a block: row col of the keys, d = col of the values.  8-bit: 16 bytes of the keys hold two operands (ksteps of 32),
-    // 8 of the values one
-    constexpr int LB = RAW ? BB : kKvBlockBytes;                 // keys or values of a block in LDS
-    const int k_lane = (((col >> 3) & 1) * (LB / 32) + (col >> 4) * 8 + (col & 7) + 16 * hi) * 16;
-    const int v_lane = RAW ? ((col & 15) + 16 * hi) * 16 + (col >> 4) * 8 : ((col >> 4) * 64 + (col & 15) + 16 * hi) * 16;
-    auto keys = [&](const unsigned char *at, int k) {            // operand k of 8
-        if constexpr (!RAW) return *reinterpret_cast<const u32x4 *>(at + k_lane + k * 512);
-        const u32x2 v = *reinterpret_cast<const u32x2 *>(at + k_lane + (k >> 2) * 1024 + (k & 1) * 512 + ((k >> 1) & 1) * 8);
-        return e4m3x8_to_bf16(v.x, v.y);
-    };
-    auto values = [&](const unsigned char *at, int dt, int t) {  // (RAW: the codes, in the first half)
-        if constexpr (!RAW) return *reinterpret_cast<const u32x4 *>(at + v_lane + dt * 2048 + t * 512);
-        const u32x2 v = *reinterpret_cast<const u32x2 *>(at + v_lane + dt * 1024 + t * 512);
-        return u32x4{v.x, v.y, 0u, 0u};
-    };
+    // this lane's place in a block: row col of the keys, d = col of the values
+    const int k_lane = (((col >> 3) & 1) * 256 + (col >> 4) * 8 + (col & 7) + 16 * hi) * 16;     // [sub 2][kstep 4][g4 4][p 16] of 16 bytes
+    const int v_lane = ((col >> 4) * 64 + (col & 15) + 16 * hi) * 16;                         // [dt 8][g4 4][dd 16] of 16 bytes
+    auto keys = [&](const unsigned char *at, int k) { return *reinterpret_cast<const bf16x8 *>(at + k_lane + k * 512); };
+    auto values = [&](const unsigned char *at, int dt, int t) { return *reinterpret_cast<const u32x4 *>(at + v_lane + dt * 2048 + t * 512); };
 
     // the wave's blocks of a step; edge: some are hidden from some row, or are nobody's; between(): called while the scores are computed
     auto attend = [&](auto edge, int step, bool there0, bool there1, auto between) {
         constexpr bool EDGE = decltype(edge)::value;
-        const unsigned char *buf = lds + (step & (STAGES - 1)) * STAGE_BYTES;
+        const unsigned char *buf = lds + (step & 1) * kPromptStepBytes;
         const int pos0 = step * kPromptStep;
         auto block = [&](int b) { return PW == 1 ? b : pw; };    // the wave's b-th block
         auto has_page = [&](int b) { return block(b) ? there1 : there0; };
@@ -213,7 +199,7 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
         for (int k = 0; k < 8; ++k)
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
-                const bf16x8 ka = __builtin_bit_cast(bf16x8, keys(buf + block(b) * 2 * LB, k));
+                const bf16x8 ka = keys(buf + block(b) * 2 * kKvBlockBytes, k);
                 sc[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(ka, qb[k], sc[b], 0, 0, 0);
             }
         if constexpr (EDGE) {
@@ -231,7 +217,7 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-            for (int dt = 0; dt < 4; ++dt) v0[t][dt] = values(buf + (2 * block(0) + 1) * LB, dt, t);
+            for (int dt = 0; dt < 4; ++dt) v0[t][dt] = values(buf + (2 * block(0) + 1) * kKvBlockBytes, dt, t);
         float mx = larger(sc[0][0], sc[NB - 1][0]);
 #pragma unroll
         for (int i = 1; i < 16; ++i) mx = larger(mx, larger(sc[0][i], sc[NB - 1][i]));
@@ -262,8 +248,7 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
             for (int t = 0; t < 2; ++t)
 #pragma unroll
                 for (int dt = 0; dt < 4; ++dt) {
-                    u32x4 va = b == 0 ? v0[t][dt] : values(buf + (2 * block(b) + 1) * LB, dt, t);
-                    if constexpr (RAW) va = e4m3x8_to_f16(va.x, va.y);
+                    u32x4 va = b == 0 ? v0[t][dt] : values(buf + (2 * block(b) + 1) * kKvBlockBytes, dt, t);
                     if constexpr (EDGE) {
                         // positions that no row sees hold whatever the page held: they must not reach the product (0 x NaN)
                         const int end = has_page(b) ? last_pos - pos0 - 32 * block(b) - 4 * (2 * t + hi) : -1;
@@ -286,15 +271,24 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
     int step = step0;
     bool settled = false;
     auto arrive = [&] {
-        settle(step, steps - 1 - step);
+        if constexpr (DIRECT) settle(step);
         lds_barrier();
     };
+    // (codes that pass through registers are widened while the scores of the step before are computed, and those of the step behind requested)
     auto request_next = [&] {
-        if (step + STAGES - 1 < steps) request(step + STAGES - 1);
+        if constexpr (DIRECT) {
+            if (step + 1 < steps) request(step + 1);
+        } else {
+            if (step + 1 < steps) settle(step + 1);
+            if (step + 2 < steps) request(step + 2);
+        }
     };
-    auto has = [&](int blk) { return __builtin_amdgcn_readfirstlane(there[2 * (step & (STAGES - 1)) + blk]) != 0; };
-    for (int i = 0; i < STAGES - 1; ++i)
-        if (step + i < steps) request(step + i);
+    auto has = [&](int blk) { return __builtin_amdgcn_readfirstlane(there[2 * (step & 3) + blk]) != 0; };
+    if (step < steps) request(step);
+    if constexpr (!DIRECT) {
+        if (step < steps) settle(step);
+        if (step + 1 < steps) request(step + 1);
+    }
     for (; step < whole; step = step + 1) {
         arrive();
         settled = !(has(0) && has(1));
