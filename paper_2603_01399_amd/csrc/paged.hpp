@@ -78,6 +78,17 @@ __device__ __forceinline__ int prefix_sums(int n, int *out, int *wave_sums, V v)
     return carry;
 }
 
+// Sum of v over the lanes up to each one (all 64 active).
+__device__ __forceinline__ int lane_sums(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0x111, 0xf, 0xf, true);               // from 1, 2, 4 and 8 lanes before, within 16 lanes
+    v += __builtin_amdgcn_update_dpp(0, v, 0x112, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x114, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x118, 0xf, 0xf, true);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x142, 0xa, 0xf, false);              // lane 15 to the 16 lanes behind it, lane 47 likewise
+    v += __builtin_amdgcn_update_dpp(0, v, 0x143, 0xc, 0xf, false);              // lane 31 to the 32 lanes behind it
+    return v;
+}
+
 template <int KV> __device__ __forceinline__ int k_page_index(int pib, int d) {
     if constexpr (KV == KV_BF16) return (int)k_cache_index(pib, d);
     return (((((pib >> 4) * 2 + (d >> 6)) * 4 + ((d & 31) >> 3)) * 16 + (pib & 15)) * 2 + ((d >> 5) & 1)) * 8 + (d & 7);

@@ -37,23 +37,57 @@ struct PromptTile {
     SeqSpan a;
 };
 
-// UNIFORM: f is the same for the wave, and so is what it finds (LDS does not say so).
-template <int ROWS, bool UNIFORM>
-__device__ __forceinline__ PromptTile prompt_tile(const PagedParams &c, const int *prefix, int f) {
+__device__ __forceinline__ PromptTile prompt_tile(const PagedParams &c, int rows, int s, const SeqSpan &a, int tile0) {
     PromptTile t;
+    t.s = s;
+    t.a = a;
+    t.R = a.n * c.G;
+    t.tile0 = tile0;
+    t.first_pos = a.len + tile0 / c.G;                           // positions up to here are visible to every row of the tile
+    t.last_pos = a.len + (min(tile0 + rows, t.R) - 1) / c.G;
+    t.steps = (blocks_of(c, t.last_pos + 1) + 1) / 2;
+    return t;
+}
+
+// Tile f of the line of all sequences' tiles.  UNIFORM: f is the same for the wave, and so is what it finds (LDS does not say so).
+template <int ROWS, bool UNIFORM>
+__device__ __forceinline__ PromptTile tile_of_line(const PagedParams &c, const int *prefix, int f) {
     int s = 0, up = c.n_seqs;
     while (up - s > 1) {
         const int mid = (s + up) >> 1;
         if (prefix[mid] <= f) s = mid; else up = mid;
     }
-    t.s = s = UNIFORM ? __builtin_amdgcn_readfirstlane(s) : s;
-    t.a = seq_span(c, s);
-    t.R = t.a.n * c.G;
-    t.tile0 = (f - (UNIFORM ? __builtin_amdgcn_readfirstlane(prefix[s]) : prefix[s])) * ROWS;
-    t.first_pos = t.a.len + t.tile0 / c.G;                       // positions up to here are visible to every row of the tile
-    t.last_pos = t.a.len + (min(t.tile0 + ROWS, t.R) - 1) / c.G;
-    t.steps = (blocks_of(c, t.last_pos + 1) + 1) / 2;
-    return t;
+    if (UNIFORM) s = __builtin_amdgcn_readfirstlane(s);
+    return prompt_tile(c, ROWS, s, seq_span(c, s), (f - (UNIFORM ? __builtin_amdgcn_readfirstlane(prefix[s]) : prefix[s])) * ROWS);
+}
+
+__device__ __forceinline__ SeqSpan span_of_lane(const SeqSpan &a, int l) {
+    return SeqSpan{__builtin_amdgcn_readlane(a.row0, l), __builtin_amdgcn_readlane(a.n, l), __builtin_amdgcn_readlane(a.len, l)};
+}
+
+// Tile `back` from the end of the line; R = 0: there are fewer.  Each wave for itself, a sequence a lane: no LDS, and nothing is read twice.
+template <int ROWS>
+__device__ __forceinline__ PromptTile tile_from_end(const PagedParams &c, int back) {
+    constexpr int AT_ONCE = 4;
+    const int lane = threadIdx.x & 63;
+    for (int end = c.n_seqs; end > 0; end -= 64 * AT_ONCE) {
+        SeqSpan a[AT_ONCE];
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int s = end - 1 - 64 * k - lane;
+            a[k] = s >= 0 ? seq_span(c, s) : SeqSpan{0, 0, 0};
+        }
+#pragma unroll
+        for (int k = 0; k < AT_ONCE; ++k) {
+            const int tiles = (a[k].n * c.G + ROWS - 1) / ROWS, upto = lane_sums(tiles), all = __builtin_amdgcn_readlane(upto, 63);
+            if (back < all) {
+                const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > back));
+                return prompt_tile(c, ROWS, end - 1 - 64 * k - l, span_of_lane(a[k], l), (__builtin_amdgcn_readlane(upto, l) - 1 - back) * ROWS);
+            }
+            back -= all;
+        }
+    }
+    return PromptTile{};
 }
 
 constexpr int kPromptStep = 64;                          // positions in LDS at a time
@@ -84,25 +118,29 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
     const float ks = c.k_scale ? c.k_scale[h] : 1.0f, vs = c.v_scale ? c.v_scale[h] : 1.0f;
     const float scale_log2 = p.scale_log2 * ks;
 
-    int tiles = prefix_sums<NW>(c.n_seqs, prefix, wave_sums, [&](int s) { return (int)(((long long)seq_span(c, s).n * c.G + ROWS - 1) / ROWS); });
-    int tile = __builtin_amdgcn_readfirstlane(tiles - 1 - worker), at = 0, end = 0;              // FLAT: steps at .. end - 1 of the line
+    int tile = 0, at = 0, end = 0;                               // FLAT: steps at .. end - 1 of the line
     FlatShare mine{};
     int goes_on = -1, goes_on_at = 0, last_worker = 0, first_slot = 0;
+    PromptTile pt{};
     if constexpr (FLAT) {
-        tiles = min(tiles, kMaxFlatTiles);                       // (more only where the rows' starts do not fit the tensor)
-        const int total = prefix_sums<NW>(tiles, line, wave_sums, [&](int f) { return prompt_tile<ROWS, false>(c, prefix, f).steps; });
+        // (more tiles than kMaxFlatTiles only where the rows' starts do not fit the tensor)
+        const int tiles = min(kMaxFlatTiles, prefix_sums<NW>(c.n_seqs, prefix, wave_sums, [&](int s) {
+            return (int)(((long long)seq_span(c, s).n * c.G + ROWS - 1) / ROWS);
+        }));
+        const int total = prefix_sums<NW>(tiles, line, wave_sums, [&](int f) { return tile_of_line<ROWS, false>(c, prefix, f).steps; });
         mine = flat_share(total, p.workers, p.least, worker);
         at = __builtin_amdgcn_readfirstlane(mine.begin);
         end = __builtin_amdgcn_readfirstlane(mine.end);
-        tile = 0;
         for (int up = tiles; up - tile > 1;) {
             const int mid = (tile + up) >> 1;
             if (line[mid] <= at) tile = mid; else up = mid;
         }
         tile = __builtin_amdgcn_readfirstlane(tile);
+    } else {
+        pt = tile_from_end<ROWS>(c, worker);
     }
-    for (; FLAT ? at < end : tile >= 0; tile = FLAT ? tile + 1 : -1) {
-    const PromptTile pt = prompt_tile<ROWS, true>(c, prefix, tile);
+    for (bool more = FLAT ? at < end : pt.R > 0; more; more = FLAT && at < end, ++tile) {
+    if constexpr (FLAT) pt = tile_of_line<ROWS, true>(c, prefix, tile);
     const SeqSpan a = pt.a;
     const int R = pt.R, tile0 = pt.tile0, first_pos = pt.first_pos, last_pos = pt.last_pos, s = pt.s;
     const int nblk = blocks_of(c, last_pos + 1);
