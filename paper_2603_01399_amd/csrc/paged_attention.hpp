@@ -305,9 +305,10 @@ __device__ __forceinline__ int shared_pieces(const int *records, int words, int 
     return n;
 }
 
-// Joins the pieces of the sequences that several workers share.  A unit is 16 rows and 16 d of a kv
-// head of such a sequence: the eight waves of a workgroup share its pieces, four of them requested at a time, and meet in LDS.  The
-// workgroups walk the units: one for every worker, head and unit were up to 8192, nearly all with nothing to do (24 us where this takes 6).
+// Joins the pieces of the sequences that several workers share.  A unit is 16 rows and 16 d of a kv head of such a sequence.  Where a workgroup
+// has one unit, its eight waves share the pieces, four of them requested at a time, and meet in LDS; where there are more units than
+// workgroups, many sequences are shared by few workers each, and every wave takes units of its own (64 x 1 tokens over up to 8192 positions, with the
+// attention: 191.9 us, and 197.5 by workgroups that walk the units; 16 x 8 over 4000: 39.2 and 44.5).
 __global__ __launch_bounds__(512) void paged_merge_kernel(const PagedAttnParams p, int NQT) {
     __shared__ float smax[8][16];
     __shared__ float slsum[8][16];
@@ -316,23 +317,24 @@ __global__ __launch_bounds__(512) void paged_merge_kernel(const PagedAttnParams 
     const PagedParams &c = p.c;
     const int *records = p.pieces;
     const int units = shared_pieces(records, 4, p.workers, list) * c.Hkv * NQT * 8;
-    const int sg = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int sg = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int g4 = lane >> 4, col = lane & 15;
-    for (int u = blockIdx.x; u < units; u += gridDim.x) {
-        const int dt = u & 7, qt = (u >> 3) % NQT, h = (u >> 3) / NQT % c.Hkv, worker = list[(u >> 3) / NQT / c.Hkv];
+    auto unit = [&](auto each_wave, int u) {
+        constexpr bool alone = decltype(each_wave)::value;       // a wave for itself
+        const int dt = u & 7, qt = (u >> 3) % NQT, h = (u >> 3) / NQT % c.Hkv, worker = __builtin_amdgcn_readfirstlane(list[(u >> 3) / NQT / c.Hkv]);
         const int s = records[worker * 4], last = records[worker * 4 + 1], first_slot = records[worker * 4 + 2];
         const SeqSpan a = seq_span(c, s);
         const int R = a.n * c.G, r = 16 * qt + col;
-        if (16 * qt >= R) continue;
-        const int count = last - worker + 1;
+        if (16 * qt >= R) return;
+        const int count = last - worker + 1, step = alone ? 1 : 8;
         float mw = -__builtin_inff(), lsum = 0.f;
         f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-        for (int k0 = sg; k0 < count; k0 += 32) {
+        for (int k0 = alone ? 0 : sg; k0 < count; k0 += 4 * step) {
             f32x4 o[4];
             u32x2 ml[4];
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const int slot = flat_part_slot(worker, first_slot, min(k0 + 8 * i, count - 1));
+                const int slot = flat_part_slot(worker, first_slot, min(k0 + step * i, count - 1));
                 const long long pb = ((long long)h * (2 * p.workers) + slot) * NQT + qt;
                 ml[i] = reinterpret_cast<const u32x2 *>(p.part_ml)[pb * 16 + col];
                 o[i] = p.part_o[(pb * 8 + dt) * 64 + lane];
@@ -340,7 +342,7 @@ __global__ __launch_bounds__(512) void paged_merge_kernel(const PagedAttnParams 
             float m_new = mw;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (k0 + 8 * i < count) m_new = fmaxf(m_new, __uint_as_float(ml[i].x));
+                if (k0 + step * i < count) m_new = fmaxf(m_new, __uint_as_float(ml[i].x));
             const float m_use = m_new == -__builtin_inff() ? 0.f : m_new;        // nothing visible in these pieces
             const float keep = exp2f(mw - m_use);
             acc *= keep;
@@ -348,35 +350,43 @@ __global__ __launch_bounds__(512) void paged_merge_kernel(const PagedAttnParams 
             mw = m_new;
 #pragma unroll
             for (int i = 0; i < 4; ++i)
-                if (k0 + 8 * i < count) {
+                if (k0 + step * i < count) {
                     const float f = exp2f(__uint_as_float(ml[i].x) - m_use);
                     lsum += f * __uint_as_float(ml[i].y);
                     acc += o[i] * f;
                 }
         }
-        sacc[sg][lane] = acc;
-        if (g4 == 0) { smax[sg][col] = mw; slsum[sg][col] = lsum; }
-        __syncthreads();
-        if (sg == 0 && r < R) {
-            float mstar = smax[0][col];
+        if constexpr (!alone) {
+            sacc[sg][lane] = acc;
+            if (g4 == 0) { smax[sg][col] = mw; slsum[sg][col] = lsum; }
+            __syncthreads();
+            if (sg == 0) {
+                float mstar = smax[0][col];
 #pragma unroll
-            for (int i = 1; i < 8; ++i) mstar = fmaxf(mstar, smax[i][col]);
-            const float m_use = mstar == -__builtin_inff() ? 0.f : mstar;
-            acc = f32x4{0.f, 0.f, 0.f, 0.f};
-            lsum = 0.f;
+                for (int i = 1; i < 8; ++i) mstar = fmaxf(mstar, smax[i][col]);
+                const float m_use = mstar == -__builtin_inff() ? 0.f : mstar;
+                acc = f32x4{0.f, 0.f, 0.f, 0.f};
+                lsum = 0.f;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float f = exp2f(smax[i][col] - m_use);
-                acc += sacc[i][lane] * f;
-                lsum += slsum[i][col] * f;
+                for (int i = 0; i < 8; ++i) {
+                    const float f = exp2f(smax[i][col] - m_use);
+                    acc += sacc[i][lane] * f;
+                    lsum += slsum[i][col] * f;
+                }
             }
+        }
+        if ((alone || sg == 0) && r < R) {
             const float vs = c.v_scale ? c.v_scale[h] : 1.0f;
             const float inv = lsum == 0.f ? 0.f : __fdiv_rn(vs, lsum);
             const int m = r / c.G, g = r % c.G;
             const u32x2 o = {float2_to_bf16_pair(acc.x * inv, acc.y * inv), float2_to_bf16_pair(acc.z * inv, acc.w * inv)};
             *reinterpret_cast<u32x2 *>(p.out + (a.row0 + m) * p.ldo + ((long long)h * c.G + g) * kHeadDim + 16 * dt + 4 * g4) = o;
         }
-        __syncthreads();
+    };
+    if (units > (int)gridDim.x) {
+        for (int u = blockIdx.x * 8 + sg; u < units; u += gridDim.x * 8) unit(std::true_type{}, u);
+    } else if ((int)blockIdx.x < units) {
+        unit(std::false_type{}, blockIdx.x);
     }
 }
 

@@ -406,21 +406,24 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
     }
 }
 
-// Joins the parts of the tiles that several workers share.  A unit is 32 rows (a wave's) and 32 d of a kv head of such a tile: the four waves
-// of a workgroup share its parts, four of them requested at a time, and meet in LDS; the workgroups walk the units.
+// Joins the parts of the tiles that several workers share.  A unit is 32 rows (a wave's) and 32 d of a kv head of such a tile.  As in
+// paged_merge_kernel, the four waves of a workgroup share its parts, four of them requested at a time, and meet in LDS, or each takes units of its
+// own where there are more of them than workgroups (4 x 700 tokens of 32 / 8 heads behind 3000
+// positions, with the attention: 110.7 us, and 115.5 by workgroups that walk the units).
 __global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptParams p, int RW /* 32 rows of a tile */) {
     __shared__ f32x4 sacc[3][4][64];
     __shared__ u32x2 sml[3][64];
     __shared__ int list[kMaxWorkers];
     const PagedParams &c = p.c;
     const int units = shared_pieces(p.pieces, 4, p.workers, list) * c.Hkv * RW * 4;
-    const int lane = threadIdx.x & 63, sg = threadIdx.x >> 6, hi = lane >> 5, col = lane & 31;
-    for (int u = blockIdx.x; u < units; u += gridDim.x) {
-        const int dt = u & 3, w = (u >> 2) % RW, h = (u >> 2) / RW % c.Hkv, worker = list[(u >> 2) / RW / c.Hkv];
+    const int lane = threadIdx.x & 63, sg = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), hi = lane >> 5, col = lane & 31;
+    auto unit = [&](auto each_wave, int u) {
+        constexpr bool alone = decltype(each_wave)::value;       // a wave for itself
+        const int dt = u & 3, w = (u >> 2) % RW, h = (u >> 2) / RW % c.Hkv, worker = __builtin_amdgcn_readfirstlane(list[(u >> 2) / RW / c.Hkv]);
         const int *piece = p.pieces + worker * 4;
         const int s = piece[0], row = piece[1] + w * 32 + col, count = piece[2] - worker + 1, first_slot = piece[3];
         const SeqSpan a = seq_span(c, s);
-        if (piece[1] + w * 32 >= a.n * c.G) continue;
+        if (piece[1] + w * 32 >= a.n * c.G) return;
         float m = -__builtin_inff(), l = 0.f;
         f32x4 acc[4];
 #pragma unroll
@@ -434,12 +437,13 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptParams p,
             for (int i = 0; i < 4; ++i) acc[i] = acc[i] * keep + o[i] * f;
             m = m_new;
         };
-        for (int k0 = sg; k0 < count; k0 += 16) {
+        const int step = alone ? 1 : 4;
+        for (int k0 = alone ? 0 : sg; k0 < count; k0 += 4 * step) {
             f32x4 o[4][4];
             u32x2 ml[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const int slot = flat_part_slot(worker, first_slot, min(k0 + 4 * j, count - 1));
+                const int slot = flat_part_slot(worker, first_slot, min(k0 + step * j, count - 1));
                 const long long part = ((long long)h * 2 * p.workers + slot) * RW + w;
                 ml[j] = *reinterpret_cast<const u32x2 *>(p.part_ml + (part * 64 + lane) * 2);
 #pragma unroll
@@ -447,32 +451,38 @@ __global__ __launch_bounds__(256) void prompt_merge_kernel(const PromptParams p,
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j)
-                if (k0 + 4 * j < count) join(ml[j], o[j]);
+                if (k0 + step * j < count) join(ml[j], o[j]);
         }
-        if (sg) {
-            sml[sg - 1][lane] = u32x2{__float_as_uint(m), __float_as_uint(l)};
+        if constexpr (!alone) {
+            if (sg) {
+                sml[sg - 1][lane] = u32x2{__float_as_uint(m), __float_as_uint(l)};
 #pragma unroll
-            for (int i = 0; i < 4; ++i) sacc[sg - 1][i][lane] = acc[i];
-        }
-        __syncthreads();
-        if (sg == 0) {
-            for (int k = 0; k < 3; ++k) {
-                const f32x4 o[4] = {sacc[k][0][lane], sacc[k][1][lane], sacc[k][2][lane], sacc[k][3][lane]};
-                join(sml[k][lane], o);
+                for (int i = 0; i < 4; ++i) sacc[sg - 1][i][lane] = acc[i];
             }
-            const float sum = l + __shfl_xor(l, 32, 64);
-            const float vs = c.v_scale ? c.v_scale[h] : 1.0f;
-            const float inv = sum == 0.f ? 0.f : __fdiv_rn(vs, sum);
-            if (row < a.n * c.G) {
-                uint16_t *to = p.out + (a.row0 + row / c.G) * p.ldo + ((long long)h * c.G + row % c.G) * kHeadDim + 32 * dt + 4 * hi;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const u32x2 o = {float2_to_bf16_pair(acc[i].x * inv, acc[i].y * inv), float2_to_bf16_pair(acc[i].z * inv, acc[i].w * inv)};
-                    *reinterpret_cast<u32x2 *>(to + 8 * i) = o;
+            __syncthreads();
+            if (sg == 0) {
+                for (int k = 0; k < 3; ++k) {
+                    const f32x4 o[4] = {sacc[k][0][lane], sacc[k][1][lane], sacc[k][2][lane], sacc[k][3][lane]};
+                    join(sml[k][lane], o);
                 }
             }
         }
-        __syncthreads();
+        const float sum = l + __shfl_xor(l, 32, 64);
+        const float vs = c.v_scale ? c.v_scale[h] : 1.0f;
+        const float inv = sum == 0.f ? 0.f : __fdiv_rn(vs, sum);
+        if ((alone || sg == 0) && row < a.n * c.G) {
+            uint16_t *to = p.out + (a.row0 + row / c.G) * p.ldo + ((long long)h * c.G + row % c.G) * kHeadDim + 32 * dt + 4 * hi;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const u32x2 o = {float2_to_bf16_pair(acc[i].x * inv, acc[i].y * inv), float2_to_bf16_pair(acc[i].z * inv, acc[i].w * inv)};
+                *reinterpret_cast<u32x2 *>(to + 8 * i) = o;
+            }
+        }
+    };
+    if (units > (int)gridDim.x) {
+        for (int u = blockIdx.x * 4 + sg; u < units; u += gridDim.x * 4) unit(std::true_type{}, u);
+    } else if ((int)blockIdx.x < units) {
+        unit(std::false_type{}, blockIdx.x);
     }
 }
 
