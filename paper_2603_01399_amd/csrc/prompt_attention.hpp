@@ -8,6 +8,15 @@
 // S^T = K Q^T and O^T = V^T P^T in 32 x 32 x 16 products: a lane owns one query column.  The
 // rows of K are permuted, row 16 t + 8 c + 4 h + b of the product being position 16 c + 8 t + 4 h + b, which makes the scores that a lane
 // holds after the first product the operand of the second as they lie, against values in the cache's own order.
+//
+// Bound by the matrix cores and the power they draw: 8192 rows of 64 / 8 heads take 1.04 to 1.10 ms (1.0 to 1.06 PFLOP/s; a large library
+// product reaches 1.36 on the same card).  Matrix cores are busy 52 % of the cycles there and the vector units 37 % with the softmax (32
+// exponentials, 32 multiply-adds, 25 maxima, 16 conversions and 16 sums a wave and step of 32 products), at about 2.0 GHz; the products
+// alone, without the softmax, took 0.82 to 0.88 ms.  LDS is busy 27 %, without bank conflicts.  Tried and slower or the same: 64 rows a
+// wave (the accumulators' registers are copied), three steps in LDS, steps of 32 positions, priorities by phase or by wave.
+// Many short prompts are bound by memory and the start of a tile: 60 of up to 300 rows 73 us, of which 32 for queries and outputs; 9 of up to 1531 110.
+// A workgroup a tile in the order of steps of all sequences' tiles evens out what is left at the end, but finds its tile later: 9 of up to 1531
+// 112.6, 60 of up to 300 behind 2000 311 where this order takes 333, 30 of up to 700 118 and 108.
 #pragma once
 
 #include <type_traits>
@@ -24,11 +33,14 @@ struct PromptParams {
     f32x4 *part_o;            // FLAT: [Hkv][2 workers][32 rows of a tile][16][64], what workers leave of a tile that they share
     float *part_ml;           // [Hkv][2 workers][32 rows of a tile][64][2]
     int *pieces;              // [workers][4]: sequence of the tile that begins with a worker and goes on (-1: none), its first row, last worker, slot
-    int workers, least;       // steps that a worker takes at least
+    int workers;              // of a kv head
     float scale_log2;         // log2(e) / sqrt(128)
 };
 
 constexpr int kPromptWaves = 4;                          // of a workgroup, two workgroups a compute unit
+// Steps of a worker at least, where steps are shared: with fewer, what the join reads costs more than the worker saves (8 tokens over up to 8000
+// positions, 64 / 8 heads, 20.5 us; two steps 24.1, three 22.7; over up to 1000, 8-bit, 15.6, 14.5 and 14.8).
+constexpr int kFlatLeast = 4;
 constexpr int kMaxFlatTiles = 2048;                      // of a launch that shares tiles: their prefix sums live in LDS
 
 // A tile of rows: its sequence, its first row there, and what its rows see.
@@ -128,7 +140,7 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
             return (int)(((long long)seq_span(c, s).n * c.G + ROWS - 1) / ROWS);
         }));
         const int total = prefix_sums<NW>(tiles, line, wave_sums, [&](int f) { return tile_of_line<ROWS, false>(c, prefix, f).steps; });
-        mine = flat_share(total, p.workers, p.least, worker);
+        mine = flat_share(total, p.workers, kFlatLeast, worker);
         at = __builtin_amdgcn_readfirstlane(mine.begin);
         end = __builtin_amdgcn_readfirstlane(mine.end);
         for (int up = tiles; up - tile > 1;) {
