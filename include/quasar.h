@@ -541,6 +541,7 @@ int quasar_verify_attention(const uint16_t *q, int64_t M, int64_t ldq, int64_t n
  * 1 <= n_seqs <= 1024, max_pages * page_len <= 2^24, n_pages <= 2^20.  Books that break these rules (a page id or row beyond its buffer, a
  * length beyond the table) give unspecified values, but nothing outside the buffers is read or written: positions without a page are
  * not visible and are not written, sequences whose rows do not fit have none.
+ * A workspace serves one call at a time: calls that may overlap (other streams, graphs that are replayed side by side) take one each.
  * Order of a step: quasar_pages_reserve, then per layer quasar_paged_prepare and quasar_paged_attention (quasar_prompt_attention), then
  * the caller adds the accepted tokens to lengths.
  */
@@ -558,7 +559,7 @@ int quasar_paged_prepare(const uint16_t *qkv, int64_t T, int64_t ld, int64_t n_q
 /* quasar_verify_attention for a batch: row i of sequence s sees positions 0 .. lengths[s] + i; rows that see nothing give 0.  For the new
  * tokens of a step: at most max_new <= 32 a sequence (a sequence with more has rows beyond that left as they were), and
  * max_new * n_q_heads / n_kv_heads <= 1024.  Work is shared by cached positions, not by sequences: ragged lengths cost no more than even ones.
- * workspace: quasar_paged_attention_workspace_bytes.  q 16-byte, out 8-byte aligned; ldq a multiple of 8, ldo of 4.  Two launches. */
+ * workspace: quasar_paged_attention_workspace_bytes.  q 16-byte, out 8-byte aligned; ldq a multiple of 8, ldo of 4.  At most two launches. */
 size_t quasar_paged_attention_workspace_bytes(int64_t max_new, int64_t n_q_heads, int64_t n_kv_heads);   /* 0 on invalid arguments */
 int quasar_paged_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n_q_heads, int64_t n_kv_heads, const int32_t *row_start,
                            int64_t n_seqs, int64_t max_new, const void *pages, int64_t n_pages, int64_t page_len, int kv_dtype,
