@@ -702,6 +702,12 @@ class PagedKvCache:
                                          pool.device.index, pool.data_ptr(), self._refs, self._lengths, self._table,
                                          0 if k_scale is None else k_scale.data_ptr(), 0 if v_scale is None else v_scale.data_ptr())
 
+    def __setattr__(self, name, value):
+        # (the handle has the buffers' addresses: another tensor in their place would not be used, and the old one freed)
+        if "_handle" in self.__dict__ and self.__dict__.get(name, value) is not value:
+            raise AttributeError(f"{name} is the cache's own: write into the tensor (cache.{name}[...] = ...), or make another cache")
+        object.__setattr__(self, name, value)
+
     def _layer(self, layer: int):
         if not 0 <= layer < self.n_layers:
             raise ValueError(f"layer must be in 0 .. {self.n_layers - 1}")
@@ -828,6 +834,8 @@ def paged_attention(q: torch.Tensor, n_q_heads: int, cache: PagedKvCache, layer:
         workspace = torch.empty(max(_lib.quasar_paged_attention_workspace_bytes(max_new, n_q_heads, cache.n_kv_heads), 16), dtype=torch.uint8, device=q.device)
     else:
         _beside(_dev(workspace, "workspace"), "workspace", cache.pool)
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
     if rows:
         _check("quasar_paged_attention",
                _lib.quasar_paged_attention(q.data_ptr(), rows, ldq, n_q_heads, cache.n_kv_heads, starts, n_seqs, max_new, *cache._layer(layer),

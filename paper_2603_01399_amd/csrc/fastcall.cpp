@@ -380,7 +380,7 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
             ws = scratch.get();
         } else {
             const at::Tensor &t = any_tensor(a[6]);
-            if (!t.is_cuda() || t.device().index() != c.device) throw NotOrdinary{};
+            if (!t.is_cuda() || t.device().index() != c.device || !t.is_contiguous()) throw NotOrdinary{};   // (an expanded one holds less than nbytes)
             ws = t.data_ptr();
             bytes = t.nbytes();
         }

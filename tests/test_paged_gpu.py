@@ -592,3 +592,76 @@ def test_refusals_of_the_binding(qb):
             bad()
     empty = qb.prompt_attention(q[:0], 4, b.cache, 0, i32_to_dev([0, 0, 0]))
     assert empty.shape == (0, 512)
+
+
+def test_an_expanded_workspace_is_refused(qb):
+    """Its nbytes count elements that share memory."""
+    say("expanded workspace")
+    b = Batch(qb, "bf16", 32, 4, 2, [30, 3], [2, 2], seed=92)
+    need = qb._lib.quasar_paged_attention_workspace_bytes(2, 4, 2)
+    with pytest.raises(ValueError):
+        qb.paged_attention(b.q(), 4, b.cache, 0, b.row_start, 2, workspace=torch.empty(1, dtype=torch.uint8, device="cuda").expand(need))
+    close(bf16_to_host(qb.paged_attention(b.q(), 4, b.cache, 0, b.row_start, 2, workspace=torch.empty(need, dtype=torch.uint8, device="cuda"))), b)
+
+
+def test_a_cache_keeps_its_buffers(qb):
+    """Calls go to the buffers that the cache was made with: another tensor in their place is refused, writing into them is not."""
+    say("buffers")
+    b = Batch(qb, "e4m3", 32, 4, 2, [30, 3], [2, 2], seed=93)
+    c = b.cache
+    for name in ("pool", "books", "refs", "lengths", "table", "k_scale", "v_scale"):
+        with pytest.raises(AttributeError):
+            setattr(c, name, getattr(c, name).clone())
+    for name in ("n_pages", "page_len", "max_pages"):
+        with pytest.raises(AttributeError):
+            setattr(c, name, getattr(c, name) + 32)
+    c.lengths += 1
+    c.lengths -= 1
+    c.table[0, 0] = c.table[0, 0]
+    c.note = "the caller's own"
+    close(bf16_to_host(qb.paged_attention(b.q(), 4, c, 0, b.row_start, 2)), b)
+
+
+def test_offsets_beyond_32_bits(qb):
+    """The pages of a small pool's layer in the second layer of one of 10 GB, counted from its end: the same bits, page for page."""
+    say("large pool")
+    hq, hk, page, n_big = 16, 8, 256, 5000
+    b = Batch(qb, "bf16", page, hq, hk, [700, 255, 0], [8, 3, 0], seed=94)
+    small = b.cache
+    big = qb.PagedKvCache(2, hk, n_big, page_len=page, max_seqs=small.max_seqs, max_pages=small.max_pages)
+    assert big.pool[1].nbytes > 1 << 32
+    away = lambda ids: torch.where(ids >= 0, n_big - 1 - ids, ids)
+    at = torch.arange(n_big - 1, n_big - 1 - small.n_pages, -1, device="cuda")
+    big.pool[1, at] = small.pool[0]
+    big.table.copy_(away(small.table)); big.lengths.copy_(small.lengths)
+    big.refs.fill_(1)                                    # (room at the end alone)
+    big.refs[at] = small.refs
+    calls = (lambda c, l: qb.paged_attention(b.q(), hq, c, l, b.row_start, 8), lambda c, l: qb.prompt_attention(b.q(), hq, c, l, b.row_start))
+    for call in calls:
+        got = bf16_to_host(call(big, 1))
+        assert np.array_equal(got, bf16_to_host(call(small, 0)))
+        close(got, b)
+    qkv = bf16_to_dev(rnd_bits((b.rows, (hq + 2 * hk) * D), 95))
+    g = torch.ones(D, dtype=torch.bfloat16, device="cuda")
+    assert torch.equal(qb.paged_prepare(qkv, hq, big, 1, b.row_start, g, g), qb.paged_prepare(qkv, hq, small, 0, b.row_start, g, g))
+    same = lambda: torch.equal(big.pool[1, at].view(torch.int16), small.pool[0].view(torch.int16))
+    assert same()
+    # a fork that writes: its copy goes to the one page that is free, which lies at the end too
+    parent, news = i32_to_dev([0, 1, 0]), i32_to_dev([0, 0, 1])
+    free = int(torch.nonzero(small.refs == 0)[0])
+    for c, end in ((small, False), (big, True)):
+        c.fork(parent)                                   # (which frees the second sequence's page without positions, too)
+        c.refs[c.refs == 0] = 1
+        c.refs[n_big - 1 - free if end else free] = 0
+        assert c.reserve(news).tolist() == [1, 1, 1]
+    assert torch.equal(away(small.table), big.table) and int(small.table[2, 2]) == free
+    assert same()
+    # and back to the beginning: with nothing else in use every page moves, as it is
+    for c in (small, big):
+        c.refs.zero_()
+        c.refs[c.table[c.table >= 0].long()] = 1
+    was = big.pool[1, big.table[0, :3].long()].clone()
+    to = big.compact()
+    live = int((big.refs > 0).sum())
+    assert int(big.table.max()) == live - 1 and (to[at[small.refs > 0]] < live).all()
+    assert torch.equal(big.pool[1, big.table[0, :3].long()].view(torch.int16), was.view(torch.int16))
