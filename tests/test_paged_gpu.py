@@ -665,3 +665,38 @@ def test_offsets_beyond_32_bits(qb):
     live = int((big.refs > 0).sum())
     assert int(big.table.max()) == live - 1 and (to[at[small.refs > 0]] < live).all()
     assert torch.equal(big.pool[1, big.table[0, :3].long()].view(torch.int16), was.view(torch.int16))
+
+
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+@pytest.mark.parametrize("group", [1, 8, 16])
+def test_rows_beyond_max_new_are_left_as_they_were(qb, kv, group):
+    say("max_new", kv, group)
+    hq, lengths, news, most = 2 * group, [70, 5, 300], [8, 2, 5], 3
+    b = Batch(qb, kv, 32, hq, 2, lengths, news, seed=300 + group, scaled=False)
+    out = torch.full((b.rows, hq * D), 5.0, dtype=torch.bfloat16, device="cuda")
+    qb.paged_attention(b.q(), hq, b.cache, 0, b.row_start, most, out=out)
+    want, tol = b.expected()
+    got = ref.bf16_bits_to_f64(bf16_to_host(out)).reshape(b.rows, hq, D)
+    row = 0
+    for n in news:
+        kept = min(n, most)
+        assert (np.abs(got - want)[row:row + kept] <= tol[row:row + kept]).all() and (got[row + kept:row + n] == 5.0).all()
+        row += n
+
+
+# kv, Hq, sequences, tokens of one at most, max_new
+MANY = [("bf16", 2, 1024, 1, 1), ("e4m3", 3, 1024, 3, 3), ("bf16", 12, 1000, 2, 2), ("bf16", 24, 1024, 2, 2), ("e4m3", 40, 1024, 1, 2), ("bf16", 32, 700, 1, 9),
+        ("bf16", 4, 1024, 0, 1), ("e4m3", 16, 257, 4, 4)]
+
+
+@pytest.mark.parametrize("kv,hq,seqs,new,most", MANY)
+def test_as_many_sequences_as_there_may_be(qb, kv, hq, seqs, new, most):
+    """Every form over a thousand sequences, many of them empty, one of them long."""
+    say("many sequences", kv, hq, seqs, new, most)
+    r = np.random.Generator(np.random.Philox(400 + hq))
+    lengths, news = r.integers(0, 90, seqs), r.integers(0, new + 1, seqs)
+    lengths[seqs // 3], news[seqs // 3], news[-1] = 2500, max(new, 1), 1
+    lengths[::5] = 0
+    b = Batch(qb, kv, 64, hq, 1, lengths.tolist(), news.tolist(), seed=401 + hq)
+    close(bf16_to_host(qb.paged_attention(b.q(), hq, b.cache, 0, b.row_start, most)), b)
+    close(bf16_to_host(qb.prompt_attention(b.q(), hq, b.cache, 0, b.row_start)), b)
