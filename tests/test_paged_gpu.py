@@ -700,3 +700,40 @@ def test_as_many_sequences_as_there_may_be(qb, kv, hq, seqs, new, most):
     b = Batch(qb, kv, 64, hq, 1, lengths.tolist(), news.tolist(), seed=401 + hq)
     close(bf16_to_host(qb.paged_attention(b.q(), hq, b.cache, 0, b.row_start, most)), b)
     close(bf16_to_host(qb.prompt_attention(b.q(), hq, b.cache, 0, b.row_start)), b)
+
+
+@pytest.mark.parametrize("group", [1, 5, 8])
+def test_the_last_positions_there_may_be(qb, group):
+    """A sequence that ends at position 2^24 - 1, of which only the last page exists: append, and both attentions over what exists."""
+    say("last positions", group)
+    hq, page, n, total = group, 1024, 8, 1 << 24
+    cache = qb.PagedKvCache(1, 1, 2, page_len=page, max_seqs=1, max_pages=total // page)
+    cache.pool.view(torch.uint8).fill_(0xFF)
+    cache.table[0, -1] = 1
+    cache.lengths[0] = total - page
+    g = rnd_bits((D,), 501, 0.1)
+    g = ref.f32_to_bf16_bits(1.0 + ref.bf16_bits_to_f64(g).astype(np.float32))
+    chunks, pos = [page - n, n], total - page
+    for i, rows in enumerate(chunks):
+        qkv = rnd_bits((rows, hq + 2, D), 502 + i)
+        starts = i32_to_dev([0, rows])
+        q = qb.paged_prepare(bf16_to_dev(qkv.reshape(rows, -1)), hq, cache, 0, starts, bf16_to_dev(g), bf16_to_dev(g))
+        want = at.head_norm_rope(qkv[:, :hq], g, 1e-6, np.arange(pos, pos + rows), 1e6)
+        got = bf16_to_host(q).reshape(rows, hq, D)
+        f64 = ref.bf16_bits_to_f64
+        size = np.abs(f64(at.head_norm_rope(qkv[:, :hq], g, 1e-6, np.zeros(rows), 1e6)))
+        # (as in test_prepare)
+        assert (np.abs(f64(got) - f64(want)) <= 2.0 ** -6 * (size + np.roll(size, D // 2, axis=2)) + 2.0 ** -7 * np.abs(f64(want))).all()
+        assert np.mean(got != want) < 0.02
+        pos += rows
+        if i == 0:
+            cache.lengths += rows
+    b = Batch.__new__(Batch)
+    b.kv, b.page_len, b.hk, b.hq, b.layer, b.cache, b.scales, b.rows, b.news, b.lengths = "bf16", page, 1, hq, 0, cache, [None, None], n, [n], [page - n]
+    raw = cache.pool[0, 1, 0].view(torch.int16).cpu().numpy().view(np.uint16)              # [block][half][4096]
+    j = np.arange(page)
+    b.keys, b.values = ([ref.bf16_bits_to_f64(raw[(j // 32)[:, None], half, pg.block_places("bf16")[half][j % 32]])[:, None]] for half in range(2))
+    b.q_bits = bf16_to_host(q).reshape(n, hq, D)
+    close(bf16_to_host(qb.paged_attention(q, hq, cache, 0, starts, n)), b)
+    close(bf16_to_host(qb.prompt_attention(q, hq, cache, 0, starts)), b)
+    assert int(cache.lengths[0]) == total - n
