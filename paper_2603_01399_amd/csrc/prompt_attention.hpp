@@ -16,9 +16,9 @@
 // wave (the accumulators' registers are copied), three steps in LDS, steps of 32 positions, priorities by phase or by wave.  Scores a block ahead, their
 // products among the instructions of the softmax before: 5 % fewer cycles, 1056 us against 1072 on one card for 8192 rows, but 209 against 196 for
 // 512 rows of 40 / 8 heads behind 16000 positions in 8-bit pages, whose start is a trip to memory longer.
-// Many short prompts are bound by memory and the start of a tile: 60 of up to 300 rows 73 us, of which 32 for queries and outputs; 9 of up to 1531 110.
-// A workgroup a tile in the order of steps of all sequences' tiles evens out what is left at the end, but finds its tile later: 9 of up to 1531
-// 112.6, 60 of up to 300 behind 2000 311 where this order takes 333, 30 of up to 700 118 and 108.
+// Many short prompts are bound by memory and the start of a tile: 60 of up to 300 rows 73 us, of which 32 for queries and outputs; 9 of up to 1531 107.
+// (Tiles in the order of their steps, of whichever sequence, share fewer keys and values at a time: 9 of up to 1531 112.6, 30 of up to 700 118
+// where the order of sequences took 108.)
 #pragma once
 
 #include <type_traits>
@@ -75,15 +75,41 @@ __device__ __forceinline__ PromptTile tile_of_line(const PagedParams &c, const i
     return prompt_tile(c, ROWS, s, seq_span(c, s), (f - (UNIFORM ? __builtin_amdgcn_readfirstlane(prefix[s]) : prefix[s])) * ROWS);
 }
 
-__device__ __forceinline__ SeqSpan span_of_lane(const SeqSpan &a, int l) {
-    return SeqSpan{__builtin_amdgcn_readlane(a.row0, l), __builtin_amdgcn_readlane(a.n, l), __builtin_amdgcn_readlane(a.len, l)};
-}
-
-// Tile `back` from the end of the line; R = 0: there are fewer.  Each wave for itself, a sequence a lane: no LDS, and nothing is read twice.
+// Tile `back` from the end of the line; R = 0: there are fewer.  Each wave for itself, a sequence a lane: no LDS, and nothing is read twice.  Of up to
+// kSortedSeqs sequences the longest one's tiles are first, which evens out what is left at the end: 9 prompts of up to 1531 rows 107.3 us, in the order
+// of sequences 111.8; 4 of up to 2048 85.4 and 90.2; 16 of up to 300 26.3 and 29.1.  Of more, finding the order costs what it gives: 60 of up to
+// 300 79.8 and 74.8, behind up to 2000 positions 308 and 324.
+constexpr int kSortedSeqs = 32;
 template <int ROWS>
 __device__ __forceinline__ PromptTile tile_from_end(const PagedParams &c, int back) {
     constexpr int AT_ONCE = 4;
     const int lane = threadIdx.x & 63;
+    auto tile_of = [&](const SeqSpan &a, int s, int &all, PromptTile &t) {       // of the sequences s of the lanes; all: their tiles
+        const int upto = lane_sums((a.n * c.G + ROWS - 1) / ROWS);
+        all = __builtin_amdgcn_readlane(upto, 63);
+        if (back >= all) return false;
+        const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > back));
+        const SeqSpan of = {__builtin_amdgcn_readlane(a.row0, l), __builtin_amdgcn_readlane(a.n, l), __builtin_amdgcn_readlane(a.len, l)};
+        t = prompt_tile(c, ROWS, __builtin_amdgcn_readlane(s, l), of, (__builtin_amdgcn_readlane(upto, l) - 1 - back) * ROWS);
+        return true;
+    };
+    PromptTile t{};
+    int all;
+    if (c.n_seqs > 1 && c.n_seqs <= kSortedSeqs) {
+        const SeqSpan a = lane < c.n_seqs ? seq_span(c, lane) : SeqSpan{0, 0, 0};
+        const int reach = lane < c.n_seqs ? a.len + a.n : -1;
+        int rank = 0;
+        // how many come first: those that reach further, or as far from a lower lane (lanes without a sequence: behind all, where they carry nothing)
+        for (int j0 = 0; j0 < c.n_seqs; j0 += 8)
+#pragma unroll
+            for (int j = j0; j < j0 + 8; ++j) {
+                const int other = __builtin_amdgcn_readlane(reach, j);
+                rank += other + (j < lane) > reach;
+            }
+        auto to_rank = [&](int v) { return __builtin_amdgcn_ds_permute(4 * rank, v); };          // (0 in the lanes that none goes to)
+        tile_of(SeqSpan{to_rank(a.row0), to_rank(a.n), to_rank(a.len)}, to_rank(lane), all, t);
+        return t;
+    }
     for (int end = c.n_seqs; end > 0; end -= 64 * AT_ONCE) {
         SeqSpan a[AT_ONCE];
 #pragma unroll
@@ -93,15 +119,11 @@ __device__ __forceinline__ PromptTile tile_from_end(const PagedParams &c, int ba
         }
 #pragma unroll
         for (int k = 0; k < AT_ONCE; ++k) {
-            const int tiles = (a[k].n * c.G + ROWS - 1) / ROWS, upto = lane_sums(tiles), all = __builtin_amdgcn_readlane(upto, 63);
-            if (back < all) {
-                const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > back));
-                return prompt_tile(c, ROWS, end - 1 - 64 * k - l, span_of_lane(a[k], l), (__builtin_amdgcn_readlane(upto, l) - 1 - back) * ROWS);
-            }
+            if (tile_of(a[k], end - 1 - 64 * k - lane, all, t)) return t;
             back -= all;
         }
     }
-    return PromptTile{};
+    return t;
 }
 
 constexpr int kPromptStep = 64;                          // positions in LDS at a time
