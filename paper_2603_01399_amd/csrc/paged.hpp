@@ -99,9 +99,9 @@ template <int KV> __device__ __forceinline__ int v_page_index(int pib, int d) {
     return ((((d >> 5) * 4 + (o >> 2)) * 16 + (d & 15)) * 2 + ((d >> 4) & 1)) * 8 + (o & 3) + ((pib >> 4) << 2);
 }
 
-// four fp32 -> four e4m3 codes (round to nearest even, saturating), value i in byte i
+// four fp32 -> four e4m3 codes (round to nearest even, saturating; not a number stays none), value i in byte i
 __device__ __forceinline__ unsigned int floats_to_e4m3x4(float a, float b, float c, float d) {
-    auto sat = [](float x) { return __builtin_amdgcn_fmed3f(x, -kE4m3Max, kE4m3Max); };
+    auto sat = [](float x) { return __builtin_elementwise_minimum(__builtin_elementwise_maximum(x, -kE4m3Max), kE4m3Max); };
     int r = __builtin_amdgcn_cvt_pk_fp8_f32(sat(a), sat(b), 0, false);
     return (unsigned int)__builtin_amdgcn_cvt_pk_fp8_f32(sat(c), sat(d), r, true);
 }

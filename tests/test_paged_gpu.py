@@ -737,3 +737,35 @@ def test_the_last_positions_there_may_be(qb, group):
     close(bf16_to_host(qb.paged_attention(q, hq, cache, 0, starts, n)), b)
     close(bf16_to_host(qb.prompt_attention(q, hq, cache, 0, starts)), b)
     assert int(cache.lengths[0]) == total - n
+
+
+@pytest.mark.parametrize("rows", [512, 16])
+def test_every_value_over_many_scales(qb, rows):
+    """All bf16 values but NaN, over scales of every kind: the codes of the fp32 quotient.  512 rows go block by block, 16 row by row."""
+    say("every value", rows)
+    r = np.random.Generator(np.random.Philox(601))
+    near = lambda x, steps: (np.float32(x).view(np.int32) + np.asarray(steps, np.int32)).view(np.float32)
+    scales = np.concatenate([near(1.0, [0, 1, -1, 2, -2, 1 << 22]), near(2.0 ** -60, [-1, 0, 1]), near(2.0 ** 60, [-1, 0, 1]), np.float32([1e-44, 1e-38, 3e38, 1 / 448, 448, 1 / 3, 0.05]),
+                             (2.0 ** r.uniform(-59, 59, 18)).astype(np.float32), (2.0 ** r.uniform(-9, 3, 27)).astype(np.float32)])
+    hk, hq = len(scales), len(scales)
+    cache = qb.PagedKvCache(1, hk, 16, page_len=32, max_seqs=1, max_pages=16, dtype=torch.float8_e4m3fn, k_scale=torch.from_numpy(scales)[None].cuda(),
+                            v_scale=torch.from_numpy(scales)[None].cuda())
+    cache.table[0] = torch.arange(16, device="cuda")
+    g = torch.ones(D, dtype=torch.bfloat16, device="cuda")
+    values = np.arange(1 << 16, dtype=np.uint32).astype(np.uint16).reshape(512, D)
+    b = Batch.__new__(Batch)
+    b.kv, b.page_len, b.hk, b.layer, b.cache = "e4m3", 32, hk, 0, cache
+    for at_ in range(0, 512, rows):
+        qkv = np.zeros((rows, hq + 2 * hk, D), np.uint16)
+        qkv[:, hq + hk:] = values[at_:at_ + rows, None]
+        qb.paged_prepare(bf16_to_dev(qkv.reshape(rows, -1)), hq, cache, 0, i32_to_dev([0, rows]), g, g)
+        cache.lengths += rows
+    got = b.read(0, 512, 1)
+    bits = (values.astype(np.uint32) << 16).view(np.float32)
+    with np.errstate(all="ignore"):
+        want = np.stack([pg.f64_to_e4m3(np.nan_to_num((bits / s).astype(np.float32), nan=0.0, posinf=np.inf, neginf=-np.inf)) for s in scales], 1)
+    number = ~np.isnan(bits)
+    assert scales.min() > 0 and number.sum() > 65000
+    wrong = (got != want) & number[:, None]
+    assert not wrong.any(), (scales[np.nonzero(wrong)[1][:5]], bits[np.nonzero(wrong)[0][:5], np.nonzero(wrong)[2][:5]])
+    assert ((got[~number[:, None].repeat(hk, 1)] & 0x7F) == 0x7F).all()
