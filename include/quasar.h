@@ -568,7 +568,8 @@ int quasar_paged_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n_
 
 /* The same attention for whole prompts, or chunks of them behind what is cached: any number of rows a sequence
  * (T * n_q_heads / n_kv_heads <= 2^26).  A workspace of quasar_prompt_attention_workspace_bytes (may be NULL; 0: none is used for this shape)
- * lets few rows over many positions be shared by the whole GPU, joined by a second launch; sums are then taken in another order. */
+ * lets few rows over many positions be shared by the whole GPU, joined by a second launch; sums are then taken in another order.  Whether that is
+ * done follows from the rows and from what they see, not from max_pages: a wider table gives the same bits. */
 size_t quasar_prompt_attention_workspace_bytes(int64_t T, int64_t n_q_heads, int64_t n_kv_heads, int64_t n_seqs);
 int quasar_prompt_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n_q_heads, int64_t n_kv_heads, const int32_t *row_start,
                             int64_t n_seqs, const void *pages, int64_t n_pages, int64_t page_len, int kv_dtype, const float *k_scale,

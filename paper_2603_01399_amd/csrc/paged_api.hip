@@ -92,9 +92,6 @@ int check_cache(const CacheArgs &a, PagedParams &p) {
 // New rows a sequence, on average, from which the append goes block by block: 40 sequences of up to 90 rows of 32 / 8 heads in 8-bit pages
 // 22.4 us row by row and 24 to 31 by blocks, 11 of up to 1531 88 and 57.
 constexpr int kBlockRows = 64;
-// Positions that a row of the table holds, up to which prompts' tiles are not shared: 512 rows without a prefix 18.1 us, shared 33.1; 61 rows
-// behind up to 900 positions 28.7 and 21.3; behind 4000 88.1 and 30.4.
-constexpr int kFlatPositions = 1024;
 constexpr float kScaleLog2 = 1.4426950408889634f / 11.313708498984761f;      // log2(e) / sqrt(128)
 
 // ---- what the attention calls share of a launch: workgroups of a kv head, and the room for what they leave of shared sequences or tiles
@@ -162,6 +159,15 @@ FlatShape prompt_shape(int64_t T, int64_t Hq, int64_t Hkv, int64_t n_seqs) {
     const int64_t per = 2 * (int64_t)compute_units() / Hkv;
     if (a.tiles <= kMaxFlatTiles && a.tiles < per) a.room(per, kPromptWaves * 16, kPromptWaves * 64 * 8, Hkv);
     return a;
+}
+// Where sharing is possible, the kernel shares tiles if the longest has more steps than a worker's share and this many: what starts of further
+// tiles and the join cost, more with more tiles.  Both ways, us, bf16, 32 / 8 heads, over a table of 262144 positions: 61 rows 17.6 shared and 11.8
+// whole, behind 400 positions (8 steps where a share is 4) 20.0 and 21.4, behind 900 21.5 and 31.2; 256 rows 27.4 and 15.9, behind 500 (12
+// and 4) 27.1 and 26.9; 512 rows 33.0 and 21.0, behind 600 (18 and 4) 34.8 and 34.1, behind 1000 (24 and 6) 38.8 and 41.5; 1900 rows (30 and
+// 15) 73.0 and 58.0, behind 2000 (61 and 45) 117.2 and 116.5; 2048 rows of 8 / 1 heads (32 and 5) 47.1 and 52.5.
+int whole_more(int64_t T, int64_t G) {
+    const int64_t tiles = (T * G + 32 * kPromptWaves - 1) / (32 * kPromptWaves);
+    return (int)(tiles < 16 ? tiles : 16);
 }
 template <int KV>
 int launch_prompt(const PromptParams &p, int64_t tiles, int PW, hipStream_t st) {
@@ -284,6 +290,7 @@ int quasar_paged_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n_
     p.c = c;
     p.q = q; p.out = out; p.ldq = ldq; p.ldo = ldo;
     p.scale_log2 = kScaleLog2;
+    p.whole_more = -kMaxPositions;                                               // (a step's tiles are shared always)
     if (shape.flat.workers) lay_out(p, shape.flat, workspace);
     return kv == KV_BF16 ? launch_prompt<KV_BF16>(p, shape.flat.tiles, shape.PW, st) : launch_prompt<KV_E4M3>(p, shape.flat.tiles, shape.PW, st);
 }
@@ -307,7 +314,10 @@ int quasar_prompt_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n
     p.q = q; p.out = out; p.ldq = ldq; p.ldo = ldo;
     p.scale_log2 = kScaleLog2;
     const FlatShape shape = prompt_shape(T, n_q_heads, n_kv_heads, n_seqs);
-    if (workspace && shape.workers && workspace_bytes >= shape.bytes() && max_pages * page_len > kFlatPositions) lay_out(p, shape, workspace);
+    p.whole_more = whole_more(T, n_q_heads / n_kv_heads);
+    // (a table so short that tiles stay whole whatever the lengths are: launched without the join)
+    const bool may_share = max_pages * page_len > (int64_t)kPromptStep * (kFlatLeast + p.whole_more);
+    if (workspace && shape.workers && workspace_bytes >= shape.bytes() && may_share) lay_out(p, shape, workspace);
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
     return kv_type(kv_dtype) == KV_BF16 ? launch_prompt<KV_BF16>(p, shape.tiles, 1, st) : launch_prompt<KV_E4M3>(p, shape.tiles, 1, st);
 }

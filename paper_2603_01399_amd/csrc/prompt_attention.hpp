@@ -36,6 +36,7 @@ struct PromptParams {
     float *part_ml;           // [Hkv][2 workers][32 rows of a tile][64][2]
     int *pieces;              // [workers][4]: sequence of the tile that begins with a worker and goes on (-1: none), its first row, last worker, slot
     int workers;              // of a kv head
+    int whole_more;           // steps that the longest tile may have beyond a worker's share while tiles stay whole
     float scale_log2;         // log2(e) / sqrt(128)
 };
 
@@ -130,8 +131,8 @@ constexpr int kPromptStep = 64;                          // positions in LDS at 
 constexpr int kPromptStepBytes = kPromptStep / kKvBlock * 2 * kKvBlockBytes;   // 32 KB: two blocks, keys and values
 
 // FLAT: the steps of all tiles as one line, in equal pieces for `workers` workgroups of a kv head (as the blocks of a step's sequences,
-// paged_attention.hpp), for launches whose tiles would leave compute units idle; else a workgroup a tile, the last ones, which see most,
-// first.
+// paged_attention.hpp), for launches whose tiles would leave compute units idle; where the longest tile has hardly more steps than a piece, each
+// tile goes to a worker as it is, and the join finds nothing (whole_more).  Else a workgroup a tile, the last ones, which see most, first.
 // PW: waves that share rows.  1: four times 32 rows, each wave over both blocks of a step.  2: twice 32 rows, each wave over one of the
 // blocks, joined at the end: for up to 64 rows a sequence, where half of four times 32 would be nobody's.
 // 8-bit pages are widened on the way into LDS, once for all waves.  (In LDS as they are, four steps of half the size with three under way, and
@@ -155,27 +156,50 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
     const float scale_log2 = p.scale_log2 * ks;
 
     int tile = 0, at = 0, end = 0;                               // FLAT: steps at .. end - 1 of the line
+    int tiles = 0, total = 0;
+    bool shared = false;
     FlatShare mine{};
     int goes_on = -1, goes_on_at = 0, last_worker = 0, first_slot = 0;
     PromptTile pt{};
     if constexpr (FLAT) {
         // (more tiles than kMaxFlatTiles only where the rows' starts do not fit the tensor)
-        const int tiles = min(kMaxFlatTiles, prefix_sums<NW>(c.n_seqs, prefix, wave_sums, [&](int s) {
+        tiles = min(kMaxFlatTiles, prefix_sums<NW>(c.n_seqs, prefix, wave_sums, [&](int s) {
             return (int)(((long long)seq_span(c, s).n * c.G + ROWS - 1) / ROWS);
         }));
-        const int total = prefix_sums<NW>(tiles, line, wave_sums, [&](int f) { return tile_of_line<ROWS, false>(c, prefix, f).steps; });
+        int longest = 0;                                         // steps of a tile, of those that this thread counts
+        total = prefix_sums<NW>(tiles, line, wave_sums, [&](int f) {
+            const int n = tile_of_line<ROWS, false>(c, prefix, f).steps;
+            longest = max(longest, n);
+            return n;
+        });
         mine = flat_share(total, p.workers, kFlatLeast, worker);
-        at = __builtin_amdgcn_readfirstlane(mine.begin);
-        end = __builtin_amdgcn_readfirstlane(mine.end);
-        for (int up = tiles; up - tile > 1;) {
-            const int mid = (tile + up) >> 1;
-            if (line[mid] <= at) tile = mid; else up = mid;
+        const bool pays = __builtin_amdgcn_ballot_w64(longest > mine.share + p.whole_more) != 0ull;
+        if (lane == 0) wave_sums[w] = pays;
+        __syncthreads();
+        for (int i = 0; i < NW; ++i) shared |= wave_sums[i] != 0;
+        shared = __builtin_amdgcn_readfirstlane(shared);
+        if (shared) {
+            at = __builtin_amdgcn_readfirstlane(mine.begin);
+            end = __builtin_amdgcn_readfirstlane(mine.end);
+            for (int up = tiles; up - tile > 1;) {
+                const int mid = (tile + up) >> 1;
+                if (line[mid] <= at) tile = mid; else up = mid;
+            }
+            tile = __builtin_amdgcn_readfirstlane(tile);
+        } else {
+            tile = worker;
+            end = __builtin_amdgcn_readfirstlane(total);
+            at = tile < tiles ? __builtin_amdgcn_readfirstlane(line[tile]) : end;
         }
-        tile = __builtin_amdgcn_readfirstlane(tile);
     } else {
         pt = tile_from_end<ROWS>(c, worker);
     }
-    for (bool more = FLAT ? at < end : pt.R > 0; more; more = FLAT && at < end, ++tile) {
+    auto next_tile = [&] {
+        tile += shared ? 1 : p.workers;
+        if (!shared) at = tile < tiles ? __builtin_amdgcn_readfirstlane(line[tile]) : end;
+        return at < end;
+    };
+    for (bool more = FLAT ? at < end : pt.R > 0; more; more = FLAT && next_tile()) {
     if constexpr (FLAT) pt = tile_of_line<ROWS, true>(c, prefix, tile);
     const SeqSpan a = pt.a;
     const int R = pt.R, tile0 = pt.tile0, first_pos = pt.first_pos, last_pos = pt.last_pos, s = pt.s;

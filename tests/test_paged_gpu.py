@@ -769,3 +769,19 @@ def test_every_value_over_many_scales(qb, rows):
     wrong = (got != want) & number[:, None]
     assert not wrong.any(), (scales[np.nonzero(wrong)[1][:5]], bits[np.nonzero(wrong)[0][:5], np.nonzero(wrong)[2][:5]])
     assert ((got[~number[:, None].repeat(hk, 1)] & 0x7F) == 0x7F).all()
+
+
+# kv, Hq, Hkv, cached, new: tiles that stay whole and tiles that are shared, on both sides of the rule
+WIDE = [("bf16", 32, 8, [0], [61]), ("bf16", 32, 8, [0], [512]), ("e4m3", 32, 8, [0], [512]), ("bf16", 32, 8, [300], [512]), ("bf16", 32, 8, [900], [61]),
+        ("e4m3", 32, 8, [400, 0, 77, 0], [61, 0, 130, 5]), ("bf16", 8, 1, [0], [700]), ("bf16", 8, 2, [0, 30], [1100, 65]), ("e4m3", 5, 1, [2000], [40])]
+
+
+@pytest.mark.parametrize("kv,hq,hk,lengths,news", WIDE)
+def test_prompts_do_not_depend_on_the_width_of_the_table(qb, kv, hq, hk, lengths, news):
+    """A table of 32768 positions, as a cache with room to grow has, gives the bits of one that just holds the sequences."""
+    say("wide table", kv, hq, hk, lengths, news)
+    a, b = (Batch(qb, kv, 64, hq, hk, lengths, news, seed=700 + hq, more_columns=0), Batch(qb, kv, 64, hq, hk, lengths, news, seed=700 + hq, more_columns=512))
+    assert np.array_equal(a.q_bits, b.q_bits) and b.cache.max_pages >= 512
+    got = [bf16_to_host(qb.prompt_attention(x.q(), hq, x.cache, 0, x.row_start)) for x in (a, b)]
+    assert np.array_equal(*got)
+    close(got[1], b)
