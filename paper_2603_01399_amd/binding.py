@@ -658,7 +658,8 @@ class PagedKvCache:
     Everything is device memory, and the methods wait for nothing: `refs` [n_pages], `lengths` [max_seqs] and `table`
     [max_seqs, max_pages] (int32) are the caller's to read and, for lengths, to advance after a step
     (cache.lengths += accepted).  dtype: torch.bfloat16, or torch.float8_e4m3fn with k_scale, v_scale [n_layers, n_kv_heads] fp32 (or
-    None for 1).  pool, books: the buffers, where the caller has them (books: refs | lengths | table in one int32 tensor).
+    None for 1).  pool, books: the buffers, where the caller has them (books: refs | lengths | table in one int32 tensor).  The buffers are
+    the cache's as long as it lives: calls refuse one that is given other memory.
     """
 
     def __init__(self, n_layers: int, n_kv_heads: int, n_pages: int, *, page_len: int = 64, max_seqs: int = 1, max_pages: int = None,
@@ -697,16 +698,28 @@ class PagedKvCache:
         self._refs, self._lengths, self._table = self.refs.data_ptr(), self.lengths.data_ptr(), self.table.data_ptr()
         self._layer_bytes = pool.nbytes // n_layers
         self._workspace_bytes = _lib.quasar_pages_workspace_bytes(max_seqs, n_pages)
-        # the ordinary calls take this handle to the native side
+        # the ordinary calls take this handle to the native side; it holds the buffers, too
         self._handle = _fast.paged_cache(n_layers, n_kv_heads, n_pages, page_len, max_seqs, max_pages, code, self._layer_bytes, self._workspace_bytes,
-                                         pool.device.index, pool.data_ptr(), self._refs, self._lengths, self._table,
-                                         0 if k_scale is None else k_scale.data_ptr(), 0 if v_scale is None else v_scale.data_ptr())
+                                         pool, books, self.refs, self.lengths, self.table, k_scale, v_scale)
+        self._own = frozenset(self.__dict__) | {"_own"}
+
+    def _refuse_own(self, name):
+        if name in self.__dict__.get("_own", ()):
+            raise AttributeError(f"{name} is the cache's own: write into the tensor (cache.{name}[...] = ...), or make another cache")
 
     def __setattr__(self, name, value):
-        # (the handle has the buffers' addresses: another tensor in their place would not be used, and the old one freed)
-        if "_handle" in self.__dict__ and self.__dict__.get(name, value) is not value:
-            raise AttributeError(f"{name} is the cache's own: write into the tensor (cache.{name}[...] = ...), or make another cache")
+        # (the calls go to the buffers that the cache was made with: another tensor in their place would not be used)
+        if self.__dict__.get(name) is not value:
+            self._refuse_own(name)
         object.__setattr__(self, name, value)
+
+    def __delattr__(self, name):
+        self._refuse_own(name)
+        object.__delattr__(self, name)
+
+    def _check_buffers(self):
+        if not _fast.paged_cache_as_made(self._handle):
+            raise ValueError("a buffer of the cache has other memory than the cache was made with")
 
     def _layer(self, layer: int):
         if not 0 <= layer < self.n_layers:
@@ -729,6 +742,7 @@ class PagedKvCache:
         done = _fast.pages_reserve(self._handle, n_new)
         if type(done) is not int or done > 0:
             return _checked("quasar_pages_reserve", done)
+        self._check_buffers()
         new = self._per_sequence(n_new, "n_new")
         status = torch.empty(self.max_seqs, dtype=torch.int32, device=self.pool.device)
         ws = torch.empty(self._workspace_bytes, dtype=torch.uint8, device=self.pool.device)
@@ -743,6 +757,7 @@ class PagedKvCache:
         status = _fast.pages_fork(self._handle, parent, keep)
         if status >= 0:
             return _check("quasar_pages_fork", status)
+        self._check_buffers()
         _check("quasar_pages_fork",
                _lib.quasar_pages_fork(self._table, self.max_pages, self.max_seqs, self.max_pages, self._lengths, self._per_sequence(parent, "parent"),
                                       None if keep is None else self._per_sequence(keep, "keep"), self._refs, self.n_pages, self.page_len,
@@ -753,6 +768,7 @@ class PagedKvCache:
         done = _fast.pages_compact(self._handle)
         if type(done) is not int or done > 0:
             return _checked("quasar_pages_compact", done)
+        self._check_buffers()
         _beside(self.books, "the cache", self.pool)
         to = torch.empty(self.n_pages, dtype=torch.int32, device=self.pool.device)
         ws = torch.empty(self._workspace_bytes, dtype=torch.uint8, device=self.pool.device)
@@ -808,6 +824,7 @@ def paged_prepare(qkv: torch.Tensor, n_q_heads: int, cache: PagedKvCache, layer:
     done = _fast.paged_prepare(cache._handle, qkv, n_q_heads, layer, row_start, q_gamma, k_gamma, eps, rope_theta, q_out)
     if type(done) is not int or done > 0:
         return _checked("quasar_paged_prepare", done)
+    cache._check_buffers()
     rows, ld = _rows_of(qkv, (n_q_heads + 2 * cache.n_kv_heads) * 128, "qkv", cache)
     starts, n_seqs = _row_start_of(row_start, cache)
     for name, gamma in (("q_gamma", q_gamma), ("k_gamma", k_gamma)):
@@ -827,6 +844,7 @@ def paged_attention(q: torch.Tensor, n_q_heads: int, cache: PagedKvCache, layer:
     done = _fast.paged_attention(cache._handle, q, n_q_heads, layer, row_start, max_new, workspace, out)
     if type(done) is not int or done > 0:
         return _checked("quasar_paged_attention", done)
+    cache._check_buffers()
     rows, ldq = _rows_of(q, n_q_heads * 128, "q", cache)
     starts, n_seqs = _row_start_of(row_start, cache)
     out, ldo = _output_like(out, rows, n_q_heads * 128, cache, "out")
@@ -849,6 +867,7 @@ def prompt_attention(q: torch.Tensor, n_q_heads: int, cache: PagedKvCache, layer
     done = _fast.prompt_attention(cache._handle, q, n_q_heads, layer, row_start, out)
     if type(done) is not int or done > 0:
         return _checked("quasar_prompt_attention", done)
+    cache._check_buffers()
     rows, ldq = _rows_of(q, n_q_heads * 128, "q", cache)
     starts, n_seqs = _row_start_of(row_start, cache)
     out, ldo = _output_like(out, rows, n_q_heads * 128, cache, "out")

@@ -238,26 +238,65 @@ PyObject *w8_gateup_swiglu(PyObject *, PyObject *const *a, Py_ssize_t n) {
 
 // ---- the paged cache: calls on a handle, which answer with the tensor that they return in Python, else with the status or -1
 
-// What PagedKvCache holds; its tensors live as long as that object, which holds this.
+// One of a cache's buffers, held, and where it lay when the cache was made: `tensor.data = ...` or a resize gives the same tensor other memory.
+struct Buffer {
+    at::Tensor t;
+    void *at = nullptr;
+    size_t bytes = 0;
+    explicit Buffer(PyObject *o) {
+        if (o == Py_None) return;
+        if (!THPVariable_Check(o)) throw NotOrdinary{};
+        t = THPVariable_Unpack(o);
+        at = t.data_ptr();
+        bytes = t.nbytes();
+    }
+    bool as_made() const { return !t.defined() || (t.is_contiguous() && t.nbytes() == bytes && t.data_ptr() == at); }
+};
+// What PagedKvCache is made of.
 struct PagedCache {
-    long long n_layers, n_kv_heads, n_pages, page_len, max_seqs, max_pages, code, layer_bytes, workspace_bytes, device;
-    unsigned long long pool, refs, lengths, table, k_scale, v_scale;
+    long long n_layers, n_kv_heads, n_pages, page_len, max_seqs, max_pages, code, layer_bytes, workspace_bytes;
+    Buffer pool, books, refs, lengths, table, k_scale, v_scale;
+    int device;
+    bool as_made() const {
+        for (const Buffer *b : {&pool, &books, &refs, &lengths, &table, &k_scale, &v_scale})
+            if (!b->as_made()) return false;
+        return true;
+    }
 };
 constexpr const char *kCacheName = "quasar.PagedCache";
 
-// (the members of PagedCache in order)
+// (the sizes in order; pool, books, refs, lengths, table, k_scale or None, v_scale or None)
 PyObject *paged_cache(PyObject *, PyObject *args) {
-    PagedCache c;
-    if (!PyArg_ParseTuple(args, "LLLLLLLLLLKKKKKK", &c.n_layers, &c.n_kv_heads, &c.n_pages, &c.page_len, &c.max_seqs, &c.max_pages, &c.code, &c.layer_bytes,
-                          &c.workspace_bytes, &c.device, &c.pool, &c.refs, &c.lengths, &c.table, &c.k_scale, &c.v_scale))
+    long long n[9];
+    PyObject *b[7];
+    if (!PyArg_ParseTuple(args, "LLLLLLLLLOOOOOOO", &n[0], &n[1], &n[2], &n[3], &n[4], &n[5], &n[6], &n[7], &n[8], &b[0], &b[1], &b[2], &b[3], &b[4], &b[5], &b[6]))
         return nullptr;
-    auto *held = new (std::nothrow) PagedCache(c);
+    PagedCache *held = nullptr;
+    try {
+        const Buffer pool(b[0]);
+        const int device = pool.t.defined() ? pool.t.device().index() : -1;
+        held = new (std::nothrow) PagedCache{n[0], n[1], n[2], n[3], n[4], n[5], n[6], n[7], n[8], pool, Buffer(b[1]), Buffer(b[2]), Buffer(b[3]), Buffer(b[4]),
+                                             Buffer(b[5]), Buffer(b[6]), device};
+    } catch (...) {
+        PyErr_SetString(PyExc_TypeError, "a cache's buffers are tensors");
+        return nullptr;
+    }
     if (!held) return PyErr_NoMemory();
     PyObject *o = PyCapsule_New(held, kCacheName, [](PyObject *o) { delete static_cast<PagedCache *>(PyCapsule_GetPointer(o, kCacheName)); });
     if (!o) delete held;
     return o;
 }
-template <class T> T *address(unsigned long long a) { return reinterpret_cast<T *>(static_cast<uintptr_t>(a)); }
+// (handle) -> whether the cache's buffers lie where they lay when it was made
+PyObject *paged_cache_as_made(PyObject *, PyObject *o) {
+    const auto *c = static_cast<const PagedCache *>(PyCapsule_GetPointer(o, kCacheName));
+    if (!c) return nullptr;
+    try {
+        return PyBool_FromLong(c->as_made());
+    } catch (...) {                                              // (a storage without memory)
+        Py_RETURN_FALSE;
+    }
+}
+template <class T> T *address(const Buffer &b, long long bytes = 0) { return reinterpret_cast<T *>(static_cast<unsigned char *>(b.at) + bytes); }
 
 // A handle and, on its device, which is the current one, what a call is given.
 struct PagedCall {
@@ -268,7 +307,7 @@ struct PagedCall {
         PyObject *dev = PyObject_CallNoArgs(g_device);
         const long now = dev ? PyLong_AsLong(dev) : -1;
         Py_XDECREF(dev);
-        if (now != c->device) throw NotOrdinary{};
+        if (now != c->device || !c->as_made()) throw NotOrdinary{};
     }
     const at::Tensor &tensor(PyObject *o, at::ScalarType type) const {
         const at::Tensor &t = cuda_tensor(o, type);
@@ -290,7 +329,7 @@ struct PagedCall {
         if (v < 0 || v >= c->n_layers) throw NotOrdinary{};
         return v;
     }
-    const float *scale(unsigned long long at, int64_t layer) const { return at ? address<const float>(at) + layer * c->n_kv_heads : nullptr; }
+    const float *scale(const Buffer &b, int64_t layer) const { return b.at ? address<const float>(b) + layer * c->n_kv_heads : nullptr; }
     at::Tensor fresh(at::IntArrayRef shape, at::ScalarType type) const {
         return at::empty(shape, at::TensorOptions().dtype(type).device(at::kCUDA, static_cast<c10::DeviceIndex>(c->device)));
     }
@@ -356,7 +395,7 @@ PyObject *paged_prepare(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const float eps = real(a[7]), theta = real(a[8]);
         out = output(p, a[9], x.size(0), hq * 128);
         return call(p_paged_prepare, bits(x), x.size(0), ld_of(x), hq, c.n_kv_heads, starts.p, starts.n_seqs, gamma[0], gamma[1], eps, theta, bits(out), ld_of(out),
-                    address<void>(c.pool + layer * c.layer_bytes), c.n_pages, c.page_len, (int)c.code, p.scale(c.k_scale, layer), p.scale(c.v_scale, layer),
+                    address<void>(c.pool, layer * c.layer_bytes), c.n_pages, c.page_len, (int)c.code, p.scale(c.k_scale, layer), p.scale(c.v_scale, layer),
                     address<const int32_t>(c.table), c.max_pages, c.max_pages, address<const int32_t>(c.lengths), current_stream());
     });
 }
@@ -384,7 +423,7 @@ PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
             ws = t.data_ptr();
             bytes = t.nbytes();
         }
-        return call(p_paged_attention, bits(q), q.size(0), ld_of(q), hq, c.n_kv_heads, starts.p, starts.n_seqs, max_new, address<const void>(c.pool + layer * c.layer_bytes),
+        return call(p_paged_attention, bits(q), q.size(0), ld_of(q), hq, c.n_kv_heads, starts.p, starts.n_seqs, max_new, address<const void>(c.pool, layer * c.layer_bytes),
                     c.n_pages, c.page_len, (int)c.code, p.scale(c.k_scale, layer), p.scale(c.v_scale, layer), address<const int32_t>(c.table), c.max_pages, c.max_pages,
                     address<const int32_t>(c.lengths), bits(out), ld_of(out), ws, bytes, stream);
     });
@@ -400,7 +439,7 @@ PyObject *prompt_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const RowStart starts(p, a[4]);
         out = output(p, a[5], q.size(0), hq * 128);
         return call_with_scratch(p_prompt_attention, p_prompt_attention_workspace_bytes(q.size(0), hq, c.n_kv_heads, starts.n_seqs), current_stream(), bits(q), q.size(0),
-                                 ld_of(q), hq, c.n_kv_heads, starts.p, starts.n_seqs, address<const void>(c.pool + layer * c.layer_bytes), c.n_pages, c.page_len, (int)c.code,
+                                 ld_of(q), hq, c.n_kv_heads, starts.p, starts.n_seqs, address<const void>(c.pool, layer * c.layer_bytes), c.n_pages, c.page_len, (int)c.code,
                                  p.scale(c.k_scale, layer), p.scale(c.v_scale, layer), address<const int32_t>(c.table), c.max_pages, c.max_pages,
                                  address<const int32_t>(c.lengths), bits(out), ld_of(out));
     });
@@ -493,7 +532,7 @@ PyObject *bound(PyObject *, PyObject *) {
 PyMethodDef methods[] = {FAST(w8_linear), FAST(bf16_linear), FAST(w8a8_linear), FAST(w4_linear),
                          FAST(w8_linear_fused), FAST(w8_gateup_swiglu),
                          FAST(paged_prepare), FAST(paged_attention), FAST(prompt_attention), FAST(pages_reserve), FAST(pages_fork), FAST(pages_compact),
-                         {"paged_cache", paged_cache, METH_VARARGS, nullptr},
+                         {"paged_cache", paged_cache, METH_VARARGS, nullptr}, {"paged_cache_as_made", paged_cache_as_made, METH_O, nullptr},
                          {"bind", bind, METH_VARARGS, nullptr}, {"bound", bound, METH_NOARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

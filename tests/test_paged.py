@@ -234,3 +234,44 @@ def test_binding_refuses_host_tensors_and_odd_shapes():
             qb.PagedKvCache(1, 8, 4, **bad)
     with pytest.raises(TypeError):
         qb.PagedKvCache(1, 8, 4, pool=torch.empty((1, 4, 8, 2, 2, 4096), dtype=torch.bfloat16))
+
+
+def test_a_cache_holds_its_buffers_and_knows_them():
+    """The handle keeps the tensors that calls go to, and says when one of them has other memory; the cache's own names stay (host tensors:
+    nothing is launched)."""
+    from paper_2603_01399_amd import binding as qb
+    pool, books, scale = torch.zeros(4, 8), torch.zeros(12, dtype=torch.int32), torch.ones(2)
+    views = [books[:4], books[4:6], books[6:].view(2, 3)]
+    handle = qb._fast.paged_cache(1, 1, 4, 32, 2, 3, 1, 128, 64, pool, books, *views, scale, None)
+    intact = lambda: qb._fast.paged_cache_as_made(handle)
+    assert intact()
+    pool[1], books[5] = 3.0, 7                            # (writing into them is what they are for)
+    assert intact()
+    for t in (pool, books, *views, scale):
+        was = t.data
+        t.data = t.data.clone()
+        assert not intact()
+        t.data = was
+        assert intact()
+        t.data = was[:1]
+        assert not intact()
+        t.data = was
+    at_ = pool.data_ptr()
+    del pool, t, was
+    fresh = [torch.zeros(4, 8) for _ in range(64)]        # (memory that had been freed would come again)
+    assert intact() and all(f.data_ptr() != at_ for f in fresh)
+    for bad in ((1, 1, 4, 32, 2, 3, 1, 128, 64, 17, books, *views, None, None), (1,) * 9):
+        with pytest.raises(TypeError):
+            qb._fast.paged_cache(*bad)
+    c = qb.PagedKvCache.__new__(qb.PagedKvCache)
+    c.pool, c._handle = books, handle
+    object.__setattr__(c, "_own", frozenset(("pool", "_handle", "_own")))
+    for name in ("pool", "_handle", "_own"):
+        with pytest.raises(AttributeError):
+            delattr(c, name)
+        with pytest.raises(AttributeError):
+            setattr(c, name, 0)
+    c.pool += 0
+    c.note = 1
+    c.note = 2
+    del c.note

@@ -785,3 +785,25 @@ def test_prompts_do_not_depend_on_the_width_of_the_table(qb, kv, hq, hk, lengths
     got = [bf16_to_host(qb.prompt_attention(x.q(), hq, x.cache, 0, x.row_start)) for x in (a, b)]
     assert np.array_equal(*got)
     close(got[1], b)
+
+
+def test_other_memory_in_a_buffer_is_refused(qb):
+    """A cache's tensor that is given other memory (by `.data`, a resize) is refused by every call before anything is launched."""
+    say("other memory")
+    b = Batch(qb, "e4m3", 32, 4, 2, [30, 3], [2, 2], seed=96, layers=2)
+    c, q, n = b.cache, b.q(), i32_to_dev([1, 1])
+    g, qkv = torch.ones(D, dtype=torch.bfloat16, device="cuda"), torch.zeros((4, 8 * D), dtype=torch.bfloat16, device="cuda")
+    calls = (lambda: qb.paged_attention(q, 4, c, 0, b.row_start, 2), lambda: qb.prompt_attention(q, 4, c, 0, b.row_start),
+             lambda: qb.paged_prepare(qkv, 4, c, 0, b.row_start, g, g), lambda: c.reserve(n), lambda: c.fork(n), lambda: c.compact())
+    for name in ("pool", "books", "refs", "lengths", "table", "k_scale", "v_scale"):
+        t = getattr(c, name)
+        was = t.data
+        for other in (was.clone(), was[:1].clone(), was[:1]):
+            t.data = other
+            for call in calls:
+                with pytest.raises(ValueError, match="other memory"):
+                    call()
+        t.data = was
+        with pytest.raises(AttributeError):
+            delattr(c, name)
+    close(bf16_to_host(qb.paged_attention(q, 4, c, 0, b.row_start, 2)), b)
