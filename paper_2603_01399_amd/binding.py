@@ -657,7 +657,8 @@ class PagedKvCache:
 
     Everything is device memory, and the methods wait for nothing: `refs` [n_pages], `lengths` [max_seqs] and `table`
     [max_seqs, max_pages] (int32) are the caller's to read and, for lengths, to advance after a step
-    (cache.lengths += accepted).  dtype: torch.bfloat16, or torch.float8_e4m3fn with k_scale, v_scale [n_layers, n_kv_heads] fp32 (or
+    (cache.lengths += accepted).  max_pages: pages of a sequence at most (None: as many as the pool or 2^24 positions have; the table has
+    max_seqs * max_pages entries).  dtype: torch.bfloat16, or torch.float8_e4m3fn with k_scale, v_scale [n_layers, n_kv_heads] fp32 (or
     None for 1).  pool, books: the buffers, where the caller has them (books: refs | lengths | table in one int32 tensor).  The buffers are
     the cache's as long as it lives: calls refuse one that is given other memory.
     """
@@ -668,10 +669,12 @@ class PagedKvCache:
         code = {torch.bfloat16: BF16, torch.float8_e4m3fn: E4M3}.get(dtype)
         if code is None:
             raise TypeError("dtype must be torch.bfloat16 or torch.float8_e4m3fn")
-        max_pages = n_pages if max_pages is None else max_pages
-        if not _lib.quasar_paged_cache_bytes(n_layers, n_kv_heads, n_pages, page_len, code) or not _lib.quasar_pages_workspace_bytes(max_seqs, n_pages) \
-                or max_pages < 1 or max_pages * page_len > 1 << 24:
+        if not _lib.quasar_paged_cache_bytes(n_layers, n_kv_heads, n_pages, page_len, code) or not _lib.quasar_pages_workspace_bytes(max_seqs, n_pages):
             raise ValueError("invalid cache shape")
+        if max_pages is None:
+            max_pages = min(n_pages, (1 << 24) // page_len)
+        if max_pages < 1 or max_pages * page_len > 1 << 24:
+            raise ValueError("max_pages: a sequence has 1 .. 2^24 positions")
         shape, n_books = (n_layers, n_pages, n_kv_heads, page_len // 32, 2, 32 * 128), n_pages + max_seqs + max_seqs * max_pages
         if pool is None:
             pool = torch.empty(shape, dtype=dtype, device=device)

@@ -807,3 +807,18 @@ def test_other_memory_in_a_buffer_is_refused(qb):
         with pytest.raises(AttributeError):
             delattr(c, name)
     close(bf16_to_host(qb.paged_attention(q, 4, c, 0, b.row_start, 2)), b)
+
+
+@pytest.mark.parametrize("page", [32, 1024])
+def test_a_pool_larger_than_a_sequence_may_be(qb, page):
+    """Without max_pages a row of the table holds what a sequence may have, 2^24 positions, also where the pool holds more."""
+    say("large pool by default", page)
+    c = qb.PagedKvCache(1, 1, (1 << 24) // page + 3, page_len=page, max_seqs=2, dtype=torch.float8_e4m3fn)
+    assert c.max_pages * page == 1 << 24 and tuple(c.table.shape) == (2, c.max_pages)
+    assert c.reserve(i32_to_dev([1 << 24, 3 * page])).tolist() == [1, 1]
+    assert int(c.table[0, -1]) == c.max_pages - 1 and c.table[1, :4].tolist() == [c.max_pages, c.max_pages + 1, c.max_pages + 2, -1]
+    assert c.reserve(i32_to_dev([0, 3 * page + 1])).tolist() == [1, 0]
+    assert qb.PagedKvCache(1, 1, 5, page_len=page).max_pages == 5
+    for bad in (0, (1 << 24) // page + 1):
+        with pytest.raises(ValueError):
+            qb.PagedKvCache(1, 1, 5, page_len=page, max_pages=bad)
