@@ -275,3 +275,30 @@ def test_a_cache_holds_its_buffers_and_knows_them():
     c.note = 1
     c.note = 2
     del c.note
+
+
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+@pytest.mark.parametrize("length,n", [(30000, 4), (100003, 1), (3000, 40), (0, 2100)])
+def test_a_block_more_or_less_shows(kv, length, n):
+    """The values of paged_marks with a mistake in the oracle: a block left out, or taken twice, wherever it lies, is beyond the tolerance that
+    the kernels are held to, for every row that sees it whole."""
+    from paged_marks import attention_and_bound, block_values
+    r = np.random.Generator(np.random.Philox(900 + n))
+    total = length + n
+    q, k = r.standard_normal((n, 1, 128)) * 0.4, r.standard_normal((total, 1, 128))
+    v = block_values(total)
+    want, tol = attention_and_bound(q, k, v[:, None], length, kv)
+    s = q[:, 0] @ k[:, 0].T / np.sqrt(128)
+    s[np.arange(total)[None, :] > length + np.arange(n)[:, None]] = -np.inf
+    w = np.exp(s - s.max(axis=1, keepdims=True))
+    for b in np.unique(np.r_[0, 1, 2, 3, total // 64, r.integers(0, total // 32, 40), total // 32 - 1]):
+        rows = length + np.arange(n) >= 32 * b + 31
+        assert rows.any()
+        for times in (0.0, 2.0):
+            wrong = w.copy()
+            wrong[:, 32 * b:32 * b + 32] *= times
+            with np.errstate(invalid="ignore"):
+                got = wrong @ v / wrong.sum(axis=1, keepdims=True)               # (a row that sees that block alone: not a number)
+            off = ~(np.abs(got - want[:, 0]) <= tol[:, 0]).all(axis=1)
+            alone = (32 * b == 0) & (length + np.arange(n) < 32)                 # (twice the only block: the same weights)
+            assert (off | ~rows | alone).all(), (b, times)

@@ -8,6 +8,7 @@ import torch
 from oracle import quasar_attention_ref as at
 from oracle import quasar_paged_ref as pg
 from oracle import quasar_ref as ref
+from paged_marks import attention_and_bound, block_values
 from paged_util import Batch, rnd_bits
 from gpu_util import bf16_to_dev, bf16_to_host, i32_to_dev
 
@@ -822,3 +823,57 @@ def test_a_pool_larger_than_a_sequence_may_be(qb, page):
     for bad in (0, (1 << 24) // page + 1):
         with pytest.raises(ValueError):
             qb.PagedKvCache(1, 1, 5, page_len=page, max_pages=bad)
+
+
+def near(got_bits, b, kv):
+    """Every row of every sequence within attention_and_bound."""
+    got, q, at_ = ref.bf16_bits_to_f64(got_bits).reshape(b.rows, b.hq, D), ref.bf16_bits_to_f64(b.q_bits), 0
+    worst = 0.0
+    for s, n in enumerate(b.news):
+        if n:
+            want, tol = attention_and_bound(q[at_:at_ + n], b.keys[s], b.values[s], b.lengths[s], kv)
+            worst = max(worst, float((np.abs(got[at_:at_ + n] - want) / tol).max()))
+            at_ += n
+    say("   worst of tolerance", worst)
+    assert np.isfinite(got).all() and worst <= 1.0
+
+
+def mark_blocks(b):
+    """The batch with block_values in its pages (times the head's scale, in 8-bit pages), and smaller queries: no position outweighs the others."""
+    places, c = pg.block_places(b.kv)[1], b.cache
+    raw = c.pool[b.layer].view(torch.int16 if b.kv == "bf16" else torch.uint8).cpu().numpy()
+    for s, (length, n) in enumerate(zip(b.lengths, b.news)):
+        v = block_values(length + n)
+        bits = ref.f32_to_bf16_bits(v.astype(np.float32)).view(np.int16) if b.kv == "bf16" else pg.f64_to_e4m3(v)
+        j = np.arange(length + n)
+        for h in range(b.hk):
+            raw[b.table[s, j // b.page_len][:, None], h, (j % b.page_len // 32)[:, None], 1, places[j % 32]] = bits
+        b.values[s] = b.decoded(np.repeat((bits.view(np.uint16) if b.kv == "bf16" else bits)[:, None], b.hk, 1), 1)
+    c.pool[b.layer].view(torch.int16 if b.kv == "bf16" else torch.uint8).copy_(torch.from_numpy(raw))
+    b.q_bits = rnd_bits((b.rows, b.hq, D), 778, 0.4)
+
+
+# call, page, Hq, Hkv, cached, new: every form, over contexts that many workers share
+BLOCKS = [("paged", 64, 8, 1, [30000, 5, 12000], [1, 1, 1]), ("paged", 32, 4, 2, [20000, 12000], [8, 3]), ("paged", 128, 8, 1, [30000, 7000], [4, 4]),
+          ("paged", 64, 8, 1, [33000, 100, 9000], [8, 8, 5]), ("paged", 1024, 16, 1, [20000, 3000], [16, 9]), ("paged", 64, 1, 1, [100003], [1]),
+          ("paged", 64, 2, 2, [2500] * 30, [1] * 30), ("prompt", 64, 8, 1, [0], [4000]), ("prompt", 64, 8, 1, [20000, 0], [300, 500]), ("prompt", 128, 4, 2, [16000], [512]),
+          ("prompt", 32, 8, 1, [50000], [20]), ("prompt", 64, 16, 8, [0, 3000, 64], [2100, 900, 700]), ("prompt", 64, 32, 8, [0], [512])]
+
+
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+@pytest.mark.parametrize("call,page,hq,hk,lengths,news", BLOCKS)
+def test_every_block_of_a_long_context_counts(qb, kv, call, page, hq, hk, lengths, news):
+    say("blocks", kv, call, page, hq, hk, lengths[:5], news[:5])
+    b = Batch(qb, kv, page, hq, hk, lengths, news, seed=800 + hq)
+    mark_blocks(b)
+    got = qb.paged_attention(b.q(), hq, b.cache, 0, b.row_start, max(news)) if call == "paged" else qb.prompt_attention(b.q(), hq, b.cache, 0, b.row_start)
+    near(bf16_to_host(got), b, kv)
+
+
+@pytest.mark.parametrize("page,hq,hk,lengths,news", [s[1:] for s in STEP if s[0] == "e4m3"] + [(64, 8, 2, [0, 100], [129, 311]), (32, 3, 1, [37], [500]), (64, 16, 1, [1500, 30], [32, 7])])
+def test_weights_over_8_bit_pages_have_11_bits(qb, page, hq, hk, lengths, news):
+    say("fp16 weights", page, hq, hk, lengths[:5], news[:5])
+    b = Batch(qb, "e4m3", page, hq, hk, lengths, news, seed=850 + hq)
+    if max(news) <= 32:
+        near(bf16_to_host(qb.paged_attention(b.q(), hq, b.cache, 0, b.row_start, max(news))), b, "e4m3")
+    near(bf16_to_host(qb.prompt_attention(b.q(), hq, b.cache, 0, b.row_start)), b, "e4m3")
