@@ -877,3 +877,47 @@ def test_weights_over_8_bit_pages_have_11_bits(qb, page, hq, hk, lengths, news):
     if max(news) <= 32:
         near(bf16_to_host(qb.paged_attention(b.q(), hq, b.cache, 0, b.row_start, max(news))), b, "e4m3")
     near(bf16_to_host(qb.prompt_attention(b.q(), hq, b.cache, 0, b.row_start)), b, "e4m3")
+
+
+# kv, page, Hq, Hkv, cached, new, heads that a workgroup of the block form takes on 256 compute units
+HEADS = [("bf16", 64, 32, 8, [0, 100], [1400, 133], 2), ("e4m3", 128, 32, 8, [31], [1520], 2), ("bf16", 32, 32, 8, [0, 7, 0], [2000, 0, 1500], 5), ("e4m3", 64, 32, 8, [5], [3500], 5),
+         ("bf16", 64, 32, 8, [40, 0], [2400, 2400], 7), ("e4m3", 64, 32, 8, [0, 1000], [4000, 810], 7), ("bf16", 64, 40, 8, [3], [5000], 8), ("e4m3", 32, 40, 8, [0, 64], [5000, 999], 8),
+         ("e4m3", 64, 6, 3, [0, 1], [9000, 9500], 6)]
+
+
+@pytest.mark.parametrize("kv,page,hq,hk,lengths,news,parts", HEADS)
+def test_prepare_with_several_heads_a_workgroup(qb, kv, page, hq, hk, lengths, news, parts):
+    """Heads one after another in a workgroup, from queries to keys and from keys to values, groups that the heads do not fill among them."""
+    heads = hq + 2 * hk
+    units = torch.cuda.get_device_properties(0).multi_processor_count
+    assert sum(news) >= 64 * len(news) and (units != 256 or min(8, sum(news) // 32 * heads // 1024) == parts)
+    test_prepare(qb, kv, page, hq, hk, lengths, news)
+
+
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+@pytest.mark.parametrize("rows", [80, 700])
+def test_prepare_by_blocks_writes_nothing_without_a_page(qb, kv, rows):
+    """As test_prepare_writes_nothing_without_a_page, block by block: no id, an id beyond the pool, a length beyond the table, a length that is none.
+    Queries are written where there is a position, and nothing of a sequence whose length is none."""
+    say("prepare by blocks without pages", kv, rows)
+    b = Batch(qb, kv, 32, 8, 4, [30, 10, 5, 40], [rows] * 4, seed=97, scaled=False)
+    b.cache.table[0, 1] = -1
+    b.cache.table[1, 0] = b.cache.n_pages
+    b.cache.table[1, 2] = 2 ** 31 - 1
+    b.cache.lengths[2] = 2 ** 24                         # beyond the table
+    b.cache.lengths[3] = -1
+    raw = b.cache.pool.view(torch.uint8)
+    before = raw.clone()
+    qkv = bf16_to_dev(rnd_bits((b.rows, 16 * D), 98))
+    g = torch.ones(D, dtype=torch.bfloat16, device="cuda")
+    q = torch.full((b.rows, 8 * D), 9.0, dtype=torch.bfloat16, device="cuda")
+    qb.paged_prepare(qkv, 8, b.cache, 0, b.row_start, g, g, q_out=q)
+    torch.cuda.synchronize()
+    assert torch.isfinite(q).all() and (q[3 * rows:] == 9).all() and (q[:3 * rows] != 9).any(dim=1).all()
+    changed = sorted((before != raw).flatten(2).any(2)[0].nonzero().flatten().tolist())
+    last = lambda s: -(-(b.lengths[s] + rows) // 32)
+    assert changed == sorted([int(b.table[0, c]) for c in range(last(0)) if c != 1] + [int(b.table[1, c]) for c in range(last(1)) if c not in (0, 2)])
+    # what is written is what a cache with all of its pages gets
+    whole = Batch(qb, kv, 32, 8, 4, [30, 10, 5, 40], [rows] * 4, seed=97, scaled=False)
+    q2 = qb.paged_prepare(qkv, 8, whole.cache, 0, whole.row_start, g, g)
+    assert torch.equal(q2[:2 * rows], q[:2 * rows]) and torch.equal(whole.cache.pool.view(torch.uint8)[0, changed], raw[0, changed])
