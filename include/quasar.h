@@ -550,7 +550,8 @@ size_t quasar_paged_cache_bytes(int64_t n_layers, int64_t n_kv_heads, int64_t n_
 /* quasar_attn_prepare for the packed rows of a batch: qkv [T, (n_q_heads + 2 n_kv_heads) * 128] bf16 (16-byte aligned, ld a multiple
  * of 8), q_out [T, n_q_heads * 128] (likewise).  `pages`: the layer's part of the pool.  Queries and keys are normalised and rotated
  * with the roundings of quasar_attn_prepare; e4m3 pages take e4m3( clamp( that bf16 value / scale, -448, 448 ) ), an fp32 division,
- * to nearest even.  The pages must be there (quasar_pages_reserve) and held by no other sequence. */
+ * to nearest even.  The pages must be there (quasar_pages_reserve) and held by no other sequence.  q_out may be the queries' part of qkv itself
+ * (q_out == qkv, ldq == ld); else the two do not overlap. */
 int quasar_paged_prepare(const uint16_t *qkv, int64_t T, int64_t ld, int64_t n_q_heads, int64_t n_kv_heads, const int32_t *row_start,
                          int64_t n_seqs, const uint16_t *q_gamma, const uint16_t *k_gamma, float eps, float rope_theta, uint16_t *q_out,
                          int64_t ldq, void *pages, int64_t n_pages, int64_t page_len, int kv_dtype, const float *k_scale, const float *v_scale,
@@ -559,14 +560,18 @@ int quasar_paged_prepare(const uint16_t *qkv, int64_t T, int64_t ld, int64_t n_q
 /* quasar_verify_attention for a batch: row i of sequence s sees positions 0 .. lengths[s] + i; rows that see nothing give 0.  For the new
  * tokens of a step: at most max_new <= 32 a sequence (a sequence with more has rows beyond that left as they were), and
  * max_new * n_q_heads / n_kv_heads <= 1024.  Work is shared by cached positions, not by sequences: ragged lengths cost no more than even ones.
- * workspace: quasar_paged_attention_workspace_bytes.  q 16-byte, out 8-byte aligned; ldq a multiple of 8, ldo of 4.  At most two launches. */
+ * workspace: quasar_paged_attention_workspace_bytes.  q 16-byte, out 8-byte aligned; ldq a multiple of 8, ldo of 4.  At most two launches.
+ * Probabilities enter the second product with 16 bits, and are divided by the sum of what enters: over bf16 pages as bf16 (8 significant bits, as in
+ * quasar_verify_attention), over e4m3 pages as fp16 (11, and no less than 2^-31 of the largest).  Scores, sums and outputs are fp32, with one rounding of
+ * the output to bf16.  A key, value or query that is not finite reaches the rows that see it and their kv head's outputs alone, of which every
+ * element is unspecified then; no other row or head is touched.  out may be q itself (out == q, ldo == ldq); else the two do not overlap. */
 size_t quasar_paged_attention_workspace_bytes(int64_t max_new, int64_t n_q_heads, int64_t n_kv_heads);   /* 0 on invalid arguments */
 int quasar_paged_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n_q_heads, int64_t n_kv_heads, const int32_t *row_start,
                            int64_t n_seqs, int64_t max_new, const void *pages, int64_t n_pages, int64_t page_len, int kv_dtype,
                            const float *k_scale, const float *v_scale, const int32_t *table, int64_t table_ld, int64_t max_pages,
                            const int32_t *lengths, uint16_t *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *hip_stream);
 
-/* The same attention for whole prompts, or chunks of them behind what is cached: any number of rows a sequence
+/* The same attention, with the same roundings, for whole prompts, or chunks of them behind what is cached: any number of rows a sequence
  * (T * n_q_heads / n_kv_heads <= 2^26).  A workspace of quasar_prompt_attention_workspace_bytes (may be NULL; 0: none is used for this shape)
  * lets few rows over many positions be shared by the whole GPU, joined by a second launch; sums are then taken in another order.  Whether that is
  * done follows from the rows and from what they see, not from max_pages: a wider table gives the same bits. */

@@ -921,3 +921,27 @@ def test_prepare_by_blocks_writes_nothing_without_a_page(qb, kv, rows):
     whole = Batch(qb, kv, 32, 8, 4, [30, 10, 5, 40], [rows] * 4, seed=97, scaled=False)
     q2 = qb.paged_prepare(qkv, 8, whole.cache, 0, whole.row_start, g, g)
     assert torch.equal(q2[:2 * rows], q[:2 * rows]) and torch.equal(whole.cache.pool.view(torch.uint8)[0, changed], raw[0, changed])
+
+
+# call, Hq, Hkv, cached, new: the forms of both attentions, and of the append
+IN_PLACE = [("paged", 8, 2, [3000, 0, 77], [1, 1, 1]), ("paged", 8, 2, [3000, 20], [8, 5]), ("paged", 16, 2, [3000, 20, 9000], [8, 5, 8]), ("paged", 16, 1, [2000, 20], [32, 7]),
+            ("prompt", 8, 2, [0, 30], [61, 200]), ("prompt", 8, 2, [4000], [100]), ("prompt", 32, 8, [0, 64], [2100, 77])]
+
+
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+@pytest.mark.parametrize("call,hq,hk,lengths,news", IN_PLACE)
+def test_queries_and_outputs_in_place(qb, kv, call, hq, hk, lengths, news):
+    """The queries' part of the projection, rotated and then replaced by the attention's output where it lies, gives what tensors of their own give."""
+    say("in place", kv, call, hq, hk, lengths, news)
+    b = Batch(qb, kv, 64, hq, hk, lengths, news, seed=860 + hq)
+    g = bf16_to_dev(ref.f32_to_bf16_bits((1.0 + 0.2 * np.random.Generator(np.random.Philox(7)).standard_normal(D)).astype(np.float32)))
+    qkv = bf16_to_dev(rnd_bits((b.rows, (hq + 2 * hk) * D), 861))
+    attend = lambda q, out: (qb.paged_attention(q, hq, b.cache, 0, b.row_start, max(news), out=out) if call == "paged" else qb.prompt_attention(q, hq, b.cache, 0, b.row_start, out=out))
+    q = qb.paged_prepare(qkv, hq, b.cache, 0, b.row_start, g, g)
+    pool = b.cache.pool.view(torch.uint8).clone()
+    want = attend(q, None)
+    rest, part = qkv[:, hq * D:].clone(), qkv[:, :hq * D]
+    qb.paged_prepare(qkv, hq, b.cache, 0, b.row_start, g, g, q_out=part)
+    assert torch.equal(part, q) and torch.equal(b.cache.pool.view(torch.uint8), pool)
+    attend(part, part)
+    assert torch.equal(part, want) and torch.equal(qkv[:, hq * D:], rest)
