@@ -235,7 +235,7 @@ __device__ __forceinline__ u32x4 norm_and_rotate(const u32x4 raw, const u32x4 gr
 // x / scale to nearest, where that makes a difference to the code; inv: 1 / scale, to nearest.  Two steps of q + (x - q scale) inv: after the first q is
 // one of the two neighbours of the quotient, x - q scale is then exact, and with a correctly rounded inverse the second gives the nearest
 // (Markstein's theorem).  Not for scales or quotients whose remainder could leave the normal range: below 2^-11 the code is a zero of x's sign,
-// beyond 2^20 the largest, by the first product already.  Fewer instructions than a division: 11 prompts of up to 1531 rows 57.7 us, and 61.3.
+// beyond 2^20 the largest, by the first product already.  Fewer instructions than a division: 11 prompts of up to 1531 rows 57.7 us, and 61.3 on the same card.
 __device__ __forceinline__ float quotient_of_code(float x, float scale, float inv) {
     const float q0 = x * inv, q1 = __builtin_fmaf(__builtin_fmaf(-q0, scale, x), inv, q0);
     const float q2 = __builtin_fmaf(__builtin_fmaf(-q1, scale, x), inv, q1);
@@ -269,7 +269,7 @@ __device__ __forceinline__ void rotation(int pos, double per_position, float &sn
 }
 
 // For few rows a sequence: a wave takes four heads of a row at a time, 16 lanes of 16 bytes each.  Bound by the launch and one trip to memory: one row of
-// one sequence 5.0 us a call, 3.8 in the kernel.
+// one sequence 5 us a call, 3.6 in the kernel.
 template <int KV>
 __global__ __launch_bounds__(256) void paged_prepare_kernel(const PrepareParams p) {
     const PagedParams &c = p.c;
@@ -338,7 +338,7 @@ __global__ __launch_bounds__(256) void paged_prepare_kernel(const PrepareParams 
 
 // For many rows a sequence: a workgroup takes the new rows of one block of 32 positions and p.parts heads.  The rotations of
 // the block are computed once, in LDS; a value head goes through LDS too, since its 16-byte units hold eight positions of one d: written
-// one by one they cost 2 bytes of every 16 a store.  11 prompts of up to 1531 rows into 8-bit pages (229 MB moved): 58 us, 4.0 TB/s where a
+// one by one they cost 2 bytes of every 16 a store.  11 prompts of up to 1531 rows into 8-bit pages (229 MB moved): 57 to 60 us, 4 TB/s where a
 // plain copy reaches 5.15; what is left is the norms and rotations, two trips through memory a workgroup.
 template <int KV>
 __global__ __launch_bounds__(256) void paged_prepare_block_kernel(const PrepareParams p) {

@@ -11,7 +11,7 @@
 //
 // Bound by memory where the cache is long: 64 sequences of one token over up to 8192 positions (1.21 GB, 32 / 8 heads) take 191 us with the
 // merge, 6.3 TB/s where a plain read reaches 6.7; in 8-bit pages 99.5, 6.1 TB/s; one sequence over up to 100003 positions 68, 6.0 TB/s.  Bound by
-// the way to memory and back where it is short: 4 over up to 1000 12.7 us, 9.3 and 4.0 in the kernels, of which 3 go by until the page table
+// the way to memory and back where it is short: 4 over up to 1000 12.6 to 13.1 us, 8.0 and 3.4 in the kernels, of which 3 go by until the page table
 // is known, and 2 for each trip.  One workgroup a compute unit: two take 200 us for the first, since more pieces are shared.
 #pragma once
 

@@ -9,7 +9,7 @@
 // rows of K are permuted, row 16 t + 8 c + 4 h + b of the product being position 16 c + 8 t + 4 h + b, which makes the scores that a lane
 // holds after the first product the operand of the second as they lie, against values in the cache's own order.
 //
-// Bound by the matrix cores and the power they draw: 8192 rows of 64 / 8 heads take 1.04 to 1.10 ms (1.0 to 1.06 PFLOP/s; a large library
+// Bound by the matrix cores and the power they draw: 8192 rows of 64 / 8 heads take 1.01 to 1.10 ms (1.0 to 1.09 PFLOP/s, in 8-bit pages 1.16 ms; a large library
 // product reaches 1.36 on the same card).  Matrix cores are busy 52 % of the cycles there and the vector units 37 % with the softmax (32
 // exponentials, 32 multiply-adds, 25 maxima, 16 conversions and 16 sums a wave and step of 32 products), at about 2.0 GHz; the products
 // alone, without the softmax, took 0.82 to 0.88 ms.  LDS is busy 27 %, without bank conflicts.  Tried and slower or the same: 64 rows a
