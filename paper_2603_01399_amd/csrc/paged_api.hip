@@ -290,7 +290,7 @@ int quasar_paged_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n_
     p.c = c;
     p.q = q; p.out = out; p.ldq = ldq; p.ldo = ldo;
     p.scale_log2 = kScaleLog2;
-    p.whole_more = -kMaxPositions;                                               // (a step's tiles are shared always)
+    p.whole_more = -(1 << 30);                                                   // (a step's tiles are shared always: minus more than any share)
     if (shape.flat.workers) lay_out(p, shape.flat, workspace);
     return kv == KV_BF16 ? launch_prompt<KV_BF16>(p, shape.flat.tiles, shape.PW, st) : launch_prompt<KV_E4M3>(p, shape.flat.tiles, shape.PW, st);
 }
