@@ -48,6 +48,9 @@ typedef enum quasar_status {
 /* QUASAR_E4M3 (8-bit floating point, largest finite value 448): pages of a paged cache only. */
 typedef enum quasar_dtype { QUASAR_F32 = 0, QUASAR_BF16 = 1, QUASAR_E4M3 = 2 } quasar_dtype;
 
+/* Which elements of a head are a pair in the rotary embedding: i and i + dims / 2, or 2 i and 2 i + 1 (quasar_paged_prepare_rope). */
+typedef enum quasar_rope_layout { QUASAR_ROPE_HALF = 0, QUASAR_ROPE_INTERLEAVED = 1 } quasar_rope_layout;
+
 /* Contraction variant used by quasar_w8_linear (for A/B measurements). */
 typedef enum quasar_path {
     QUASAR_PATH_AUTO = 0,  /* library's choice by M */
@@ -557,6 +560,16 @@ int quasar_paged_prepare(const uint16_t *qkv, int64_t T, int64_t ld, int64_t n_q
                          int64_t ldq, void *pages, int64_t n_pages, int64_t page_len, int kv_dtype, const float *k_scale, const float *v_scale,
                          const int32_t *table, int64_t table_ld, int64_t max_pages, const int32_t *lengths, void *hip_stream);
 
+/* The same for other rotary positions.  The first rope_dims (16, 32 .. 128) elements of every query and key head are rotated, in pairs as rope_layout
+ * says: pair i by the angle position * inv_freq[i], (a, b) -> magnitude (a cos - b sin, b cos + a sin), the others stay as they are.  inv_freq: device
+ * fp64 [rope_dims / 2], radians a position (angles are reduced in fp64).  q_gamma, k_gamma: both, or both NULL for heads that are not
+ * normalised.  One rounding to bf16 behind the rotation.  Everything else, limits and errors as above. */
+int quasar_paged_prepare_rope(const uint16_t *qkv, int64_t T, int64_t ld, int64_t n_q_heads, int64_t n_kv_heads, const int32_t *row_start,
+                              int64_t n_seqs, const uint16_t *q_gamma, const uint16_t *k_gamma, float eps, int rope_layout, int64_t rope_dims,
+                              const double *inv_freq, float magnitude, uint16_t *q_out, int64_t ldq, void *pages, int64_t n_pages, int64_t page_len,
+                              int kv_dtype, const float *k_scale, const float *v_scale, const int32_t *table, int64_t table_ld, int64_t max_pages,
+                              const int32_t *lengths, void *hip_stream);
+
 /* quasar_verify_attention for a batch: row i of sequence s sees positions 0 .. lengths[s] + i; rows that see nothing give 0.  For the new
  * tokens of a step: at most max_new <= 32 a sequence (a sequence with more has rows beyond that left as they were), and
  * max_new * n_q_heads / n_kv_heads <= 1024.  Work is shared by cached positions, not by sequences: ragged lengths cost no more than even ones.
@@ -581,6 +594,21 @@ int quasar_prompt_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n
                             const float *v_scale, const int32_t *table, int64_t table_ld, int64_t max_pages, const int32_t *lengths,
                             uint16_t *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *hip_stream);
 
+/* Both for layers whose rows see a window: row i of sequence s, at position P = lengths[s] + i, sees positions j <= P with j > P - window or j < sinks
+ * (window >= 1 counts the row's own position; sinks >= 0: the first positions of a sequence stay visible; positions are the ones that the keys were rotated
+ * by).  Nothing outside is read as a value or a key of any weight, and pages there need not exist (quasar_pages_trim).  Time and reads follow the window, not the
+ * length.  Workspaces, roundings, limits and errors as above; a window or sinks beyond 2^25 count as 2^25. */
+int quasar_paged_attention_window(const uint16_t *q, int64_t T, int64_t ldq, int64_t n_q_heads, int64_t n_kv_heads, const int32_t *row_start,
+                                  int64_t n_seqs, int64_t max_new, const void *pages, int64_t n_pages, int64_t page_len, int kv_dtype,
+                                  const float *k_scale, const float *v_scale, const int32_t *table, int64_t table_ld, int64_t max_pages,
+                                  const int32_t *lengths, int64_t window, int64_t sinks, uint16_t *out, int64_t ldo, void *workspace,
+                                  size_t workspace_bytes, void *hip_stream);
+int quasar_prompt_attention_window(const uint16_t *q, int64_t T, int64_t ldq, int64_t n_q_heads, int64_t n_kv_heads, const int32_t *row_start,
+                                   int64_t n_seqs, const void *pages, int64_t n_pages, int64_t page_len, int kv_dtype, const float *k_scale,
+                                   const float *v_scale, const int32_t *table, int64_t table_ld, int64_t max_pages, const int32_t *lengths,
+                                   int64_t window, int64_t sinks, uint16_t *out, int64_t ldo, void *workspace, size_t workspace_bytes,
+                                   void *hip_stream);
+
 /*
  * The books.  Each result is determined by the arguments alone: of the free pages (refs 0) the lowest are taken first, in the order of
  * sequences and, within one, of positions.  workspace: quasar_pages_workspace_bytes (scratch).
@@ -594,6 +622,10 @@ int quasar_prompt_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n
  * quasar_pages_fork     a gather over the rows of the table: sequence s becomes sequence parent[s] as it was before the call, cut to keep[s] positions
  *   (keep may be NULL: not cut; fewer than 0 count as 0), with the pages that hold positions and no others.  parent[s] = s keeps (or cuts) it,
  *   another one forks or moves it, -1 (or anything that is no row) frees it.  refs follow.  No page is copied.  Two launches.
+ * quasar_pages_trim     gives pages back that no row at position lengths[s] or behind sees in a layer of this window and sinks: columns c of the table with
+ *   c * page_len >= sinks and (c + 1) * page_len <= lengths[s] - window + 1 become -1, refs follow.  For caches all of whose layers have a window, the longest
+ *   of which is given, and behind the step: a sequence that is cut back afterwards (quasar_pages_fork) may be left with rows that miss pages.
+ *   One launch.
  * quasar_pages_compact  with n pages in use (refs > 0), the i-th in use at n and beyond moves, in all layers, to the i-th free page below n; table
  *   and refs follow; out_to [n_pages] says where each page went (pages that did not move: themselves).  Two launches.
  */
@@ -603,6 +635,8 @@ int quasar_pages_reserve(int32_t *table, int64_t table_ld, int64_t n_seqs, int64
                          int64_t n_kv_heads, int kv_dtype, void *workspace, size_t workspace_bytes, void *hip_stream);
 int quasar_pages_fork(int32_t *table, int64_t table_ld, int64_t n_seqs, int64_t max_pages, int32_t *lengths, const int32_t *parent,
                       const int32_t *keep, int32_t *refs, int64_t n_pages, int64_t page_len, void *hip_stream);
+int quasar_pages_trim(int32_t *table, int64_t table_ld, int64_t n_seqs, int64_t max_pages, const int32_t *lengths, int64_t window, int64_t sinks,
+                      int32_t *refs, int64_t n_pages, int64_t page_len, void *hip_stream);
 int quasar_pages_compact(int32_t *table, int64_t table_ld, int64_t n_seqs, int64_t max_pages, int32_t *refs, int64_t n_pages,
                          int64_t page_len, int32_t *out_to, void *pool, int64_t n_layers, int64_t n_kv_heads, int kv_dtype,
                          void *workspace, size_t workspace_bytes, void *hip_stream);

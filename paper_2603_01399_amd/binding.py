@@ -8,6 +8,7 @@ this module without the built library raises.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
 
 import torch  # imported first so that the library binds to the HIP runtime torch loaded
@@ -41,6 +42,7 @@ EXPORTS = (
     "quasar_verify_attention",
     "quasar_paged_cache_bytes", "quasar_paged_prepare", "quasar_paged_attention_workspace_bytes", "quasar_paged_attention",
     "quasar_prompt_attention_workspace_bytes", "quasar_prompt_attention", "quasar_pages_workspace_bytes", "quasar_pages_reserve", "quasar_pages_fork", "quasar_pages_compact",
+    "quasar_paged_prepare_rope", "quasar_paged_attention_window", "quasar_prompt_attention_window", "quasar_pages_trim",
 )
 
 
@@ -151,6 +153,11 @@ def _load() -> ctypes.CDLL:
     lib.quasar_pages_reserve.argtypes = [vp, i64, i64, i64, vp, vp, vp, i64, i64, vp, vp, i64, i64, ci, vp, sz, vp]
     lib.quasar_pages_fork.argtypes = [vp, i64, i64, i64, vp, vp, vp, vp, i64, i64, vp]
     lib.quasar_pages_compact.argtypes = [vp, i64, i64, i64, vp, i64, i64, vp, vp, i64, i64, ci, vp, sz, vp]
+    f32 = ctypes.c_float
+    lib.quasar_paged_prepare_rope.argtypes = [vp, i64, i64, i64, i64, vp, i64, vp, vp, f32, ci, i64, vp, f32, vp, i64, *paged, vp]
+    lib.quasar_paged_attention_window.argtypes = [vp, i64, i64, i64, i64, vp, i64, i64, *paged, i64, i64, vp, i64, vp, sz, vp]
+    lib.quasar_prompt_attention_window.argtypes = [vp, i64, i64, i64, i64, vp, i64, *paged, i64, i64, vp, i64, vp, sz, vp]
+    lib.quasar_pages_trim.argtypes = [vp, i64, i64, i64, vp, i64, i64, vp, i64, i64, vp]
     lib.quasar_drafter_create.argtypes = [ci, ci, i64]
     lib.quasar_drafter_create.restype = vp
     lib.quasar_drafter_destroy.argtypes = [vp]
@@ -198,7 +205,8 @@ _NATIVE_ENTRIES = ("quasar_w8_linear", "quasar_bf16_linear", "quasar_w8a8_linear
                    "quasar_w8a8_workspace_bytes", "quasar_w4_workspace_bytes", "quasar_w8_linear_fused_split",
                    "quasar_w8_gateup_swiglu_split", "quasar_w8_fused_workspace_bytes", "quasar_w8_gateup_workspace_bytes",
                    "quasar_paged_prepare", "quasar_paged_attention", "quasar_paged_attention_workspace_bytes", "quasar_prompt_attention",
-                   "quasar_prompt_attention_workspace_bytes", "quasar_pages_reserve", "quasar_pages_fork", "quasar_pages_compact")
+                   "quasar_prompt_attention_workspace_bytes", "quasar_pages_reserve", "quasar_pages_fork", "quasar_pages_compact",
+                   "quasar_paged_prepare_rope", "quasar_paged_attention_window", "quasar_prompt_attention_window", "quasar_pages_trim")
 
 
 def _native_addresses(lib):
@@ -766,6 +774,17 @@ class PagedKvCache:
                                       None if keep is None else self._per_sequence(keep, "keep"), self._refs, self.n_pages, self.page_len,
                                       _stream()))
 
+    def trim(self, window: int, sinks: int = 0) -> None:
+        """Gives the pages back that no row to come sees anything of, in layers of this window (the longest one's) and sinks."""
+        status = _fast.pages_trim(self._handle, window, sinks)
+        if status >= 0:
+            return _check("quasar_pages_trim", status)
+        self._check_buffers()
+        _beside(self.books, "the cache", self.pool)
+        _check("quasar_pages_trim",
+               _lib.quasar_pages_trim(self._table, self.max_pages, self.max_seqs, self.max_pages, self._lengths, *_window_arg(window, sinks), self._refs,
+                                      self.n_pages, self.page_len, _stream()))
+
     def compact(self) -> torch.Tensor:
         """Moves the pages in use together at the beginning of the pool.  -> int32 [n_pages]: where each page went."""
         done = _fast.pages_compact(self._handle)
@@ -821,9 +840,62 @@ def _output_like(out, rows, width, cache, name):
     return out, ld
 
 
+ROPE_LAYOUTS = {"half": 0, "interleaved": 1}
+
+
+class Rope:
+    """Rotary positions of a model's heads, for paged_prepare(rope=...): made once, kept by the program.
+
+    The first `dims` (16, 32 .. 128) elements of a head are rotated, pair i at position p by p * inv_freq[i]; layout "half": pair i is elements i and
+    i + dims / 2, "interleaved": 2 i and 2 i + 1.  Cosines and sines are multiplied by `magnitude`.
+    inv_freq (fp64 [dims / 2], any device) is taken as it is, or follows from theta: theta^(-2 i / dims), and for contexts beyond the trained ones
+      scaling="linear"     divided by factor (positions closer together);
+      scaling="ntk"        of theta * factor^(dims / (dims - 2)): the fastest pair as it was, the slowest divided by factor;
+      scaling="by_parts"   pairs that turn `fast` times or more in trained_len positions as they are, those that turn `slow` times or less divided by
+                           factor, a blend between (linear in the turns); magnitude 1 + 0.1 ln(factor) unless it is given.
+    """
+
+    def __init__(self, dims: int = 128, theta: float = 1.0e6, *, layout: str = "half", scaling: str = None, factor: float = 1.0, trained_len: int = None,
+                 slow: float = 1.0, fast: float = 32.0, magnitude: float = None, inv_freq: torch.Tensor = None, device="cuda"):
+        if layout not in ROPE_LAYOUTS:
+            raise ValueError(f"layout must be one of {tuple(ROPE_LAYOUTS)}")
+        if dims % 16 or not 16 <= dims <= 128:
+            raise ValueError("dims must be a multiple of 16, 16 .. 128")
+        if scaling not in (None, "linear", "ntk", "by_parts"):
+            raise ValueError('scaling must be None, "linear", "ntk" or "by_parts"')
+        if inv_freq is not None:
+            if scaling is not None or inv_freq.shape != (dims // 2,) or inv_freq.dtype != torch.float64:
+                raise ValueError("inv_freq must be an fp64 [dims / 2] vector, without a scaling")
+            f = inv_freq
+        else:
+            if not theta > 1.0 or not factor > 0.0:
+                raise ValueError("theta must be above 1, factor above 0")
+            if scaling == "ntk":
+                theta = theta * factor ** (dims / (dims - 2.0))
+            f = theta ** (-2.0 * torch.arange(dims // 2, dtype=torch.float64) / dims)
+            if scaling == "linear":
+                f = f / factor
+            elif scaling == "by_parts":
+                if trained_len is None or trained_len < 1 or not 0.0 <= slow < fast:
+                    raise ValueError("by_parts needs trained_len and slow < fast")
+                keep = ((trained_len * f / (2.0 * math.pi) - slow) / (fast - slow)).clamp(0.0, 1.0)
+                f = keep * f + (1.0 - keep) * f / factor
+                if magnitude is None:
+                    magnitude = 1.0 + 0.1 * math.log(factor)
+        magnitude = 1.0 if magnitude is None else float(magnitude)
+        if not 0.0 < magnitude < math.inf:
+            raise ValueError("magnitude must be above 0 and finite")
+        self.dims, self.layout, self.magnitude = dims, layout, magnitude
+        self.inv_freq = f.to(device).contiguous()
+        self._code = ROPE_LAYOUTS[layout]
+
+
 def paged_prepare(qkv: torch.Tensor, n_q_heads: int, cache: PagedKvCache, layer: int, row_start: torch.Tensor, q_gamma: torch.Tensor,
-                  k_gamma: torch.Tensor, eps: float = 1e-6, rope_theta: float = 1.0e6, q_out: torch.Tensor = None) -> torch.Tensor:
-    """attn_prepare for the packed rows of a batch: row_start [sequences + 1], positions from cache.lengths on."""
+                  k_gamma: torch.Tensor, eps: float = 1e-6, rope_theta: float = 1.0e6, q_out: torch.Tensor = None, *, rope: Rope = None) -> torch.Tensor:
+    """attn_prepare for the packed rows of a batch: row_start [sequences + 1], positions from cache.lengths on.
+    rope: other rotary positions than all of the head by rope_theta (which then counts for nothing); with it, q_gamma and k_gamma may be None."""
+    if rope is not None:
+        return _paged_prepare_rope(qkv, n_q_heads, cache, layer, row_start, q_gamma, k_gamma, eps, rope, q_out)
     done = _fast.paged_prepare(cache._handle, qkv, n_q_heads, layer, row_start, q_gamma, k_gamma, eps, rope_theta, q_out)
     if type(done) is not int or done > 0:
         return _checked("quasar_paged_prepare", done)
@@ -841,13 +913,55 @@ def paged_prepare(qkv: torch.Tensor, n_q_heads: int, cache: PagedKvCache, layer:
     return q_out
 
 
-def paged_attention(q: torch.Tensor, n_q_heads: int, cache: PagedKvCache, layer: int, row_start: torch.Tensor, max_new: int,
-                    workspace: torch.Tensor = None, out: torch.Tensor = None) -> torch.Tensor:
-    """Attention of the new tokens of a step, at most max_new (1 .. 32) a sequence, over their sequences' pages."""
-    done = _fast.paged_attention(cache._handle, q, n_q_heads, layer, row_start, max_new, workspace, out)
+def _paged_prepare_rope(qkv, n_q_heads, cache, layer, row_start, q_gamma, k_gamma, eps, rope, q_out):
+    done = _fast.paged_prepare_rope(cache._handle, qkv, n_q_heads, layer, row_start, q_gamma, k_gamma, eps, rope._code, rope.dims, rope.inv_freq, rope.magnitude,
+                                    q_out)
     if type(done) is not int or done > 0:
-        return _checked("quasar_paged_attention", done)
+        return _checked("quasar_paged_prepare_rope", done)
     cache._check_buffers()
+    rows, ld = _rows_of(qkv, (n_q_heads + 2 * cache.n_kv_heads) * 128, "qkv", cache)
+    starts, n_seqs = _row_start_of(row_start, cache)
+    if (q_gamma is None) != (k_gamma is None):
+        raise ValueError("q_gamma and k_gamma are both given or both None")
+    for name, gamma in (("q_gamma", q_gamma), ("k_gamma", k_gamma)):
+        if gamma is not None:
+            _gamma_arg(gamma, 128)
+            _beside(gamma, name, cache.pool)
+    f = _dev(rope.inv_freq, "rope.inv_freq", torch.float64)
+    if f.shape != (rope.dims // 2,) or not f.is_contiguous():
+        raise ValueError("rope.inv_freq must be a contiguous [dims / 2] vector")
+    _beside(f, "rope.inv_freq", cache.pool)
+    q_out, ldq = _output_like(q_out, rows, n_q_heads * 128, cache, "q_out")
+    if rows:
+        _check("quasar_paged_prepare_rope",
+               _lib.quasar_paged_prepare_rope(qkv.data_ptr(), rows, ld, n_q_heads, cache.n_kv_heads, starts, n_seqs, _ptr(q_gamma), _ptr(k_gamma), eps, rope._code,
+                                              rope.dims, f.data_ptr(), rope.magnitude, q_out.data_ptr(), ldq, *cache._layer(layer), _stream()))
+    return q_out
+
+
+def _window_arg(window, sinks):
+    for name, v, least in (("window", window, 1), ("sinks", sinks, 0)):
+        if isinstance(v, bool) or not isinstance(v, int):
+            raise TypeError(f"{name} must be an integer")
+        if v < least:
+            raise ValueError(f"{name} must be at least {least}")
+    return min(window, 1 << 25), min(sinks, 1 << 25)
+
+
+def paged_attention(q: torch.Tensor, n_q_heads: int, cache: PagedKvCache, layer: int, row_start: torch.Tensor, max_new: int,
+                    workspace: torch.Tensor = None, out: torch.Tensor = None, *, window: int = None, sinks: int = 0) -> torch.Tensor:
+    """Attention of the new tokens of a step, at most max_new (1 .. 32) a sequence, over their sequences' pages.
+    window: a row sees its own and the window - 1 positions ahead of it, and the first `sinks` of the sequence (None: all ahead of it)."""
+    if window is None:
+        if sinks:
+            raise ValueError("sinks belong to a window")
+        done = _fast.paged_attention(cache._handle, q, n_q_heads, layer, row_start, max_new, workspace, out)
+    else:
+        done = _fast.paged_attention_window(cache._handle, q, n_q_heads, layer, row_start, max_new, window, sinks, workspace, out)
+    if type(done) is not int or done > 0:
+        return _checked("quasar_paged_attention" + ("" if window is None else "_window"), done)
+    cache._check_buffers()
+    seen = None if window is None else _window_arg(window, sinks)
     rows, ldq = _rows_of(q, n_q_heads * 128, "q", cache)
     starts, n_seqs = _row_start_of(row_start, cache)
     out, ldo = _output_like(out, rows, n_q_heads * 128, cache, "out")
@@ -858,27 +972,39 @@ def paged_attention(q: torch.Tensor, n_q_heads: int, cache: PagedKvCache, layer:
         if not workspace.is_contiguous():
             raise ValueError("workspace must be contiguous")
     if rows:
-        _check("quasar_paged_attention",
-               _lib.quasar_paged_attention(q.data_ptr(), rows, ldq, n_q_heads, cache.n_kv_heads, starts, n_seqs, max_new, *cache._layer(layer),
-                                           out.data_ptr(), ldo, workspace.data_ptr(), workspace.nbytes, _stream()))
+        given = (q.data_ptr(), rows, ldq, n_q_heads, cache.n_kv_heads, starts, n_seqs, max_new, *cache._layer(layer))
+        to = (out.data_ptr(), ldo, workspace.data_ptr(), workspace.nbytes, _stream())
+        if seen is None:
+            _check("quasar_paged_attention", _lib.quasar_paged_attention(*given, *to))
+        else:
+            _check("quasar_paged_attention_window", _lib.quasar_paged_attention_window(*given, *seen, *to))
     return out
 
 
 def prompt_attention(q: torch.Tensor, n_q_heads: int, cache: PagedKvCache, layer: int, row_start: torch.Tensor,
-                     out: torch.Tensor = None) -> torch.Tensor:
-    """Causal attention of whole prompts, or of chunks behind what is cached: any number of rows a sequence."""
-    done = _fast.prompt_attention(cache._handle, q, n_q_heads, layer, row_start, out)
+                     out: torch.Tensor = None, *, window: int = None, sinks: int = 0) -> torch.Tensor:
+    """Causal attention of whole prompts, or of chunks behind what is cached: any number of rows a sequence.  window, sinks: as in paged_attention."""
+    if window is None:
+        if sinks:
+            raise ValueError("sinks belong to a window")
+        done = _fast.prompt_attention(cache._handle, q, n_q_heads, layer, row_start, out)
+    else:
+        done = _fast.prompt_attention_window(cache._handle, q, n_q_heads, layer, row_start, window, sinks, out)
     if type(done) is not int or done > 0:
-        return _checked("quasar_prompt_attention", done)
+        return _checked("quasar_prompt_attention" + ("" if window is None else "_window"), done)
     cache._check_buffers()
+    seen = None if window is None else _window_arg(window, sinks)
     rows, ldq = _rows_of(q, n_q_heads * 128, "q", cache)
     starts, n_seqs = _row_start_of(row_start, cache)
     out, ldo = _output_like(out, rows, n_q_heads * 128, cache, "out")
     if rows:
         ws, need = _scratch(_lib.quasar_prompt_attention_workspace_bytes(rows, n_q_heads, cache.n_kv_heads, n_seqs), q.device)
-        _check("quasar_prompt_attention",
-               _lib.quasar_prompt_attention(q.data_ptr(), rows, ldq, n_q_heads, cache.n_kv_heads, starts, n_seqs, *cache._layer(layer),
-                                            out.data_ptr(), ldo, _ptr(ws), need, _stream()))
+        given = (q.data_ptr(), rows, ldq, n_q_heads, cache.n_kv_heads, starts, n_seqs, *cache._layer(layer))
+        to = (out.data_ptr(), ldo, _ptr(ws), need, _stream())
+        if seen is None:
+            _check("quasar_prompt_attention", _lib.quasar_prompt_attention(*given, *to))
+        else:
+            _check("quasar_prompt_attention_window", _lib.quasar_prompt_attention_window(*given, *seen, *to))
     return out
 
 

@@ -47,6 +47,10 @@ decltype(&quasar_prompt_attention_workspace_bytes) p_prompt_attention_workspace_
 decltype(&quasar_pages_reserve) p_pages_reserve;
 decltype(&quasar_pages_fork) p_pages_fork;
 decltype(&quasar_pages_compact) p_pages_compact;
+decltype(&quasar_paged_prepare_rope) p_paged_prepare_rope;
+decltype(&quasar_paged_attention_window) p_paged_attention_window;
+decltype(&quasar_prompt_attention_window) p_prompt_attention_window;
+decltype(&quasar_pages_trim) p_pages_trim;
 PyObject *g_device, *g_stream;
 
 struct NotOrdinary {};
@@ -378,70 +382,106 @@ int64_t heads_of(PyObject *o) {
     return n;
 }
 
+int64_t window_of(PyObject *o, int64_t least) {
+    const int64_t n = integer(o);
+    if (n < least) throw NotOrdinary{};
+    return n;
+}
+
+// qkv, n_q_heads, layer, row_start, q_gamma, k_gamma (None where they may be): entry(.., gammas, rope.., q_out, ..)
+template <typename Entry, typename... Rope>
+int prepare_on(Entry entry, const PagedCall &p, PyObject *const *a, bool normed, PyObject *given, at::Tensor &out, float eps, Rope... rope) {
+    const PagedCache &c = *p.c;
+    const int64_t hq = heads_of(a[1]), layer = p.layer(a[2]);
+    const at::Tensor &x = p.rows(a[0], (hq + 2 * c.n_kv_heads) * 128);
+    const RowStart starts(p, a[3]);
+    const uint16_t *gamma[2] = {nullptr, nullptr};
+    for (int i = 0; normed && i < 2; ++i) {
+        const at::Tensor &g = p.tensor(a[4 + i], at::kBFloat16);
+        if (g.numel() != 128 || !g.is_contiguous()) throw NotOrdinary{};
+        gamma[i] = bits(g);
+    }
+    out = output(p, given, x.size(0), hq * 128);
+    return call(entry, bits(x), x.size(0), ld_of(x), hq, c.n_kv_heads, starts.p, starts.n_seqs, gamma[0], gamma[1], eps, rope..., bits(out), ld_of(out),
+                address<void>(c.pool, layer * c.layer_bytes), c.n_pages, c.page_len, (int)c.code, p.scale(c.k_scale, layer), p.scale(c.v_scale, layer),
+                address<const int32_t>(c.table), c.max_pages, c.max_pages, address<const int32_t>(c.lengths), current_stream());
+}
 // (handle, qkv, n_q_heads, layer, row_start, q_gamma, k_gamma, eps, rope_theta, q_out)
 PyObject *paged_prepare(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return tensor_of(n, 10, [&](at::Tensor &out) {
+        return prepare_on(p_paged_prepare, PagedCall(a[0]), a + 1, true, a[9], out, real(a[7]), real(a[8]));
+    });
+}
+// (handle, qkv, n_q_heads, layer, row_start, q_gamma, k_gamma, eps, layout, dims, inv_freq, magnitude, q_out)
+PyObject *paged_prepare_rope(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return tensor_of(n, 13, [&](at::Tensor &out) {
         const PagedCall p(a[0]);
-        const PagedCache &c = *p.c;
-        const int64_t hq = heads_of(a[2]), layer = p.layer(a[3]);
-        const at::Tensor &x = p.rows(a[1], (hq + 2 * c.n_kv_heads) * 128);
-        const RowStart starts(p, a[4]);
-        const uint16_t *gamma[2];
-        for (int i = 0; i < 2; ++i) {
-            const at::Tensor &g = p.tensor(a[5 + i], at::kBFloat16);
-            if (g.numel() != 128 || !g.is_contiguous()) throw NotOrdinary{};
-            gamma[i] = bits(g);
-        }
-        const float eps = real(a[7]), theta = real(a[8]);
-        out = output(p, a[9], x.size(0), hq * 128);
-        return call(p_paged_prepare, bits(x), x.size(0), ld_of(x), hq, c.n_kv_heads, starts.p, starts.n_seqs, gamma[0], gamma[1], eps, theta, bits(out), ld_of(out),
-                    address<void>(c.pool, layer * c.layer_bytes), c.n_pages, c.page_len, (int)c.code, p.scale(c.k_scale, layer), p.scale(c.v_scale, layer),
-                    address<const int32_t>(c.table), c.max_pages, c.max_pages, address<const int32_t>(c.lengths), current_stream());
+        const int64_t dims = integer(a[9]);
+        const at::Tensor &f = p.tensor(a[10], at::kDouble);
+        if (f.dim() != 1 || 2 * f.numel() != dims || !f.is_contiguous()) throw NotOrdinary{};
+        return prepare_on(p_paged_prepare_rope, p, a + 1, a[5] != Py_None || a[6] != Py_None, a[12], out, real(a[7]), (int)integer(a[8]), dims,
+                          static_cast<const double *>(f.data_ptr()), real(a[11]));
     });
 }
 
+// q, n_q_heads, layer, row_start, max_new: entry(.., window.., out, ..)
+template <typename Entry, typename... Window>
+int step_on(Entry entry, const PagedCall &p, PyObject *const *a, PyObject *workspace, PyObject *given, at::Tensor &out, Window... window) {
+    const PagedCache &c = *p.c;
+    const int64_t hq = heads_of(a[1]), layer = p.layer(a[2]), max_new = integer(a[4]);
+    const at::Tensor &q = p.rows(a[0], hq * 128);
+    const RowStart starts(p, a[3]);
+    out = output(p, given, q.size(0), hq * 128);
+    void *ws, *stream = current_stream();
+    size_t bytes;
+    c10::DataPtr scratch;
+    if (workspace == Py_None) {
+        bytes = p_paged_attention_workspace_bytes(max_new, hq, c.n_kv_heads);
+        if (!bytes) throw NotOrdinary{};
+        scratch = scratch_of(bytes);
+        ws = scratch.get();
+    } else {
+        const at::Tensor &t = any_tensor(workspace);
+        if (!t.is_cuda() || t.device().index() != c.device || !t.is_contiguous()) throw NotOrdinary{};   // (an expanded one holds less than nbytes)
+        ws = t.data_ptr();
+        bytes = t.nbytes();
+    }
+    return call(entry, bits(q), q.size(0), ld_of(q), hq, c.n_kv_heads, starts.p, starts.n_seqs, max_new, address<const void>(c.pool, layer * c.layer_bytes),
+                c.n_pages, c.page_len, (int)c.code, p.scale(c.k_scale, layer), p.scale(c.v_scale, layer), address<const int32_t>(c.table), c.max_pages, c.max_pages,
+                address<const int32_t>(c.lengths), window..., bits(out), ld_of(out), ws, bytes, stream);
+}
 // (handle, q, n_q_heads, layer, row_start, max_new, workspace, out)
 PyObject *paged_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    return tensor_of(n, 8, [&](at::Tensor &out) {
-        const PagedCall p(a[0]);
-        const PagedCache &c = *p.c;
-        const int64_t hq = heads_of(a[2]), layer = p.layer(a[3]), max_new = integer(a[5]);
-        const at::Tensor &q = p.rows(a[1], hq * 128);
-        const RowStart starts(p, a[4]);
-        out = output(p, a[7], q.size(0), hq * 128);
-        void *ws, *stream = current_stream();
-        size_t bytes;
-        c10::DataPtr scratch;
-        if (a[6] == Py_None) {
-            bytes = p_paged_attention_workspace_bytes(max_new, hq, c.n_kv_heads);
-            if (!bytes) throw NotOrdinary{};
-            scratch = scratch_of(bytes);
-            ws = scratch.get();
-        } else {
-            const at::Tensor &t = any_tensor(a[6]);
-            if (!t.is_cuda() || t.device().index() != c.device || !t.is_contiguous()) throw NotOrdinary{};   // (an expanded one holds less than nbytes)
-            ws = t.data_ptr();
-            bytes = t.nbytes();
-        }
-        return call(p_paged_attention, bits(q), q.size(0), ld_of(q), hq, c.n_kv_heads, starts.p, starts.n_seqs, max_new, address<const void>(c.pool, layer * c.layer_bytes),
-                    c.n_pages, c.page_len, (int)c.code, p.scale(c.k_scale, layer), p.scale(c.v_scale, layer), address<const int32_t>(c.table), c.max_pages, c.max_pages,
-                    address<const int32_t>(c.lengths), bits(out), ld_of(out), ws, bytes, stream);
+    return tensor_of(n, 8, [&](at::Tensor &out) { return step_on(p_paged_attention, PagedCall(a[0]), a + 1, a[6], a[7], out); });
+}
+// (handle, q, n_q_heads, layer, row_start, max_new, window, sinks, workspace, out)
+PyObject *paged_attention_window(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return tensor_of(n, 10, [&](at::Tensor &out) {
+        return step_on(p_paged_attention_window, PagedCall(a[0]), a + 1, a[8], a[9], out, window_of(a[6], 1), window_of(a[7], 0));
     });
 }
 
+// q, n_q_heads, layer, row_start: entry(.., window.., out, ..)
+template <typename Entry, typename... Window>
+int prompt_on(Entry entry, const PagedCall &p, PyObject *const *a, PyObject *given, at::Tensor &out, Window... window) {
+    const PagedCache &c = *p.c;
+    const int64_t hq = heads_of(a[1]), layer = p.layer(a[2]);
+    const at::Tensor &q = p.rows(a[0], hq * 128);
+    const RowStart starts(p, a[3]);
+    out = output(p, given, q.size(0), hq * 128);
+    return call_with_scratch(entry, p_prompt_attention_workspace_bytes(q.size(0), hq, c.n_kv_heads, starts.n_seqs), current_stream(), bits(q), q.size(0),
+                             ld_of(q), hq, c.n_kv_heads, starts.p, starts.n_seqs, address<const void>(c.pool, layer * c.layer_bytes), c.n_pages, c.page_len, (int)c.code,
+                             p.scale(c.k_scale, layer), p.scale(c.v_scale, layer), address<const int32_t>(c.table), c.max_pages, c.max_pages,
+                             address<const int32_t>(c.lengths), window..., bits(out), ld_of(out));
+}
 // (handle, q, n_q_heads, layer, row_start, out)
 PyObject *prompt_attention(PyObject *, PyObject *const *a, Py_ssize_t n) {
-    return tensor_of(n, 6, [&](at::Tensor &out) {
-        const PagedCall p(a[0]);
-        const PagedCache &c = *p.c;
-        const int64_t hq = heads_of(a[2]), layer = p.layer(a[3]);
-        const at::Tensor &q = p.rows(a[1], hq * 128);
-        const RowStart starts(p, a[4]);
-        out = output(p, a[5], q.size(0), hq * 128);
-        return call_with_scratch(p_prompt_attention, p_prompt_attention_workspace_bytes(q.size(0), hq, c.n_kv_heads, starts.n_seqs), current_stream(), bits(q), q.size(0),
-                                 ld_of(q), hq, c.n_kv_heads, starts.p, starts.n_seqs, address<const void>(c.pool, layer * c.layer_bytes), c.n_pages, c.page_len, (int)c.code,
-                                 p.scale(c.k_scale, layer), p.scale(c.v_scale, layer), address<const int32_t>(c.table), c.max_pages, c.max_pages,
-                                 address<const int32_t>(c.lengths), bits(out), ld_of(out));
+    return tensor_of(n, 6, [&](at::Tensor &out) { return prompt_on(p_prompt_attention, PagedCall(a[0]), a + 1, a[5], out); });
+}
+// (handle, q, n_q_heads, layer, row_start, window, sinks, out)
+PyObject *prompt_attention_window(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return tensor_of(n, 8, [&](at::Tensor &out) {
+        return prompt_on(p_prompt_attention_window, PagedCall(a[0]), a + 1, a[7], out, window_of(a[5], 1), window_of(a[6], 0));
     });
 }
 
@@ -469,6 +509,16 @@ PyObject *pages_fork(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// (handle, window, sinks)
+PyObject *pages_trim(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return status_of(n, 3, [&] {
+        const PagedCall p(a[0]);
+        const PagedCache &c = *p.c;
+        return call(p_pages_trim, address<int32_t>(c.table), c.max_pages, c.max_seqs, c.max_pages, address<const int32_t>(c.lengths), window_of(a[1], 1), window_of(a[2], 0),
+                    address<int32_t>(c.refs), c.n_pages, c.page_len, current_stream());
+    });
+}
+
 // (handle)
 PyObject *pages_compact(PyObject *, PyObject *const *a, Py_ssize_t n) {
     return tensor_of(n, 1, [&](at::Tensor &out) {
@@ -488,6 +538,7 @@ template <typename Each> void each_entry(Each each) {
     each(p_w4_workspace_bytes); each(p_w8_linear_fused); each(p_w8_gateup_swiglu); each(p_w8_fused_workspace_bytes); each(p_w8_gateup_workspace_bytes);
     each(p_paged_prepare); each(p_paged_attention); each(p_paged_attention_workspace_bytes); each(p_prompt_attention); each(p_prompt_attention_workspace_bytes);
     each(p_pages_reserve); each(p_pages_fork); each(p_pages_compact);
+    each(p_paged_prepare_rope); each(p_paged_attention_window); each(p_prompt_attention_window); each(p_pages_trim);
 }
 Py_ssize_t entries() {
     Py_ssize_t n = 0;
@@ -532,6 +583,7 @@ PyObject *bound(PyObject *, PyObject *) {
 PyMethodDef methods[] = {FAST(w8_linear), FAST(bf16_linear), FAST(w8a8_linear), FAST(w4_linear),
                          FAST(w8_linear_fused), FAST(w8_gateup_swiglu),
                          FAST(paged_prepare), FAST(paged_attention), FAST(prompt_attention), FAST(pages_reserve), FAST(pages_fork), FAST(pages_compact),
+                         FAST(paged_prepare_rope), FAST(paged_attention_window), FAST(prompt_attention_window), FAST(pages_trim),
                          {"paged_cache", paged_cache, METH_VARARGS, nullptr}, {"paged_cache_as_made", paged_cache_as_made, METH_O, nullptr},
                          {"bind", bind, METH_VARARGS, nullptr}, {"bound", bound, METH_NOARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

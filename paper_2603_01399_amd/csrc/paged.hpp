@@ -19,6 +19,9 @@ namespace quasar {
 
 constexpr float kE4m3Max = 448.f;            // largest finite e4m3 value: beyond it the append saturates
 
+constexpr int kBlockShift = 5;               // a block of 32 positions
+static_assert(kKvBlock == 1 << kBlockShift, "positions of a block");
+
 enum { KV_BF16 = 0, KV_E4M3 = 1 };
 template <int KV> constexpr int kv_block_bytes = KV == KV_E4M3 ? kKvBlockBytes / 2 : kKvBlockBytes;   // keys or values of 32 positions of a head
 
@@ -182,6 +185,22 @@ template <int KV> __device__ __forceinline__ int drop_nonfinite(u32x4 &v, int fi
     return at;
 }
 
+// The same where a row may see a later position and not an earlier one: clears them, and says which positions of the block of 32 had one, of the wave.
+// `first`: the lane's slot 0 in the block.
+template <int KV> __device__ __forceinline__ unsigned int drop_nonfinite_of_block(u32x4 &v, int first) {
+    unsigned int at = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const unsigned int bad = nonfinite_halves<KV>(v[j]);
+        const int pos = first + 16 * (j >> 1) + 2 * (j & 1);
+        if (bad & 0x80000000u) { v[j] &= 0x0000FFFFu; at |= 2u << pos; }
+        if (bad & 0x00008000u) { v[j] &= 0xFFFF0000u; at |= 1u << pos; }
+    }
+#pragma unroll
+    for (int off = 32; off >= 1; off >>= 1) at |= __shfl_xor(at, off, 64);
+    return at;
+}
+
 template <int KV> __device__ __forceinline__ f32x16 values_times_weights(const u32x4 v, const u32x4 w, const f32x16 acc) {
     if constexpr (KV == KV_BF16) return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, v), __builtin_bit_cast(bf16x8, w), acc, 0, 0, 0);
     else return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(f16x8, v), __builtin_bit_cast(f16x8, w), acc, 0, 0, 0);
@@ -203,10 +222,69 @@ struct PrepareParams {
     float eps;
     double log2_theta;
     int parts;                // waves that share a row's heads; heads of a workgroup in the block form
+    // forms other than ROPE_THETA
+    const double *inv_freq;   // [dims / 2] radians a position
+    float magnitude;          // of cosines and sines
+    int dims;                 // of a head, from its first on, that are rotated: a multiple of 16
 };
 
-// What a lane does with its eight elements of a head, d = 8 j .. 8 j + 7, of lanes 16 h + j: the norm with its two roundings to bf16, then the
-// rotation; the rotary partner (d +- 64) is lane j ^ 8.  sinv is negative in the first half (x1 cos - x2 sin).
+// How a head is rotated.  ROPE_THETA: all of it, pairs d and d + 64, angles from theta, behind the norm.  The others: pairs d and d + dims / 2
+// (ROPE_HALF) or 2 d and 2 d + 1 (ROPE_PAIRS) of the first `dims`, angles from a table, behind the norm or without one (gammas NULL).
+enum { ROPE_THETA = 0, ROPE_HALF = 1, ROPE_PAIRS = 2 };
+
+// What a lane does with its eight elements of a head, d = 8 j .. 8 j + 7, of lanes 16 h + j: the norm, with its two roundings to bf16 ...
+__device__ __forceinline__ u32x4 normed(const u32x4 raw, const u32x4 graw, float eps) {
+    float x[8];
+    u32x4 out;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        x[2 * e] = __uint_as_float(raw[e] << 16);
+        x[2 * e + 1] = __uint_as_float(raw[e] & 0xFFFF0000u);
+    }
+    float ss = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) ss += x[e] * x[e];
+#pragma unroll
+    for (int off = 8; off >= 1; off >>= 1) ss += __shfl_xor(ss, off, 64);
+    const float r = __fdiv_rn(1.0f, __fsqrt_rn(__fdiv_rn(ss, (float)kHeadDim) + eps));
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const unsigned int n = float2_to_bf16_pair(x[2 * e] * r, x[2 * e + 1] * r);
+        out[e] = float2_to_bf16_pair(__uint_as_float(n << 16) * __uint_as_float(graw[e] << 16),
+                                     __uint_as_float(n & 0xFFFF0000u) * __uint_as_float(graw[e] & 0xFFFF0000u));
+    }
+    return out;
+}
+
+// ... then the rotation of the first `turned` = dims / 8 lanes' elements, others as they are.  ROPE_HALF: the partner (d +- dims / 2) is turned / 2 lanes
+// away and sinv negative in the first half (x1 cos - x2 sin); ROPE_PAIRS: both are in one word, whose angle is cosv[e], sinv[e] of word e.
+template <int ROPE>
+__device__ __forceinline__ u32x4 rotated(const u32x4 x, int turned, const float (&cosv)[8], const float (&sinv)[8]) {
+    const int lane = threadIdx.x & 63, j = lane & 15;
+    u32x4 out;
+    if constexpr (ROPE == ROPE_HALF) {
+        const int partner = (lane & 48) + (j < turned / 2 ? j + turned / 2 : j < turned ? j - turned / 2 : j);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const unsigned int other = __shfl(x[e], partner, 64);
+            out[e] = float2_to_bf16_pair(__uint_as_float(x[e] << 16) * cosv[2 * e] + __uint_as_float(other << 16) * sinv[2 * e],
+                                         __uint_as_float(x[e] & 0xFFFF0000u) * cosv[2 * e + 1] + __uint_as_float(other & 0xFFFF0000u) * sinv[2 * e + 1]);
+        }
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float a = __uint_as_float(x[e] << 16), b = __uint_as_float(x[e] & 0xFFFF0000u);
+            out[e] = float2_to_bf16_pair(a * cosv[e] - b * sinv[e], b * cosv[e] + a * sinv[e]);
+        }
+    }
+    return j < turned ? out : x;
+}
+// Which angle of the table a lane's element e takes (word e in ROPE_PAIRS); lanes that are not turned take any.
+template <int ROPE> __device__ __forceinline__ int angle_of(int j, int e, int turned) {
+    return ROPE == ROPE_HALF ? (8 * (j < turned / 2 ? j : j - turned / 2) + e) & 63 : (4 * j + e) & 63;
+}
+
+// The norm and the rotation in one: the rotary partner (d +- 64) is lane j ^ 8.  sinv is negative in the first half (x1 cos - x2 sin).
 __device__ __forceinline__ u32x4 norm_and_rotate(const u32x4 raw, const u32x4 graw, float eps, const float (&cosv)[8], const float (&sinv)[8]) {
     float x[8], o[8];
 #pragma unroll
@@ -268,9 +346,15 @@ __device__ __forceinline__ void rotation(int pos, double per_position, float &sn
     sincospif(2.0f * (float)(turns - rint(turns)), &sn, &cs);
 }
 
+// Turns a position of the angle that a lane has in hand, 0 where there are fewer.
+template <int ROPE> __device__ __forceinline__ double turns_of_lane(const PrepareParams &p, int lane) {
+    if constexpr (ROPE == ROPE_THETA) return turns_per_position(p.log2_theta, lane);
+    return lane < p.dims / 2 ? p.inv_freq[lane] * 0.15915494309189535 : 0.0;
+}
+
 // For few rows a sequence: a wave takes four heads of a row at a time, 16 lanes of 16 bytes each.  Bound by the launch and one trip to memory: one row of
 // one sequence 5 us a call, 3.6 in the kernel.
-template <int KV>
+template <int KV, int ROPE>
 __global__ __launch_bounds__(256) void paged_prepare_kernel(const PrepareParams p) {
     const PagedParams &c = p.c;
     const int lane = threadIdx.x & 63;
@@ -284,13 +368,25 @@ __global__ __launch_bounds__(256) void paged_prepare_kernel(const PrepareParams 
     const int pos = sp.len + t - sp.row0;
     const int j = lane & 15;
     float sn, cs;
-    rotation(pos, turns_per_position(p.log2_theta, lane), sn, cs);
+    rotation(pos, turns_of_lane<ROPE>(p, lane), sn, cs);
     float cosv[8], sinv[8];
+    const int turned = ROPE == ROPE_THETA ? 16 : p.dims / 8;
+    if constexpr (ROPE == ROPE_THETA) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        cosv[e] = __shfl(cs, 8 * (j & 7) + e, 64);
-        sinv[e] = __shfl(sn, 8 * (j & 7) + e, 64);
-        if (j < 8) sinv[e] = -sinv[e];
+        for (int e = 0; e < 8; ++e) {
+            cosv[e] = __shfl(cs, 8 * (j & 7) + e, 64);
+            sinv[e] = __shfl(sn, 8 * (j & 7) + e, 64);
+            if (j < 8) sinv[e] = -sinv[e];
+        }
+    } else {
+        cs *= p.magnitude;
+        sn *= p.magnitude;
+#pragma unroll
+        for (int e = 0; e < (ROPE == ROPE_HALF ? 8 : 4); ++e) {
+            cosv[e] = __shfl(cs, angle_of<ROPE>(j, e, turned), 64);
+            sinv[e] = __shfl(sn, angle_of<ROPE>(j, e, turned), 64);
+            if (ROPE == ROPE_HALF && j < turned / 2) sinv[e] = -sinv[e];
+        }
     }
     const int blk = pos / kKvBlock, pib = pos % kKvBlock, col = blk >> c.block_shift;
     const int page = col < c.columns ? c.table[s * c.table_ld + col] : -1;
@@ -303,11 +399,18 @@ __global__ __launch_bounds__(256) void paged_prepare_kernel(const PrepareParams 
         const bool live = h < heads;
         u32x4 raw = {0u, 0u, 0u, 0u};
         if (live) raw = *reinterpret_cast<const u32x4 *>(p.qkv + t * p.ld + (long long)h * kHeadDim + 8 * j);
-        const u32x4 graw = *reinterpret_cast<const u32x4 *>((h < c.Hq ? p.q_gamma : p.k_gamma) + 8 * j);
-        const u32x4 turned = norm_and_rotate(raw, graw, p.eps, cosv, sinv);      // (all lanes: it exchanges)
+        u32x4 done;                                                              // (all lanes: they exchange)
+        if constexpr (ROPE == ROPE_THETA) {
+            const u32x4 graw = *reinterpret_cast<const u32x4 *>((h < c.Hq ? p.q_gamma : p.k_gamma) + 8 * j);
+            done = norm_and_rotate(raw, graw, p.eps, cosv, sinv);
+        } else {
+            done = raw;
+            if (p.q_gamma) done = normed(raw, *reinterpret_cast<const u32x4 *>((h < c.Hq ? p.q_gamma : p.k_gamma) + 8 * j), p.eps);
+            done = rotated<ROPE>(done, turned, cosv, sinv);
+        }
         if (!live) continue;
         const bool value = h >= c.Hq + c.Hkv;
-        const u32x4 rounded = value ? raw : turned;                              // (values are stored as they are)
+        const u32x4 rounded = value ? raw : done;                                // (values are stored as they are)
         if (h < c.Hq) {
             *reinterpret_cast<u32x4 *>(p.q_out + t * p.ldq + (long long)h * kHeadDim + 8 * j) = rounded;
             continue;
@@ -340,7 +443,7 @@ __global__ __launch_bounds__(256) void paged_prepare_kernel(const PrepareParams 
 // the block are computed once, in LDS; a value head goes through LDS too, since its 16-byte units hold eight positions of one d: written
 // one by one they cost 2 bytes of every 16 a store.  11 prompts of up to 1531 rows into 8-bit pages (229 MB moved): 57 to 60 us, 4 TB/s where a
 // plain copy reaches 5.15; what is left is the norms and rotations, two trips through memory a workgroup.
-template <int KV>
+template <int KV, int ROPE>
 __global__ __launch_bounds__(256) void paged_prepare_block_kernel(const PrepareParams p) {
     constexpr int BB = kv_block_bytes<KV>, STRIDE = kHeadDim + 8;                // (of a row of the values in LDS)
     __shared__ float2 turned[kKvBlock][kHeadDim / 2];
@@ -349,7 +452,8 @@ __global__ __launch_bounds__(256) void paged_prepare_block_kernel(const PrepareP
     __shared__ int wave_sums[4];
     const PagedParams &c = p.c;
     const int tid = threadIdx.x, lane = tid & 63, j = tid & 15, r0 = tid >> 4;
-    const double per_position = turns_per_position(p.log2_theta, lane);
+    const double per_position = turns_of_lane<ROPE>(p, lane);
+    const int turned_lanes = ROPE == ROPE_THETA ? 16 : p.dims / 8;
 
     auto blocks_with_rows = [&](int s) {
         const SeqSpan a = seq_span(c, s);
@@ -383,29 +487,36 @@ __global__ __launch_bounds__(256) void paged_prepare_block_kernel(const PrepareP
         for (int r = tid >> 6; r < kKvBlock; r += 4) {
             float sn, cs;
             rotation(pos0 + r, per_position, sn, cs);
-            turned[r][lane] = float2{cs, sn};
+            turned[r][lane] = ROPE == ROPE_THETA ? float2{cs, sn} : float2{cs * p.magnitude, sn * p.magnitude};
         }
         __syncthreads();
 #pragma unroll
         for (int i = 0; i < 2; ++i)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                const float2 v = turned[r0 + 16 * i][8 * (j & 7) + e];
+            for (int e = 0; e < (ROPE == ROPE_PAIRS ? 4 : 8); ++e) {
+                const float2 v = turned[r0 + 16 * i][ROPE == ROPE_THETA ? 8 * (j & 7) + e : angle_of<ROPE>(j, e, turned_lanes)];
                 cosv[i][e] = v.x;
-                sinv[i][e] = j < 8 ? -v.y : v.y;
+                sinv[i][e] = ROPE != ROPE_PAIRS && j < turned_lanes / 2 ? -v.y : v.y;
             }
     }
     for (int h = h0; h < h1; ++h) {
         u32x4 next[2];
         if (h + 1 < h1) { next[0] = load(h + 1, 0); next[1] = load(h + 1, 1); }
         if (h < c.Hq + c.Hkv) {
-            const u32x4 graw = *reinterpret_cast<const u32x4 *>((h < c.Hq ? p.q_gamma : p.k_gamma) + 8 * j);
+            u32x4 graw = {0u, 0u, 0u, 0u};
+            if (ROPE == ROPE_THETA || p.q_gamma) graw = *reinterpret_cast<const u32x4 *>((h < c.Hq ? p.q_gamma : p.k_gamma) + 8 * j);
             const float sc = KV == KV_E4M3 && h >= c.Hq && c.k_scale ? c.k_scale[h - c.Hq] : 1.0f;
             unsigned char *dst = c.pages + base + (h - c.Hq) * head_step;
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 const int r = r0 + 16 * i;
-                const u32x4 o = norm_and_rotate(x[i], graw, p.eps, cosv[i], sinv[i]);
+                u32x4 o = x[i];
+                if constexpr (ROPE == ROPE_THETA) {
+                    o = norm_and_rotate(o, graw, p.eps, cosv[i], sinv[i]);
+                } else {
+                    if (p.q_gamma) o = normed(o, graw, p.eps);
+                    o = rotated<ROPE>(o, turned_lanes, cosv[i], sinv[i]);
+                }
                 if (!is_new(r)) continue;
                 if (h < c.Hq) *reinterpret_cast<u32x4 *>(p.q_out + row_of(r) * p.ldq + (long long)h * kHeadDim + 8 * j) = o;
                 else if (!stored) continue;

@@ -92,6 +92,39 @@ int check_cache(const CacheArgs &a, PagedParams &p) {
 // New rows a sequence, on average, from which the append goes block by block: 40 sequences of up to 90 rows of 32 / 8 heads in 8-bit pages
 // 22.4 us row by row and 24 to 31 by blocks, 11 of up to 1531 88 and 57.
 constexpr int kBlockRows = 64;
+// ---- the append
+int check_prepare(const CacheArgs &a, PrepareParams &p) {
+    if (const int e = check_cache(a, p.c)) return e;
+    if (p.ld < (a.Hq + 2 * a.Hkv) * kHeadDim || p.ldq < a.Hq * kHeadDim || p.ld % 8 || p.ldq % 8) return QUASAR_ERR_SHAPE;
+    return p.eps >= 0.f && p.eps < 1.f ? QUASAR_OK : QUASAR_ERR_SHAPE;
+}
+bool prepare_aligned(const PrepareParams &p) { return aligned(p.qkv, 16) && aligned(p.q_out, 16) && aligned(p.q_gamma, 16) && aligned(p.k_gamma, 16); }
+template <int ROPE>
+int launch_prepare(const CacheArgs &a, PrepareParams &p, hipStream_t st) {
+    const int64_t heads = a.Hq + 2 * a.Hkv, T = a.T;
+    const bool bf16 = kv_type(a.kv_dtype) == KV_BF16;
+    if (T >= kBlockRows * a.n_seqs) {
+        // as many heads a workgroup as keep four workgroups a compute unit, eight at most: 512 rows of 32 / 8 heads 8.3 us with one (eight: 14.7),
+        // 11 prompts of up to 1531 rows in 8-bit pages 57 with eight (four: 60)
+        const int64_t blocks = T / kKvBlock + 2 * a.n_seqs;                  // (two ragged ones a sequence)
+        int64_t parts = (T / kKvBlock * heads) / (4 * compute_units());
+        parts = parts < 1 ? 1 : parts > 8 ? 8 : parts;
+        p.parts = (int)parts;
+        const dim3 grid((unsigned int)blocks, (unsigned int)((heads + parts - 1) / parts));
+        if (bf16) hipLaunchKernelGGL((paged_prepare_block_kernel<KV_BF16, ROPE>), grid, dim3(256), 0, st, p);
+        else hipLaunchKernelGGL((paged_prepare_block_kernel<KV_E4M3, ROPE>), grid, dim3(256), 0, st, p);
+        return launched();
+    }
+    const int64_t quads = (heads + 3) / 4;
+    int64_t parts = 4096 / T;
+    parts = parts < 1 ? 1 : parts > quads ? quads : parts;
+    p.parts = (int)parts;
+    const dim3 grid((unsigned int)((T * parts + 3) / 4));
+    if (bf16) hipLaunchKernelGGL((paged_prepare_kernel<KV_BF16, ROPE>), grid, dim3(256), 0, st, p);
+    else hipLaunchKernelGGL((paged_prepare_kernel<KV_E4M3, ROPE>), grid, dim3(256), 0, st, p);
+    return launched();
+}
+
 constexpr float kScaleLog2 = 1.4426950408889634f / 11.313708498984761f;      // log2(e) / sqrt(128)
 
 // ---- what the attention calls share of a launch: workgroups of a kv head, and the room for what they leave of shared sequences or tiles
@@ -140,11 +173,11 @@ int launch_attention(unsigned int workgroups_x, unsigned int workgroups_y, int l
     hipLaunchKernelGGL(Kernel, dim3(workgroups_x, workgroups_y), dim3(kPromptWaves * 64), lds, st, p);
     return launched();
 }
-template <int KV>
+template <int KV, bool WINDOW>
 int launch_step(const PagedAttnParams &p, int NQT, hipStream_t st) {
     const int lds = kPagedWaves * NQT * (8 * 64 * 16 + 16 * 2 * 4) + (kPagedWaves + 4 * (p.c.n_seqs + 1)) * 4;
-    const int e = NQT == 1 ? launch_attention<paged_attention_kernel<KV, 1>>(p.workers, p.c.Hkv, lds, st, p)
-                           : launch_attention<paged_attention_kernel<KV, 2>>(p.workers, p.c.Hkv, lds, st, p);
+    const int e = NQT == 1 ? launch_attention<paged_attention_kernel<KV, 1, WINDOW>>(p.workers, p.c.Hkv, lds, st, p)
+                           : launch_attention<paged_attention_kernel<KV, 2, WINDOW>>(p.workers, p.c.Hkv, lds, st, p);
     if (e || p.workers == 1) return e;                                       // (one worker finishes every sequence)
     hipLaunchKernelGGL(paged_merge_kernel, dim3((unsigned int)(2 * compute_units())), dim3(512), 0, st, p, NQT);
     return launched();
@@ -169,13 +202,13 @@ int whole_more(int64_t T, int64_t G) {
     const int64_t tiles = (T * G + 32 * kPromptWaves - 1) / (32 * kPromptWaves);
     return (int)(tiles < 16 ? tiles : 16);
 }
-template <int KV>
+template <int KV, bool WINDOW>
 int launch_prompt(const PromptParams &p, int64_t tiles, int PW, hipStream_t st) {
     const int lds = 2 * kPromptStepBytes + (kMaxSeqs + kPromptWaves + 8) * 4;
-    if (!p.workers) return launch_attention<prompt_attention_kernel<KV, false, 1>>((unsigned int)(tiles * p.c.Hkv), 1, lds, st, p);
+    if (!p.workers) return launch_attention<prompt_attention_kernel<KV, false, 1, WINDOW>>((unsigned int)(tiles * p.c.Hkv), 1, lds, st, p);
     const unsigned int n = (unsigned int)(p.workers * p.c.Hkv);
-    const int e = PW == 1 ? launch_attention<prompt_attention_kernel<KV, true, 1>>(n, 1, lds + kMaxFlatTiles * 4, st, p)
-                          : launch_attention<prompt_attention_kernel<KV, true, 2>>(n, 1, lds + kMaxFlatTiles * 4, st, p);
+    const int e = PW == 1 ? launch_attention<prompt_attention_kernel<KV, true, 1, WINDOW>>(n, 1, lds + kMaxFlatTiles * 4, st, p)
+                          : launch_attention<prompt_attention_kernel<KV, true, 2, WINDOW>>(n, 1, lds + kMaxFlatTiles * 4, st, p);
     if (e || p.workers == 1) return e;
     hipLaunchKernelGGL(prompt_merge_kernel, dim3((unsigned int)(4 * compute_units())), dim3(256), 0, st, p, kPromptWaves / PW);
     return launched();
@@ -187,6 +220,94 @@ template <class Params> void lay_out(Params &p, const FlatShape &a, void *worksp
     p.part_o = static_cast<f32x4 *>(workspace);
     p.part_ml = reinterpret_cast<float *>(static_cast<unsigned char *>(workspace) + a.part_o);
     p.pieces = reinterpret_cast<int *>(static_cast<unsigned char *>(workspace) + a.part_o + a.part_ml);
+}
+
+// What both attentions are given beside the cache.
+struct AttentionArgs {
+    const uint16_t *q;
+    int64_t ldq;
+    uint16_t *out;
+    int64_t ldo;
+    void *workspace;
+    size_t workspace_bytes;
+    void *stream;
+};
+bool window_of(int64_t size, int64_t sinks, Window &w) {
+    if (size < 1 || sinks < 0) return false;
+    w.size = (int)(size < kMostWindow ? size : kMostWindow);
+    w.sinks = (int)(sinks < kMostWindow ? sinks : kMostWindow);
+    return true;
+}
+// A window that no context of this table is longer than, or first tokens as many, hide nothing: the kernels without one.
+bool hides(const Window *w, const CacheArgs &a) {
+    const int64_t most = a.max_pages * a.page_len;
+    return w && w->size < most && w->sinks < most;
+}
+
+int step_attention(const CacheArgs &a, const AttentionArgs &t, int64_t max_new, const Window *window) {
+    if (!t.q || !t.out) return QUASAR_ERR_NULL;
+    PagedParams c{};
+    if (const int e = check_cache(a, c)) return e;
+    StepShape shape{};
+    if (!step_shape(max_new, a.Hq, a.Hkv, a.n_seqs, shape)) return QUASAR_ERR_SHAPE;
+    if (t.ldq < a.Hq * kHeadDim || t.ldo < a.Hq * kHeadDim || t.ldq % 8 || t.ldo % 4) return QUASAR_ERR_SHAPE;
+    if (!aligned(t.q, 16) || !aligned(t.out, 8)) return QUASAR_ERR_ALIGN;
+    if (!t.workspace || t.workspace_bytes < quasar_paged_attention_workspace_bytes(max_new, a.Hq, a.Hkv)) return QUASAR_ERR_WORKSPACE;
+    if (!aligned(t.workspace, 16)) return QUASAR_ERR_ALIGN;
+    c.max_new = (int)max_new;
+    hipStream_t st = static_cast<hipStream_t>(t.stream);
+    const bool bf16 = kv_type(a.kv_dtype) == KV_BF16, windowed = hides(window, a);
+    if (shape.NQT) {
+        PagedAttnParams p{};
+        p.c = c;
+        p.q = t.q; p.out = t.out; p.ldq = t.ldq; p.ldo = t.ldo;
+        p.scale_log2 = kScaleLog2;
+        lay_out(p, shape.flat, t.workspace);
+        if (windowed) {
+            p.window = *window;
+            return bf16 ? launch_step<KV_BF16, true>(p, shape.NQT, st) : launch_step<KV_E4M3, true>(p, shape.NQT, st);
+        }
+        return bf16 ? launch_step<KV_BF16, false>(p, shape.NQT, st) : launch_step<KV_E4M3, false>(p, shape.NQT, st);
+    }
+    PromptParams p{};
+    p.c = c;
+    p.q = t.q; p.out = t.out; p.ldq = t.ldq; p.ldo = t.ldo;
+    p.scale_log2 = kScaleLog2;
+    p.whole_more = -(1 << 30);                                                   // (a step's tiles are shared always: minus more than any share)
+    if (shape.flat.workers) lay_out(p, shape.flat, t.workspace);
+    if (windowed) {
+        p.window = *window;
+        return bf16 ? launch_prompt<KV_BF16, true>(p, shape.flat.tiles, shape.PW, st) : launch_prompt<KV_E4M3, true>(p, shape.flat.tiles, shape.PW, st);
+    }
+    return bf16 ? launch_prompt<KV_BF16, false>(p, shape.flat.tiles, shape.PW, st) : launch_prompt<KV_E4M3, false>(p, shape.flat.tiles, shape.PW, st);
+}
+
+int prompts_attention(const CacheArgs &a, const AttentionArgs &t, const Window *window) {
+    if (!t.q || !t.out) return QUASAR_ERR_NULL;
+    PromptParams p{};
+    if (const int e = check_cache(a, p.c)) return e;
+    if (a.T * (a.Hq / a.Hkv) > (1 << 26)) return QUASAR_ERR_SHAPE;               // (the tiles of all sequences are counted in 32 bits)
+    if (t.ldq < a.Hq * kHeadDim || t.ldo < a.Hq * kHeadDim || t.ldq % 8 || t.ldo % 4) return QUASAR_ERR_SHAPE;
+    if (!aligned(t.q, 16) || !aligned(t.out, 8) || !aligned(t.workspace, 16)) return QUASAR_ERR_ALIGN;
+    p.q = t.q; p.out = t.out; p.ldq = t.ldq; p.ldo = t.ldo;
+    p.scale_log2 = kScaleLog2;
+    const FlatShape shape = prompt_shape(a.T, a.Hq, a.Hkv, a.n_seqs);
+    p.whole_more = whole_more(a.T, a.Hq / a.Hkv);
+    // (a table or a window so short that tiles stay whole whatever the lengths are: launched without the join)
+    int64_t reach = a.max_pages * a.page_len;
+    const bool windowed = hides(window, a);
+    if (windowed) {
+        p.window = *window;
+        // positions of the steps that a tile sees: those of the first ones, and of the window of its first row up to its last
+        const int64_t tile = 32 * kPromptWaves, most = (int64_t)window->size + window->sinks + tile + 3 * kPromptStep;
+        reach = reach < most ? reach : most;
+    }
+    const bool may_share = reach > (int64_t)kPromptStep * (kFlatLeast + p.whole_more);
+    if (t.workspace && shape.workers && t.workspace_bytes >= shape.bytes() && may_share) lay_out(p, shape, t.workspace);
+    hipStream_t st = static_cast<hipStream_t>(t.stream);
+    const bool bf16 = kv_type(a.kv_dtype) == KV_BF16;
+    if (windowed) return bf16 ? launch_prompt<KV_BF16, true>(p, shape.tiles, 1, st) : launch_prompt<KV_E4M3, true>(p, shape.tiles, 1, st);
+    return bf16 ? launch_prompt<KV_BF16, false>(p, shape.tiles, 1, st) : launch_prompt<KV_E4M3, false>(p, shape.tiles, 1, st);
 }
 
 BooksParams books(int32_t *table, int64_t table_ld, int64_t n_seqs, int64_t max_pages, int32_t *lengths, int32_t *refs, int64_t n_pages, int64_t page_len) {
@@ -225,35 +346,32 @@ int quasar_paged_prepare(const uint16_t *qkv, int64_t T, int64_t ld, int64_t n_q
     if (!qkv || !q_gamma || !k_gamma || !q_out) return QUASAR_ERR_NULL;
     PrepareParams p{};
     const CacheArgs a{T, n_q_heads, n_kv_heads, pages, n_pages, page_len, kv_dtype, k_scale, v_scale, table, table_ld, n_seqs, max_pages, lengths, row_start};
-    if (const int e = check_cache(a, p.c)) return e;
-    if (ld < (n_q_heads + 2 * n_kv_heads) * kHeadDim || ldq < n_q_heads * kHeadDim || ld % 8 || ldq % 8) return QUASAR_ERR_SHAPE;
-    if (!(eps >= 0.f && eps < 1.f) || !(rope_theta > 1.f) || !(rope_theta < 1e30f)) return QUASAR_ERR_SHAPE;
-    if (!aligned(qkv, 16) || !aligned(q_out, 16) || !aligned(q_gamma, 16) || !aligned(k_gamma, 16)) return QUASAR_ERR_ALIGN;
     p.qkv = qkv; p.q_gamma = q_gamma; p.k_gamma = k_gamma; p.q_out = q_out;
     p.ld = ld; p.ldq = ldq; p.eps = eps;
+    if (const int e = check_prepare(a, p)) return e;
+    if (!(rope_theta > 1.f) || !(rope_theta < 1e30f)) return QUASAR_ERR_SHAPE;
+    if (!prepare_aligned(p)) return QUASAR_ERR_ALIGN;
     p.log2_theta = std::log2((double)rope_theta);
+    return launch_prepare<ROPE_THETA>(a, p, static_cast<hipStream_t>(hip_stream));
+}
+
+int quasar_paged_prepare_rope(const uint16_t *qkv, int64_t T, int64_t ld, int64_t n_q_heads, int64_t n_kv_heads, const int32_t *row_start,
+                              int64_t n_seqs, const uint16_t *q_gamma, const uint16_t *k_gamma, float eps, int rope_layout, int64_t rope_dims,
+                              const double *inv_freq, float magnitude, uint16_t *q_out, int64_t ldq, void *pages, int64_t n_pages, int64_t page_len,
+                              int kv_dtype, const float *k_scale, const float *v_scale, const int32_t *table, int64_t table_ld, int64_t max_pages,
+                              const int32_t *lengths, void *hip_stream) {
+    if (!qkv || !q_out || !inv_freq || !q_gamma != !k_gamma) return QUASAR_ERR_NULL;
+    PrepareParams p{};
+    const CacheArgs a{T, n_q_heads, n_kv_heads, pages, n_pages, page_len, kv_dtype, k_scale, v_scale, table, table_ld, n_seqs, max_pages, lengths, row_start};
+    p.qkv = qkv; p.q_gamma = q_gamma; p.k_gamma = k_gamma; p.q_out = q_out;
+    p.ld = ld; p.ldq = ldq; p.eps = eps;
+    if (const int e = check_prepare(a, p)) return e;
+    if (rope_layout != QUASAR_ROPE_HALF && rope_layout != QUASAR_ROPE_INTERLEAVED) return QUASAR_ERR_DTYPE;
+    if (rope_dims < 16 || rope_dims > kHeadDim || rope_dims % 16 || !(magnitude > 0.f) || !std::isfinite(magnitude)) return QUASAR_ERR_SHAPE;
+    if (!prepare_aligned(p) || !aligned(inv_freq, 8)) return QUASAR_ERR_ALIGN;
+    p.inv_freq = inv_freq; p.magnitude = magnitude; p.dims = (int)rope_dims;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    const int64_t heads = n_q_heads + 2 * n_kv_heads;
-    if (T >= kBlockRows * n_seqs) {
-        // as many heads a workgroup as keep four workgroups a compute unit, eight at most: 512 rows of 32 / 8 heads 8.3 us with one (eight: 14.7),
-        // 11 prompts of up to 1531 rows in 8-bit pages 57 with eight (four: 60)
-        const int64_t blocks = T / kKvBlock + 2 * n_seqs;                    // (two ragged ones a sequence)
-        int64_t parts = (T / kKvBlock * heads) / (4 * compute_units());
-        parts = parts < 1 ? 1 : parts > 8 ? 8 : parts;
-        p.parts = (int)parts;
-        const dim3 grid((unsigned int)blocks, (unsigned int)((heads + parts - 1) / parts));
-        if (kv_type(kv_dtype) == KV_BF16) hipLaunchKernelGGL(paged_prepare_block_kernel<KV_BF16>, grid, dim3(256), 0, st, p);
-        else hipLaunchKernelGGL(paged_prepare_block_kernel<KV_E4M3>, grid, dim3(256), 0, st, p);
-        return launched();
-    }
-    const int64_t quads = (heads + 3) / 4;
-    int64_t parts = 4096 / T;
-    parts = parts < 1 ? 1 : parts > quads ? quads : parts;
-    p.parts = (int)parts;
-    const dim3 grid((unsigned int)((T * parts + 3) / 4));
-    if (kv_type(kv_dtype) == KV_BF16) hipLaunchKernelGGL(paged_prepare_kernel<KV_BF16>, grid, dim3(256), 0, st, p);
-    else hipLaunchKernelGGL(paged_prepare_kernel<KV_E4M3>, grid, dim3(256), 0, st, p);
-    return launched();
+    return rope_layout == QUASAR_ROPE_HALF ? launch_prepare<ROPE_HALF>(a, p, st) : launch_prepare<ROPE_PAIRS>(a, p, st);
 }
 
 size_t quasar_paged_attention_workspace_bytes(int64_t max_new, int64_t n_q_heads, int64_t n_kv_heads) {
@@ -265,34 +383,19 @@ int quasar_paged_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n_
                            int64_t n_seqs, int64_t max_new, const void *pages, int64_t n_pages, int64_t page_len, int kv_dtype,
                            const float *k_scale, const float *v_scale, const int32_t *table, int64_t table_ld, int64_t max_pages,
                            const int32_t *lengths, uint16_t *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *hip_stream) {
-    if (!q || !out) return QUASAR_ERR_NULL;
-    PagedParams c{};
     const CacheArgs a{T, n_q_heads, n_kv_heads, pages, n_pages, page_len, kv_dtype, k_scale, v_scale, table, table_ld, n_seqs, max_pages, lengths, row_start};
-    if (const int e = check_cache(a, c)) return e;
-    const int kv = kv_type(kv_dtype);
-    StepShape shape{};
-    if (!step_shape(max_new, n_q_heads, n_kv_heads, n_seqs, shape)) return QUASAR_ERR_SHAPE;
-    if (ldq < n_q_heads * kHeadDim || ldo < n_q_heads * kHeadDim || ldq % 8 || ldo % 4) return QUASAR_ERR_SHAPE;
-    if (!aligned(q, 16) || !aligned(out, 8)) return QUASAR_ERR_ALIGN;
-    if (!workspace || workspace_bytes < quasar_paged_attention_workspace_bytes(max_new, n_q_heads, n_kv_heads)) return QUASAR_ERR_WORKSPACE;
-    if (!aligned(workspace, 16)) return QUASAR_ERR_ALIGN;
-    c.max_new = (int)max_new;
-    hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (shape.NQT) {
-        PagedAttnParams p{};
-        p.c = c;
-        p.q = q; p.out = out; p.ldq = ldq; p.ldo = ldo;
-        p.scale_log2 = kScaleLog2;
-        lay_out(p, shape.flat, workspace);
-        return kv == KV_BF16 ? launch_step<KV_BF16>(p, shape.NQT, st) : launch_step<KV_E4M3>(p, shape.NQT, st);
-    }
-    PromptParams p{};
-    p.c = c;
-    p.q = q; p.out = out; p.ldq = ldq; p.ldo = ldo;
-    p.scale_log2 = kScaleLog2;
-    p.whole_more = -(1 << 30);                                                   // (a step's tiles are shared always: minus more than any share)
-    if (shape.flat.workers) lay_out(p, shape.flat, workspace);
-    return kv == KV_BF16 ? launch_prompt<KV_BF16>(p, shape.flat.tiles, shape.PW, st) : launch_prompt<KV_E4M3>(p, shape.flat.tiles, shape.PW, st);
+    return step_attention(a, {q, ldq, out, ldo, workspace, workspace_bytes, hip_stream}, max_new, nullptr);
+}
+
+int quasar_paged_attention_window(const uint16_t *q, int64_t T, int64_t ldq, int64_t n_q_heads, int64_t n_kv_heads, const int32_t *row_start,
+                                  int64_t n_seqs, int64_t max_new, const void *pages, int64_t n_pages, int64_t page_len, int kv_dtype,
+                                  const float *k_scale, const float *v_scale, const int32_t *table, int64_t table_ld, int64_t max_pages,
+                                  const int32_t *lengths, int64_t window, int64_t sinks, uint16_t *out, int64_t ldo, void *workspace,
+                                  size_t workspace_bytes, void *hip_stream) {
+    const CacheArgs a{T, n_q_heads, n_kv_heads, pages, n_pages, page_len, kv_dtype, k_scale, v_scale, table, table_ld, n_seqs, max_pages, lengths, row_start};
+    Window w{};
+    if (!window_of(window, sinks, w)) return QUASAR_ERR_SHAPE;
+    return step_attention(a, {q, ldq, out, ldo, workspace, workspace_bytes, hip_stream}, max_new, &w);
 }
 
 size_t quasar_prompt_attention_workspace_bytes(int64_t T, int64_t n_q_heads, int64_t n_kv_heads, int64_t n_seqs) {
@@ -304,22 +407,19 @@ int quasar_prompt_attention(const uint16_t *q, int64_t T, int64_t ldq, int64_t n
                             int64_t n_seqs, const void *pages, int64_t n_pages, int64_t page_len, int kv_dtype, const float *k_scale,
                             const float *v_scale, const int32_t *table, int64_t table_ld, int64_t max_pages, const int32_t *lengths,
                             uint16_t *out, int64_t ldo, void *workspace, size_t workspace_bytes, void *hip_stream) {
-    if (!q || !out) return QUASAR_ERR_NULL;
-    PromptParams p{};
     const CacheArgs a{T, n_q_heads, n_kv_heads, pages, n_pages, page_len, kv_dtype, k_scale, v_scale, table, table_ld, n_seqs, max_pages, lengths, row_start};
-    if (const int e = check_cache(a, p.c)) return e;
-    if (T * (n_q_heads / n_kv_heads) > (1 << 26)) return QUASAR_ERR_SHAPE;       // (the tiles of all sequences are counted in 32 bits)
-    if (ldq < n_q_heads * kHeadDim || ldo < n_q_heads * kHeadDim || ldq % 8 || ldo % 4) return QUASAR_ERR_SHAPE;
-    if (!aligned(q, 16) || !aligned(out, 8) || !aligned(workspace, 16)) return QUASAR_ERR_ALIGN;
-    p.q = q; p.out = out; p.ldq = ldq; p.ldo = ldo;
-    p.scale_log2 = kScaleLog2;
-    const FlatShape shape = prompt_shape(T, n_q_heads, n_kv_heads, n_seqs);
-    p.whole_more = whole_more(T, n_q_heads / n_kv_heads);
-    // (a table so short that tiles stay whole whatever the lengths are: launched without the join)
-    const bool may_share = max_pages * page_len > (int64_t)kPromptStep * (kFlatLeast + p.whole_more);
-    if (workspace && shape.workers && workspace_bytes >= shape.bytes() && may_share) lay_out(p, shape, workspace);
-    hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    return kv_type(kv_dtype) == KV_BF16 ? launch_prompt<KV_BF16>(p, shape.tiles, 1, st) : launch_prompt<KV_E4M3>(p, shape.tiles, 1, st);
+    return prompts_attention(a, {q, ldq, out, ldo, workspace, workspace_bytes, hip_stream}, nullptr);
+}
+
+int quasar_prompt_attention_window(const uint16_t *q, int64_t T, int64_t ldq, int64_t n_q_heads, int64_t n_kv_heads, const int32_t *row_start,
+                                   int64_t n_seqs, const void *pages, int64_t n_pages, int64_t page_len, int kv_dtype, const float *k_scale,
+                                   const float *v_scale, const int32_t *table, int64_t table_ld, int64_t max_pages, const int32_t *lengths,
+                                   int64_t window, int64_t sinks, uint16_t *out, int64_t ldo, void *workspace, size_t workspace_bytes,
+                                   void *hip_stream) {
+    const CacheArgs a{T, n_q_heads, n_kv_heads, pages, n_pages, page_len, kv_dtype, k_scale, v_scale, table, table_ld, n_seqs, max_pages, lengths, row_start};
+    Window w{};
+    if (!window_of(window, sinks, w)) return QUASAR_ERR_SHAPE;
+    return prompts_attention(a, {q, ldq, out, ldo, workspace, workspace_bytes, hip_stream}, &w);
 }
 
 size_t quasar_pages_workspace_bytes(int64_t n_seqs, int64_t n_pages) {
@@ -359,6 +459,19 @@ int quasar_pages_fork(int32_t *table, int64_t table_ld, int64_t n_seqs, int64_t 
                        (unsigned int)(n_seqs * kForkColumns * 4), st, b, parent, keep);
     if (const int e = launched()) return e;
     hipLaunchKernelGGL(pages_fork_lengths_kernel, dim3(1), dim3(1024), 0, st, b, parent, keep);
+    return launched();
+}
+
+int quasar_pages_trim(int32_t *table, int64_t table_ld, int64_t n_seqs, int64_t max_pages, const int32_t *lengths, int64_t window, int64_t sinks,
+                      int32_t *refs, int64_t n_pages, int64_t page_len, void *hip_stream) {
+    if (!table || !lengths || !refs) return QUASAR_ERR_NULL;
+    Window w{};
+    if (!window_of(window, sinks, w)) return QUASAR_ERR_SHAPE;
+    if (const int e = check_books(table_ld, n_seqs, max_pages, n_pages, page_len)) return e;
+    if (!aligned(table, 4) || !aligned(lengths, 4) || !aligned(refs, 4)) return QUASAR_ERR_ALIGN;
+    const BooksParams b = books(table, table_ld, n_seqs, max_pages, const_cast<int32_t *>(lengths), refs, n_pages, page_len);
+    const unsigned int parts = (unsigned int)((max_pages + kTrimColumns - 1) / kTrimColumns);
+    hipLaunchKernelGGL(pages_trim_kernel, dim3((unsigned int)n_seqs, parts < 64 ? parts : 64), dim3(256), 0, static_cast<hipStream_t>(hip_stream), b, w);
     return launched();
 }
 

@@ -31,12 +31,15 @@ struct PagedAttnParams {
     int *pieces;              // [workers][4]: sequence that begins here and goes on (-1: none), last worker, slot
     int workers;
     float scale_log2;         // log2(e) / sqrt(128)
+    Window window;            // WINDOW
 };
 
 constexpr int kPagedWaves = 4;
 constexpr int kMaxWorkers = 512;             // of a kv head
 
-template <int KV, int NQT>
+// WINDOW: a sequence's blocks are those that its rows see some position of; those between the first tokens and the window have no place in
+// the line, whatever the context's length.
+template <int KV, int NQT, bool WINDOW>
 __global__ __launch_bounds__(kPagedWaves * 64, NQT == 1 ? 2 : 1) void paged_attention_kernel(const PagedAttnParams p) {
     constexpr int NW = kPagedWaves, BB = kv_block_bytes<KV>, NL = BB / 1024;     // 16-byte loads of a lane per block
     extern __shared__ __align__(16) unsigned char lds[];
@@ -54,7 +57,9 @@ __global__ __launch_bounds__(kPagedWaves * 64, NQT == 1 ? 2 : 1) void paged_atte
     const int total = prefix_sums<NW>(c.n_seqs, prefix, wave_sums, [&](int s) {
         const SeqSpan a = seq_span(c, s);
         spans[s] = a;
-        return a.n ? blocks_of(c, a.len + a.n) : 0;
+        const int blocks = a.n ? blocks_of(c, a.len + a.n) : 0;
+        if constexpr (WINDOW) return window_units(p.window, a.len, blocks, kBlockShift).count;
+        return blocks;
     });
     if (tid == 0) prefix[c.n_seqs] = total;
     __syncthreads();
@@ -84,6 +89,12 @@ __global__ __launch_bounds__(kPagedWaves * 64, NQT == 1 ? 2 : 1) void paged_atte
         const int n = a.n, R = n * c.G;
         const int b0 = f - s_begin, b1 = (s_end < f_end ? s_end : f_end) - s_begin;
         const int32_t *pages_of = c.table + s * c.table_ld;
+        WindowUnits units{};
+        if constexpr (WINDOW) units = window_units(p.window, a.len, blocks_of(c, a.len + n), kBlockShift);
+        auto block_at = [&](int i) {          // the i-th of the sequence's blocks
+            if constexpr (WINDOW) return units.at(i);
+            return i;
+        };
 
         // queries as B operands: lane (query column col, k group g4) holds d = 32 ks + 8 g4 .. + 7
         bf16x8 qb[NQT][4];
@@ -132,7 +143,8 @@ __global__ __launch_bounds__(kPagedWaves * 64, NQT == 1 ? 2 : 1) void paged_atte
         // `there`: the table names a page of the cache for the block; else its positions count as hidden
         auto process = [&](int b, bool there) {
             const int pos0 = b * kKvBlock, end = there ? a.len + n : 0;
-            const bool edge = pos0 + kKvBlock - 1 > a.len || !there;   // some position may be hidden from some query
+            bool edge = pos0 + kKvBlock - 1 > a.len || !there;         // some position may be hidden from some query
+            if constexpr (WINDOW) edge |= pos0 <= a.len + n - 1 - p.window.size && pos0 + kKvBlock > p.window.sinks;
             unsigned int keep[4] = {~0u, ~0u, ~0u, ~0u};
             if (edge) {
                 // positions behind the sequence hold whatever the page held: values there must not reach the product (0 x NaN)
@@ -140,6 +152,14 @@ __global__ __launch_bounds__(kPagedWaves * 64, NQT == 1 ? 2 : 1) void paged_atte
                 for (int j = 0; j < 4; ++j) {
                     const int oa = pos0 + 4 * g4 + (j & 1) * 2 + (j >> 1) * 16;
                     keep[j] = (oa < end ? 0x0000FFFFu : 0u) | (oa + 1 < end ? 0xFFFF0000u : 0u);
+                }
+                if constexpr (WINDOW) {                        // (nor values that the first row's window has passed)
+                    const unsigned int seen = seen_of_block(p.window, a.len, pos0) | ~bits_through(a.len - pos0);
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const unsigned int pair = seen >> (4 * g4 + (j & 1) * 2 + (j >> 1) * 16);
+                        keep[j] &= (pair & 1u ? 0x0000FFFFu : 0u) | (pair & 2u ? 0xFFFF0000u : 0u);
+                    }
                 }
             }
             f32x4 sc[NQT][2];
@@ -155,12 +175,16 @@ __global__ __launch_bounds__(kPagedWaves * 64, NQT == 1 ? 2 : 1) void paged_atte
                 }
             if (edge) {
 #pragma unroll
-                for (int qt = 0; qt < NQT; ++qt)
+                for (int qt = 0; qt < NQT; ++qt) {
+                    unsigned int seen = 0;
+                    if constexpr (WINDOW) seen = there ? seen_of_block(p.window, limit[qt], pos0) >> (4 * g4) : 0u;
 #pragma unroll
                     for (int sub = 0; sub < 2; ++sub)
 #pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (pos0 + 16 * sub + 4 * g4 + i > limit[qt] || !there) sc[qt][sub][i] = -__builtin_inff();
+                        for (int i = 0; i < 4; ++i) {
+                            if (WINDOW ? !(seen & 1u << (16 * sub + i)) : pos0 + 16 * sub + 4 * g4 + i > limit[qt] || !there) sc[qt][sub][i] = -__builtin_inff();
+                        }
+                }
             }
             u32x4 pb16[NQT];
             bool moved = false;
@@ -202,10 +226,17 @@ __global__ __launch_bounds__(kPagedWaves * 64, NQT == 1 ? 2 : 1) void paged_atte
                     v.z &= keep[2];
                     v.w &= keep[3];
                     if (n > 1 && any_nonfinite<KV>(v)) {
-                        const int first = drop_nonfinite<KV>(v, pos0 + 4 * g4);
+                        if constexpr (WINDOW) {
+                            const unsigned int bad = drop_nonfinite_of_block<KV>(v, 4 * g4);
 #pragma unroll
-                        for (int qt = 0; qt < NQT; ++qt)
-                            if (limit[qt] >= first) lrow[qt] = __builtin_nanf("");
+                            for (int qt = 0; qt < NQT; ++qt)
+                                if (bad & seen_of_block(p.window, limit[qt], pos0)) lrow[qt] = __builtin_nanf("");
+                        } else {
+                            const int first = drop_nonfinite<KV>(v, pos0 + 4 * g4);
+#pragma unroll
+                            for (int qt = 0; qt < NQT; ++qt)
+                                if (limit[qt] >= first) lrow[qt] = __builtin_nanf("");
+                        }
                     }
                 }
 #pragma unroll
@@ -217,23 +248,23 @@ __global__ __launch_bounds__(kPagedWaves * 64, NQT == 1 ? 2 : 1) void paged_atte
         for (int bs = b0 + w; bs < b1; bs += 64 * NW) {
             const int ahead = bs + NW * lane;
             int id = -1;
-            if (ahead < b1) id = pages_of[ahead >> c.block_shift];
+            if (ahead < b1) id = pages_of[block_at(ahead) >> c.block_shift];
             const int cnt = min(64, (b1 - bs + NW - 1) / NW);
             auto page_at = [&](int i) { return __builtin_amdgcn_readlane(id, i); };
             auto good = [&](int page) { return page_exists(page, c.n_pages); };
             // one block of prefetch, the last block of a wave without one: the number of loads in flight is known at every use
             int page = page_at(0);
-            load_block(bs, good(page) ? page : 0, kc, vc);
+            load_block(block_at(bs), good(page) ? page : 0, kc, vc);
             for (int i = 0; i + 1 < cnt; ++i) {
                 u32x4 kn[NL], vn[NL];
                 const int next = page_at(i + 1), b = bs + NW * i;
-                load_block(b + NW, good(next) ? next : 0, kn, vn);
-                process(b, good(page));
+                load_block(block_at(b + NW), good(next) ? next : 0, kn, vn);
+                process(block_at(b), good(page));
 #pragma unroll
                 for (int l = 0; l < NL; ++l) { kc[l] = kn[l]; vc[l] = vn[l]; }
                 page = next;
             }
-            process(bs + NW * (cnt - 1), good(page));
+            process(block_at(bs + NW * (cnt - 1)), good(page));
         }
         // the four lanes of a query column hold partial row sums; the maxima go on in log2 units
 #pragma unroll

@@ -205,6 +205,34 @@ __global__ __launch_bounds__(1024) void pages_fork_lengths_kernel(const BooksPar
 }
 
 // ---------------------------------------------------------------------------------------------
+// Gives pages back that no row to come sees anything of: those behind the first tokens and ahead of the window of the next token.  A sequence's columns
+// in stretches of kTrimColumns, four of them requested at a time.
+// ---------------------------------------------------------------------------------------------
+constexpr int kTrimColumns = 1024;
+
+__global__ __launch_bounds__(256) void pages_trim_kernel(const BooksParams b, const Window window) {
+    const int s = blockIdx.x, len = b.lengths[s];
+    if (len < 0 || len > kMaxPositions) return;
+    const Columns gone = columns_behind(window, len, b.block_shift + kBlockShift);
+    const int end = min(gone.end, b.columns);
+    int32_t *row = b.table + s * b.table_ld;
+    for (long long c0 = gone.begin + (long long)blockIdx.y * kTrimColumns; c0 < end; c0 += (long long)gridDim.y * kTrimColumns) {
+        int id[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int col = (int)c0 + 256 * i + threadIdx.x;
+            id[i] = col < end ? row[col] : -1;
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if (id[i] < 0) continue;
+            row[(int)c0 + 256 * i + threadIdx.x] = -1;
+            if (is_page(b, id[i])) atomicSub(&b.refs[id[i]], 1);
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
 // Compaction: with n pages in use, the i-th of those at n and beyond goes to the i-th free page below n.  One workgroup finds the
 // pairs; tables and pages follow in a launch that fills the card.  holes, moved: [n_pages] of the workspace each.
 // ---------------------------------------------------------------------------------------------

@@ -38,8 +38,10 @@ struct PromptParams {
     int workers;              // of a kv head
     int whole_more;           // steps that the longest tile may have beyond a worker's share while tiles stay whole
     float scale_log2;         // log2(e) / sqrt(128)
+    Window window;            // WINDOW
 };
 
+constexpr int kPromptStep = 64, kStepShift = 6;          // positions in LDS at a time
 constexpr int kPromptWaves = 4;                          // of a workgroup, two workgroups a compute unit
 // Steps of a worker at least, where steps are shared: with fewer, what the join reads costs more than the worker saves (8 tokens over up to 8000
 // positions, 64 / 8 heads, 20.5 us; two steps 24.1, three 22.7; over up to 1000, 8-bit, 15.6, 14.5 and 14.8).
@@ -50,9 +52,17 @@ constexpr int kMaxFlatTiles = 2048;                      // of a launch that sha
 struct PromptTile {
     int s, tile0, R, first_pos, last_pos, steps;
     SeqSpan a;
+    TileUnits units;          // WINDOW: which steps they are
 };
 
-__device__ __forceinline__ PromptTile prompt_tile(const PagedParams &c, int rows, int s, const SeqSpan &a, int tile0) {
+// What the search of a tile needs: WINDOW or not, at compile time.
+template <bool WINDOW> struct TileView {
+    const PagedParams &c;
+    Window window;
+};
+template <bool WINDOW>
+__device__ __forceinline__ PromptTile prompt_tile(const TileView<WINDOW> &view, int rows, int s, const SeqSpan &a, int tile0) {
+    const PagedParams &c = view.c;
     PromptTile t;
     t.s = s;
     t.a = a;
@@ -61,19 +71,24 @@ __device__ __forceinline__ PromptTile prompt_tile(const PagedParams &c, int rows
     t.first_pos = a.len + tile0 / c.G;                           // positions up to here are visible to every row of the tile
     t.last_pos = a.len + (min(tile0 + rows, t.R) - 1) / c.G;
     t.steps = (blocks_of(c, t.last_pos + 1) + 1) / 2;
+    if constexpr (WINDOW) {
+        t.units = tile_units(view.window, t.first_pos, t.last_pos, t.steps, kStepShift);
+        t.steps = t.units.u.count;
+    }
     return t;
 }
 
 // Tile f of the line of all sequences' tiles.  UNIFORM: f is the same for the wave, and so is what it finds (LDS does not say so).
-template <int ROWS, bool UNIFORM>
-__device__ __forceinline__ PromptTile tile_of_line(const PagedParams &c, const int *prefix, int f) {
+template <int ROWS, bool UNIFORM, bool WINDOW>
+__device__ __forceinline__ PromptTile tile_of_line(const TileView<WINDOW> &view, const int *prefix, int f) {
+    const PagedParams &c = view.c;
     int s = 0, up = c.n_seqs;
     while (up - s > 1) {
         const int mid = (s + up) >> 1;
         if (prefix[mid] <= f) s = mid; else up = mid;
     }
     if (UNIFORM) s = __builtin_amdgcn_readfirstlane(s);
-    return prompt_tile(c, ROWS, s, seq_span(c, s), (f - (UNIFORM ? __builtin_amdgcn_readfirstlane(prefix[s]) : prefix[s])) * ROWS);
+    return prompt_tile(view, ROWS, s, seq_span(c, s), (f - (UNIFORM ? __builtin_amdgcn_readfirstlane(prefix[s]) : prefix[s])) * ROWS);
 }
 
 // Tile `back` from the end of the line; R = 0: there are fewer.  Each wave for itself, a sequence a lane: no LDS, and nothing is read twice.  Of up to
@@ -81,8 +96,9 @@ __device__ __forceinline__ PromptTile tile_of_line(const PagedParams &c, const i
 // of sequences 111.8; 4 of up to 2048 85.4 and 90.2; 16 of up to 300 26.3 and 29.1.  Of more, finding the order costs what it gives: 60 of up to
 // 300 79.8 and 74.8, behind up to 2000 positions 308 and 324.
 constexpr int kSortedSeqs = 32;
-template <int ROWS>
-__device__ __forceinline__ PromptTile tile_from_end(const PagedParams &c, int back) {
+template <int ROWS, bool WINDOW>
+__device__ __forceinline__ PromptTile tile_from_end(const TileView<WINDOW> &view, int back) {
+    const PagedParams &c = view.c;
     constexpr int AT_ONCE = 4;
     const int lane = threadIdx.x & 63;
     auto tile_of = [&](const SeqSpan &a, int s, int &all, PromptTile &t) {       // of the sequences s of the lanes; all: their tiles
@@ -91,7 +107,7 @@ __device__ __forceinline__ PromptTile tile_from_end(const PagedParams &c, int ba
         if (back >= all) return false;
         const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(upto > back));
         const SeqSpan of = {__builtin_amdgcn_readlane(a.row0, l), __builtin_amdgcn_readlane(a.n, l), __builtin_amdgcn_readlane(a.len, l)};
-        t = prompt_tile(c, ROWS, __builtin_amdgcn_readlane(s, l), of, (__builtin_amdgcn_readlane(upto, l) - 1 - back) * ROWS);
+        t = prompt_tile(view, ROWS, __builtin_amdgcn_readlane(s, l), of, (__builtin_amdgcn_readlane(upto, l) - 1 - back) * ROWS);
         return true;
     };
     PromptTile t{};
@@ -127,7 +143,6 @@ __device__ __forceinline__ PromptTile tile_from_end(const PagedParams &c, int ba
     return t;
 }
 
-constexpr int kPromptStep = 64;                          // positions in LDS at a time
 constexpr int kPromptStepBytes = kPromptStep / kKvBlock * 2 * kKvBlockBytes;   // 32 KB: two blocks, keys and values
 
 // FLAT: the steps of all tiles as one line, in equal pieces for `workers` workgroups of a kv head (as the blocks of a step's sequences,
@@ -137,7 +152,9 @@ constexpr int kPromptStepBytes = kPromptStep / kKvBlock * 2 * kKvBlockBytes;   /
 // blocks, joined at the end: for up to 64 rows a sequence, where half of four times 32 would be nobody's.
 // 8-bit pages are widened on the way into LDS, once for all waves.  (In LDS as they are, four steps of half the size with three under way, and
 // widened by each wave that reads them, 2 x 8 tokens of 64 / 8 heads over 100003 positions take 75.7 us, and 76.6 so.)
-template <int KV, bool FLAT, int PW>
+// WINDOW: a tile's steps are those that its rows see some position of, the ones that every row sees whole first (the order is free), so that the two
+// loops over them are the same.
+template <int KV, bool FLAT, int PW, bool WINDOW>
 __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(const PromptParams p) {
     constexpr int NW = kPromptWaves, RW = NW / PW, ROWS = 32 * RW, NB = 2 / PW;  // row groups; blocks of a step for a wave
     constexpr bool DIRECT = KV == KV_BF16;                       // from memory into LDS
@@ -147,6 +164,7 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
     int *there = wave_sums + NW;                                 // [step & 3][block]: the block has a page
     int *line = there + 8;                                       // FLAT: steps ahead of a tile
     const PagedParams &c = p.c;
+    const TileView<WINDOW> view{c, p.window};
     const int tid = threadIdx.x, lane = tid & 63;
     const int w = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int rw = w % RW, pw = w / RW;
@@ -168,7 +186,7 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
         }));
         int longest = 0;                                         // steps of a tile, of those that this thread counts
         total = prefix_sums<NW>(tiles, line, wave_sums, [&](int f) {
-            const int n = tile_of_line<ROWS, false>(c, prefix, f).steps;
+            const int n = tile_of_line<ROWS, false>(view, prefix, f).steps;
             longest = max(longest, n);
             return n;
         });
@@ -192,7 +210,7 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
             at = tile < tiles ? __builtin_amdgcn_readfirstlane(line[tile]) : end;
         }
     } else {
-        pt = tile_from_end<ROWS>(c, worker);
+        pt = tile_from_end<ROWS>(view, worker);
     }
     auto next_tile = [&] {
         tile += shared ? 1 : p.workers;
@@ -200,10 +218,14 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
         return at < end;
     };
     for (bool more = FLAT ? at < end : pt.R > 0; more; more = FLAT && next_tile()) {
-    if constexpr (FLAT) pt = tile_of_line<ROWS, true>(c, prefix, tile);
+    if constexpr (FLAT) pt = tile_of_line<ROWS, true>(view, prefix, tile);
     const SeqSpan a = pt.a;
     const int R = pt.R, tile0 = pt.tile0, first_pos = pt.first_pos, last_pos = pt.last_pos, s = pt.s;
     const int nblk = blocks_of(c, last_pos + 1);
+    auto step_at = [&](int i) {                                  // the i-th of the tile's steps
+        if constexpr (WINDOW) return pt.units.at(i);
+        return i;
+    };
     int step0 = 0, steps = pt.steps;                             // the piece's part of the tile's steps
     if constexpr (FLAT) {
         step0 = at - __builtin_amdgcn_readfirstlane(line[tile]);
@@ -234,13 +256,13 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
     auto request = [&](int step) {
         if (step >= ids_at + 64 || ids_at < 0) {
             ids_at = step;
-            const int b = 2 * (step + lane) + my_blk;
+            const int b = 2 * step_at(step + lane) + my_blk;
             ids = b < nblk ? pages_of[b >> c.block_shift] : -1;
         }
         const int page = __builtin_amdgcn_readlane(ids, step - ids_at);
         const bool good = page_exists(page, c.n_pages);
         if (my_at == 0 && lane == 0) there[2 * (step & 3) + my_blk] = good;
-        const unsigned char *from = head + (good ? page : 0) * page_step + ((2 * step + my_blk) & in_page) * (2 * BB);
+        const unsigned char *from = head + (good ? page : 0) * page_step + ((2 * step_at(step) + my_blk) & in_page) * (2 * BB);
         if constexpr (DIRECT) {
             // (scalar registers, which the load takes; the compiler may have them in vector ones)
             const unsigned int to = __builtin_amdgcn_readfirstlane(lds_address_of(lds) + (step & 1) * kPromptStepBytes + w * PART);
@@ -285,7 +307,7 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
     auto attend = [&](auto edge, int step, bool there0, bool there1, auto between) {
         constexpr bool EDGE = decltype(edge)::value;
         const unsigned char *buf = lds + (step & 1) * kPromptStepBytes;
-        const int pos0 = step * kPromptStep;
+        const int pos0 = step_at(step) * kPromptStep;
         auto block = [&](int b) { return PW == 1 ? b : pw; };    // the wave's b-th block
         auto has_page = [&](int b) { return block(b) ? there1 : there0; };
         f32x16 sc[NB];
@@ -304,10 +326,17 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
 #pragma unroll
             for (int b = 0; b < NB; ++b) {
                 // register 4 (2 t + c) + b: position 16 c + 8 t + 4 hi + b
-                const int left = has_page(b) ? limit - pos0 - 32 * block(b) - 4 * hi : -1;
+                if constexpr (WINDOW) {
+                    const unsigned int seen = has_page(b) ? seen_of_block(p.window, limit, pos0 + 32 * block(b)) >> (4 * hi) : 0u;
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    if (16 * ((i >> 2) & 1) + 8 * (i >> 3) + (i & 3) > left) sc[b][i] = -__builtin_inff();
+                    for (int i = 0; i < 16; ++i)
+                        if (!(seen & 1u << (16 * ((i >> 2) & 1) + 8 * (i >> 3) + (i & 3)))) sc[b][i] = -__builtin_inff();
+                } else {
+                    const int left = has_page(b) ? limit - pos0 - 32 * block(b) - 4 * hi : -1;
+#pragma unroll
+                    for (int i = 0; i < 16; ++i)
+                        if (16 * ((i >> 2) & 1) + 8 * (i >> 3) + (i & 3) > left) sc[b][i] = -__builtin_inff();
+                }
             }
         }
         between();                                               // (dozens of scalar instructions: while the products are under way)
@@ -356,8 +385,13 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
                             va[j] &= (at <= end ? 0x0000FFFFu : 0u) | (at + 1 <= end ? 0xFFFF0000u : 0u);
                         }
                         if (any_nonfinite<KV>(va)) {
-                            const int first = drop_nonfinite<KV>(va, pos0 + 32 * block(b) + 4 * (2 * t + hi));
-                            if (limit >= first) lrow = __builtin_nanf("");
+                            if constexpr (WINDOW) {
+                                const unsigned int bad = drop_nonfinite_of_block<KV>(va, 4 * (2 * t + hi));
+                                if (bad & seen_of_block(p.window, limit, pos0 + 32 * block(b))) lrow = __builtin_nanf("");
+                            } else {
+                                const int first = drop_nonfinite<KV>(va, pos0 + 32 * block(b) + 4 * (2 * t + hi));
+                                if (limit >= first) lrow = __builtin_nanf("");
+                            }
                         }
                     }
                     oacc[dt] = values_times_weights<KV>(va, pb[b][t], oacc[dt]);
@@ -365,7 +399,7 @@ __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(
     };
     // The steps that every row sees whole, then the others (and all from the first that lacks a page on): two loops, since the outputs'
     // registers would be copied once a step where the two ways met.
-    const int whole = min((first_pos + 1) / kPromptStep, steps);
+    const int whole = min(WINDOW ? pt.units.whole : (first_pos + 1) / kPromptStep, steps);
     int step = step0;
     bool settled = false;
     auto arrive = [&] {
