@@ -642,6 +642,44 @@ int quasar_pages_compact(int32_t *table, int64_t table_ld, int64_t n_seqs, int64
                          void *workspace, size_t workspace_bytes, void *hip_stream);
 
 /*
+ * ---- Tokens from the logits of a batch's rows (Sec. 3.1: sampling of the verified distribution, the acceptance and resampling rules with a deterministic
+ * drafter; Sec. 3.3 "Lossless Rejection Sampling") ----
+ *
+ * logits: device [T, V], QUASAR_F32 or QUASAR_BF16, row stride ld >= V, or 0 for one row that stands for all, element-aligned; any V up to 2^20, T up to 2^20.  A logit that is not a
+ * number counts as minus infinity, plus infinity as the largest finite value.
+ * Filters: device arrays, of a row (quasar_sample_tokens, [T]) or of a sequence (quasar_verify_tokens, [n_seqs]); each may be NULL.  In this order, of the
+ * tokens by falling logit, equal ones by their place in the vocabulary:
+ *   temperature  fp32; weights exp((z - max z) / temperature).  Not above 0: the first token alone (the argmax, lowest index).        NULL: 1
+ *   top_k        int32; the first top_k tokens.  Below 1 or from V on: all.                                                         NULL: all
+ *   top_p        fp32; of these the first ones, until they hold top_p of their mass (the token that reaches it is the last, and the first one always
+ *                stays).  From 1 on: all.                                                                                           NULL: 1
+ *   min_p        fp32; of these the ones with at least min_p times the largest weight.  Not above 0: all; above 1 counts as 1.       NULL: 0
+ * Weights and sums are held in 64 bits; a token of less than 2^-46 of the largest weight is not drawn.  The draw is the inverse CDF in vocabulary order, as
+ * in quasar_lmhead_verify_sample: token = min{ v left : C(v) > u C(V - 1) }, u in [0, 1) (below 0 or not a number: as 0; from 1 on: the last).
+ *
+ * quasar_sample_tokens   a token of every row.  u: [T] fp32; out_token [T] int32; out_p [T] fp32 (may be NULL): the probability that it had.
+ *                        A row without a finite logit: token -1, probability 0.
+ * quasar_verify_tokens   rows row_start[s] .. row_start[s + 1] - 1 ([n_seqs + 1] int32, n_seqs <= 1024; bounded as those of the paged cache) are those of sequence s, in
+ *                        order: draft_ids[t] ([T] int32) is the token that was proposed behind row t, that of a sequence's last row counts for nothing.
+ *                        Candidate t is accepted iff u_accept[t] < p_t(draft_ids[t]) under the row's filtered distribution;
+ *     out_accept_len[s]  leading accepted candidates, at most rows - 1;
+ *     out_token[s]       drawn with u_sample[t] of the row t behind them: without its draft's mass (norm(max(0, p - q))) where that was refused,
+ *                        from the whole where the row is the last.  A sequence without rows, or whose row has nothing left: -1.
+ *     out_p_draft        [T] fp32 (may be NULL): p_t(draft_ids[t]); rows of no sequence are left as they were.  Ids outside [0, V) have probability 0.
+ * Results are determined by the arguments alone.  Two launches for every 512 rows, quasar_verify_tokens one more.  workspace: as many bytes as asked, 16-byte
+ * aligned, one call at a time.
+ */
+size_t quasar_sample_tokens_workspace_bytes(int64_t T, int64_t V);   /* 0 on invalid arguments */
+size_t quasar_verify_tokens_workspace_bytes(int64_t T, int64_t V);
+int quasar_sample_tokens(const void *logits, int logits_dtype, int64_t T, int64_t V, int64_t ld, const float *temperature, const int32_t *top_k,
+                         const float *top_p, const float *min_p, const float *u, int32_t *out_token, float *out_p, void *workspace,
+                         size_t workspace_bytes, void *hip_stream);
+int quasar_verify_tokens(const void *logits, int logits_dtype, int64_t T, int64_t V, int64_t ld, const int32_t *row_start, int64_t n_seqs,
+                         const int32_t *draft_ids, const float *temperature, const int32_t *top_k, const float *top_p, const float *min_p,
+                         const float *u_accept, const float *u_sample, int32_t *out_accept_len, int32_t *out_token, float *out_p_draft,
+                         void *workspace, size_t workspace_bytes, void *hip_stream);
+
+/*
  * ---- Prompt-lookup n-gram drafter (Sec. 2: drafts by n-gram matching against the context;
  * Sec. 4 "Implementation Details": lookup length adjusted dynamically between a minimum and a
  * maximum, 1 and 4 in the paper; Sec. 4.4: range (K_min, K_max), gamma speculative tokens) ----

@@ -43,6 +43,7 @@ EXPORTS = (
     "quasar_paged_cache_bytes", "quasar_paged_prepare", "quasar_paged_attention_workspace_bytes", "quasar_paged_attention",
     "quasar_prompt_attention_workspace_bytes", "quasar_prompt_attention", "quasar_pages_workspace_bytes", "quasar_pages_reserve", "quasar_pages_fork", "quasar_pages_compact",
     "quasar_paged_prepare_rope", "quasar_paged_attention_window", "quasar_prompt_attention_window", "quasar_pages_trim",
+    "quasar_sample_tokens_workspace_bytes", "quasar_sample_tokens", "quasar_verify_tokens_workspace_bytes", "quasar_verify_tokens",
 )
 
 
@@ -158,6 +159,11 @@ def _load() -> ctypes.CDLL:
     lib.quasar_paged_attention_window.argtypes = [vp, i64, i64, i64, i64, vp, i64, i64, *paged, i64, i64, vp, i64, vp, sz, vp]
     lib.quasar_prompt_attention_window.argtypes = [vp, i64, i64, i64, i64, vp, i64, *paged, i64, i64, vp, i64, vp, sz, vp]
     lib.quasar_pages_trim.argtypes = [vp, i64, i64, i64, vp, i64, i64, vp, i64, i64, vp]
+    for name in ("quasar_sample_tokens_workspace_bytes", "quasar_verify_tokens_workspace_bytes"):
+        getattr(lib, name).argtypes = [i64, i64]
+        getattr(lib, name).restype = sz
+    lib.quasar_sample_tokens.argtypes = [vp, ci, i64, i64, i64, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+    lib.quasar_verify_tokens.argtypes = [vp, ci, i64, i64, i64, vp, i64, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
     lib.quasar_drafter_create.argtypes = [ci, ci, i64]
     lib.quasar_drafter_create.restype = vp
     lib.quasar_drafter_destroy.argtypes = [vp]
@@ -206,7 +212,8 @@ _NATIVE_ENTRIES = ("quasar_w8_linear", "quasar_bf16_linear", "quasar_w8a8_linear
                    "quasar_w8_gateup_swiglu_split", "quasar_w8_fused_workspace_bytes", "quasar_w8_gateup_workspace_bytes",
                    "quasar_paged_prepare", "quasar_paged_attention", "quasar_paged_attention_workspace_bytes", "quasar_prompt_attention",
                    "quasar_prompt_attention_workspace_bytes", "quasar_pages_reserve", "quasar_pages_fork", "quasar_pages_compact",
-                   "quasar_paged_prepare_rope", "quasar_paged_attention_window", "quasar_prompt_attention_window", "quasar_pages_trim")
+                   "quasar_paged_prepare_rope", "quasar_paged_attention_window", "quasar_prompt_attention_window", "quasar_pages_trim",
+                   "quasar_sample_tokens", "quasar_sample_tokens_workspace_bytes", "quasar_verify_tokens", "quasar_verify_tokens_workspace_bytes")
 
 
 def _native_addresses(lib):
@@ -1006,6 +1013,82 @@ def prompt_attention(q: torch.Tensor, n_q_heads: int, cache: PagedKvCache, layer
         else:
             _check("quasar_prompt_attention_window", _lib.quasar_prompt_attention_window(*given, *seen, *to))
     return out
+
+
+def _vector(t, name, dtype, n, beside):
+    """A contiguous vector of n elements on the current device, its address."""
+    _dev(t, name, dtype)
+    if t.shape != (n,) or not t.is_contiguous():
+        raise ValueError(f"{name} must be a contiguous vector of {n} elements")
+    if t.device != beside.device:
+        raise ValueError(f"{name} and logits must be on the same device")
+    return t.data_ptr()
+
+
+def _logits_arg(logits):
+    _dev(logits, "logits")
+    code = {torch.float32: F32, torch.bfloat16: BF16}.get(logits.dtype)
+    if code is None:
+        raise TypeError("logits must be float32 or bfloat16")
+    if logits.dim() != 2 or logits.shape[1] < 1 or (logits.stride(1) != 1 and logits.shape[1] != 1):
+        raise ValueError("logits must be [rows, vocabulary] with a contiguous last dimension")
+    if logits.device.index != _current_device():
+        raise ValueError("logits must be on the current device")
+    T, V = logits.shape
+    return code, T, V, logits.stride(0) if T > 1 else V
+
+
+def _filter_args(n, logits, temperature, top_k, top_p, min_p):
+    return [None if t is None else _vector(t, name, dtype, n, logits)
+            for t, name, dtype in ((temperature, "temperature", torch.float32), (top_k, "top_k", torch.int32), (top_p, "top_p", torch.float32), (min_p, "min_p", torch.float32))]
+
+
+def sample_tokens(logits: torch.Tensor, u: torch.Tensor, *, temperature: torch.Tensor = None, top_k: torch.Tensor = None, top_p: torch.Tensor = None,
+                  min_p: torch.Tensor = None):
+    """A token of every row of logits [T, V] (fp32 or bf16), drawn with the numbers u [T] in [0, 1).
+    temperature, top_p, min_p [T] fp32, top_k [T] int32: each row's filters, in the order temperature, top_k, top_p, min_p (None: 1, all, all, all).
+    -> (tokens int32 [T], -1 of a row without a finite logit; the probabilities that they had, fp32 [T])."""
+    done = _fast.sample_tokens(logits, u, temperature, top_k, top_p, min_p)
+    if type(done) is not int or done > 0:
+        return _checked("quasar_sample_tokens", done)
+    code, T, V, ld = _logits_arg(logits)
+    filters = _filter_args(T, logits, temperature, top_k, top_p, min_p)
+    numbers = _vector(u, "u", torch.float32, T, logits)
+    token, p = (torch.empty(T, dtype=t, device=logits.device) for t in (torch.int32, torch.float32))
+    if T:
+        ws = torch.empty(_lib.quasar_sample_tokens_workspace_bytes(T, V), dtype=torch.uint8, device=logits.device)
+        _check("quasar_sample_tokens",
+               _lib.quasar_sample_tokens(logits.data_ptr(), code, T, V, ld, *filters, numbers, token.data_ptr(), p.data_ptr(), _ptr(ws), ws.nbytes, _stream()))
+    return token, p
+
+
+def verify_tokens(logits: torch.Tensor, row_start: torch.Tensor, draft_ids: torch.Tensor, u_accept: torch.Tensor, u_sample: torch.Tensor, *,
+                  temperature: torch.Tensor = None, top_k: torch.Tensor = None, top_p: torch.Tensor = None, min_p: torch.Tensor = None):
+    """Verifies the drafts of a batch: rows row_start[s] .. row_start[s + 1] - 1 of logits [T, V] are those of sequence s, draft_ids [T] int32 the token
+    that was proposed behind each (of a sequence's last row: none).  Candidates are accepted where u_accept [T] lies below their probability under the
+    filters of their sequence ([sequences], as in sample_tokens).
+    -> (accepted int32 [sequences], the next tokens int32 [sequences], the drafts' probabilities fp32 [T]): cache.lengths[:B] += accepted + 1."""
+    done = _fast.verify_tokens(logits, row_start, draft_ids, u_accept, u_sample, temperature, top_k, top_p, min_p)
+    if type(done) is not int or done > 0:
+        return _checked("quasar_verify_tokens", done)
+    code, T, V, ld = _logits_arg(logits)
+    _dev(row_start, "row_start", torch.int32)
+    if row_start.dim() != 1 or not 2 <= row_start.numel() <= 1025:
+        raise ValueError("row_start must be a vector of 2 .. 1025 elements")
+    seqs = row_start.numel() - 1
+    starts = _vector(row_start, "row_start", torch.int32, seqs + 1, logits)
+    draft = _vector(draft_ids, "draft_ids", torch.int32, T, logits)
+    ua, us = (_vector(t, name, torch.float32, T, logits) for t, name in ((u_accept, "u_accept"), (u_sample, "u_sample")))
+    filters = _filter_args(seqs, logits, temperature, top_k, top_p, min_p)
+    accepted, token = (torch.empty(seqs, dtype=torch.int32, device=logits.device) for _ in range(2))
+    p = torch.empty(T, dtype=torch.float32, device=logits.device)
+    if not T:
+        return accepted.zero_(), token.fill_(-1), p
+    ws = torch.empty(_lib.quasar_verify_tokens_workspace_bytes(T, V), dtype=torch.uint8, device=logits.device)
+    _check("quasar_verify_tokens",
+           _lib.quasar_verify_tokens(logits.data_ptr(), code, T, V, ld, starts, seqs, draft, *filters, ua, us, accepted.data_ptr(), token.data_ptr(), p.data_ptr(),
+                                     _ptr(ws), ws.nbytes, _stream()))
+    return accepted, token, p
 
 
 class Drafter:

@@ -12,8 +12,8 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libquasar.so")
 FAST = os.path.join(HERE, "_fastcall.so")
 SOURCES = ["quasar_api.hip", "direct_int8.hip", "direct_bf16.hip", "direct_w8a8.hip", "direct_w4.hip",
-           "outer_w8a8.hip", "outer_w4.hip", "paged_api.hip"]
-HEADERS = ["quasar_device.hpp", "launch.hpp", "shares.hpp", "stream_gemm.hpp", "stream_direct.hpp", "stream_direct_a8.hpp", "stream_direct_w4.hpp", "stream_outer.hpp", "norm.hpp", "stream_sequence.hpp", "stream_w8a8.hpp", "stream_w4.hpp", "drafter.hpp", "kv_layout.hpp", "books.hpp", "attention.hpp", "paged.hpp", "paged_attention.hpp", "prompt_attention.hpp", "pages.hpp", "sample.hpp", "draw.hpp", "pack.hpp", "probe.hpp", "unlocked.hpp"]
+           "outer_w8a8.hip", "outer_w4.hip", "paged_api.hip", "tokens_api.hip"]
+HEADERS = ["quasar_device.hpp", "launch.hpp", "shares.hpp", "stream_gemm.hpp", "stream_direct.hpp", "stream_direct_a8.hpp", "stream_direct_w4.hpp", "stream_outer.hpp", "norm.hpp", "stream_sequence.hpp", "stream_w8a8.hpp", "stream_w4.hpp", "drafter.hpp", "kv_layout.hpp", "books.hpp", "attention.hpp", "paged.hpp", "paged_attention.hpp", "prompt_attention.hpp", "pages.hpp", "sample.hpp", "draw.hpp", "token_math.hpp", "tokens.hpp", "pack.hpp", "probe.hpp", "unlocked.hpp"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",

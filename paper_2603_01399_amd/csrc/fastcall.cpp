@@ -51,6 +51,10 @@ decltype(&quasar_paged_prepare_rope) p_paged_prepare_rope;
 decltype(&quasar_paged_attention_window) p_paged_attention_window;
 decltype(&quasar_prompt_attention_window) p_prompt_attention_window;
 decltype(&quasar_pages_trim) p_pages_trim;
+decltype(&quasar_sample_tokens) p_sample_tokens;
+decltype(&quasar_sample_tokens_workspace_bytes) p_sample_tokens_workspace_bytes;
+decltype(&quasar_verify_tokens) p_verify_tokens;
+decltype(&quasar_verify_tokens_workspace_bytes) p_verify_tokens_workspace_bytes;
 PyObject *g_device, *g_stream;
 
 struct NotOrdinary {};
@@ -532,6 +536,102 @@ PyObject *pages_compact(PyObject *, PyObject *const *a, Py_ssize_t n) {
     });
 }
 
+// ---- tokens: calls that answer with a tuple of tensors, else with the status or -1
+
+template <size_t N, typename Body>
+PyObject *tensors_of(Py_ssize_t got, Py_ssize_t want, Body body) {
+    at::Tensor out[N];
+    long status = -1;
+    try {
+        if (got == want) status = body(out);
+        if (status == 0) {
+            PyObject *t = PyTuple_New(N);
+            for (size_t i = 0; t && i < N; ++i) {
+                PyObject *o = THPVariable_Wrap(std::move(out[i]));
+                if (!o) Py_CLEAR(t);
+                else PyTuple_SET_ITEM(t, i, o);
+            }
+            if (t) return t;
+            status = -1;
+        }
+    } catch (...) {
+        status = -1;
+    }
+    if (PyErr_Occurred()) PyErr_Clear();
+    return PyLong_FromLong(status);
+}
+// Logits of one row or more on the current device, and vectors beside them.
+struct Logits {
+    const at::Tensor &t;
+    int dtype, device;
+    explicit Logits(PyObject *o) : t(any_tensor(o)) {
+        if (!t.is_cuda() || t.dim() != 2 || t.size(0) < 1 || t.size(1) < 1 || t.stride(1) != 1) throw NotOrdinary{};
+        if (t.scalar_type() != at::kFloat && t.scalar_type() != at::kBFloat16) throw NotOrdinary{};
+        dtype = t.scalar_type() == at::kFloat ? QUASAR_F32 : QUASAR_BF16;
+        PyObject *dev = PyObject_CallNoArgs(g_device);
+        const long now = dev ? PyLong_AsLong(dev) : -1;
+        Py_XDECREF(dev);
+        device = t.device().index();
+        if (now != device) throw NotOrdinary{};
+    }
+    int64_t rows() const { return t.size(0); }
+    template <class T> const T *vector(PyObject *o, at::ScalarType type, int64_t n) const {
+        const at::Tensor &v = cuda_tensor(o, type);
+        if (v.device().index() != device || v.dim() != 1 || v.size(0) != n || !v.is_contiguous()) throw NotOrdinary{};
+        return static_cast<const T *>(v.data_ptr());
+    }
+    template <class T> const T *vector_or_none(PyObject *o, at::ScalarType type, int64_t n) const { return o == Py_None ? nullptr : vector<T>(o, type, n); }
+    at::Tensor fresh(int64_t n, at::ScalarType type) const {
+        return at::empty({n}, at::TensorOptions().dtype(type).device(at::kCUDA, static_cast<c10::DeviceIndex>(device)));
+    }
+};
+struct TokenFilters {
+    const float *temperature;
+    const int32_t *top_k;
+    const float *top_p, *min_p;
+    TokenFilters(const Logits &z, PyObject *const *a, int64_t n)
+        : temperature(z.vector_or_none<float>(a[0], at::kFloat, n)), top_k(z.vector_or_none<int32_t>(a[1], at::kInt, n)),
+          top_p(z.vector_or_none<float>(a[2], at::kFloat, n)), min_p(z.vector_or_none<float>(a[3], at::kFloat, n)) {}
+};
+
+// (logits, u, temperature, top_k, top_p, min_p) -> (token, p)
+PyObject *sample_tokens(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return tensors_of<2>(n, 6, [&](at::Tensor *out) {
+        const Logits z(a[0]);
+        const int64_t T = z.rows(), V = z.t.size(1);
+        const TokenFilters f(z, a + 2, T);
+        const float *u = z.vector<float>(a[1], at::kFloat, T);
+        const size_t bytes = p_sample_tokens_workspace_bytes(T, V);
+        if (!bytes) throw NotOrdinary{};
+        out[0] = z.fresh(T, at::kInt);
+        out[1] = z.fresh(T, at::kFloat);
+        const c10::DataPtr scratch = scratch_of(bytes);
+        return call(p_sample_tokens, static_cast<const void *>(z.t.data_ptr()), z.dtype, T, V, ld_of(z.t), f.temperature, f.top_k, f.top_p, f.min_p, u,
+                    static_cast<int32_t *>(out[0].data_ptr()), static_cast<float *>(out[1].data_ptr()), scratch.get(), bytes, current_stream());
+    });
+}
+
+// (logits, row_start, draft_ids, u_accept, u_sample, temperature, top_k, top_p, min_p) -> (accepted, token, p)
+PyObject *verify_tokens(PyObject *, PyObject *const *a, Py_ssize_t n) {
+    return tensors_of<3>(n, 9, [&](at::Tensor *out) {
+        const Logits z(a[0]);
+        const int64_t T = z.rows(), V = z.t.size(1), seqs = any_tensor(a[1]).numel() - 1;
+        if (seqs < 1 || seqs > 1024) throw NotOrdinary{};
+        const int32_t *starts = z.vector<int32_t>(a[1], at::kInt, seqs + 1), *draft = z.vector<int32_t>(a[2], at::kInt, T);
+        const float *ua = z.vector<float>(a[3], at::kFloat, T), *us = z.vector<float>(a[4], at::kFloat, T);
+        const TokenFilters f(z, a + 5, seqs);
+        const size_t bytes = p_verify_tokens_workspace_bytes(T, V);
+        if (!bytes) throw NotOrdinary{};
+        out[0] = z.fresh(seqs, at::kInt);
+        out[1] = z.fresh(seqs, at::kInt);
+        out[2] = z.fresh(T, at::kFloat);
+        const c10::DataPtr scratch = scratch_of(bytes);
+        return call(p_verify_tokens, static_cast<const void *>(z.t.data_ptr()), z.dtype, T, V, ld_of(z.t), starts, seqs, draft, f.temperature, f.top_k, f.top_p, f.min_p,
+                    ua, us, static_cast<int32_t *>(out[0].data_ptr()), static_cast<int32_t *>(out[1].data_ptr()), static_cast<float *>(out[2].data_ptr()),
+                    scratch.get(), bytes, current_stream());
+    });
+}
+
 // every entry point, in the order of binding.py's _NATIVE_ENTRIES
 template <typename Each> void each_entry(Each each) {
     each(p_w8_linear); each(p_bf16_linear); each(p_w8a8_linear); each(p_w4_linear); each(p_w4_packed_bytes); each(p_w8a8_workspace_bytes);
@@ -539,6 +639,7 @@ template <typename Each> void each_entry(Each each) {
     each(p_paged_prepare); each(p_paged_attention); each(p_paged_attention_workspace_bytes); each(p_prompt_attention); each(p_prompt_attention_workspace_bytes);
     each(p_pages_reserve); each(p_pages_fork); each(p_pages_compact);
     each(p_paged_prepare_rope); each(p_paged_attention_window); each(p_prompt_attention_window); each(p_pages_trim);
+    each(p_sample_tokens); each(p_sample_tokens_workspace_bytes); each(p_verify_tokens); each(p_verify_tokens_workspace_bytes);
 }
 Py_ssize_t entries() {
     Py_ssize_t n = 0;
@@ -583,7 +684,7 @@ PyObject *bound(PyObject *, PyObject *) {
 PyMethodDef methods[] = {FAST(w8_linear), FAST(bf16_linear), FAST(w8a8_linear), FAST(w4_linear),
                          FAST(w8_linear_fused), FAST(w8_gateup_swiglu),
                          FAST(paged_prepare), FAST(paged_attention), FAST(prompt_attention), FAST(pages_reserve), FAST(pages_fork), FAST(pages_compact),
-                         FAST(paged_prepare_rope), FAST(paged_attention_window), FAST(prompt_attention_window), FAST(pages_trim),
+                         FAST(paged_prepare_rope), FAST(paged_attention_window), FAST(prompt_attention_window), FAST(pages_trim), FAST(sample_tokens), FAST(verify_tokens),
                          {"paged_cache", paged_cache, METH_VARARGS, nullptr}, {"paged_cache_as_made", paged_cache_as_made, METH_O, nullptr},
                          {"bind", bind, METH_VARARGS, nullptr}, {"bound", bound, METH_NOARGS, nullptr}, {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_fastcall", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

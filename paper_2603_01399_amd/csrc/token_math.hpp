@@ -1,0 +1,126 @@
+// The arithmetic of drawing tokens from filtered logits (tokens.hpp): weights, the order that the filters go by, buckets.  Plain C++ for both sides: the
+// kernels run it on the GPU, the tests run the same functions on the CPU.
+//
+// Weights are exp((z - largest) / temperature) in 64 bits, taken as whole multiples of 2^-bits of a reference: sums are exact in any order, so
+// that atomics change no result, and what is drawn inside a part of the vocabulary is drawn from exactly the mass that was counted there.
+#pragma once
+
+#include <math.h>
+#include <stdint.h>
+#include <string.h>
+
+#include "draw.hpp"
+
+namespace quasar {
+
+typedef unsigned long long u64;
+
+constexpr int kBuckets = 512, kBucketsPerUnit = 16;          // of (largest - z) / temperature: the first 32 units; what lies behind weighs less than 2^-46
+constexpr int kPartBits = 48;                                // a part of the vocabulary has at most 2^13 tokens
+constexpr int kListBits = 42;                                // a whole vocabulary has at most 2^20
+constexpr int kIndexBits = 20;
+constexpr float kLargest = 3.4028234663852886e38f;
+
+// A logit as it counts: none for what is not a number, the largest finite value for infinity, one zero.
+QUASAR_BOTH float logit_value(float z) {
+    if (!(z == z)) return -__builtin_inff();
+    return (z < kLargest ? z : kLargest) + 0.0f;
+}
+
+// 2^f for |f| <= 1/2: its Taylor series up to the 12th power, whose rest is below 2^-52 of it.
+QUASAR_BOTH double exp2_of_fraction(double f) {
+    double r = 0x1.c3bd650fc2986p-36;                        // (ln 2)^k / k!
+    r = __builtin_fma(r, f, 0x1.e8cac7351bb25p-32);
+    r = __builtin_fma(r, f, 0x1.e4cf5158b8ecap-28);
+    r = __builtin_fma(r, f, 0x1.b5253d395e7c4p-24);
+    r = __builtin_fma(r, f, 0x1.62c0223a5c824p-20);
+    r = __builtin_fma(r, f, 0x1.ffcbfc588b0c7p-17);
+    r = __builtin_fma(r, f, 0x1.430912f86c787p-13);
+    r = __builtin_fma(r, f, 0x1.5d87fe78a6731p-10);
+    r = __builtin_fma(r, f, 0x1.3b2ab6fba4e77p-7);
+    r = __builtin_fma(r, f, 0x1.c6b08d704a0c0p-5);
+    r = __builtin_fma(r, f, 0x1.ebfbdff82c58fp-3);
+    r = __builtin_fma(r, f, 0x1.62e42fefa39efp-1);
+    return __builtin_fma(r, f, 1.0);
+}
+// exp((z - ref) / temperature) for z <= ref, 0 below 2^-60; rate: log2(e) / temperature.
+QUASAR_BOTH double weight_of(float z, float ref, double rate) {
+    const double y = ((double)z - (double)ref) * rate;
+    if (!(y > -60.0)) return y == y ? 0.0 : 1.0;             // (not a number: a rate of 0 and no distance, or both infinite)
+    const double n = __builtin_rint(y);
+    return __builtin_ldexp(exp2_of_fraction(y - n), (int)n);
+}
+// The same in whole multiples of 2^-bits, to nearest (bits <= 51).
+QUASAR_BOTH u64 weight_units(float z, float ref, double rate, int bits) {
+    const double y = ((double)z - (double)ref) * rate;
+    if (!(y > -60.0) || z == -__builtin_inff()) return 0;
+    const double n = __builtin_rint(y);
+    const double shifted = __builtin_ldexp(exp2_of_fraction(y - n), (int)n + bits) + 0x1p52;
+    u64 u;
+    memcpy(&u, &shifted, 8);
+    return u & ((1ull << 52) - 1);
+}
+
+// The order of the filters: larger logits first, equal ones by their place.  53 bits at most.
+QUASAR_BOTH uint32_t ordered_bits(float z) {                 // grows with z
+    uint32_t u;
+    memcpy(&u, &z, 4);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+QUASAR_BOTH float value_of_ordered(uint32_t u) {
+    u = u & 0x80000000u ? u & 0x7FFFFFFFu : ~u;
+    float z;
+    memcpy(&z, &u, 4);
+    return z;
+}
+QUASAR_BOTH u64 rank_key(float z, int v) { return (u64)(uint32_t)~ordered_bits(z) << kIndexBits | (u64)(uint32_t)v; }
+QUASAR_BOTH float key_value(u64 key) { return value_of_ordered(~(uint32_t)(key >> kIndexBits)); }
+QUASAR_BOTH int key_token(u64 key) { return (int)(key & ((1u << kIndexBits) - 1)); }
+
+// A logit's place on the line of buckets: whole, falls with z never, and the same for every part of a vocabulary.
+QUASAR_BOTH float bucket_line(float z, float scale) {
+    float x = z * scale;
+    x = x < kLargest ? x : kLargest;
+    return __builtin_floorf(x > -kLargest ? x : -kLargest);
+}
+// Bucket of a logit, 0 for those nearest the largest one (line_top: its place); kBuckets: beyond them all.
+QUASAR_BOTH int bucket_of(float z, float scale, float line_top) {
+    if (z == -__builtin_inff()) return kBuckets;
+    const float d = line_top - bucket_line(z, scale);
+    return d < (float)kBuckets ? (int)d : kBuckets;
+}
+
+// What a row's filters come to.
+struct Filters {
+    double rate;              // log2(e) / temperature
+    float scale;              // kBucketsPerUnit / temperature
+    int k;                    // 0: no limit
+    float p;                  // 1: no limit
+    float min_p;              // 0: no limit
+};
+QUASAR_BOTH Filters filters_of(float temperature, int top_k, float top_p, float min_p, int V) {
+    Filters f;
+    f.k = top_k > 0 && top_k < V ? top_k : 0;
+    f.p = top_p < 1.0f ? top_p : 1.0f;                       // (not a number: no limit)
+    f.min_p = min_p > 0x1p-50f ? (min_p < 1.0f ? min_p : 1.0f) : 0.0f;   // (what weighs less is beyond the buckets)
+    if (!(temperature > 0.0f)) temperature = 1.0f, f.k = 1;
+    if (f.p <= 0.0f) f.p = 1.0f, f.k = 1;                    // (the first is always left)
+    f.rate = 1.4426950408889634 / (double)temperature;
+    const float scale = (float)kBucketsPerUnit / temperature;
+    f.scale = scale < kLargest ? scale : kLargest;
+    return f;
+}
+// The smallest logit whose weight is at least min_p (> 0); most: the largest logit.
+QUASAR_BOTH float least_logit(float most, double rate, float min_p) {
+    const double at = (double)most + log2((double)min_p) / rate;
+    float z = at > -(double)kLargest ? (float)at : -kLargest;
+    for (int i = 0; i < 4 && z < most && weight_of(z, most, rate) < (double)min_p; ++i) z = value_of_ordered(ordered_bits(z) + 1);
+    for (int i = 0; i < 4 && z > -kLargest; ++i) {
+        const float below = value_of_ordered(ordered_bits(z) - 1);
+        if (weight_of(below, most, rate) < (double)min_p) break;
+        z = below;
+    }
+    return z < most ? z : most;
+}
+
+}  // namespace quasar
