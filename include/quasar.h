@@ -654,7 +654,7 @@ int quasar_pages_compact(int32_t *table, int64_t table_ld, int64_t n_seqs, int64
  *   top_p        fp32; of these the first ones, until they hold top_p of their mass (the token that reaches it is the last, and the first one always
  *                stays).  From 1 on: all.                                                                                           NULL: 1
  *   min_p        fp32; of these the ones with at least min_p times the largest weight.  Not above 0: all; above 1 counts as 1.       NULL: 0
- * Weights and sums are held in 64 bits; a token of less than 2^-46 of the largest weight is not drawn.  The draw is the inverse CDF in vocabulary order, as
+ * Weights and sums are held in 64 bits; a token of less than 2^-46 of the largest weight may be left out.  The draw is the inverse CDF in vocabulary order, as
  * in quasar_lmhead_verify_sample: token = min{ v left : C(v) > u C(V - 1) }, u in [0, 1) (below 0 or not a number: as 0; from 1 on: the last).
  *
  * quasar_sample_tokens   a token of every row.  u: [T] fp32; out_token [T] int32; out_p [T] fp32 (may be NULL): the probability that it had.

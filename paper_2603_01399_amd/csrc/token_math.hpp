@@ -77,17 +77,13 @@ QUASAR_BOTH u64 rank_key(float z, int v) { return (u64)(uint32_t)~ordered_bits(z
 QUASAR_BOTH float key_value(u64 key) { return value_of_ordered(~(uint32_t)(key >> kIndexBits)); }
 QUASAR_BOTH int key_token(u64 key) { return (int)(key & ((1u << kIndexBits) - 1)); }
 
-// A logit's place on the line of buckets: whole, falls with z never, and the same for every part of a vocabulary.
-QUASAR_BOTH float bucket_line(float z, float scale) {
-    float x = z * scale;
-    x = x < kLargest ? x : kLargest;
-    return __builtin_floorf(x > -kLargest ? x : -kLargest);
-}
-// Bucket of a logit, 0 for those nearest the largest one (line_top: its place); kBuckets: beyond them all.
+// A logit's place on the line of buckets: whole, falls with z never, and the same for every part of a vocabulary.  (fmax takes what is not a number,
+// -inf times a scale of 0, for the smallest.)
+QUASAR_BOTH float bucket_line(float z, float scale) { return __builtin_floorf(__builtin_fminf(__builtin_fmaxf(z * scale, -kLargest), kLargest)); }
+// Bucket of a logit, 0 for those nearest the largest one (line_top: its place, of a finite logit); kBuckets: beyond them all, as -inf is.
 QUASAR_BOTH int bucket_of(float z, float scale, float line_top) {
-    if (z == -__builtin_inff()) return kBuckets;
     const float d = line_top - bucket_line(z, scale);
-    return d < (float)kBuckets ? (int)d : kBuckets;
+    return z == -__builtin_inff() ? kBuckets : (int)__builtin_fminf(d, (float)kBuckets);
 }
 
 // What a row's filters come to.

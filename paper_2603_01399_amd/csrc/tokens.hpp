@@ -42,7 +42,7 @@ struct TokenParams {
 };
 
 template <int DT> constexpr int lane_tokens = DT == 1 ? 8 : 4;               // of a 16-byte load: bf16, fp32
-template <int DT> constexpr int chunk_tokens = 64 * lane_tokens<DT>;         // of a wave's load
+template <int DT> constexpr int chunk_tokens = 16 * lane_tokens<DT>;         // of sixteen lanes' load: whose largest logit is kept
 template <int DT> constexpr int part_chunks = kPartTokens / chunk_tokens<DT>;
 
 // Whose parameters a row goes by (-1: nobody's row), and whether it is the last of its sequence.
@@ -63,153 +63,308 @@ __device__ __forceinline__ Filters filters_at(const TokenParams &p, int who) {
     return filters_of(p.temperature ? p.temperature[who] : 1.0f, p.top_k ? p.top_k[who] : 0, p.top_p ? p.top_p[who] : 1.0f, p.min_p ? p.min_p[who] : 0.0f, p.V);
 }
 
-// A row whose first token may lie anywhere: places are counted from the 16-byte border ahead of it.
+// A row whose first token may lie anywhere: places are counted from the 16-byte border ahead of it, in units of 16 bytes.  Requests are made by every
+// lane, without a branch, so that many are under way together: a unit that is not whole, or not there, asks for the nearest whole one, and what it has is
+// read one by one where the request is used (two units of a row at most have some).
 template <int DT> struct LogitRow {
+    static constexpr int N = lane_tokens<DT>;
     const unsigned char *border;
-    int skew, V;
+    int skew, V, first, last;                                    // first and last whole unit; last < first: none
     __device__ LogitRow(const TokenParams &p, int row) : V(p.V) {
         constexpr int E = DT == 1 ? 2 : 4;
         const u64 at = reinterpret_cast<u64>(p.logits) + (u64)row * p.ld * E;
         border = reinterpret_cast<const unsigned char *>(at & ~15ull);
         skew = (int)(at & 15) / E;
+        first = skew ? 1 : 0;
+        last = (skew + V) / N - 1;
     }
     __device__ __forceinline__ float one(int v) const {
         if constexpr (DT == 1) return logit_value(bf16_bits_to_float(reinterpret_cast<const uint16_t *>(border)[skew + v]));
         else return logit_value(reinterpret_cast<const float *>(border)[skew + v]);
     }
-    // the tokens at places at .. (a whole load); -inf where there are none
-    __device__ __forceinline__ void load(int at, float (&x)[lane_tokens<DT>]) const {
-        constexpr int N = lane_tokens<DT>;
-        if (at >= skew && at + N <= skew + V) {
-            const u32x4 v = *reinterpret_cast<const u32x4 *>(border + 16ll * (at / N));
+    __device__ __forceinline__ u32x4 request(int unit) const {
+        if (last < first) return u32x4{0u, 0u, 0u, 0u};          // (the same for every lane)
+        return *reinterpret_cast<const u32x4 *>(border + 16ll * min(max(unit, first), last));
+    }
+    // the tokens of a requested unit, as they count (AS_THEY_ARE: not a number and infinities as such); -inf where there are none
+    template <bool AS_THEY_ARE = false>
+    __device__ __forceinline__ void values(int unit, const u32x4 v, float (&x)[N]) const {
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            const float z = DT == 1 ? __uint_as_float(e & 1 ? v[DT == 1 ? e >> 1 : 0] & 0xFFFF0000u : v[DT == 1 ? e >> 1 : 0] << 16) : __uint_as_float(v[e & 3]);
+            x[e] = AS_THEY_ARE ? z : logit_value(z);
+        }
+        if (unit < first || unit > last) {
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                if constexpr (DT == 1) x[e] = logit_value(__uint_as_float(e & 1 ? v[e >> 1] & 0xFFFF0000u : v[e >> 1] << 16));
-                else x[e] = logit_value(__uint_as_float(v[e]));
+                const int at = unit * N + e;
+                x[e] = at >= skew && at < skew + V ? one(at - skew) : -__builtin_inff();
             }
-        } else {
-#pragma unroll
-            for (int e = 0; e < N; ++e) x[e] = at + e >= skew && at + e < skew + V ? one(at + e - skew) : -__builtin_inff();
         }
     }
 };
 
-// the largest over the wave, in every lane
-__device__ __forceinline__ float wave_max(float v) {
-    auto step = [&](auto ctrl, auto mask) {
-        const int o = __builtin_amdgcn_update_dpp(__float_as_int(v), __float_as_int(v), decltype(ctrl)::value, decltype(mask)::value, 0xf, false);
-        v = fmaxf(v, __int_as_float(o));
-    };
-    step(std::integral_constant<int, 0x111>{}, std::integral_constant<int, 0xf>{});      // from 1, 2, 4 and 8 lanes before, within 16 lanes
-    step(std::integral_constant<int, 0x112>{}, std::integral_constant<int, 0xf>{});
-    step(std::integral_constant<int, 0x114>{}, std::integral_constant<int, 0xf>{});
-    step(std::integral_constant<int, 0x118>{}, std::integral_constant<int, 0xf>{});
-    step(std::integral_constant<int, 0x142>{}, std::integral_constant<int, 0xa>{});      // lane 15 to the 16 lanes behind it, lane 47 likewise
-    step(std::integral_constant<int, 0x143>{}, std::integral_constant<int, 0xc>{});      // lane 31 to the 32 lanes behind it
-    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+// v of the lanes up to each one combined by op, whose neutral value is `none`: within 16 lanes, then from their last lanes on.
+template <int CTRL, int ROWS, class N>
+__device__ __forceinline__ N from_lane(N v, N none) {
+    if constexpr (sizeof(N) == 4) {
+        return __builtin_bit_cast(N, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, v), CTRL, ROWS, 0xf, false));
+    } else {
+        const u32x2 x = __builtin_bit_cast(u32x2, v), o = __builtin_bit_cast(u32x2, none);
+        return __builtin_bit_cast(N, u32x2{(unsigned int)__builtin_amdgcn_update_dpp((int)o.x, (int)x.x, CTRL, ROWS, 0xf, false),
+                                           (unsigned int)__builtin_amdgcn_update_dpp((int)o.y, (int)x.y, CTRL, ROWS, 0xf, false)});
+    }
+}
+template <bool ALL_LANES, class N, class Op>
+__device__ __forceinline__ N lanes_through(N v, N none, Op op) {
+    v = op(v, from_lane<0x111, 0xf>(v, none));
+    v = op(v, from_lane<0x112, 0xf>(v, none));
+    v = op(v, from_lane<0x114, 0xf>(v, none));
+    v = op(v, from_lane<0x118, 0xf>(v, none));
+    if constexpr (ALL_LANES) {
+        v = op(v, from_lane<0x142, 0xa>(v, none));
+        v = op(v, from_lane<0x143, 0xc>(v, none));
+    }
+    return v;
+}
+template <class N> __device__ __forceinline__ N lane_sums_through(N v) {
+    return lanes_through<true>(v, N(0), [](N a, N b) { return a + b; });
+}
+template <class N> __device__ __forceinline__ N of_lane(N v, int lane) {
+    if constexpr (sizeof(N) == 4) {
+        return __builtin_bit_cast(N, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), lane));
+    } else {
+        const u32x2 x = __builtin_bit_cast(u32x2, v);
+        return __builtin_bit_cast(N, u32x2{(unsigned int)__builtin_amdgcn_readlane((int)x.x, lane), (unsigned int)__builtin_amdgcn_readlane((int)x.y, lane)});
+    }
+}
+__device__ __forceinline__ float wave_max(float v) {             // in every lane
+    return of_lane(lanes_through<true>(v, -__builtin_inff(), [](float a, float b) { return fmaxf(a, b); }), 63);
+}
+template <class N> __device__ __forceinline__ N wave_sum(N v) { return of_lane(lane_sums_through(v), 63); }
+
+// How a row is drawn.  ALL: nothing is filtered.  FEW: top-k of at most kFew, so that all that is left can be gathered.  MANY: a cut anywhere.
+enum { DRAW_ALL = 0, DRAW_FEW = 1, DRAW_MANY = 2 };
+constexpr int kFew = 2048;
+__device__ __forceinline__ int draw_mode(const Filters &f) {
+    if (f.k && f.k <= kFew) return DRAW_FEW;
+    return f.k || f.p < 1.0f || f.min_p > 0.0f ? DRAW_MANY : DRAW_ALL;
 }
 
-// Grid (parts, rows).  A part's 16 tokens a thread stay in registers between its largest logit and the buckets.
+// Grid (parts, rows).  A part's 16 tokens a thread stay in registers between its largest logit and the buckets.  What the row asks for is counted and nothing
+// else: the whole part's mass (ALL), counts (FEW), masses, and counts where there is a top-k (MANY).  The buckets lie four times in LDS, for the lanes 4 i + c each: a
+// wave's tokens share some dozens of buckets, and what meets in one is added one after the other.
+constexpr int kCopies = 4;
 template <int DT>
 __global__ __launch_bounds__(kPartThreads) void token_parts_kernel(const TokenParams p) {
     constexpr int N = lane_tokens<DT>, LOADS = kPartLane / N, CHUNKS = part_chunks<DT>;
-    __shared__ u64 mass[kBuckets];
-    __shared__ unsigned int count[kBuckets];
+    __shared__ u64 mass[kBuckets * kCopies];
+    __shared__ unsigned int count[kBuckets * kCopies];
     __shared__ float wave_largest[kPartWaves];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), b = blockIdx.x, r = blockIdx.y;
     const LogitRow<DT> row(p, p.row0 + r);
-    float x[LOADS][N];
+    u32x4 raw[LOADS];
+    auto unit = [&](int i) { return b * (kPartTokens / N) + (w * LOADS + i) * 64 + lane; };
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) row.load(b * kPartTokens + (w * LOADS + i) * chunk_tokens<DT> + lane * N, x[i]);
+    for (int i = 0; i < LOADS; ++i) raw[i] = row.request(unit(i));
     const RowOf of = row_of(p, p.row0 + r);
     if (of.who < 0) return;
     const Filters f = filters_at(p, of.who);
-    for (int i = tid; i < kBuckets; i += kPartThreads) mass[i] = 0, count[i] = 0;
+    float x[LOADS][N];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) row.values(unit(i), raw[i], x[i]);
+    const int mode = draw_mode(f);
+    const bool counts = f.k != 0, masses = mode == DRAW_MANY;
+    if (masses)
+        for (int i = tid; i < kBuckets * kCopies; i += kPartThreads) mass[i] = 0;
+    if (counts)
+        for (int i = tid; i < kBuckets * kCopies; i += kPartThreads) count[i] = 0;
     float largest = -__builtin_inff();
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
         float m = x[i][0];
 #pragma unroll
         for (int e = 1; e < N; ++e) m = fmaxf(m, x[i][e]);
-        m = wave_max(m);
-        if (lane == 0) p.chunk_max[((long long)r * p.nb + b) * CHUNKS + w * LOADS + i] = m;
+        m = lanes_through<false>(m, -__builtin_inff(), [](float a, float b) { return fmaxf(a, b); });
+        if ((lane & 15) == 15) p.chunk_max[((long long)r * p.nb + b) * CHUNKS + (w * LOADS + i) * 4 + (lane >> 4)] = m;
         largest = fmaxf(largest, m);
     }
+    largest = wave_max((lane & 15) == 15 ? largest : -__builtin_inff());
     if (lane == 0) wave_largest[w] = largest;
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kPartWaves; ++i) largest = fmaxf(largest, wave_largest[i]);
     if (tid == 0) p.part_max[(long long)r * p.nb + b] = largest;
     const float top = bucket_line(largest, f.scale);
+    const long long to = ((long long)r * p.nb + b) * kBuckets;
+    // (a token that min_p keeps from being left in its part cannot be left in the row; where top-p counts it for the whole all the same, it is taken)
+    int last = kBuckets - 1;
+    if (mode == DRAW_MANY && !counts && f.p >= 1.0f) last = min(last, (int)(-0.6931472f * kBucketsPerUnit * __log2f(f.min_p)) + 2);
+    u64 whole = 0;
     if (largest > -__builtin_inff()) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i)
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                const int at = bucket_of(x[i][e], f.scale, top);
-                if (at >= kBuckets) continue;
-                atomicAdd(&mass[at], weight_units(x[i][e], largest, f.rate, kPartBits));
-                if (f.k) atomicAdd(&count[at], 1u);
+                const int at = bucket_of(x[i][e], f.scale, top), place = at * kCopies + (lane & (kCopies - 1));
+                if (mode != DRAW_FEW && (mode == DRAW_ALL || at <= last)) {
+                    const u64 units = weight_units(x[i][e], largest, f.rate, kPartBits);
+                    if (mode == DRAW_ALL) whole += units;
+                    else atomicAdd(&mass[place], units);
+                }
+                if (counts && at <= last) atomicAdd(&count[place], 1u);
             }
     }
+    if (mode == DRAW_ALL) {
+        whole = wave_sum(whole);
+        if (lane == 0) mass[w] = whole;
+        __syncthreads();
+        if (tid == 0) {
+            for (int i = 1; i < kPartWaves; ++i) whole += mass[i];
+            p.mass[to] = whole;
+        }
+        return;
+    }
     __syncthreads();
-    const long long to = ((long long)r * p.nb + b) * kBuckets;
-    for (int i = tid; i < kBuckets; i += kPartThreads) {
-        p.mass[to + i] = mass[i];
-        if (f.k) p.count[to + i] = count[i];
+    static_assert(kBuckets == kPartThreads, "a bucket a thread");
+    if (masses) {
+        u64 sum = 0;
+#pragma unroll
+        for (int c = 0; c < kCopies; ++c) sum += mass[tid * kCopies + c];
+        p.mass[to + tid] = sum;
+    }
+    if (counts) {
+        unsigned int sum = 0;
+#pragma unroll
+        for (int c = 0; c < kCopies; ++c) sum += count[tid * kCopies + c];
+        p.count[to + tid] = sum;
     }
 }
 
-// Sum of v over the threads up to each one, of a workgroup of kDrawThreads; wave_sums: [kDrawWaves] of LDS.
-template <class N>
-__device__ __forceinline__ N sums_through(N v, N *wave_sums) {
-    const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-        const N up = __shfl_up(v, off, 64);
-        if (lane >= off) v += up;
+// What the waves of a workgroup tell each other: a value a wave, combined by every wave.  One barrier: the places are taken in turn, and a place comes again
+// only behind another's barrier.
+constexpr int kTurns = 4;
+struct WaveTalk {
+    u64 (*places)[kDrawWaves];                                   // [kTurns] of LDS
+    int turn;
+    template <class N> __device__ __forceinline__ N told(N v) {                  // lane i: what wave i % kDrawWaves has said
+        static_assert(kDrawWaves == 16, "sixteen lanes");
+        N *place = reinterpret_cast<N *>(places[turn]);
+        turn = (turn + 1) % kTurns;
+        if ((threadIdx.x & 63) == 0) place[threadIdx.x >> 6] = v;
+        __syncthreads();
+        return place[threadIdx.x & 15];
     }
-    __syncthreads();                                             // (wave_sums may still be read from the last call)
-    if (lane == 63) wave_sums[w] = v;
-    __syncthreads();
-    N before = 0;
-#pragma unroll
-    for (int i = 0; i < kDrawWaves; ++i) before += i < w ? wave_sums[i] : N(0);
-    return before + v;
+    template <class N, class Op> __device__ __forceinline__ N all(N v, N none, Op op) {        // v: the wave's
+        return of_lane(lanes_through<false>(told(v), none, op), 15);
+    }
+    // sum of v over the threads up to this one
+    template <class N> __device__ __forceinline__ N sum_through(N v) {
+        v = lane_sums_through(v);
+        const N other = told(of_lane(v, 63));
+        const bool ahead = (int)(threadIdx.x & 15) < __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+        return v + of_lane(lanes_through<false>(ahead ? other : N(0), N(0), [](N a, N b) { return a + b; }), 15);
+    }
+    template <class N> __device__ __forceinline__ N sum(N v) {
+        return all(wave_sum(v), N(0), [](N a, N b) { return a + b; });
+    }
+    // the first thread that a holds for (kDrawThreads: none), and the last that b holds for (-1).  (By ballots: what many threads add to one place in LDS is
+    // added one after the other, ten cycles each.)
+    __device__ __forceinline__ void ends(bool a, bool b, int &first, int &last) {
+        const unsigned long long as = __builtin_amdgcn_ballot_w64(a), bs = __builtin_amdgcn_ballot_w64(b);
+        const int w = threadIdx.x >> 6;
+        const unsigned int f = as ? kDrawThreads - (64 * w + __builtin_ctzll(as)) : 0, l = bs ? 64 * w + 64 - __builtin_clzll(bs) : 0;
+        const unsigned int r = all(f << 16 | l, 0u, [](unsigned int x, unsigned int y) {
+            return max(x & 0xFFFF0000u, y & 0xFFFF0000u) | max(x & 0xFFFFu, y & 0xFFFFu);
+        });
+        first = kDrawThreads - (int)(r >> 16);
+        last = (int)(r & 0xFFFFu) - 1;
+    }
+};
+
+// The smallest logit of buckets 0 .. j, found by the lanes of a wave side by side: around where the line says, else anywhere.  (Zero in the form that
+// orders ahead of the other.)
+__device__ __forceinline__ uint32_t least_ordered_of_bucket(int j, float scale, float top, float most) {
+    const int lane = threadIdx.x & 63;
+    const float place = top - (float)j;
+    const uint32_t least = ordered_bits(-kLargest), largest = ordered_bits(most);
+    auto holds = [&](uint32_t at) { return bucket_line(value_of_ordered(at), scale) >= place; };
+    const float guess = __builtin_fminf(__builtin_fmaxf(place / scale, -kLargest), most);
+    const long long around = (long long)ordered_bits(guess) - 32 + lane;
+    const uint32_t at = around < (long long)least ? least : around > (long long)largest ? largest : (uint32_t)around;
+    unsigned long long mask = __builtin_amdgcn_ballot_w64(holds(at));
+    uint32_t found;
+    if (mask && (!(mask & 1) || (uint32_t)of_lane((int)at, 0) == least)) {
+        found = (uint32_t)of_lane((int)at, __builtin_ctzll(mask));
+    } else {
+        uint32_t lo = least, hi = largest;                       // (it holds for the largest)
+        while (lo < hi) {
+            const uint32_t step = (hi - lo) / 64 + 1;
+            const unsigned long long to = (unsigned long long)lo + (unsigned long long)step * lane;
+            const uint32_t here = to > hi ? hi : (uint32_t)to;
+            mask = __builtin_amdgcn_ballot_w64(holds(here));
+            if (!mask) {
+                lo = (uint32_t)of_lane((int)here, 63) + 1;
+                continue;
+            }
+            const int l = __builtin_ctzll(mask);
+            hi = (uint32_t)of_lane((int)here, l);
+            if (l) lo = (uint32_t)of_lane((int)here, l - 1) + 1;
+        }
+        found = hi;
+    }
+    return found == ordered_bits(0.0f) ? found - 1 : found;
 }
 
-// A workgroup a row.
+// A workgroup a row.  Two things bound it.  It is a chain of steps that each wait for the one before (a trip to memory 1 us, a barrier of sixteen waves 0.2): requests are made
+// together and ahead, and no step is one thread's.  And a compute unit does one instruction for 64 tokens a cycle, 1 us for each that is done for every token of
+// 152 K: what chunks hold is compared with the ends of the gathered buckets, two instructions, and only what lies between is worked on.
 template <int DT>
 __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenParams p) {
     constexpr int N = lane_tokens<DT>, CHUNKS = part_chunks<DT>;
+    constexpr int AHEAD = 4;                                     // chunks' largest logits of a thread that are requested at the start: of vocabularies up to 2^18 or 2^19 all
+    constexpr int DEPTH = 24 / N;                                // loads of a wave under way where chunks are read
     constexpr u64 ALL = ~0ull;
+    constexpr int kPairs = 512;                                  // tokens up to which each is compared with each
+    extern __shared__ unsigned short chunks[];                   // that may hold some of the gathered buckets
     __shared__ double bucket_mass[kBuckets], through_mass[kBuckets];
     __shared__ unsigned int through_count[kBuckets];
-    __shared__ u64 list[kListed];                                // rank keys of a bucket's tokens, in no order
+    __shared__ u64 list[kListed];                                // rank keys of the gathered tokens, in no order
     __shared__ u64 bin_mass[kDrawThreads];
     __shared__ unsigned int bin_count[kDrawThreads];
+    __shared__ u64 edge[kPairs];                                 // those among which the cut lies
     __shared__ double factor[kMaxTokenParts];                    // of a part's units in the row's
     __shared__ u64 part_mass[kMaxTokenParts];
     __shared__ float part_max[kMaxTokenParts];
     __shared__ int shift[kMaxTokenParts];                        // of a part's buckets in the row's
-    __shared__ unsigned short chunks[kMaxTokenParts * CHUNKS];   // that may hold some of the bucket
-    __shared__ u64 wave_units[kDrawWaves];
-    __shared__ double wave_mass[kDrawWaves];
-    __shared__ unsigned int wave_count[kDrawWaves];
-    __shared__ int found, n_chunks, n_listed;
-    __shared__ u64 chosen[4];
+    __shared__ u64 talk_places[kTurns][kDrawWaves];
+    __shared__ int n_chunks, n_listed, n_edge;
+    __shared__ u64 chosen[3];
     __shared__ double drawn_total;
-    __shared__ int drawn_part;
+    __shared__ int drawn_part, drawn_banned;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r = blockIdx.x, row_at = p.row0 + r;
+    const int nb = p.nb, maxima = nb * CHUNKS;
+    const LogitRow<DT> row(p, row_at);
+    auto chunk_max_at = [&](int i) {
+        const int at = tid + i * kDrawThreads;
+        return at < maxima ? p.chunk_max[(long long)r * maxima + at] : -__builtin_inff();
+    };
+    float chunk_max[AHEAD];
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) chunk_max[i] = chunk_max_at(i);
+    float most = -__builtin_inff();
+    for (int b = lane; b < nb; b += 64) most = fmaxf(most, p.part_max[(long long)r * nb + b]);
+    const float mine_max = tid < nb ? p.part_max[(long long)r * nb + tid] : -__builtin_inff();
+    const u64 mine_mass = tid < nb ? p.mass[((long long)r * nb + tid) * kBuckets] : 0;           // (of the whole part in DRAW_ALL)
+    const float u_at = p.u[row_at];
+    const int draft = p.draft ? p.draft[row_at] : -1;
     const RowOf of = row_of(p, row_at);
     if (of.who < 0) return;
     const Filters f = filters_at(p, of.who);
-    const LogitRow<DT> row(p, row_at);
-    const int nb = p.nb;
+    const int mode = draw_mode(f);
+    WaveTalk talk{talk_places, 0};
 
     // ---- the row's largest logit, and how the parts' buckets lie on its line
-    float most = -__builtin_inff();
-    for (int b = lane; b < nb; b += 64) most = fmaxf(most, p.part_max[(long long)r * nb + b]);
     most = wave_max(most);
     if (!(most > -__builtin_inff())) {                           // nothing to draw from
         if (tid == 0) {
@@ -220,258 +375,323 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
         return;
     }
     const float top = bucket_line(most, f.scale);
-    for (int b = tid; b < nb; b += kDrawThreads) {
-        const float m = p.part_max[(long long)r * nb + b];
-        part_max[b] = m;
-        shift[b] = bucket_of(m, f.scale, top);
-        factor[b] = m > -__builtin_inff() ? weight_of(m, most, f.rate) : 0.0;
+    const float draft_logit = draft >= 0 && draft < p.V ? row.one(draft) : -__builtin_inff();    // (one address for the workgroup)
+    static_assert(kMaxTokenParts <= kDrawThreads, "a part a thread");
+    if (tid < nb) {
+        part_max[tid] = mine_max;
+        shift[tid] = bucket_of(mine_max, f.scale, top);
+        factor[tid] = mine_max > -__builtin_inff() ? weight_of(mine_max, most, f.rate) : 0.0;
+        part_mass[tid] = mode == DRAW_ALL ? mine_mass : 0;
     }
     __syncthreads();
 
-    // ---- buckets of the row: count and mass of each, and through it
-    {
+    // Ten requests at a time of what the parts have in this thread's bucket, of every other part: take(part, what it has).
+    auto merged = [&](auto place, auto take) {
         const int j = tid % kBuckets;
-        double mass = 0.0;
-        unsigned int count = 0;
-        for (int b = tid / kBuckets; b < nb; b += kDrawThreads / kBuckets) {
-            const int from = j - shift[b];
-            if (from < 0) continue;
-            const long long at = ((long long)r * nb + b) * kBuckets + from;
-            mass += (double)p.mass[at] * (factor[b] * (1.0 / (double)(1ull << kPartBits)));
-            if (f.k) count += p.count[at];
+#pragma unroll 1
+        for (int b0 = tid / kBuckets; b0 < nb; b0 += 20) {
+            decltype(place(0ll)) v[10];
+            bool ok[10];
+#pragma unroll
+            for (int i = 0; i < 10; ++i) {
+                const int b = b0 + 2 * i;
+                ok[i] = b < nb && j >= shift[min(b, nb - 1)];
+                v[i] = place(((long long)r * nb + (ok[i] ? b : 0)) * kBuckets + (ok[i] ? j - shift[b] : 0));
+            }
+#pragma unroll
+            for (int i = 0; i < 10; ++i)
+                if (ok[i]) take(b0 + 2 * i, v[i]);
         }
-        reinterpret_cast<double *>(bin_mass)[tid] = mass;
+    };
+    // ---- buckets of the row: how many tokens, or what mass, through each
+    if (f.k) {
+        unsigned int count = 0;
+        merged([&](long long at) { return p.count[at]; }, [&](int, unsigned int n) { count += n; });
         bin_count[tid] = count;
         __syncthreads();
-        mass = 0.0;
-        count = 0;
-        if (tid < kBuckets) {
-            mass = reinterpret_cast<double *>(bin_mass)[tid] + reinterpret_cast<double *>(bin_mass)[tid + kBuckets];
-            count = bin_count[tid] + bin_count[tid + kBuckets];
-        }
-        const double mass_through = sums_through(mass, wave_mass);
-        const unsigned int count_through = sums_through(count, wave_count);
-        if (tid < kBuckets) bucket_mass[tid] = mass, through_mass[tid] = mass_through, through_count[tid] = count_through;
+        const unsigned int through = talk.sum_through(tid < kBuckets ? bin_count[tid] + bin_count[tid + kBuckets] : 0u);
+        if (tid < kBuckets) through_count[tid] = through;
+        __syncthreads();
+    }
+    if (mode == DRAW_MANY) {
+        double mass = 0.0;
+        merged([&](long long at) { return p.mass[at]; }, [&](int b, u64 units) { mass += (double)units * (factor[b] * (1.0 / (double)(1ull << kPartBits))); });
+        reinterpret_cast<double *>(bin_mass)[tid] = mass;
+        __syncthreads();
+        mass = tid < kBuckets ? reinterpret_cast<double *>(bin_mass)[tid] + reinterpret_cast<double *>(bin_mass)[tid + kBuckets] : 0.0;
+        const double through = talk.sum_through(mass);
+        if (tid < kBuckets) bucket_mass[tid] = mass, through_mass[tid] = through;
         __syncthreads();
     }
 
-    // The tokens of a bucket: their keys into the list, as many as it takes; how many.
-    auto each_of_chunks = [&](int bucket, auto body) {
-        for (int q0 = w; q0 < n_chunks; q0 += 4 * kDrawWaves) {
-            float x[4][N];
-            int at[4];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                at[i] = q0 + i * kDrawWaves < n_chunks ? chunks[q0 + i * kDrawWaves] * chunk_tokens<DT> + lane * N : -1;
-                if (at[i] >= 0) row.load(at[i], x[i]);
-            }
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int e = 0; e < N; ++e)
-                    if (at[i] >= 0 && bucket_of(x[i][e], f.scale, top) == bucket) body(rank_key(x[i][e], at[i] + e - row.skew));
-        }
-    };
-    int listed_bucket = -1;
-    auto gather = [&](int bucket) {
-        if (tid == 0) n_chunks = 0, n_listed = 0;
-        __syncthreads();
-        for (int i = tid; i < nb * CHUNKS; i += kDrawThreads)
-            if (bucket_of(p.chunk_max[(long long)r * nb * CHUNKS + i], f.scale, top) <= bucket) chunks[atomicAdd(&n_chunks, 1)] = (unsigned short)i;
-        __syncthreads();
-        each_of_chunks(bucket, [&](u64 key) {
-            const int at = atomicAdd(&n_listed, 1);
-            if (at < kListed) list[at] = key;
-        });
-        __syncthreads();
-        listed_bucket = bucket;
-    };
-    auto each = [&](auto body) {                                 // of the gathered bucket
+    // The gathered tokens: their keys in the list, as many as it takes, or, where there are more, read again wherever they are asked for.  (The steps below are one loop, so that
+    // gathering and selecting stand in the code once: as often as they are called it was 216 KB.)
+    float gathered_from = 0.0f, gathered_to = 0.0f;              // their smallest and largest logit
+    int gathered = -1;                                           // buckets: first << 16 | last
+    auto each = [&](auto body) {
         if (n_listed <= kListed) {
             for (int i = tid; i < n_listed; i += kDrawThreads) body(list[i]);
-        } else {
-            each_of_chunks(listed_bucket, body);
+            return;
         }
-    };
-    // Of the gathered bucket's tokens up to `cut`, in their order: the first `need` (by_mass: those ahead of which less than `limit` of the row's mass
-    // lies).  The last of them becomes the cut; their mass.  A digit of ten bits of the keys at a time, until one token is left: keys differ.
-    auto select = [&](bool by_mass, unsigned int need, double limit, u64 &cut) {
-        u64 lo = ALL, hi = 0;
-        each([&](u64 key) {
-            if (key > cut) return;
-            lo = key < lo ? key : lo;
-            hi = key > hi ? key : hi;
-        });
+        for (int q = 4 * w + (lane >> 4); q < n_chunks; q += 4 * kDrawWaves) {
+            const int unit = chunks[q] * 16 + (lane & 15);
+            float x[N];
+            row.template values<true>(unit, row.request(unit), x);
 #pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) {
-            const u64 a = __shfl_xor(lo, off, 64), b = __shfl_xor(hi, off, 64);
-            lo = a < lo ? a : lo;
-            hi = b > hi ? b : hi;
+            for (int e = 0; e < N; ++e)
+                if (x[e] >= gathered_from && x[e] <= gathered_to) body(rank_key(logit_value(x[e]), unit * N + e - row.skew));
         }
-        if (lane == 0) bin_mass[w] = lo, bin_mass[kDrawWaves + w] = hi;
-        __syncthreads();
-#pragma unroll
-        for (int i = 0; i < kDrawWaves; ++i) {
-            lo = bin_mass[i] < lo ? bin_mass[i] : lo;
-            hi = bin_mass[kDrawWaves + i] > hi ? bin_mass[kDrawWaves + i] : hi;
-        }
-        if (lo > hi) return 0.0;                                 // (no token: nothing is cut)
-        const float ref = key_value(lo);
-        const double to_row = weight_of(ref, most, f.rate) * (1.0 / (double)(1ull << kListBits));
-        const double units = __builtin_ceil(limit / to_row);
-        const u64 want = by_mass ? (units < 1.0 ? 1ull : units < 0x1p62 ? (u64)units : 1ull << 62) : ALL;
-        u64 mass_before = 0;
-        unsigned int count_before = 0;
-        for (;;) {
-            const u64 span = hi - lo;
-            const int digit = span < kDrawThreads ? 0 : 54 - __builtin_clzll(span);
-            __syncthreads();
-            bin_mass[tid] = 0;
-            bin_count[tid] = 0;
-            if (tid == 0) found = kDrawThreads, chosen[3] = 0;
-            __syncthreads();
-            each([&](u64 key) {
-                if (key < lo || key > hi) return;
-                const int at = (int)((key - lo) >> digit);
-                atomicAdd(&bin_count[at], 1u);
-                atomicAdd(&bin_mass[at], weight_units(key_value(key), ref, f.rate, kListBits));
-            });
-            __syncthreads();
-            const u64 mass = bin_mass[tid];
-            const unsigned int count = bin_count[tid];
-            const u64 mass_through = mass_before + sums_through(mass, wave_units);
-            const unsigned int count_through = count_before + sums_through(count, wave_count);
-            if (count) {
-                if (by_mass ? mass_through >= want : count_through >= need) atomicMin(&found, tid);
-                atomicMax(&chosen[3], (u64)tid + 1);             // (none reaches it: the last that holds any)
-            }
-            __syncthreads();
-            const int bin = found < kDrawThreads ? found : (int)chosen[3] - 1;
-            if (tid == bin) chosen[0] = mass_through, chosen[1] = mass, chosen[2] = (u64)count_through << 32 | count;
-            __syncthreads();
-            const u64 end = lo + ((u64)(bin + 1) << digit) - 1;
-            hi = end < hi ? end : hi;
-            const unsigned int inside = (unsigned int)chosen[2];
-            if (inside <= 1 || digit == 0) {
-                cut = hi;
-                return (double)chosen[0] * to_row;
-            }
-            lo += (u64)bin << digit;
-            mass_before = chosen[0] - chosen[1];
-            count_before = (unsigned int)(chosen[2] >> 32) - inside;
-        }
-    };
-    // The first bucket below `limit` that a condition holds for, or `limit`.
-    auto first_bucket = [&](int limit, auto holds) {
-        if (tid == 0) found = limit;
-        __syncthreads();
-        if (tid < limit && holds(tid)) atomicMin(&found, tid);
-        __syncthreads();
-        const int at = found;
-        __syncthreads();
-        return at;
     };
 
-    // ---- the cut
+    // ---- the cut: by top-k, then by top-p, then by min_p; at last the tokens of the bucket in which it lies
+    enum { BY_COUNT, BY_MASS, OF_BORDER, STEPS };
     u64 cut = ALL;
-    int border = kBuckets;                                       // the bucket in which it lies
-    double total = through_mass[kBuckets - 1];
-    if (f.k) {
-        const int at = first_bucket(kBuckets, [&](int j) { return through_count[j] >= (unsigned int)f.k; });
-        if (at < kBuckets) {                                     // (else what is beyond the buckets has no mass)
-            gather(at);
-            border = at;
-            total = (at ? through_mass[at - 1] : 0.0) + select(false, (unsigned int)f.k - (at ? through_count[at - 1] : 0u), 0.0, cut);
+    int border = kBuckets;                                       // the bucket in which it lies (FEW: the last one gathered)
+    double total = mode == DRAW_MANY ? through_mass[kBuckets - 1] : 0.0;
+#pragma unroll 1
+    for (int step = mode == DRAW_ALL ? (int)STEPS : (int)BY_COUNT; step < STEPS; ++step) {
+        int from = 0, to = border, last;
+        double limit = 0.0;
+        unsigned int need = 0;
+        if (step == BY_COUNT) {
+            if (!f.k) continue;
+            talk.ends(tid < kBuckets && through_count[tid % kBuckets] >= (unsigned int)f.k, false, to, last);
+            if (mode == DRAW_MANY && to >= kBuckets) continue;   // (what is beyond the buckets has no mass)
+            to = min(to, kBuckets - 1);
+            from = mode == DRAW_FEW ? 0 : to;
+            need = (unsigned int)f.k - (to ? through_count[to - 1] : 0u);        // of bucket `to`
+        } else if (step == BY_MASS) {
+            if (!(f.p < 1.0f)) continue;
+            limit = (double)f.p * total;
+            if (mode == DRAW_MANY) {
+                talk.ends(tid < border && bucket_mass[tid % kBuckets] > 0.0 && through_mass[tid % kBuckets] >= limit, false, to, last);
+                to = min(to, border);
+                if (to == kBuckets) continue;
+                from = to;
+                limit -= through_mass[to] - bucket_mass[to];
+            }
+        } else {
+            if (f.min_p > 0.0f) {
+                const float least = least_logit(most, f.rate, f.min_p);
+                const u64 key = rank_key(least, (1 << kIndexBits) - 1);
+                if (key < cut) {
+                    cut = key;
+                    if (mode == DRAW_MANY) border = bucket_of(least, f.scale, top);
+                }
+            }
+            if (mode == DRAW_FEW || border == kBuckets) break;
+            from = to = border;
+        }
+        const uint32_t least = least_ordered_of_bucket(to, f.scale, top, most);
+        if (gathered != (from << 16 | to)) {
+            gathered = from << 16 | to;
+            gathered_from = value_of_ordered(least);
+            gathered_to = from ? value_of_ordered(least_ordered_of_bucket(from - 1, f.scale, top, most) - 1) : __builtin_inff();
+            if (tid == 0) n_chunks = 0, n_listed = 0;
+            __syncthreads();
+#pragma unroll 1
+            for (int i = 0; i * kDrawThreads < maxima; ++i) {
+                const float largest = i == 0 ? chunk_max[0] : i == 1 ? chunk_max[1] : i == 2 ? chunk_max[2] : i == 3 ? chunk_max[3] : chunk_max_at(i);
+                const bool may = largest >= gathered_from;
+                const unsigned long long mask = __builtin_amdgcn_ballot_w64(may);
+                if (!mask) continue;
+                int at = 0;
+                if (lane == 0) at = atomicAdd(&n_chunks, (int)__popcll(mask));
+                at = __builtin_amdgcn_readfirstlane(at);
+                if (may) chunks[at + __popcll(mask & ((1ull << lane) - 1))] = (unsigned short)(tid + i * kDrawThreads);
+            }
+            __syncthreads();
+#pragma unroll 1
+            for (int q0 = w * 4 * DEPTH; q0 < n_chunks; q0 += kDrawWaves * 4 * DEPTH) {
+                u32x4 raw[DEPTH];
+                int unit[DEPTH];
+#pragma unroll
+                for (int i = 0; i < DEPTH; ++i) {
+                    unit[i] = chunks[min(q0 + 4 * i + (lane >> 4), n_chunks - 1)] * 16 + (lane & 15);
+                    raw[i] = row.request(unit[i]);
+                }
+                float x[DEPTH][N];
+                unsigned int in = 0;
+#pragma unroll
+                for (int i = 0; i < DEPTH; ++i) {
+                    row.template values<true>(unit[i], raw[i], x[i]);
+                    unsigned int bits = 0;
+#pragma unroll
+                    for (int e = 0; e < N; ++e) bits |= x[i][e] >= gathered_from && x[i][e] <= gathered_to ? 1u << (i * N + e) : 0u;
+                    if (q0 + 4 * i + (lane >> 4) < n_chunks) in |= bits;
+                }
+                const int n = __popc(in), through = lane_sums_through(n), all = __builtin_amdgcn_readlane(through, 63);
+                if (!all) continue;
+                int at = 0;
+                if (lane == 0) at = atomicAdd(&n_listed, all);
+                at = __builtin_amdgcn_readfirstlane(at) + through - n;
+#pragma unroll
+                for (int i = 0; i < DEPTH; ++i)
+#pragma unroll
+                    for (int e = 0; e < N; ++e)
+                        if (in & 1u << (i * N + e)) {
+                            if (at < kListed) list[at] = rank_key(logit_value(x[i][e]), unit[i] * N + e - row.skew);
+                            ++at;
+                        }
+            }
+            __syncthreads();
+        }
+        if (step == OF_BORDER) break;
+        border = to;
+        // Among the keys lo .. hi, `inside` of them, the first `want` (tokens, or units of mass: those ahead of which less lies).  Masses are relative to the largest
+        // logit there may be among them.
+        const bool by_mass = step == BY_MASS, one = !by_mass || from;            // (one bucket's)
+        const float ref = one && to ? value_of_ordered(least_ordered_of_bucket(to - 1, f.scale, top, most) - 1) : most;
+        const double to_row = weight_of(ref, most, f.rate) * (1.0 / (double)(1ull << kListBits));
+        u64 lo = one && to ? rank_key(ref, 0) : 0, hi = rank_key(value_of_ordered(least), (1 << kIndexBits) - 1), before = 0;
+        hi = cut < hi ? cut : hi;
+        int inside = from || by_mass ? n_listed : (int)(through_count[to] - (to ? through_count[to - 1] : 0u));
+        const double units = by_mass ? __builtin_ceil(limit / to_row) : (double)need;
+        const u64 want = units < 1.0 ? 1ull : units < 0x1p62 ? (u64)units : 1ull << 62;
+        if (by_mass || need < (unsigned int)inside) {
+#pragma unroll 1
+            while (inside > kPairs && lo < hi) {                 // a digit of ten bits at a time
+                const u64 span = hi - lo;
+                const int digit = span < kDrawThreads ? 0 : 54 - __builtin_clzll(span);
+                bin_mass[tid] = 0;
+                bin_count[tid] = 0;
+                __syncthreads();
+                each([&](u64 key) {
+                    if (key < lo || key > hi) return;
+                    const int at = (int)((key - lo) >> digit);
+                    atomicAdd(&bin_count[at], 1u);
+                    if (by_mass) atomicAdd(&bin_mass[at], weight_units(key_value(key), ref, f.rate, kListBits));
+                });
+                __syncthreads();
+                const unsigned int count = bin_count[tid];
+                const u64 mine = by_mass ? bin_mass[tid] : count, through = before + talk.sum_through(mine);
+                int bin, last;
+                talk.ends(count && through >= want, count != 0, bin, last);
+                if (bin == kDrawThreads) bin = max(last, 0);     // (none reaches it: the last that holds any)
+                if (tid == bin) chosen[0] = through - mine, chosen[1] = count;
+                __syncthreads();
+                const u64 end = lo + ((u64)(bin + 1) << digit) - 1;
+                hi = end < hi ? end : hi;
+                lo += (u64)bin << digit;
+                before = chosen[0];
+                inside = (int)chosen[1];
+            }
+            if (inside > 1 && lo < hi) {                         // each is compared with each, two or four lanes to a token
+                if (tid == 0) n_edge = 0, chosen[2] = hi;
+                __syncthreads();
+                each([&](u64 key) {
+                    if (key < lo || key > hi) return;
+                    const int at = atomicAdd(&n_edge, 1);
+                    if (at < kPairs) edge[at] = key;             // (there are no more)
+                });
+                __syncthreads();
+                const int n = min(n_edge, kPairs), share = n <= kDrawThreads / 4 ? 2 : 1, mine = tid >> share, part = tid & ((1 << share) - 1);
+                if (tid < n) bin_mass[tid] = by_mass ? weight_units(key_value(edge[tid]), ref, f.rate, kListBits) : 1;
+                __syncthreads();
+                if ((n << share) > (tid & ~63)) {                // (whole waves)
+                    const u64 key = mine < n ? edge[mine] : ALL;
+                    u64 ahead = 0;
+                    for (int i = part; i < n; i += 1 << share)
+                        if (edge[i] < key) ahead += bin_mass[i];
+                    for (int off = 1; off < 1 << share; off <<= 1) ahead += __shfl_xor(ahead, off, 64);
+                    ahead += before;
+                    if (mine < n && part == 0 && ahead < want && ahead + bin_mass[mine] >= want) chosen[2] = key;     // (one of them, or none: all are in)
+                }
+                __syncthreads();
+                hi = chosen[2];
+            }
+        }
+        cut = hi;
+        if (!by_mass && f.p < 1.0f) {                            // the mass up to the cut
+            u64 mass = 0;
+            each([&](u64 key) {
+                if (key <= cut) mass += weight_units(key_value(key), most, f.rate, kListBits);
+            });
+            total = (double)talk.sum(mass) * (1.0 / (double)(1ull << kListBits)) + (from ? through_mass[from - 1] : 0.0);
         }
     }
-    if (f.p < 1.0f) {
-        const double target = (double)f.p * total;
-        const int at = first_bucket(border, [&](int j) { return bucket_mass[j] > 0.0 && through_mass[j] >= target; });
-        if (at < kBuckets) {
-            if (listed_bucket != at) gather(at);
-            border = at;
-            select(true, 0u, target - (through_mass[at] - bucket_mass[at]), cut);
-        }
-    }
-    if (f.min_p > 0.0f) {
-        const float least = least_logit(most, f.rate, f.min_p);
-        const u64 key = rank_key(least, (1 << kIndexBits) - 1);
-        if (key < cut) {
-            cut = key;
-            border = bucket_of(least, f.scale, top);
-        }
-    }
-    auto kept = [&](float z, int v) {
-        const int at = bucket_of(z, f.scale, top);
-        return at < border || (at == border && at < kBuckets && rank_key(z, v) <= cut);
-    };
+    auto kept = [&](float z, int v) { return rank_key(z, v) <= cut && (mode != DRAW_MANY || bucket_of(z, f.scale, top) < kBuckets); };
 
     // ---- what is left of each part
     __syncthreads();
-    for (int b = w; b < nb; b += kDrawWaves) {
-        u64 sum = 0;
-        for (int j = lane; j < border - shift[b]; j += 64) sum += p.mass[((long long)r * nb + b) * kBuckets + j];
+    if (mode == DRAW_MANY) {
+#pragma unroll 1
+        for (int b = w; b < nb; b += kDrawWaves) {
+            u64 v[kBuckets / 64], sum = 0;
+            const int n = border - shift[b];
 #pragma unroll
-        for (int off = 32; off >= 1; off >>= 1) sum += __shfl_xor(sum, off, 64);
-        if (lane == 0) part_mass[b] = sum;
-    }
-    if (border < kBuckets) {
-        if (listed_bucket != border) gather(border);
+            for (int i = 0; i < kBuckets / 64; ++i) {
+                const int j = 64 * i + lane;
+                v[i] = j < n ? p.mass[((long long)r * nb + b) * kBuckets + j] : 0;
+            }
+#pragma unroll
+            for (int i = 0; i < kBuckets / 64; ++i) sum += v[i];
+            sum = wave_sum(sum);
+            if (lane == 0) part_mass[b] = sum;
+        }
         __syncthreads();
+    }
+    if (mode == DRAW_FEW || (mode == DRAW_MANY && border < kBuckets)) {
         each([&](u64 key) {
             if (key > cut) return;
             const int b = (key_token(key) + row.skew) / kPartTokens;
             atomicAdd(&part_mass[b], weight_units(key_value(key), part_max[b], f.rate, kPartBits));
         });
+        __syncthreads();
     }
-    __syncthreads();
-    int banned = -1;
-    if (tid == 0) {
-        double whole = 0.0;
-        for (int b = 0; b < nb; ++b) whole += (double)part_mass[b] * factor[b];
+    // ---- a refused draft is left out; the part that the draw falls in: the first whose running mass exceeds it, else the last that has any
+    if (w == 0) {
+        constexpr int EACH = (kMaxTokenParts + 63) / 64;
+        const int per = (nb + 63) / 64;
+        const bool in = draft >= 0 && draft < p.V && draft_logit > -__builtin_inff() && kept(draft_logit, draft);
+        const int draft_part = in ? (draft + row.skew) / kPartTokens : 0;
+        const u64 draft_units = in ? weight_units(draft_logit, part_max[draft_part], f.rate, kPartBits) : 0;
+        u64 units[EACH];
+        double sum = 0.0, through;
+        auto add_up = [&] {
+            sum = 0.0;
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) sum += i < per && lane * per + i < nb ? (double)units[i] * factor[lane * per + i] : 0.0;
+            through = lane_sums_through(sum);
+            return of_lane(through, 63);
+        };
+#pragma unroll
+        for (int i = 0; i < EACH; ++i) units[i] = i < per && lane * per + i < nb ? part_mass[lane * per + i] : 0;
+        double whole = add_up();
         if (p.draft) {
-            const int d = p.draft[row_at];
-            double of_draft = 0.0;
-            if (!of.last && d >= 0 && d < p.V) {
-                const float z = row.one(d);
-                if (kept(z, d)) {
-                    const int b = (d + row.skew) / kPartTokens;
-                    const u64 units = weight_units(z, part_max[b], f.rate, kPartBits);
-                    of_draft = (double)units * factor[b] / whole;
-                    part_mass[b] -= units;                       // what a refusal draws from
-                }
-                banned = d;
-                whole = 0.0;
-                for (int b = 0; b < nb; ++b) whole += (double)part_mass[b] * factor[b];
-            } else if (d >= 0 && d < p.V && kept(row.one(d), d)) {
-                const int b = (d + row.skew) / kPartTokens;
-                of_draft = (double)weight_units(row.one(d), part_max[b], f.rate, kPartBits) * factor[b] / whole;
+            const double of_draft = (double)draft_units * factor[draft_part] / whole;
+            if (lane == 0) {
+                if (p.p) p.p[row_at] = (float)of_draft;
+                p.accepted[row_at] = !of.last && (double)p.u_accept[row_at] < of_draft;
             }
-            if (p.p) p.p[row_at] = (float)of_draft;
-            p.accepted[row_at] = !of.last && (double)p.u_accept[row_at] < of_draft;
+            if (!of.last && draft_units) {
+#pragma unroll
+                for (int i = 0; i < EACH; ++i)
+                    if (i < per && lane * per + i == draft_part) units[i] -= draft_units;
+                whole = add_up();
+            }
         }
-        // the part that the draw falls in: the first whose running mass exceeds it, else the last that has any
-        const float u = p.u[row_at];
-        const double target = u > 0.0f ? (double)u * whole : 0.0;
-        double through = 0.0, ahead = 0.0;
-        int part = -1;
-        for (int b = 0; b < nb; ++b) {
-            if (!part_mass[b]) continue;
-            part = b;
-            ahead = through;
-            through += (double)part_mass[b] * factor[b];
-            if (through > target) break;
-        }
-        u64 units = 0;
-        if (part >= 0) {
+        const double target = u_at > 0.0f ? (double)u_at * whole : 0.0;
+        const unsigned long long mass = __builtin_amdgcn_ballot_w64(sum > 0.0), reach = __builtin_amdgcn_ballot_w64(sum > 0.0 && through > target);
+        const int owner = mass ? draw_lane(reach, mass) : -1;
+        if (lane == 0) drawn_part = -1, drawn_total = whole, drawn_banned = !of.last ? draft : -1;
+        if (lane == owner) {
+            double ahead = through - sum;
+            int part = -1;
+            u64 of_part = 0;
+#pragma unroll
+            for (int i = 0; i < EACH; ++i) {
+                if (i >= per || !units[i] || !(factor[lane * per + i] > 0.0) || (part >= 0 && ahead + (double)of_part * factor[part] > target)) continue;
+                if (part >= 0) ahead += (double)of_part * factor[part];
+                part = lane * per + i;
+                of_part = units[i];
+            }
             const double left = (target - ahead) / factor[part];
-            units = left > 0.0 ? (left < 0x1p62 ? (u64)left : 1ull << 62) : 0;
-            if (units >= part_mass[part]) units = part_mass[part] - 1;
+            u64 at = left > 0.0 ? (left < 0x1p62 ? (u64)left : 1ull << 62) : 0;
+            if (at >= of_part) at = of_part - 1;
+            drawn_part = part;
+            chosen[0] = at;
         }
-        drawn_part = part;
-        drawn_total = whole;
-        chosen[0] = units;
-        chosen[1] = (u64)(banned + 1);
     }
     __syncthreads();
     const int part = drawn_part;
@@ -483,21 +703,26 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
         return;
     }
     // ---- the token: eight places a thread, in order
-    banned = (int)chosen[1] - 1;
+    const int banned = drawn_banned;
     const u64 ahead = chosen[0];
-    float x[kPartTokens / kDrawThreads / N][N];
+    constexpr int LAST = kPartTokens / kDrawThreads / N;         // loads
+    u32x4 raw[LAST];
+    float x[LAST][N];
     const int at0 = part * kPartTokens + tid * (kPartTokens / kDrawThreads);
     u64 units[kPartTokens / kDrawThreads], sum = 0;
 #pragma unroll
-    for (int i = 0; i < kPartTokens / kDrawThreads / N; ++i) row.load(at0 + i * N, x[i]);
+    for (int i = 0; i < LAST; ++i) raw[i] = row.request(at0 / N + i);
+#pragma unroll
+    for (int i = 0; i < LAST; ++i) row.values(at0 / N + i, raw[i], x[i]);
 #pragma unroll
     for (int i = 0; i < kPartTokens / kDrawThreads; ++i) {
         const int v = at0 + i - row.skew;
         const float z = x[i / N][i % N];
-        units[i] = kept(z, v) && v != banned ? weight_units(z, part_max[part], f.rate, kPartBits) : 0;
+        units[i] = 0;
+        if (kept(z, v) && v != banned) units[i] = weight_units(z, part_max[part], f.rate, kPartBits);
         sum += units[i];
     }
-    const u64 through = sums_through(sum, wave_units);
+    const u64 through = talk.sum_through(sum);
     if (through > ahead && through - sum <= ahead) {
         u64 at = through - sum;
 #pragma unroll

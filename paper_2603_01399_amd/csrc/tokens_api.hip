@@ -3,6 +3,7 @@
 
 #include <hip/hip_runtime.h>
 
+#include <atomic>
 #include <type_traits>
 
 #include "tokens.hpp"
@@ -26,7 +27,7 @@ struct TokenRoom {
         rows = T < kRowsAtOnce ? T : kRowsAtOnce;
         mass = (size_t)(rows * nb) * kBuckets * 8;
         count = (size_t)(rows * nb) * kBuckets * 4;
-        chunk_max = (size_t)(rows * nb) * (kPartTokens / 256) * 4;
+        chunk_max = (size_t)(rows * nb) * part_chunks<0> * 4;            // (fp32's chunks are the smaller ones)
         part_max = ((size_t)(rows * nb) * 4 + 15) & ~(size_t)15;
         rows_out = drafts ? ((size_t)T * 4 + 15) & ~(size_t)15 : 0;
     }
@@ -44,14 +45,28 @@ int check_tokens(TokenParams &p, int dtype, int64_t T, int64_t V, int64_t ld, co
     return aligned(workspace, 16) ? QUASAR_OK : QUASAR_ERR_ALIGN;
 }
 
+// The opt-in to more dynamic LDS than the default, once for each kernel and device (done: a bit a device).
+bool large_lds(const void *kernel, std::atomic<unsigned long long> &done) {
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess) return false;
+    const unsigned long long bit = 1ull << (dev & 63);
+    if (dev < 64 && (done.load() & bit)) return true;
+    if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kMaxTokenParts * part_chunks<0> * (int)sizeof(unsigned short)) != hipSuccess) return false;
+    if (dev < 64) done.fetch_or(bit);
+    return true;
+}
+
 template <int DT>
 int launch_tokens(TokenParams p, const TokenRoom &room, int64_t T, hipStream_t st) {
+    static std::atomic<unsigned long long> done{0};
+    const unsigned int chunks = (unsigned int)room.nb * part_chunks<DT> * sizeof(unsigned short);
+    if (!large_lds(reinterpret_cast<const void *>(token_draw_kernel<DT>), done)) return QUASAR_ERR_HIP;
     for (int64_t row0 = 0; row0 < T; row0 += room.rows) {
         const unsigned int rows = (unsigned int)(T - row0 < room.rows ? T - row0 : room.rows);
         p.row0 = (int)row0;
         hipLaunchKernelGGL(token_parts_kernel<DT>, dim3((unsigned int)room.nb, rows), dim3(kPartThreads), 0, st, p);
         if (const int e = launched()) return e;
-        hipLaunchKernelGGL(token_draw_kernel<DT>, dim3(rows), dim3(kDrawThreads), 0, st, p);
+        hipLaunchKernelGGL(token_draw_kernel<DT>, dim3(rows), dim3(kDrawThreads), chunks, st, p);
         if (const int e = launched()) return e;
     }
     return QUASAR_OK;
