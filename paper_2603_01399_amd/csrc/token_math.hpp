@@ -61,7 +61,8 @@ QUASAR_BOTH u64 weight_units(float z, float ref, double rate, int bits) {
     return u & ((1ull << 52) - 1);
 }
 
-// The order of the filters: larger logits first, equal ones by their place.  53 bits at most.
+// The order of the filters: larger logits first, equal ones by their place.  A logit's rank is its bits in falling order: 32 of an fp32 one, 16 of a bf16 one
+// (DT 1), so that keys are dense: 52 or 36 bits with the place.
 QUASAR_BOTH uint32_t ordered_bits(float z) {                 // grows with z
     uint32_t u;
     memcpy(&u, &z, 4);
@@ -73,9 +74,27 @@ QUASAR_BOTH float value_of_ordered(uint32_t u) {
     memcpy(&z, &u, 4);
     return z;
 }
-QUASAR_BOTH u64 rank_key(float z, int v) { return (u64)(uint32_t)~ordered_bits(z) << kIndexBits | (u64)(uint32_t)v; }
-QUASAR_BOTH float key_value(u64 key) { return value_of_ordered(~(uint32_t)(key >> kIndexBits)); }
-QUASAR_BOTH int key_token(u64 key) { return (int)(key & ((1u << kIndexBits) - 1)); }
+constexpr int kLastPlace = (1 << kIndexBits) - 1;
+template <int DT> QUASAR_BOTH u64 rank_key(float z, int v) {
+    return (u64)(~ordered_bits(z) >> (DT == 1 ? 16 : 0)) << kIndexBits | (u64)(uint32_t)v;
+}
+template <int DT> QUASAR_BOTH float key_value(u64 key) {
+    const uint32_t rank = (uint32_t)(key >> kIndexBits);
+    // (a bf16's lower bits are 0: those of the ordered form where it is not negative, of its complement where it is)
+    return value_of_ordered(DT == 1 ? (rank < 0x8000u ? ~rank << 16 : ~(rank << 16)) : ~rank);
+}
+QUASAR_BOTH int key_token(u64 key) { return (int)(key & (u64)kLastPlace); }
+// The last key of logits whose ordered bits are at least these: of the smallest bf16 that is not below them.
+template <int DT> QUASAR_BOTH u64 last_key(uint32_t least) {
+    if (DT == 1) least = least & 0x80000000u ? (least + 0xFFFFu) & 0xFFFF0000u : least | 0xFFFFu;
+    return (u64)(~least >> (DT == 1 ? 16 : 0)) << kIndexBits | (u64)kLastPlace;
+}
+
+// The first key of logits whose ordered bits are at most these: of the largest bf16 that is not above them.
+template <int DT> QUASAR_BOTH u64 first_key(uint32_t most) {
+    if (DT == 1 && !(most & 0x80000000u)) most = ((most + 1) & 0xFFFF0000u) - 1;
+    return (u64)(~most >> (DT == 1 ? 16 : 0)) << kIndexBits;
+}
 
 // A logit's place on the line of buckets: whole, falls with z never, and the same for every part of a vocabulary.  (fmax takes what is not a number,
 // -inf times a scale of 0, for the smallest.)

@@ -439,7 +439,7 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
             row.template values<true>(unit, row.request(unit), x);
 #pragma unroll
             for (int e = 0; e < N; ++e)
-                if (x[e] >= gathered_from && x[e] <= gathered_to) body(rank_key(logit_value(x[e]), unit * N + e - row.skew));
+                if (x[e] >= gathered_from && x[e] <= gathered_to) body(rank_key<DT>(logit_value(x[e]), unit * N + e - row.skew));
         }
     };
 
@@ -473,7 +473,7 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
         } else {
             if (f.min_p > 0.0f) {
                 const float least = least_logit(most, f.rate, f.min_p);
-                const u64 key = rank_key(least, (1 << kIndexBits) - 1);
+                const u64 key = last_key<DT>(ordered_bits(least));
                 if (key < cut) {
                     cut = key;
                     if (mode == DRAW_MANY) border = bucket_of(least, f.scale, top);
@@ -525,14 +525,26 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
                 int at = 0;
                 if (lane == 0) at = atomicAdd(&n_listed, all);
                 at = __builtin_amdgcn_readfirstlane(at) + through - n;
+                for (; in; in &= in - 1, ++at) {                 // (as often as the lane that has most; the places alone: logits are indexed at compile time)
+                    const int bit = __builtin_ctz(in), q = q0 + 4 * (bit / N) + (lane >> 4);
+                    if (at < kListed) list[at] = (u64)((chunks[q] * 16 + (lane & 15)) * N + bit % N - row.skew);
+                }
+            }
+            __syncthreads();
+            // their keys: the logits once more, side by side
+            if (n_listed <= kListed) {
+#pragma unroll 1
+                for (int i0 = tid; i0 < n_listed; i0 += 4 * kDrawThreads) {
+                    int v[4];
+                    float z[4];
 #pragma unroll
-                for (int i = 0; i < DEPTH; ++i)
+                    for (int i = 0; i < 4; ++i) v[i] = (int)list[i0 + i * kDrawThreads < n_listed ? i0 + i * kDrawThreads : i0];    // (its own: others become keys)
 #pragma unroll
-                    for (int e = 0; e < N; ++e)
-                        if (in & 1u << (i * N + e)) {
-                            if (at < kListed) list[at] = rank_key(logit_value(x[i][e]), unit[i] * N + e - row.skew);
-                            ++at;
-                        }
+                    for (int i = 0; i < 4; ++i) z[i] = row.one(v[i]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        if (i0 + i * kDrawThreads < n_listed) list[i0 + i * kDrawThreads] = rank_key<DT>(z[i], v[i]);
+                }
             }
             __syncthreads();
         }
@@ -541,9 +553,10 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
         // Among the keys lo .. hi, `inside` of them, the first `want` (tokens, or units of mass: those ahead of which less lies).  Masses are relative to the largest
         // logit there may be among them.
         const bool by_mass = step == BY_MASS, one = !by_mass || from;            // (one bucket's)
-        const float ref = one && to ? value_of_ordered(least_ordered_of_bucket(to - 1, f.scale, top, most) - 1) : most;
+        const uint32_t largest = one && to ? least_ordered_of_bucket(to - 1, f.scale, top, most) - 1 : ordered_bits(most);
+        const float ref = value_of_ordered(largest);
         const double to_row = weight_of(ref, most, f.rate) * (1.0 / (double)(1ull << kListBits));
-        u64 lo = one && to ? rank_key(ref, 0) : 0, hi = rank_key(value_of_ordered(least), (1 << kIndexBits) - 1), before = 0;
+        u64 lo = first_key<DT>(largest), hi = last_key<DT>(least), before = 0;
         hi = cut < hi ? cut : hi;
         int inside = from || by_mass ? n_listed : (int)(through_count[to] - (to ? through_count[to - 1] : 0u));
         const double units = by_mass ? __builtin_ceil(limit / to_row) : (double)need;
@@ -560,7 +573,7 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
                     if (key < lo || key > hi) return;
                     const int at = (int)((key - lo) >> digit);
                     atomicAdd(&bin_count[at], 1u);
-                    if (by_mass) atomicAdd(&bin_mass[at], weight_units(key_value(key), ref, f.rate, kListBits));
+                    if (by_mass) atomicAdd(&bin_mass[at], weight_units(key_value<DT>(key), ref, f.rate, kListBits));
                 });
                 __syncthreads();
                 const unsigned int count = bin_count[tid];
@@ -586,7 +599,7 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
                 });
                 __syncthreads();
                 const int n = min(n_edge, kPairs), share = n <= kDrawThreads / 4 ? 2 : 1, mine = tid >> share, part = tid & ((1 << share) - 1);
-                if (tid < n) bin_mass[tid] = by_mass ? weight_units(key_value(edge[tid]), ref, f.rate, kListBits) : 1;
+                if (tid < n) bin_mass[tid] = by_mass ? weight_units(key_value<DT>(edge[tid]), ref, f.rate, kListBits) : 1;
                 __syncthreads();
                 if ((n << share) > (tid & ~63)) {                // (whole waves)
                     const u64 key = mine < n ? edge[mine] : ALL;
@@ -605,12 +618,12 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
         if (!by_mass && f.p < 1.0f) {                            // the mass up to the cut
             u64 mass = 0;
             each([&](u64 key) {
-                if (key <= cut) mass += weight_units(key_value(key), most, f.rate, kListBits);
+                if (key <= cut) mass += weight_units(key_value<DT>(key), most, f.rate, kListBits);
             });
             total = (double)talk.sum(mass) * (1.0 / (double)(1ull << kListBits)) + (from ? through_mass[from - 1] : 0.0);
         }
     }
-    auto kept = [&](float z, int v) { return rank_key(z, v) <= cut && (mode != DRAW_MANY || bucket_of(z, f.scale, top) < kBuckets); };
+    auto kept = [&](float z, int v) { return rank_key<DT>(z, v) <= cut && (mode != DRAW_MANY || bucket_of(z, f.scale, top) < kBuckets); };
 
     // ---- what is left of each part
     __syncthreads();
@@ -635,7 +648,7 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
         each([&](u64 key) {
             if (key > cut) return;
             const int b = (key_token(key) + row.skew) / kPartTokens;
-            atomicAdd(&part_mass[b], weight_units(key_value(key), part_max[b], f.rate, kPartBits));
+            atomicAdd(&part_mass[b], weight_units(key_value<DT>(key), part_max[b], f.rate, kPartBits));
         });
         __syncthreads();
     }

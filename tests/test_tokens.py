@@ -24,7 +24,7 @@ def model(tmp_path_factory):
                     str(HERE / "token_model.cpp")], check=True)
     lib = ctypes.CDLL(str(out))
     f, d, i, u = ctypes.c_float, ctypes.c_double, ctypes.c_int, ctypes.c_uint64
-    for name, result, args in (("weight_model", d, [f, f, d]), ("units_model", u, [f, f, d, i]), ("value_model", f, [f]), ("key_model", u, [f, i]), ("key_value_model", f, [u]),
+    for name, result, args in (("weight_model", d, [f, f, d]), ("units_model", u, [f, f, d, i]), ("value_model", f, [f]), ("key_model", u, [f, i, i]), ("key_value_model", f, [u, i]), ("last_key_model", u, [f, i]), ("first_key_model", u, [f, i]),
                                ("key_token_model", i, [u]), ("bucket_model", i, [f, f, f]), ("least_model", f, [f, d, f]),
                                ("filters_model", None, [f, i, f, f, i, ctypes.c_void_p])):
         getattr(lib, name).restype, getattr(lib, name).argtypes = result, args
@@ -105,11 +105,23 @@ def test_values_and_order(model):
     assert math.copysign(1, model.value_model(-0.0)) == 1.0
     r = np.random.Generator(np.random.Philox(3))
     z = np.concatenate([r.standard_normal(300) * np.exp(r.normal(size=300) * 20), [0.0, LARGEST, -LARGEST, 1e-45, -1e-45, 1.0, -1.0], np.repeat(2.5, 20)]).astype(np.float32)
-    v = r.permutation(1 << 20)[:len(z)]
-    keys = [model.key_model(a, int(b)) for a, b in zip(z, v)]
-    assert [int(i) for i in np.argsort(np.array(keys, np.uint64))] == [int(i) for i in np.lexsort((v, -z.astype(np.float64)))]
-    for a, b, key in zip(z, v, keys):
-        assert model.key_value_model(key) == a and model.key_token_model(key) == b and key < 1 << 52
+    for bf16 in (0, 1):
+        if bf16:
+            z = np.unique(torch.from_numpy(z).bfloat16().float().numpy() + 0.0).clip(-3.3e38, 3.3e38)
+            z = np.concatenate([z, np.repeat(z[50], 30)])
+            z = torch.from_numpy(z).bfloat16().float().numpy()
+        v = r.permutation(1 << 20)[:len(z)]
+        keys = [model.key_model(a, int(b), bf16) for a, b in zip(z, v)]
+        assert [int(i) for i in np.argsort(np.array(keys, np.uint64))] == [int(i) for i in np.lexsort((v, -z.astype(np.float64)))]
+        for a, b, key in zip(z, v, keys):
+            assert model.key_value_model(key, bf16) == a and model.key_token_model(key) == b and key < 1 << (36 if bf16 else 52)
+        # a logit counts up to the last key of a bound exactly where it is not below it, and from the first on exactly where it is not above it
+        for bound in np.concatenate([z[::7], (r.standard_normal(60) * np.exp(r.normal(size=60) * 20)).astype(np.float32), np.nextafter(z[::5], np.float32(math.inf)),
+                                     np.nextafter(z[::5], np.float32(-math.inf))]).clip(-3.3e38, 3.3e38):
+            last = model.last_key_model(bound, bf16)
+            assert [key <= last for key in keys] == [bool(a >= bound) for a in z], bound
+            first = model.first_key_model(bound, bf16)
+            assert [key >= first for key in keys] == [bool(a <= bound) for a in z], bound
 
 
 @pytest.mark.parametrize("scale", [16.0, 0.0, 1.0, 16000.0, 1e30, LARGEST, 3e-5])
