@@ -21,44 +21,47 @@ constexpr int kListBits = 42;                                // a whole vocabula
 constexpr int kIndexBits = 20;
 constexpr float kLargest = 3.4028234663852886e38f;
 
-// A logit as it counts: none for what is not a number, the largest finite value for infinity, one zero.
-QUASAR_BOTH float logit_value(float z) {
-    if (!(z == z)) return -__builtin_inff();
-    return (z < kLargest ? z : kLargest) + 0.0f;
-}
+// A logit as it counts: none for what is not a number, the largest finite value for infinity ...
+QUASAR_BOTH float logit_weighed(float z) { return __builtin_fminf(__builtin_fmaxf(z, -__builtin_inff()), kLargest); }
+// ... and, where it is ordered, one zero.
+QUASAR_BOTH float logit_value(float z) { return logit_weighed(z) + 0.0f; }
 
-// 2^f for |f| <= 1/2: its Taylor series up to the 12th power, whose rest is below 2^-52 of it.
-QUASAR_BOTH double exp2_of_fraction(double f) {
-    double r = 0x1.c3bd650fc2986p-36;                        // (ln 2)^k / k!
-    r = __builtin_fma(r, f, 0x1.e8cac7351bb25p-32);
-    r = __builtin_fma(r, f, 0x1.e4cf5158b8ecap-28);
-    r = __builtin_fma(r, f, 0x1.b5253d395e7c4p-24);
-    r = __builtin_fma(r, f, 0x1.62c0223a5c824p-20);
-    r = __builtin_fma(r, f, 0x1.ffcbfc588b0c7p-17);
-    r = __builtin_fma(r, f, 0x1.430912f86c787p-13);
-    r = __builtin_fma(r, f, 0x1.5d87fe78a6731p-10);
-    r = __builtin_fma(r, f, 0x1.3b2ab6fba4e77p-7);
-    r = __builtin_fma(r, f, 0x1.c6b08d704a0c0p-5);
-    r = __builtin_fma(r, f, 0x1.ebfbdff82c58fp-3);
-    r = __builtin_fma(r, f, 0x1.62e42fefa39efp-1);
-    return __builtin_fma(r, f, 1.0);
+QUASAR_BOTH u64 bits_of(double x) {
+    u64 u;
+    memcpy(&u, &x, 8);
+    return u;
 }
-// exp((z - ref) / temperature) for z <= ref, 0 below 2^-60; rate: log2(e) / temperature.
+QUASAR_BOTH double double_of(u64 u) {
+    double x;
+    memcpy(&x, &u, 8);
+    return x;
+}
+// 2^y for -1000 < y < 1000: y's nearest whole number, by the sum with 1.5 2^52, goes to the exponent; 2^f of the rest, |f| <= 1/2, by the polynomial of degree ten that
+// meets it at the Chebyshev points of the interval: off by at most 2^-51.5 of it.  extra: added to the exponent.
+QUASAR_BOTH double exp2_by(double y, int extra) {
+    const double t = y + 0x1.8p52, f = y - (t - 0x1.8p52);
+    double r = 0x1.e6063f7217bc6p-28;
+    r = __builtin_fma(r, f, 0x1.b675bca4eeebbp-24);
+    r = __builtin_fma(r, f, 0x1.62bfd47773353p-20);
+    r = __builtin_fma(r, f, 0x1.ffcb54062e698p-17);
+    r = __builtin_fma(r, f, 0x1.430913096fd9fp-13);
+    r = __builtin_fma(r, f, 0x1.5d87fe9d7a584p-10);
+    r = __builtin_fma(r, f, 0x1.3b2ab6fba1ddap-7);
+    r = __builtin_fma(r, f, 0x1.c6b08d703ce49p-5);
+    r = __builtin_fma(r, f, 0x1.ebfbdff82c598p-3);
+    r = __builtin_fma(r, f, 0x1.62e42fefa3a19p-1);
+    r = __builtin_fma(r, f, 1.0);
+    return double_of(bits_of(r) + ((u64)((uint32_t)bits_of(t) + (uint32_t)extra) << 52));
+}
+// exp((z - ref) / temperature) for z <= ref, 0 below 2^-60 (and of -inf, also times a rate of 0); rate: log2(e) / temperature.
 QUASAR_BOTH double weight_of(float z, float ref, double rate) {
     const double y = ((double)z - (double)ref) * rate;
-    if (!(y > -60.0)) return y == y ? 0.0 : 1.0;             // (not a number: a rate of 0 and no distance, or both infinite)
-    const double n = __builtin_rint(y);
-    return __builtin_ldexp(exp2_of_fraction(y - n), (int)n);
+    return y > -60.0 ? exp2_by(y, 0) : 0.0;
 }
 // The same in whole multiples of 2^-bits, to nearest (bits <= 51).
 QUASAR_BOTH u64 weight_units(float z, float ref, double rate, int bits) {
     const double y = ((double)z - (double)ref) * rate;
-    if (!(y > -60.0) || z == -__builtin_inff()) return 0;
-    const double n = __builtin_rint(y);
-    const double shifted = __builtin_ldexp(exp2_of_fraction(y - n), (int)n + bits) + 0x1p52;
-    u64 u;
-    memcpy(&u, &shifted, 8);
-    return u & ((1ull << 52) - 1);
+    return y > -60.0 ? bits_of(exp2_by(y, bits) + 0x1p52) & ((1ull << 52) - 1) : 0;
 }
 
 // The order of the filters: larger logits first, equal ones by their place.  A logit's rank is its bits in falling order: 32 of an fp32 one, 16 of a bf16 one

@@ -86,13 +86,13 @@ template <int DT> struct LogitRow {
         if (last < first) return u32x4{0u, 0u, 0u, 0u};          // (the same for every lane)
         return *reinterpret_cast<const u32x4 *>(border + 16ll * min(max(unit, first), last));
     }
-    // the tokens of a requested unit, as they count (AS_THEY_ARE: not a number and infinities as such); -inf where there are none
-    template <bool AS_THEY_ARE = false>
-    __device__ __forceinline__ void values(int unit, const u32x4 v, float (&x)[N]) const {
+    // the tokens of a requested unit as form(logit) has them; -inf where there are none
+    template <class Form>
+    __device__ __forceinline__ void values(int unit, const u32x4 v, float (&x)[N], Form form) const {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             const float z = DT == 1 ? __uint_as_float(e & 1 ? v[DT == 1 ? e >> 1 : 0] & 0xFFFF0000u : v[DT == 1 ? e >> 1 : 0] << 16) : __uint_as_float(v[e & 3]);
-            x[e] = AS_THEY_ARE ? z : logit_value(z);
+            x[e] = form(z);
         }
         if (unit < first || unit > last) {
 #pragma unroll
@@ -172,7 +172,7 @@ __global__ __launch_bounds__(kPartThreads) void token_parts_kernel(const TokenPa
     const Filters f = filters_at(p, of.who);
     float x[LOADS][N];
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) row.values(unit(i), raw[i], x[i]);
+    for (int i = 0; i < LOADS; ++i) row.values(unit(i), raw[i], x[i], [](float z) { return logit_weighed(z); });
     const int mode = draw_mode(f);
     const bool counts = f.k != 0, masses = mode == DRAW_MANY;
     if (masses)
@@ -200,22 +200,12 @@ __global__ __launch_bounds__(kPartThreads) void token_parts_kernel(const TokenPa
     // (a token that min_p keeps from being left in its part cannot be left in the row; where top-p counts it for the whole all the same, it is taken)
     int last = kBuckets - 1;
     if (mode == DRAW_MANY && !counts && f.p >= 1.0f) last = min(last, (int)(-0.6931472f * kBucketsPerUnit * __log2f(f.min_p)) + 2);
-    u64 whole = 0;
-    if (largest > -__builtin_inff()) {
+    if (mode == DRAW_ALL) {
+        u64 whole = 0;
 #pragma unroll
         for (int i = 0; i < LOADS; ++i)
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const int at = bucket_of(x[i][e], f.scale, top), place = at * kCopies + (lane & (kCopies - 1));
-                if (mode != DRAW_FEW && (mode == DRAW_ALL || at <= last)) {
-                    const u64 units = weight_units(x[i][e], largest, f.rate, kPartBits);
-                    if (mode == DRAW_ALL) whole += units;
-                    else atomicAdd(&mass[place], units);
-                }
-                if (counts && at <= last) atomicAdd(&count[place], 1u);
-            }
-    }
-    if (mode == DRAW_ALL) {
+            for (int e = 0; e < N; ++e) whole += weight_units(x[i][e], largest, f.rate, kPartBits);
         whole = wave_sum(whole);
         if (lane == 0) mass[w] = whole;
         __syncthreads();
@@ -224,6 +214,17 @@ __global__ __launch_bounds__(kPartThreads) void token_parts_kernel(const TokenPa
             p.mass[to] = whole;
         }
         return;
+    }
+    if (largest > -__builtin_inff()) {
+#pragma unroll
+        for (int i = 0; i < LOADS; ++i)
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                const int at = bucket_of(x[i][e], f.scale, top), place = at * kCopies + (lane & (kCopies - 1));
+                if (at > last) continue;
+                if (masses) atomicAdd(&mass[place], weight_units(x[i][e], largest, f.rate, kPartBits));
+                if (counts) atomicAdd(&count[place], 1u);
+            }
     }
     __syncthreads();
     static_assert(kBuckets == kPartThreads, "a bucket a thread");
@@ -436,7 +437,7 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
         for (int q = 4 * w + (lane >> 4); q < n_chunks; q += 4 * kDrawWaves) {
             const int unit = chunks[q] * 16 + (lane & 15);
             float x[N];
-            row.template values<true>(unit, row.request(unit), x);
+            row.values(unit, row.request(unit), x, [](float z) { return z; });
 #pragma unroll
             for (int e = 0; e < N; ++e)
                 if (x[e] >= gathered_from && x[e] <= gathered_to) body(rank_key<DT>(logit_value(x[e]), unit * N + e - row.skew));
@@ -514,7 +515,7 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
                 unsigned int in = 0;
 #pragma unroll
                 for (int i = 0; i < DEPTH; ++i) {
-                    row.template values<true>(unit[i], raw[i], x[i]);
+                    row.values(unit[i], raw[i], x[i], [](float z) { return z; });
                     unsigned int bits = 0;
 #pragma unroll
                     for (int e = 0; e < N; ++e) bits |= x[i][e] >= gathered_from && x[i][e] <= gathered_to ? 1u << (i * N + e) : 0u;
@@ -726,7 +727,7 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
 #pragma unroll
     for (int i = 0; i < LAST; ++i) raw[i] = row.request(at0 / N + i);
 #pragma unroll
-    for (int i = 0; i < LAST; ++i) row.values(at0 / N + i, raw[i], x[i]);
+    for (int i = 0; i < LAST; ++i) row.values(at0 / N + i, raw[i], x[i], [](float z) { return logit_value(z); });
 #pragma unroll
     for (int i = 0; i < kPartTokens / kDrawThreads; ++i) {
         const int v = at0 + i - row.skew;
