@@ -21,6 +21,7 @@ namespace quasar {
 constexpr int kPartTokens = 8192, kPartThreads = 512, kPartWaves = kPartThreads / 64, kPartLane = kPartTokens / kPartThreads;
 constexpr int kMaxTokenParts = ((1 << kIndexBits) + 7 + kPartTokens - 1) / kPartTokens;
 constexpr int kDrawThreads = 1024, kDrawWaves = kDrawThreads / 64;
+constexpr int kChunkTurn = 24;               // chunks that a wave reads at a time, at most
 constexpr int kListed = 3584;                // tokens of a bucket that are kept in LDS; more are read again where they are asked for
 
 struct TokenParams {
@@ -84,22 +85,28 @@ template <int DT> struct LogitRow {
     }
     __device__ __forceinline__ u32x4 request(int unit) const {
         if (last < first) return u32x4{0u, 0u, 0u, 0u};          // (the same for every lane)
-        return *reinterpret_cast<const u32x4 *>(border + 16ll * min(max(unit, first), last));
+        return *reinterpret_cast<const u32x4 *>(border + (unsigned int)(16 * min(max(unit, first), last)));    // (a row has at most 4 MB)
     }
     // the tokens of a requested unit as form(logit) has them; -inf where there are none
     template <class Form>
-    __device__ __forceinline__ void values(int unit, const u32x4 v, float (&x)[N], Form form) const {
+    __device__ __forceinline__ void as_whole(const u32x4 v, float (&x)[N], Form form) const {
 #pragma unroll
         for (int e = 0; e < N; ++e) {
             const float z = DT == 1 ? __uint_as_float(e & 1 ? v[DT == 1 ? e >> 1 : 0] & 0xFFFF0000u : v[DT == 1 ? e >> 1 : 0] << 16) : __uint_as_float(v[e & 3]);
             x[e] = form(z);
         }
-        if (unit < first || unit > last) {
+    }
+    template <class Form> __device__ __forceinline__ void values(int unit, const u32x4 v, float (&x)[N], Form form) const {
+        as_whole(v, x, form);
+        if (!whole(unit)) at_end(unit, x);
+    }
+    __device__ __forceinline__ bool whole(int unit) const { return unit >= first && unit <= last; }
+    __device__ __forceinline__ bool partial(int unit) const { return !whole(unit) && unit * N < skew + V; }     // (unit 0 has the row's first place, if any)
+    __device__ __forceinline__ void at_end(int unit, float (&x)[N]) const {
 #pragma unroll
-            for (int e = 0; e < N; ++e) {
-                const int at = unit * N + e;
-                x[e] = at >= skew && at < skew + V ? one(at - skew) : -__builtin_inff();
-            }
+        for (int e = 0; e < N; ++e) {
+            const int at = unit * N + e;
+            x[e] = at >= skew && at < skew + V ? one(at - skew) : -__builtin_inff();
         }
     }
 };
@@ -324,7 +331,7 @@ template <int DT>
 __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenParams p) {
     constexpr int N = lane_tokens<DT>, CHUNKS = part_chunks<DT>;
     constexpr int AHEAD = 4;                                     // chunks' largest logits of a thread that are requested at the start: of vocabularies up to 2^18 or 2^19 all
-    constexpr int DEPTH = 24 / N;                                // loads of a wave under way where chunks are read
+    constexpr int DEPTH = DT == 1 ? 4 : 6;                       // loads of a turn of a wave that reads chunks (a bit a token: 32 at most); two turns are under way
     constexpr u64 ALL = ~0ull;
     constexpr int kPairs = 512;                                  // tokens up to which each is compared with each
     extern __shared__ unsigned short chunks[];                   // that may hold some of the gathered buckets
@@ -502,24 +509,55 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
                 if (may) chunks[at + __popcll(mask & ((1ull << lane) - 1))] = (unsigned short)(tid + i * kDrawThreads);
             }
             __syncthreads();
+            // (to a whole number of a wave's turns, of chunks behind the last one, which hold nothing)
+            constexpr int TURN = 4 * DEPTH;
+            static_assert(TURN <= kChunkTurn, "room behind the chunks");
+            const int turns = (n_chunks + TURN - 1) / TURN;
+            if (tid < turns * TURN - n_chunks) chunks[n_chunks + tid] = (unsigned short)maxima;
+            __syncthreads();
+            const int in_chunk = lane & 15;
+            u32x4 next[DEPTH];
+            int next_unit[DEPTH];
+            auto ask = [&](int turn) {
+#pragma unroll
+                for (int i = 0; i < DEPTH; ++i) next_unit[i] = chunks[turn * TURN + 4 * i + (lane >> 4)] * 16 + in_chunk;
+#pragma unroll
+                for (int i = 0; i < DEPTH; ++i) next[i] = row.request(next_unit[i]);
+            };
+            if (w < turns) ask(w);
 #pragma unroll 1
-            for (int q0 = w * 4 * DEPTH; q0 < n_chunks; q0 += kDrawWaves * 4 * DEPTH) {
+            for (int turn = w; turn < turns; turn += kDrawWaves) {
+                const unsigned short *ids = chunks + turn * TURN + (lane >> 4);
                 u32x4 raw[DEPTH];
                 int unit[DEPTH];
 #pragma unroll
-                for (int i = 0; i < DEPTH; ++i) {
-                    unit[i] = chunks[min(q0 + 4 * i + (lane >> 4), n_chunks - 1)] * 16 + (lane & 15);
-                    raw[i] = row.request(unit[i]);
-                }
-                float x[DEPTH][N];
+                for (int i = 0; i < DEPTH; ++i) raw[i] = next[i], unit[i] = next_unit[i];
+                if (turn + kDrawWaves < turns) ask(turn + kDrawWaves);
                 unsigned int in = 0;
-#pragma unroll
-                for (int i = 0; i < DEPTH; ++i) {
-                    row.values(unit[i], raw[i], x[i], [](float z) { return z; });
+                bool ends = false;
+                auto between = [&](const float (&x)[N]) {
                     unsigned int bits = 0;
 #pragma unroll
-                    for (int e = 0; e < N; ++e) bits |= x[i][e] >= gathered_from && x[i][e] <= gathered_to ? 1u << (i * N + e) : 0u;
-                    if (q0 + 4 * i + (lane >> 4) < n_chunks) in |= bits;
+                    for (int e = 0; e < N; ++e) bits |= x[e] >= gathered_from && x[e] <= gathered_to ? 1u << e : 0u;
+                    return bits;
+                };
+#pragma unroll
+                for (int i = 0; i < DEPTH; ++i) {
+                    float x[N];
+                    row.as_whole(raw[i], x, [](float z) { return z; });
+                    const unsigned int bits = between(x) << (i * N);
+                    in |= row.whole(unit[i]) ? bits : 0u;
+                    ends |= row.partial(unit[i]);
+                }
+                if (__builtin_amdgcn_ballot_w64(ends)) {         // a row's first and last places
+#pragma unroll 1
+                    for (int i = 0; i < DEPTH; ++i) {
+                        const int u = ids[4 * i] * 16 + in_chunk;
+                        if (!row.partial(u)) continue;
+                        float x[N];
+                        row.at_end(u, x);
+                        in |= between(x) << (i * N);
+                    }
                 }
                 const int n = __popc(in), through = lane_sums_through(n), all = __builtin_amdgcn_readlane(through, 63);
                 if (!all) continue;
@@ -527,8 +565,8 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
                 if (lane == 0) at = atomicAdd(&n_listed, all);
                 at = __builtin_amdgcn_readfirstlane(at) + through - n;
                 for (; in; in &= in - 1, ++at) {                 // (as often as the lane that has most; the places alone: logits are indexed at compile time)
-                    const int bit = __builtin_ctz(in), q = q0 + 4 * (bit / N) + (lane >> 4);
-                    if (at < kListed) list[at] = (u64)((chunks[q] * 16 + (lane & 15)) * N + bit % N - row.skew);
+                    const int bit = __builtin_ctz(in);
+                    if (at < kListed) list[at] = (u64)((ids[4 * (bit / N)] * 16 + in_chunk) * N + bit % N - row.skew);
                 }
             }
             __syncthreads();

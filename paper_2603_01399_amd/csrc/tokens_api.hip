@@ -51,7 +51,7 @@ bool large_lds(const void *kernel, std::atomic<unsigned long long> &done) {
     if (hipGetDevice(&dev) != hipSuccess) return false;
     const unsigned long long bit = 1ull << (dev & 63);
     if (dev < 64 && (done.load() & bit)) return true;
-    if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, kMaxTokenParts * part_chunks<0> * (int)sizeof(unsigned short)) != hipSuccess) return false;
+    if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (kMaxTokenParts * part_chunks<0> + kChunkTurn) * (int)sizeof(unsigned short)) != hipSuccess) return false;
     if (dev < 64) done.fetch_or(bit);
     return true;
 }
@@ -59,7 +59,7 @@ bool large_lds(const void *kernel, std::atomic<unsigned long long> &done) {
 template <int DT>
 int launch_tokens(TokenParams p, const TokenRoom &room, int64_t T, hipStream_t st) {
     static std::atomic<unsigned long long> done{0};
-    const unsigned int chunks = (unsigned int)room.nb * part_chunks<DT> * sizeof(unsigned short);
+    const unsigned int chunks = ((unsigned int)room.nb * part_chunks<DT> + kChunkTurn) * sizeof(unsigned short);
     if (!large_lds(reinterpret_cast<const void *>(token_draw_kernel<DT>), done)) return QUASAR_ERR_HIP;
     for (int64_t row0 = 0; row0 < T; row0 += room.rows) {
         const unsigned int rows = (unsigned int)(T - row0 < room.rows ? T - row0 : room.rows);
