@@ -159,14 +159,15 @@ __device__ __forceinline__ int draw_mode(const Filters &f) {
 }
 
 // Grid (parts, rows).  A part's 16 tokens a thread stay in registers between its largest logit and the buckets.  What the row asks for is counted and nothing
-// else: the whole part's mass (ALL), counts (FEW), masses, and counts where there is a top-k (MANY).  The buckets lie four times in LDS, for the lanes 4 i + c each: a
-// wave's tokens share some dozens of buckets, and what meets in one is added one after the other.
-constexpr int kCopies = 4;
+// else: the whole part's mass (ALL), counts (FEW), masses, and counts where there is a top-k (MANY).  Bound by instructions: a compute unit does one for 64 tokens a
+// cycle, 0.25 us for each that is done for every token of 64 rows of 152 K.  64 rows more of fp32 logits take 7 us (FEW: 39 MB, 5.6 TB/s), 12 (ALL) and 21 (MANY), of which
+// exponentials of 25 instructions 5.  Tried: two, four or eight copies of the buckets in LDS for the lanes of a wave, fewer workgroups a compute unit, so that some load
+// while others compute: the same.
 template <int DT>
 __global__ __launch_bounds__(kPartThreads) void token_parts_kernel(const TokenParams p) {
     constexpr int N = lane_tokens<DT>, LOADS = kPartLane / N, CHUNKS = part_chunks<DT>;
-    __shared__ u64 mass[kBuckets * kCopies];
-    __shared__ unsigned int count[kBuckets * kCopies];
+    __shared__ u64 mass[kBuckets];
+    __shared__ unsigned int count[kBuckets];
     __shared__ float wave_largest[kPartWaves];
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), b = blockIdx.x, r = blockIdx.y;
     const LogitRow<DT> row(p, p.row0 + r);
@@ -182,10 +183,9 @@ __global__ __launch_bounds__(kPartThreads) void token_parts_kernel(const TokenPa
     for (int i = 0; i < LOADS; ++i) row.values(unit(i), raw[i], x[i], [](float z) { return logit_weighed(z); });
     const int mode = draw_mode(f);
     const bool counts = f.k != 0, masses = mode == DRAW_MANY;
-    if (masses)
-        for (int i = tid; i < kBuckets * kCopies; i += kPartThreads) mass[i] = 0;
-    if (counts)
-        for (int i = tid; i < kBuckets * kCopies; i += kPartThreads) count[i] = 0;
+    static_assert(kBuckets == kPartThreads, "a bucket a thread");
+    mass[tid] = 0;
+    count[tid] = 0;
     float largest = -__builtin_inff();
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
@@ -227,26 +227,15 @@ __global__ __launch_bounds__(kPartThreads) void token_parts_kernel(const TokenPa
         for (int i = 0; i < LOADS; ++i)
 #pragma unroll
             for (int e = 0; e < N; ++e) {
-                const int at = bucket_of(x[i][e], f.scale, top), place = at * kCopies + (lane & (kCopies - 1));
+                const int at = bucket_of(x[i][e], f.scale, top);
                 if (at > last) continue;
-                if (masses) atomicAdd(&mass[place], weight_units(x[i][e], largest, f.rate, kPartBits));
-                if (counts) atomicAdd(&count[place], 1u);
+                if (masses) atomicAdd(&mass[at], weight_units(x[i][e], largest, f.rate, kPartBits));
+                if (counts) atomicAdd(&count[at], 1u);
             }
     }
     __syncthreads();
-    static_assert(kBuckets == kPartThreads, "a bucket a thread");
-    if (masses) {
-        u64 sum = 0;
-#pragma unroll
-        for (int c = 0; c < kCopies; ++c) sum += mass[tid * kCopies + c];
-        p.mass[to + tid] = sum;
-    }
-    if (counts) {
-        unsigned int sum = 0;
-#pragma unroll
-        for (int c = 0; c < kCopies; ++c) sum += count[tid * kCopies + c];
-        p.count[to + tid] = sum;
-    }
+    if (masses) p.mass[to + tid] = mass[tid];
+    if (counts) p.count[to + tid] = count[tid];
 }
 
 // What the waves of a workgroup tell each other: a value a wave, combined by every wave.  One barrier: the places are taken in turn, and a place comes again
@@ -794,18 +783,20 @@ __global__ __launch_bounds__(256) void token_verify_kernel(const int32_t *row_st
     const int lane = threadIdx.x & 63, s = blockIdx.x * 4 + (threadIdx.x >> 6);
     if (s >= n_seqs) return;
     const SeqSpan a = span_of(row_start[s], row_start[s + 1], 0, T);
-    int n = 0;
+    int n = 0, drawn = -1;
     for (; n < a.n; n += 64) {
-        const bool goes_on = n + lane < a.n && accepted[a.row0 + n + lane] != 0;
+        const int at = min(n + lane, a.n - 1), candidate = token[a.row0 + at];   // (asked for together)
+        const bool goes_on = n + lane < a.n && accepted[a.row0 + at] != 0;
         const unsigned long long stops = ~__builtin_amdgcn_ballot_w64(goes_on);
         if (stops) {
+            drawn = __builtin_amdgcn_readlane(candidate, __builtin_ctzll(stops));
             n += __builtin_ctzll(stops);
             break;
         }
     }
     if (lane == 0) {
         out_accept_len[s] = a.n ? n : 0;
-        out_token[s] = a.n ? token[a.row0 + n] : -1;
+        out_token[s] = drawn;
     }
 }
 
