@@ -666,7 +666,7 @@ int quasar_pages_compact(int32_t *table, int64_t table_ld, int64_t n_seqs, int64
  *     out_token[s]       drawn with u_sample[t] of the row t behind them: without its draft's mass (norm(max(0, p - q))) where that was refused,
  *                        from the whole where the row is the last.  A sequence without rows, or whose row has nothing left: -1.
  *     out_p_draft        [T] fp32 (may be NULL): p_t(draft_ids[t]); rows of no sequence are left as they were.  Ids outside [0, V) have probability 0.
- * Results are determined by the arguments alone.  Two launches for every 512 rows, quasar_verify_tokens one more.  workspace: as many bytes as asked, 16-byte
+ * Results are determined by the arguments alone.  Two launches for every 512 rows.  workspace: as many bytes as asked, 16-byte
  * aligned, one call at a time.
  */
 size_t quasar_sample_tokens_workspace_bytes(int64_t T, int64_t V);   /* 0 on invalid arguments */

@@ -7,7 +7,7 @@
 //                        512 buckets of 1/16 (in units of the temperature) below the part's largest;
 //   token_draw_kernel    a workgroup a row: adds the parts' buckets up, finds the bucket in which a cut falls, gathers that bucket's tokens from the chunks
 //                        that can hold some, finds the cut among them digit by digit, and draws: from what each part has left, the part, then the token;
-//   token_verify_kernel  drafts: the leading accepted ones of each sequence, and the token that its first refusal (or last row) has drawn.
+//                        Of a sequence's rows with drafts the workgroup that is done last says how many of them are accepted, and what the row behind them has drawn.
 // Weights are whole numbers (token_math.hpp), sums of them exact, and what is added up in fp64 is added in a fixed order: results are determined by the
 // arguments alone.
 #pragma once
@@ -33,7 +33,8 @@ struct TokenParams {
     const float *u_accept, *u;
     int32_t *token;                              // [T]
     float *p;                                    // [T], of the token or of the draft; may be NULL
-    int32_t *accepted;                           // [T]: drafts: the row's is accepted
+    // drafts: a row's is accepted [T]; rows of a sequence that are done, and what it comes to [n_seqs]
+    int32_t *accepted, *done, *out_accept_len, *out_token;
     // of the rows of this launch
     float *part_max, *chunk_max;                 // [rows][nb], [rows][nb][chunks of a part]
     u64 *mass;                                   // [rows][nb][kBuckets]
@@ -46,19 +47,22 @@ template <int DT> constexpr int lane_tokens = DT == 1 ? 8 : 4;               // 
 template <int DT> constexpr int chunk_tokens = 16 * lane_tokens<DT>;         // of sixteen lanes' load: whose largest logit is kept
 template <int DT> constexpr int part_chunks = kPartTokens / chunk_tokens<DT>;
 
-// Whose parameters a row goes by (-1: nobody's row), and whether it is the last of its sequence.
-struct RowOf { int who; bool last; };
+// Whose parameters a row goes by (-1: nobody's row), and the rows of its sequence.
+struct RowOf {
+    int who, row0, n;
+    __device__ bool last(int row) const { return row == row0 + n - 1; }
+};
 __device__ __forceinline__ RowOf row_of(const TokenParams &p, int row) {
-    if (!p.row_start) return RowOf{row, true};
+    if (!p.row_start) return RowOf{row, row, 1};
     const int lane = threadIdx.x & 63;
     int s = 0;
     for (int i = 0; i < p.n_seqs; i += 64) {
         const bool before = i + lane < p.n_seqs && p.row_start[i + lane + 1] <= row;
         s += __popcll(__builtin_amdgcn_ballot_w64(before));
     }
-    if (s >= p.n_seqs) return RowOf{-1, true};
+    if (s >= p.n_seqs) return RowOf{-1, 0, 0};
     const SeqSpan a = span_of(p.row_start[s], p.row_start[s + 1], 0, p.T);
-    return row >= a.row0 && row < a.row0 + a.n ? RowOf{s, row == a.row0 + a.n - 1} : RowOf{-1, true};
+    return RowOf{row >= a.row0 && row < a.row0 + a.n ? s : -1, a.row0, a.n};
 }
 __device__ __forceinline__ Filters filters_at(const TokenParams &p, int who) {
     return filters_of(p.temperature ? p.temperature[who] : 1.0f, p.top_k ? p.top_k[who] : 0, p.top_p ? p.top_p[who] : 1.0f, p.min_p ? p.min_p[who] : 0.0f, p.V);
@@ -175,6 +179,8 @@ __global__ __launch_bounds__(kPartThreads) void token_parts_kernel(const TokenPa
     auto unit = [&](int i) { return b * (kPartTokens / N) + (w * LOADS + i) * 64 + lane; };
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) raw[i] = row.request(unit(i));
+    if (p.row_start && b == 0 && p.row0 + r == 0)                // (what sequences come to that no rows speak for)
+        for (int s = tid; s < p.n_seqs; s += kPartThreads) p.out_accept_len[s] = 0, p.out_token[s] = -1, p.done[s] = 0;
     const RowOf of = row_of(p, p.row0 + r);
     if (of.who < 0) return;
     const Filters f = filters_at(p, of.who);
@@ -338,7 +344,7 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
     __shared__ int n_chunks, n_listed, n_edge;
     __shared__ u64 chosen[3];
     __shared__ double drawn_total;
-    __shared__ int drawn_part, drawn_banned;
+    __shared__ int drawn_part, drawn_banned, drawn_token;
     const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), r = blockIdx.x, row_at = p.row0 + r;
     const int nb = p.nb, maxima = nb * CHUNKS;
     const LogitRow<DT> row(p, row_at);
@@ -355,20 +361,50 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
     const u64 mine_mass = tid < nb ? p.mass[((long long)r * nb + tid) * kBuckets] : 0;           // (of the whole part in DRAW_ALL)
     const float u_at = p.u[row_at];
     const int draft = p.draft ? p.draft[row_at] : -1;
+    const float u_accept = p.draft ? p.u_accept[row_at] : 0.0f;
     const RowOf of = row_of(p, row_at);
     if (of.who < 0) return;
+    const bool last_row = of.last(row_at);
     const Filters f = filters_at(p, of.who);
     const int mode = draw_mode(f);
     WaveTalk talk{talk_places, 0};
 
     // ---- the row's largest logit, and how the parts' buckets lie on its line
     most = wave_max(most);
-    if (!(most > -__builtin_inff())) {                           // nothing to draw from
-        if (tid == 0) {
-            p.token[row_at] = -1;
-            if (p.p) p.p[row_at] = 0.0f;
-            if (p.accepted) p.accepted[row_at] = 0;
+    // The row is done.  Drafts: the last of a sequence's rows to be done finds how many of them are accepted ahead of the first that is not.
+    auto finish = [&](int token, bool accepted) {                // (thread 0's arguments)
+        if (!p.row_start) {
+            if (tid == 0) p.token[row_at] = token;
+            return;
         }
+        if (tid == 0) {
+            p.token[row_at] = token;
+            p.accepted[row_at] = accepted;
+            n_edge = __hip_atomic_fetch_add(&p.done[of.who], 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == of.n - 1;
+        }
+        __syncthreads();
+        if (!n_edge || w) return;
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "agent");
+        int n = 0, drawn = -1;
+        for (; n < of.n; n += 64) {
+            const int at = of.row0 + min(n + lane, of.n - 1);
+            const int candidate = __hip_atomic_load(&p.token[at], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            const int goes_on = __hip_atomic_load(&p.accepted[at], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            const unsigned long long stops = __builtin_amdgcn_ballot_w64(n + lane >= of.n || !goes_on);
+            if (stops) {                                         // (a sequence's last row never goes on)
+                drawn = __builtin_amdgcn_readlane(candidate, __builtin_ctzll(stops));
+                n += __builtin_ctzll(stops);
+                break;
+            }
+        }
+        if (lane == 0) {
+            p.out_accept_len[of.who] = n;
+            p.out_token[of.who] = drawn;
+        }
+    };
+    if (!(most > -__builtin_inff())) {                           // nothing to draw from
+        if (tid == 0 && p.p) p.p[row_at] = 0.0f;
+        finish(-1, false);
         return;
     }
     const float top = bucket_line(most, f.scale);
@@ -681,6 +717,7 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
         __syncthreads();
     }
     // ---- a refused draft is left out; the part that the draw falls in: the first whose running mass exceeds it, else the last that has any
+    bool accepted = false;
     if (w == 0) {
         constexpr int EACH = (kMaxTokenParts + 63) / 64;
         const int per = (nb + 63) / 64;
@@ -701,11 +738,9 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
         double whole = add_up();
         if (p.draft) {
             const double of_draft = (double)draft_units * factor[draft_part] / whole;
-            if (lane == 0) {
-                if (p.p) p.p[row_at] = (float)of_draft;
-                p.accepted[row_at] = !of.last && (double)p.u_accept[row_at] < of_draft;
-            }
-            if (!of.last && draft_units) {
+            if (lane == 0 && p.p) p.p[row_at] = (float)of_draft;
+            accepted = !last_row && (double)u_accept < of_draft;
+            if (!last_row && draft_units) {
 #pragma unroll
                 for (int i = 0; i < EACH; ++i)
                     if (i < per && lane * per + i == draft_part) units[i] -= draft_units;
@@ -715,7 +750,7 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
         const double target = u_at > 0.0f ? (double)u_at * whole : 0.0;
         const unsigned long long mass = __builtin_amdgcn_ballot_w64(sum > 0.0), reach = __builtin_amdgcn_ballot_w64(sum > 0.0 && through > target);
         const int owner = mass ? draw_lane(reach, mass) : -1;
-        if (lane == 0) drawn_part = -1, drawn_total = whole, drawn_banned = !of.last ? draft : -1;
+        if (lane == 0) drawn_part = -1, drawn_total = whole, drawn_banned = !last_row ? draft : -1;
         if (lane == owner) {
             double ahead = through - sum;
             int part = -1;
@@ -737,10 +772,7 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
     __syncthreads();
     const int part = drawn_part;
     if (part < 0) {                                              // (all mass was the draft's)
-        if (tid == 0) {
-            p.token[row_at] = -1;
-            if (p.p && !p.draft) p.p[row_at] = 0.0f;
-        }
+        finish(-1, accepted);
         return;
     }
     // ---- the token: eight places a thread, in order
@@ -769,35 +801,14 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
 #pragma unroll
         for (int i = 0; i < kPartTokens / kDrawThreads; ++i) {
             if (at <= ahead && at + units[i] > ahead) {
-                p.token[row_at] = at0 + i - row.skew;
+                drawn_token = at0 + i - row.skew;
                 if (p.p && !p.draft) p.p[row_at] = (float)((double)units[i] * factor[part] / drawn_total);
             }
             at += units[i];
         }
     }
-}
-
-// A wave a sequence: how many of its drafts are accepted ahead of the first refusal, and what the row behind them has drawn.
-__global__ __launch_bounds__(256) void token_verify_kernel(const int32_t *row_start, int n_seqs, int T, const int32_t *accepted, const int32_t *token,
-                                                           int32_t *out_accept_len, int32_t *out_token) {
-    const int lane = threadIdx.x & 63, s = blockIdx.x * 4 + (threadIdx.x >> 6);
-    if (s >= n_seqs) return;
-    const SeqSpan a = span_of(row_start[s], row_start[s + 1], 0, T);
-    int n = 0, drawn = -1;
-    for (; n < a.n; n += 64) {
-        const int at = min(n + lane, a.n - 1), candidate = token[a.row0 + at];   // (asked for together)
-        const bool goes_on = n + lane < a.n && accepted[a.row0 + at] != 0;
-        const unsigned long long stops = ~__builtin_amdgcn_ballot_w64(goes_on);
-        if (stops) {
-            drawn = __builtin_amdgcn_readlane(candidate, __builtin_ctzll(stops));
-            n += __builtin_ctzll(stops);
-            break;
-        }
-    }
-    if (lane == 0) {
-        out_accept_len[s] = a.n ? n : 0;
-        out_token[s] = drawn;
-    }
+    __syncthreads();
+    finish(drawn_token, accepted);
 }
 
 }  // namespace quasar

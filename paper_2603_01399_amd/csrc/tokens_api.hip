@@ -21,7 +21,7 @@ constexpr int64_t kRowsAtOnce = 512;
 
 struct TokenRoom {
     int64_t nb, rows;
-    size_t mass, count, chunk_max, part_max, rows_out;
+    size_t mass, count, chunk_max, part_max, rows_out, done;
     TokenRoom(int64_t T, int64_t V, bool drafts) {
         nb = (V + 7 + kPartTokens - 1) / kPartTokens;            // (a row may begin seven places behind a 16-byte border)
         rows = T < kRowsAtOnce ? T : kRowsAtOnce;
@@ -30,8 +30,9 @@ struct TokenRoom {
         chunk_max = (size_t)(rows * nb) * part_chunks<0> * 4;            // (fp32's chunks are the smaller ones)
         part_max = ((size_t)(rows * nb) * 4 + 15) & ~(size_t)15;
         rows_out = drafts ? ((size_t)T * 4 + 15) & ~(size_t)15 : 0;
+        done = drafts ? kMaxSeqs * 4 : 0;
     }
-    size_t bytes() const { return mass + count + chunk_max + part_max + 2 * rows_out; }
+    size_t bytes() const { return mass + count + chunk_max + part_max + 2 * rows_out + done; }
 };
 bool token_shape(int64_t T, int64_t V) { return T >= 1 && T <= kMaxTokenRows && V >= 1 && V <= kMaxVocabulary; }
 
@@ -86,6 +87,7 @@ int run_tokens(TokenParams &p, int dtype, const TokenRoom &room, int64_t T, void
     if (room.rows_out) {
         p.token = reinterpret_cast<int32_t *>(take(room.rows_out));
         p.accepted = reinterpret_cast<int32_t *>(take(room.rows_out));
+        p.done = reinterpret_cast<int32_t *>(take(room.done));
     }
     p.nb = (int)room.nb;
     return dtype == QUASAR_BF16 ? launch_tokens<1>(p, room, T, st) : launch_tokens<0>(p, room, T, st);
@@ -128,10 +130,8 @@ int quasar_verify_tokens(const void *logits, int logits_dtype, int64_t T, int64_
     if (!aligned(out_accept_len, 4) || !aligned(out_token, 4)) return QUASAR_ERR_ALIGN;
     p.V = (int)V; p.T = (int)T; p.n_seqs = (int)n_seqs;
     hipStream_t st = static_cast<hipStream_t>(hip_stream);
-    if (const int e = run_tokens(p, logits_dtype, room, T, workspace, st)) return e;
-    hipLaunchKernelGGL(token_verify_kernel, dim3((unsigned int)((n_seqs + 3) / 4)), dim3(256), 0, st, row_start, (int)n_seqs, (int)T, p.accepted, p.token,
-                       out_accept_len, out_token);
-    return launched();
+    p.out_accept_len = out_accept_len; p.out_token = out_token;
+    return run_tokens(p, logits_dtype, room, T, workspace, st);
 }
 
 }  // extern "C"
