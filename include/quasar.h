@@ -624,8 +624,8 @@ int quasar_prompt_attention_window(const uint16_t *q, int64_t T, int64_t ldq, in
  *   another one forks or moves it, -1 (or anything that is no row) frees it.  refs follow.  No page is copied.  Two launches.
  * quasar_pages_trim     gives pages back that no row at position lengths[s] or behind sees in a layer of this window and sinks: columns c of the table with
  *   c * page_len >= sinks and (c + 1) * page_len <= lengths[s] - window + 1 become -1, refs follow.  For caches all of whose layers have a window, the longest
- *   of which is given, and behind the step: a sequence that is cut back afterwards (quasar_pages_fork) may be left with rows that miss pages.
- *   One launch.
+ *   of which is given, and behind the step: a sequence is not to be cut back (quasar_pages_fork) to fewer positions than it had here, since what its
+ *   rows would see is gone.  One launch.
  * quasar_pages_compact  with n pages in use (refs > 0), the i-th in use at n and beyond moves, in all layers, to the i-th free page below n; table
  *   and refs follow; out_to [n_pages] says where each page went (pages that did not move: themselves).  Two launches.
  */

@@ -782,7 +782,8 @@ class PagedKvCache:
                                       _stream()))
 
     def trim(self, window: int, sinks: int = 0) -> None:
-        """Gives the pages back that no row to come sees anything of, in layers of this window (the longest one's) and sinks."""
+        """Gives the pages back that no row to come sees anything of, in layers of this window (the longest one's) and sinks.  Behind a step: what is
+        cut back to fewer positions than it has here misses pages."""
         status = _fast.pages_trim(self._handle, window, sinks)
         if status >= 0:
             return _check("quasar_pages_trim", status)

@@ -209,3 +209,12 @@ def test_binding_refuses_host_tensors():
         qb.sample_tokens(z, u)
     with pytest.raises(TypeError):
         qb.verify_tokens(z, torch.zeros(2, dtype=torch.int32), torch.zeros(2, dtype=torch.int32), u, u)
+
+
+def test_native_calls_without_a_gpu_or_enough_arguments():
+    from paper_2603_01399_amd import binding as qb
+    z, u = torch.zeros(2, 8), torch.zeros(2)
+    assert qb._fast.sample_tokens(z, u, None, None, None, None) == -1 and qb._fast.sample_tokens() == -1 and qb._fast.sample_tokens(None, u, None, None, None, None) == -1
+    assert qb._fast.verify_tokens(z, u.int(), u.int(), u, u, None, None, None, None) == -1 and qb._fast.verify_tokens(z, u) == -1
+    for call in (qb._fast.paged_prepare_rope, qb._fast.paged_attention_window, qb._fast.prompt_attention_window, qb._fast.pages_trim):
+        assert call() == -1 and call(None) == -1

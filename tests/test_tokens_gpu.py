@@ -190,6 +190,20 @@ def test_many_rows(qb):
         check_draw(host[i], u[i], int(token[i]), p[i], V, **as_seen(rows[i]))
 
 
+def test_logits_of_more_than_4_gb(qb):
+    """Rows behind the 2^32nd byte and the 2^31st logit; equal logits of 2^k tokens have equal shares, exactly."""
+    say("4 GB of logits")
+    V, T = 131072, 17000
+    z = torch.zeros(T, V, dtype=torch.bfloat16, device="cuda")
+    r = np.random.Generator(np.random.Philox(17))
+    z[-3:] = dev(logits_of(r, 3, V), torch.float32).bfloat16()
+    u = (torch.arange(T, device="cuda") % 4096 + 0.5) / 4096
+    token, p = qb.sample_tokens(z, u)
+    assert torch.equal(token[:-3], (u[:-3] * V).int()) and (p[:-3] == 1 / V).all()
+    for i in range(T - 3, T):
+        check_draw(seen(z[i]), float(u[i]), int(token[i]), p[i], V)
+
+
 def test_the_draw_follows_the_distribution(qb):
     """Numbers on a grid give every token its share: the inverse CDF, through all steps of a draw."""
     say("shares")
@@ -262,6 +276,21 @@ def test_verify(qb, dtype, V, news):
         ua, us = r.random(T).astype(np.float32) * np.float32(0.5), r.random(T).astype(np.float32)
         some += check_verify(qb, z, starts, drafts, ua, us, [as_seen(f) for f in seqs], params(seqs))
     assert V < 200 or max(some) > 0
+
+
+def test_verify_of_more_rows_than_are_in_the_workspace_at_a_time(qb):
+    """Sequences whose rows lie in one launch's rows, in two, in three."""
+    say("many rows of drafts")
+    r = np.random.Generator(np.random.Philox(16))
+    V, news = 300, [300, 0, 400, 1, 1100, 7]
+    starts = np.concatenate([[0], np.cumsum(news)])
+    T = int(starts[-1])
+    z = dev(logits_of(r, T, V), torch.float32)
+    seqs = [FILTERS[i] for i in (0, 4, 13, 8, 13, 12)]
+    drafts = seen(z).argmax(1)
+    ua, us = np.zeros(T, np.float32), r.random(T).astype(np.float32)
+    ua[[150, 1700]] = 1.0
+    assert check_verify(qb, z, starts, drafts, ua, us, [as_seen(f) for f in seqs], params(seqs)) == [150, 0, 399, 0, 999, 6]
 
 
 def test_verify_of_odd_drafts_and_rows(qb):
@@ -398,3 +427,27 @@ def test_refusals_of_the_binding(qb):
             qb.verify_tokens(**(dict(logits=z, row_start=starts, draft_ids=ids, u_accept=u, u_sample=u) | bad))
     with pytest.raises(qb.QuasarError):
         qb.sample_tokens(torch.zeros(1, (1 << 20) + 1, device="cuda"), u[:1])
+
+
+class _Sub(torch.Tensor):
+    pass
+
+
+def test_calls_that_are_not_ordinary(qb):
+    """What the native side leaves to the Python path has the same bits; what it takes is what the public functions give."""
+    say("not ordinary")
+    r = np.random.Generator(np.random.Philox(18))
+    T, V = 4, 5000
+    z, u = dev(logits_of(r, T, V), torch.float32), dev(r.random(T), torch.float32)
+    f, pair = params([FILTERS[12]] * T), params([FILTERS[12]] * 2)
+    starts, ids = dev([0, 3, 4], torch.int32), z.argmax(1).int()
+    sample, verify = (z, u, *f.values()), (z, starts, ids, u, u, *pair.values())
+    for native, args, public in ((qb._fast.sample_tokens, sample, qb.sample_tokens(z, u, **f)), (qb._fast.verify_tokens, verify, qb.verify_tokens(z, starts, ids, u, u, **pair))):
+        assert all(torch.equal(a, b) for a, b in zip(native(*args), public))
+        assert native(*args[:-1]) == -1 and native(*args, None) == -1
+        for i in range(len(args)):
+            assert native(*args[:i], args[i].cpu(), *args[i + 1:]) == -1 and native(*args[:i], "x", *args[i + 1:]) == -1
+    sub = z.as_subclass(_Sub)
+    assert qb._fast.sample_tokens(sub, *sample[1:]) == -1 and qb._fast.verify_tokens(sub, *verify[1:]) == -1
+    assert all(torch.equal(a, b) for a, b in zip(qb.sample_tokens(sub, u, **f), qb.sample_tokens(z, u, **f)))
+    assert all(torch.equal(a, b) for a, b in zip(qb.verify_tokens(sub, starts, ids, u, u, **pair), qb.verify_tokens(z, starts, ids, u, u, **pair)))

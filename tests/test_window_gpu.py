@@ -300,3 +300,58 @@ def test_a_windowed_run_of_steps_in_few_pages(qb):
         assert torch.equal(out[0], out[2]) and torch.equal(out[1], out[3]) and torch.isfinite(out[0]).all()
         peak = max(peak, int((small.refs > 0).sum()))
     assert int(large.lengths.min()) > 200 and peak <= seqs * 4
+
+
+class _Sub(torch.Tensor):
+    pass
+
+
+def test_calls_that_are_not_ordinary(qb):
+    """What the native side leaves to the Python path has the same bits."""
+    say("not ordinary")
+    b = Batch(qb, "bf16", 64, 8, 2, [100, 700], [2, 5], seed=42)
+    q, sub = b.q(), b.q().as_subclass(_Sub)
+    assert qb._fast.paged_attention_window(b.cache._handle, sub, 8, 0, b.row_start, 5, 90, 3, None, None) == -1
+    assert qb._fast.prompt_attention_window(b.cache._handle, sub, 8, 0, b.row_start, 90, 3, None) == -1
+    for args in ((5, 0, 0), (5, 90, -1), (5, 90.0, 3), (5, True, 3)):
+        assert qb._fast.paged_attention_window(b.cache._handle, q, 8, 0, b.row_start, *args, None, None) == -1
+        assert qb._fast.prompt_attention_window(b.cache._handle, q, 8, 0, b.row_start, *args[1:], None) == -1
+    w = dict(window=90, sinks=3)
+    assert torch.equal(qb.paged_attention(sub, 8, b.cache, 0, b.row_start, 5, **w), qb.paged_attention(q, 8, b.cache, 0, b.row_start, 5, **w))
+    assert torch.equal(qb.prompt_attention(sub, 8, b.cache, 0, b.row_start, **w), qb.prompt_attention(q, 8, b.cache, 0, b.row_start, **w))
+    qkv = torch.randn(7, 12 * D, device="cuda").bfloat16()
+    rope = qb.Rope(32, 1e4)
+    append = lambda x: qb.paged_prepare(x, 8, b.cache, 0, b.row_start, None, None, rope=rope)
+    assert torch.equal(append(qkv.as_subclass(_Sub)), append(qkv))
+    before = b.cache.table.clone()
+    assert qb._fast.pages_trim(b.cache._handle, 0, 0) == -1 and qb._fast.pages_trim(b.cache._handle, 90, -1) == -1 and torch.equal(before, b.cache.table)
+
+
+def test_forks_and_moves_of_trimmed_sequences(qb):
+    """A trimmed sequence is forked, steps on twice over, and its pages move: every output is that of a cache which keeps everything."""
+    say("forks of trimmed")
+    hq, hk, page, window, sinks = 4, 1, 32, 40, 2
+    small, large = (qb.PagedKvCache(1, hk, n, page_len=page, max_seqs=3, max_pages=30) for n in (24, 90))
+    rope = qb.Rope(128, 1e4)
+
+    def step(news, seed):
+        starts, new = i32_to_dev(np.concatenate([[0], np.cumsum(news)])), i32_to_dev(news)
+        qkv = torch.randn(sum(news), (hq + 2 * hk) * D, device="cuda", generator=torch.Generator("cuda").manual_seed(seed)).bfloat16()
+        outs = []
+        for cache in (small, large):
+            assert cache.reserve(new).tolist() == [1] * 3
+            q = qb.paged_prepare(qkv, hq, cache, 0, starts, None, None, rope=rope)
+            outs.append(qb.prompt_attention(q, hq, cache, 0, starts, window=window, sinks=sinks))
+            cache.lengths.add_(new)
+        small.trim(window, sinks)
+        assert torch.equal(*outs) and torch.isfinite(outs[0]).all()
+    step([200, 0, 250], 1)
+    for turn, parent in enumerate(([0, 0, 2], [2, 1, 2], [1, 0, 0])):
+        for cache in (small, large):
+            cache.fork(i32_to_dev(parent))
+        for i in range(4):
+            step([7, 20, 1], 10 * turn + i + 2)
+        small.compact()
+        held = np.bincount(small.table.cpu().numpy()[small.table.cpu().numpy() >= 0], minlength=24)
+        assert (small.refs.cpu().numpy() == held).all()
+    assert int(large.lengths.max()) > 300 and (small.table[:, 1:4] == -1).all()
