@@ -470,8 +470,9 @@ int quasar_pages_trim(int32_t *table, int64_t table_ld, int64_t n_seqs, int64_t 
     if (const int e = check_books(table_ld, n_seqs, max_pages, n_pages, page_len)) return e;
     if (!aligned(table, 4) || !aligned(lengths, 4) || !aligned(refs, 4)) return QUASAR_ERR_ALIGN;
     const BooksParams b = books(table, table_ld, n_seqs, max_pages, const_cast<int32_t *>(lengths), refs, n_pages, page_len);
-    const unsigned int parts = (unsigned int)((max_pages + kTrimColumns - 1) / kTrimColumns);
-    hipLaunchKernelGGL(pages_trim_kernel, dim3((unsigned int)n_seqs, parts < 64 ? parts : 64), dim3(256), 0, static_cast<hipStream_t>(hip_stream), b, w);
+    const int64_t parts = (max_pages + kTrimThreads - 1) / kTrimThreads;
+    hipLaunchKernelGGL(pages_trim_kernel, dim3((unsigned int)((n_seqs + kTrimSeqs - 1) / kTrimSeqs), (unsigned int)(parts < 64 ? parts : 64)), dim3(kTrimThreads), 0,
+                       static_cast<hipStream_t>(hip_stream), b, w);
     return launched();
 }
 

@@ -205,29 +205,39 @@ __global__ __launch_bounds__(1024) void pages_fork_lengths_kernel(const BooksPar
 }
 
 // ---------------------------------------------------------------------------------------------
-// Gives pages back that no row to come sees anything of: those behind the first tokens and ahead of the window of the next token.  A sequence's columns
-// in stretches of kTrimColumns, four of them requested at a time.
+// Gives pages back that no row to come sees anything of: those behind the first tokens and ahead of the window of the next token.  A thread has a column of
+// neighbouring sequences, whose ids are requested together; a page that several of them share is taken from its count once.  Bound by the counts' atomics, 25 a ns,
+// where there are many: 200 sequences of 100000 positions in pages of 32 that are forks of each other 10 us (a thread a column: 61), of pairs 12.9 (16.4), of
+// no other's 26.5 (24).  With four sequences a thread 17, 12.5 and 25.  Else by the launch and three trips to memory.
 // ---------------------------------------------------------------------------------------------
-constexpr int kTrimColumns = 1024;
+constexpr int kTrimThreads = 256, kTrimSeqs = 8;
 
-__global__ __launch_bounds__(256) void pages_trim_kernel(const BooksParams b, const Window window) {
-    const int s = blockIdx.x, len = b.lengths[s];
-    if (len < 0 || len > kMaxPositions) return;
-    const Columns gone = columns_behind(window, len, b.block_shift + kBlockShift);
-    const int end = min(gone.end, b.columns);
-    int32_t *row = b.table + s * b.table_ld;
-    for (long long c0 = gone.begin + (long long)blockIdx.y * kTrimColumns; c0 < end; c0 += (long long)gridDim.y * kTrimColumns) {
-        int id[4];
+__global__ __launch_bounds__(kTrimThreads) void pages_trim_kernel(const BooksParams b, const Window window) {
+    const int s0 = blockIdx.x * kTrimSeqs;
+    int begin = 0, end[kTrimSeqs], furthest = 0;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int col = (int)c0 + 256 * i + threadIdx.x;
-            id[i] = col < end ? row[col] : -1;
-        }
+    for (int i = 0; i < kTrimSeqs; ++i) {
+        const int len = s0 + i < b.n_seqs ? b.lengths[s0 + i] : -1;
+        const Columns gone = columns_behind(window, len, b.block_shift + kBlockShift);
+        begin = gone.begin;                                      // (the same for all)
+        end[i] = len < 0 || len > kMaxPositions ? 0 : min(gone.end, b.columns);
+        furthest = max(furthest, end[i]);
+    }
+    int32_t *rows = b.table + s0 * b.table_ld;
+    for (long long col = begin + (long long)blockIdx.y * kTrimThreads + threadIdx.x; col < furthest; col += (long long)gridDim.y * kTrimThreads) {
+        int id[kTrimSeqs];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            if (id[i] < 0) continue;
-            row[(int)c0 + 256 * i + threadIdx.x] = -1;
-            if (is_page(b, id[i])) atomicSub(&b.refs[id[i]], 1);
+        for (int i = 0; i < kTrimSeqs; ++i) id[i] = col < end[i] ? rows[i * b.table_ld + col] : -1;
+#pragma unroll
+        for (int i = 0; i < kTrimSeqs; ++i)
+            if (id[i] >= 0) rows[i * b.table_ld + col] = -1;
+#pragma unroll
+        for (int i = 0; i < kTrimSeqs; ++i) {
+            int n = 1;
+#pragma unroll
+            for (int k = i + 1; k < kTrimSeqs; ++k)
+                if (id[k] == id[i]) ++n, id[k] = -1;
+            if (id[i] >= 0 && is_page(b, id[i])) atomicSub(&b.refs[id[i]], n);
         }
     }
 }

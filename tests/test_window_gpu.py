@@ -260,6 +260,23 @@ def test_trim(qb, page, seqs, columns, window, sinks):
         assert c.refs.tolist() == want_refs and c.table.tolist() == want_table and c.lengths.tolist() == lengths.tolist()
 
 
+@pytest.mark.parametrize("seqs,parents", [(2, 1), (9, 1), (29, 2), (64, 5), (1024, 3)])
+def test_trim_of_forks(qb, seqs, parents):
+    """Pages that many sequences share, in neighbouring rows and others, of different lengths."""
+    say("trim, forks", seqs, parents)
+    r = np.random.Generator(np.random.Philox(seqs))
+    columns, page = 300, 32
+    table = r.permutation(parents * columns).reshape(parents, columns)[np.sort(r.integers(0, parents, seqs)) if seqs < 64 else r.integers(0, parents, seqs)]
+    lengths = r.integers(columns * page // 2, columns * page + 1, seqs)
+    table = np.where(np.arange(columns) * page < lengths[:, None], table, -1)
+    refs = np.bincount(table[table >= 0], minlength=parents * columns)
+    c = qb.PagedKvCache(1, 1, parents * columns, page_len=page, max_seqs=seqs, max_pages=columns)
+    c.refs.copy_(i32_to_dev(refs)); c.lengths.copy_(i32_to_dev(lengths)); c.table.copy_(i32_to_dev(table))
+    want_refs, want_table = win.trim(refs.tolist(), lengths.tolist(), table.tolist(), page, 700, 40)
+    c.trim(700, 40)
+    assert c.refs.tolist() == want_refs and c.table.tolist() == want_table
+
+
 def test_trim_leaves_odd_books(qb):
     """Lengths that are none leave their rows; ids beyond the pool go without touching a count."""
     say("trim, odd books")
