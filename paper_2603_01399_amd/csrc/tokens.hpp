@@ -328,14 +328,14 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
     constexpr int AHEAD = 4;                                     // chunks' largest logits of a thread that are requested at the start: of vocabularies up to 2^18 or 2^19 all
     constexpr int DEPTH = DT == 1 ? 4 : 6;                       // loads of a turn of a wave that reads chunks (a bit a token: 32 at most); two turns are under way
     constexpr u64 ALL = ~0ull;
-    constexpr int kPairs = 512;                                  // tokens up to which each is compared with each
+    constexpr int kPairs = 128;                                  // tokens up to which each is compared with each (of 16 bytes from LDS a pair: 512 tokens take 15 us, a digit 3)
     extern __shared__ unsigned short chunks[];                   // that may hold some of the gathered buckets
     __shared__ double bucket_mass[kBuckets], through_mass[kBuckets];
     __shared__ unsigned int through_count[kBuckets];
     __shared__ u64 list[kListed];                                // rank keys of the gathered tokens, in no order
     __shared__ u64 bin_mass[kDrawThreads];
     __shared__ unsigned int bin_count[kDrawThreads];
-    __shared__ u64 edge[kPairs];                                 // those among which the cut lies
+    __shared__ u64 edge[kPairs + 16];                                //  those among which the cut lies
     __shared__ double factor[kMaxTokenParts];                    // of a part's units in the row's
     __shared__ u64 part_mass[kMaxTokenParts];
     __shared__ float part_max[kMaxTokenParts];
@@ -653,7 +653,7 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
                 before = chosen[0];
                 inside = (int)chosen[1];
             }
-            if (inside > 1 && lo < hi) {                         // each is compared with each, two or four lanes to a token
+            if (inside > 1 && lo < hi) {                         // each is compared with each, four lanes to a token
                 if (tid == 0) n_edge = 0, chosen[2] = hi;
                 __syncthreads();
                 each([&](u64 key) {
@@ -662,15 +662,22 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
                     if (at < kPairs) edge[at] = key;             // (there are no more)
                 });
                 __syncthreads();
-                const int n = min(n_edge, kPairs), share = n <= kDrawThreads / 4 ? 2 : 1, mine = tid >> share, part = tid & ((1 << share) - 1);
+                const int n = min(n_edge, kPairs), mine = tid / 4, part = tid % 4;
                 if (tid < n) bin_mass[tid] = by_mass ? weight_units(key_value<DT>(edge[tid]), ref, f.rate, kListBits) : 1;
+                else if (tid < n + 16) edge[tid] = ALL;          // (ahead of none)
                 __syncthreads();
-                if ((n << share) > (tid & ~63)) {                // (whole waves)
+                if (4 * n > (tid & ~63)) {                       // (whole waves)
                     const u64 key = mine < n ? edge[mine] : ALL;
                     u64 ahead = 0;
-                    for (int i = part; i < n; i += 1 << share)
-                        if (edge[i] < key) ahead += bin_mass[i];
-                    for (int off = 1; off < 1 << share; off <<= 1) ahead += __shfl_xor(ahead, off, 64);
+                    for (int i = part; i < n; i += 16) {
+                        u64 other[4], units[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) other[e] = edge[i + 4 * e], units[e] = bin_mass[i + 4 * e];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) ahead += other[e] < key ? units[e] : 0;
+                    }
+                    ahead += __shfl_xor(ahead, 1, 64);
+                    ahead += __shfl_xor(ahead, 2, 64);
                     ahead += before;
                     if (mine < n && part == 0 && ahead < want && ahead + bin_mass[mine] >= want) chosen[2] = key;     // (one of them, or none: all are in)
                 }
