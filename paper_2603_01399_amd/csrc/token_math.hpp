@@ -36,22 +36,32 @@ QUASAR_BOTH double double_of(u64 u) {
     memcpy(&x, &u, 8);
     return x;
 }
-// 2^y for -1000 < y < 1000: y's nearest whole number, by the sum with 1.5 2^52, goes to the exponent; 2^f of the rest, |f| <= 1/2, by the polynomial of degree ten that
-// meets it at the Chebyshev points of the interval: off by at most 2^-51.5 of it.  extra: added to the exponent.
-QUASAR_BOTH double exp2_by(double y, int extra) {
-    const double t = y + 0x1.8p52, f = y - (t - 0x1.8p52);
+// A constant, SCALAR: in a scalar register pair on the GPU, which a multiply-add takes as it is.  Else the compiler copies each into vector registers where it is
+// used, two instructions beside every multiply-add.  That costs where many tokens' weights bound a kernel (64 rows of 151936 logits without filters 26.1 us, and 25.2
+// so), not where a few wait for one another (one row 12.3, and 12.8 so).
+template <bool SCALAR> QUASAR_BOTH double constant(double c) {
+#ifdef __HIP_DEVICE_COMPILE__
+    if (SCALAR) asm("" : "+s"(c));
+#endif
+    return c;
+}
+// 2^(y + extra) for -1000 < y < 1000: y's nearest whole number, by the sum with 1.5 2^52 (and extra), goes to the exponent; 2^f of the rest, |f| <= 1/2, by the
+// polynomial of degree ten that meets it at the Chebyshev points of the interval: off by at most 2^-51.5 of it.
+template <bool SCALAR = false> QUASAR_BOTH double exp2_by(double y, int extra) {
+    const double whole = 0x1.8p52 + (double)extra, t = y + whole, f = y - (t - whole);
     double r = 0x1.e6063f7217bc6p-28;
-    r = __builtin_fma(r, f, 0x1.b675bca4eeebbp-24);
-    r = __builtin_fma(r, f, 0x1.62bfd47773353p-20);
-    r = __builtin_fma(r, f, 0x1.ffcb54062e698p-17);
-    r = __builtin_fma(r, f, 0x1.430913096fd9fp-13);
-    r = __builtin_fma(r, f, 0x1.5d87fe9d7a584p-10);
-    r = __builtin_fma(r, f, 0x1.3b2ab6fba1ddap-7);
-    r = __builtin_fma(r, f, 0x1.c6b08d703ce49p-5);
-    r = __builtin_fma(r, f, 0x1.ebfbdff82c598p-3);
-    r = __builtin_fma(r, f, 0x1.62e42fefa3a19p-1);
+    r = __builtin_fma(r, f, constant<SCALAR>(0x1.b675bca4eeebbp-24));
+    r = __builtin_fma(r, f, constant<SCALAR>(0x1.62bfd47773353p-20));
+    r = __builtin_fma(r, f, constant<SCALAR>(0x1.ffcb54062e698p-17));
+    r = __builtin_fma(r, f, constant<SCALAR>(0x1.430913096fd9fp-13));
+    r = __builtin_fma(r, f, constant<SCALAR>(0x1.5d87fe9d7a584p-10));
+    r = __builtin_fma(r, f, constant<SCALAR>(0x1.3b2ab6fba1ddap-7));
+    r = __builtin_fma(r, f, constant<SCALAR>(0x1.c6b08d703ce49p-5));
+    r = __builtin_fma(r, f, constant<SCALAR>(0x1.ebfbdff82c598p-3));
+    r = __builtin_fma(r, f, constant<SCALAR>(0x1.62e42fefa3a19p-1));
     r = __builtin_fma(r, f, 1.0);
-    return double_of(bits_of(r) + ((u64)((uint32_t)bits_of(t) + (uint32_t)extra) << 52));
+    const u64 at = bits_of(r);
+    return double_of((u64)((uint32_t)(at >> 32) + ((uint32_t)bits_of(t) << 20)) << 32 | (uint32_t)at);
 }
 // exp((z - ref) / temperature) for z <= ref, 0 below 2^-60 (and of -inf, also times a rate of 0); rate: log2(e) / temperature.
 QUASAR_BOTH double weight_of(float z, float ref, double rate) {
@@ -59,9 +69,9 @@ QUASAR_BOTH double weight_of(float z, float ref, double rate) {
     return y > -60.0 ? exp2_by(y, 0) : 0.0;
 }
 // The same in whole multiples of 2^-bits, to nearest (bits <= 51).
-QUASAR_BOTH u64 weight_units(float z, float ref, double rate, int bits) {
-    const double y = ((double)z - (double)ref) * rate;
-    return y > -60.0 ? bits_of(exp2_by(y, bits) + 0x1p52) & ((1ull << 52) - 1) : 0;
+template <bool SCALAR = false> QUASAR_BOTH u64 weight_units(float z, float ref, double rate, int bits) {
+    const double y = __builtin_fmax(((double)z - (double)ref) * rate, -110.0);   // (which rounds to none)
+    return bits_of(exp2_by<SCALAR>(y, bits) + 0x1p52) & ((1ull << 52) - 1);
 }
 
 // The order of the filters: larger logits first, equal ones by their place.  A logit's rank is its bits in falling order: 32 of an fp32 one, 16 of a bf16 one

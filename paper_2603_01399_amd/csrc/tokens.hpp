@@ -218,7 +218,7 @@ __global__ __launch_bounds__(kPartThreads) void token_parts_kernel(const TokenPa
 #pragma unroll
         for (int i = 0; i < LOADS; ++i)
 #pragma unroll
-            for (int e = 0; e < N; ++e) whole += weight_units(x[i][e], largest, f.rate, kPartBits);
+            for (int e = 0; e < N; ++e) whole += weight_units<true>(x[i][e], largest, f.rate, kPartBits);
         whole = wave_sum(whole);
         if (lane == 0) mass[w] = whole;
         __syncthreads();
@@ -235,7 +235,7 @@ __global__ __launch_bounds__(kPartThreads) void token_parts_kernel(const TokenPa
             for (int e = 0; e < N; ++e) {
                 const int at = bucket_of(x[i][e], f.scale, top);
                 if (at > last) continue;
-                if (masses) atomicAdd(&mass[at], weight_units(x[i][e], largest, f.rate, kPartBits));
+                if (masses) atomicAdd(&mass[at], weight_units<true>(x[i][e], largest, f.rate, kPartBits));
                 if (counts) atomicAdd(&count[at], 1u);
             }
     }
