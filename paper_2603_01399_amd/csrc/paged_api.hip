@@ -178,7 +178,7 @@ int launch_step(const PagedAttnParams &p, int NQT, hipStream_t st) {
     const int lds = kPagedWaves * NQT * (8 * 64 * 16 + 16 * 2 * 4) + (kPagedWaves + 4 * (p.c.n_seqs + 1)) * 4;
     const int e = NQT == 1 ? launch_attention<paged_attention_kernel<KV, 1, WINDOW>>(p.workers, p.c.Hkv, lds, st, p)
                            : launch_attention<paged_attention_kernel<KV, 2, WINDOW>>(p.workers, p.c.Hkv, lds, st, p);
-    if (e || p.workers == 1) return e;                                       // (one worker finishes every sequence)
+    if (e || p.workers == 1 || p.each) return e;                             // (one worker finishes every sequence)
     hipLaunchKernelGGL(paged_merge_kernel, dim3((unsigned int)(2 * compute_units())), dim3(512), 0, st, p, NQT);
     return launched();
 }
@@ -205,6 +205,8 @@ int whole_more(int64_t T, int64_t G) {
 template <int KV, bool WINDOW>
 int launch_prompt(const PromptParams &p, int64_t tiles, int PW, hipStream_t st) {
     const int lds = 2 * kPromptStepBytes + (kMaxSeqs + kPromptWaves + 8) * 4;
+    if constexpr (WINDOW)                                                    // (up to 64 rows, whole: half of a tile of 128 would be nobody's, 20.6 us and 27.0)
+        if (!p.workers && PW == 2) return launch_attention<prompt_attention_kernel<KV, false, 2, WINDOW>>((unsigned int)(tiles * p.c.Hkv), 1, lds, st, p);
     if (!p.workers) return launch_attention<prompt_attention_kernel<KV, false, 1, WINDOW>>((unsigned int)(tiles * p.c.Hkv), 1, lds, st, p);
     const unsigned int n = (unsigned int)(p.workers * p.c.Hkv);
     const int e = PW == 1 ? launch_attention<prompt_attention_kernel<KV, true, 1, WINDOW>>(n, 1, lds + kMaxFlatTiles * 4, st, p)
@@ -244,6 +246,12 @@ bool hides(const Window *w, const CacheArgs &a) {
     return w && w->size < most && w->sinks < most;
 }
 
+// Steps of windows: a sequence (a tile of it) to a worker, where the longest then has at most `more` blocks beyond an even share of all; else they are shared as
+// without a window, and joined by a second launch.  Windows are short and nearly even, so that the join mostly costs more than it gives.  One token of 64 sequences,
+// 32 / 8 heads, windows of 128, 512 and 2048 positions: 12.6, 27.8 and 84.9 us, shared 20.8, 35.5 and 97.0; of 4 sequences 7.2, 9.7 and 25.4, and 12.6, 12.9 and 15.3 (which
+// is why there is a limit); 8 tokens of 16 sequences, 64 / 8 heads, 14.3, 20.6 and 58, and 22.8, 28.7 and 39.7.  A single sequence's join is short: half the limit.
+bool stays_whole(int64_t tiles, int64_t longest, int64_t workers, int64_t more) { return tiles >= workers || longest * (workers - tiles) <= more * workers; }
+
 int step_attention(const CacheArgs &a, const AttentionArgs &t, int64_t max_new, const Window *window) {
     if (!t.q || !t.out) return QUASAR_ERR_NULL;
     PagedParams c{};
@@ -257,6 +265,11 @@ int step_attention(const CacheArgs &a, const AttentionArgs &t, int64_t max_new, 
     c.max_new = (int)max_new;
     hipStream_t st = static_cast<hipStream_t>(t.stream);
     const bool bf16 = kv_type(a.kv_dtype) == KV_BF16, windowed = hides(window, a);
+    auto each = [&](int64_t more, int64_t workers, int64_t tiles) {
+        if (!windowed) return false;
+        const int64_t reach = a.max_pages * a.page_len, seen = window->size + max_new - 1, blocks = (seen + kKvBlock - 2) / kKvBlock + 1 + (window->sinks + kKvBlock - 1) / kKvBlock;
+        return stays_whole(a.n_seqs * tiles * a.Hkv, blocks < reach / kKvBlock ? blocks : reach / kKvBlock, workers, a.n_seqs > 1 ? more : more / 2);
+    };
     if (shape.NQT) {
         PagedAttnParams p{};
         p.c = c;
@@ -265,6 +278,9 @@ int step_attention(const CacheArgs &a, const AttentionArgs &t, int64_t max_new, 
         lay_out(p, shape.flat, t.workspace);
         if (windowed) {
             p.window = *window;
+            // (two tiles of rows a worker, one workgroup a compute unit: of many rounds the starts cost more, 256 sequences 90.5 us, shared 81.8)
+            p.each = each(28, (3 - shape.NQT) * compute_units(), 1) && (shape.NQT == 1 || a.n_seqs * a.Hkv <= 4 * compute_units());
+            if (p.each) p.workers = (int)a.n_seqs;
             return bf16 ? launch_step<KV_BF16, true>(p, shape.NQT, st) : launch_step<KV_E4M3, true>(p, shape.NQT, st);
         }
         return bf16 ? launch_step<KV_BF16, false>(p, shape.NQT, st) : launch_step<KV_E4M3, false>(p, shape.NQT, st);
@@ -274,7 +290,7 @@ int step_attention(const CacheArgs &a, const AttentionArgs &t, int64_t max_new, 
     p.q = t.q; p.out = t.out; p.ldq = t.ldq; p.ldo = t.ldo;
     p.scale_log2 = kScaleLog2;
     p.whole_more = -(1 << 30);                                                   // (a step's tiles are shared always: minus more than any share)
-    if (shape.flat.workers) lay_out(p, shape.flat, t.workspace);
+    if (shape.flat.workers && !each(8 * kPromptStep / kKvBlock, 2 * compute_units(), (max_new * (a.Hq / a.Hkv) + 127) / 128)) lay_out(p, shape.flat, t.workspace);
     if (windowed) {
         p.window = *window;
         return bf16 ? launch_prompt<KV_BF16, true>(p, shape.flat.tiles, shape.PW, st) : launch_prompt<KV_E4M3, true>(p, shape.flat.tiles, shape.PW, st);

@@ -32,6 +32,7 @@ struct PagedAttnParams {
     int workers;
     float scale_log2;         // log2(e) / sqrt(128)
     Window window;            // WINDOW
+    bool each;                // WINDOW: a worker has a sequence, nothing is shared
 };
 
 constexpr int kPagedWaves = 4;
@@ -63,7 +64,8 @@ __global__ __launch_bounds__(kPagedWaves * 64, NQT == 1 ? 2 : 1) void paged_atte
     });
     if (tid == 0) prefix[c.n_seqs] = total;
     __syncthreads();
-    const FlatShare mine = flat_share(total, p.workers, NW, worker);             // (a block for each wave)
+    FlatShare mine = flat_share(total, p.workers, NW, worker);                   // (a block for each wave)
+    if (WINDOW && p.each) mine = FlatShare{1, prefix[worker], prefix[worker + 1]};
     int f = mine.begin;
     const int f_end = mine.end;
     int *piece = p.pieces + worker * 4;
@@ -319,7 +321,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, NQT == 1 ? 2 : 1) void paged_atte
         __syncthreads();                                                         // (the next sequence's merge reuses the LDS)
         f = s_begin + b1;
     }
-    if (h == 0 && tid == 0) {
+    if (h == 0 && tid == 0 && !(WINDOW && p.each)) {
         piece[0] = goes_on;
         piece[1] = last_worker;
         piece[2] = first_slot;

@@ -96,6 +96,24 @@ def test_windows_of_any_number_of_rows(qb, kv, group, new):
     close(bf16_to_host(attend(qb, "paged", b, 90, 5)), b, 90, 5)
 
 
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+@pytest.mark.parametrize("group,new", [(1, 1), (4, 4), (4, 7), (8, 8), (16, 8)])
+def test_windows_that_workers_share(qb, kv, group, new):
+    """Windows so long beside the number of sequences that several workers have parts of one, with pieces that end anywhere."""
+    say("shared", kv, group, new)
+    b = Batch(qb, kv, 64, 2 * group, 2, [3000, 31, 1400, 0, 5000], [new, 1, max(new - 1, 0), new, new], seed=300 + group + new)
+    for window, sinks in ((1300, 40), (2500, 0)):
+        close(bf16_to_host(attend(qb, "paged", b, window, sinks)), b, window, sinks)
+
+
+@pytest.mark.parametrize("group,new,seqs", [(2, 1, 1000), (2, 4, 1000), (16, 2, 600), (16, 2, 500), (32, 2, 300)])
+def test_windows_of_many_sequences(qb, group, new, seqs):
+    say("many sequences", group, new, seqs)
+    r = np.random.Generator(np.random.Philox(group + seqs))
+    b = Batch(qb, "bf16", 32, 2 * group, 2, r.integers(0, 90, seqs).tolist(), r.integers(0, new + 1, seqs).tolist(), seed=400 + group)
+    close(bf16_to_host(attend(qb, "paged", b, 33, 3)), b, 33, 3)
+
+
 @pytest.mark.parametrize("call", CALLS)
 def test_a_window_of_everything_gives_the_same_bits(qb, call):
     """Windows and first tokens that hide nothing: the kernels without a window where the table says so, and the same sums where it does not (one
