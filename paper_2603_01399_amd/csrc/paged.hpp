@@ -353,7 +353,7 @@ template <int ROPE> __device__ __forceinline__ double turns_of_lane(const Prepar
 }
 
 // For few rows a sequence: a wave takes four heads of a row at a time, 16 lanes of 16 bytes each.  Bound by the launch and one trip to memory: one row of
-// one sequence 5 us a call, 3.6 in the kernel.
+// one sequence 5 us a call, 3.6 in the kernel; of another rotation the same.
 template <int KV, int ROPE>
 __global__ __launch_bounds__(256) void paged_prepare_kernel(const PrepareParams p) {
     const PagedParams &c = p.c;
@@ -442,7 +442,7 @@ __global__ __launch_bounds__(256) void paged_prepare_kernel(const PrepareParams 
 // For many rows a sequence: a workgroup takes the new rows of one block of 32 positions and p.parts heads.  The rotations of
 // the block are computed once, in LDS; a value head goes through LDS too, since its 16-byte units hold eight positions of one d: written
 // one by one they cost 2 bytes of every 16 a store.  11 prompts of up to 1531 rows into 8-bit pages (229 MB moved): 57 to 60 us, 4 TB/s where a
-// plain copy reaches 5.15; what is left is the norms and rotations, two trips through memory a workgroup.
+// plain copy reaches 5.15; what is left is the norms and rotations, two trips through memory a workgroup.  Rotations of a part of the head 62.
 template <int KV, int ROPE>
 __global__ __launch_bounds__(256) void paged_prepare_block_kernel(const PrepareParams p) {
     constexpr int BB = kv_block_bytes<KV>, STRIDE = kHeadDim + 8;                // (of a row of the values in LDS)

@@ -39,7 +39,8 @@ constexpr int kPagedWaves = 4;
 constexpr int kMaxWorkers = 512;             // of a kv head
 
 // WINDOW: a sequence's blocks are those that its rows see some position of; those between the first tokens and the window have no place in
-// the line, whatever the context's length.
+// the line, whatever the context's length.  64 sequences of one token over up to 16000 positions in 8-bit pages, 32 / 8 heads, windows of 4096 (518 MB): 81.5 us,
+// 6.4 TB/s.
 template <int KV, int NQT, bool WINDOW>
 __global__ __launch_bounds__(kPagedWaves * 64, NQT == 1 ? 2 : 1) void paged_attention_kernel(const PagedAttnParams p) {
     constexpr int NW = kPagedWaves, BB = kv_block_bytes<KV>, NL = BB / 1024;     // 16-byte loads of a lane per block
