@@ -388,6 +388,28 @@ def test_captured_and_on_another_stream(qb):
         assert all(torch.equal(x, y) for x, y in zip((*a, *b), want))
 
 
+def test_calls_on_two_streams_at_once(qb):
+    """Each with scratch of its own; the results are those of calls one after another."""
+    say("two streams")
+    r = np.random.Generator(np.random.Philox(19))
+    T, V = 40, 30000
+    z = [dev(logits_of(r, T, V), torch.float32) for _ in range(2)]
+    u, f = dev(r.random(T), torch.float32), params([FILTERS[i % len(FILTERS)] for i in range(T)])
+    starts, seqs = dev(np.arange(0, T + 1, 8), torch.int32), params([FILTERS[i] for i in (0, 5, 11, 8, 4)])
+    ids = [x.argmax(1).int() for x in z]
+    call = lambda i: (*qb.sample_tokens(z[i], u, **f), *qb.verify_tokens(z[i], starts, ids[i], u, u, **seqs))
+    want = [call(0), call(1)]
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    got = [[], []]
+    for _ in range(10):
+        for i in range(2):
+            with torch.cuda.stream(streams[i]):
+                got[i].append(call(i))
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for i in range(2) for g in got[i] for a, b in zip(g, want[i]))
+
+
 def test_a_step_of_a_batch(qb):
     """Logits as a linear writes them, drafts, the cache's lengths: a step goes on from what verify_tokens says, without the host."""
     say("a step")

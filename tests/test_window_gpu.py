@@ -220,6 +220,22 @@ def test_books_that_do_not_fit(qb, call):
 
 
 @pytest.mark.parametrize("call", CALLS)
+@pytest.mark.parametrize("hq,hk,lengths,news,window", [(8, 2, [3000, 40, 0, 700], [2, 1, 3, 0], 60), (8, 2, [3000, 40, 0, 700], [2, 1, 3, 0], 1500), (16, 2, [900, 2500], [8, 7], 100),
+                                                       (16, 2, [900, 2500], [8, 7], 1500), (16, 1, [300, 64], [30, 32], 200)])
+def test_in_place(qb, call, hq, hk, lengths, news, window):
+    """The output over the queries: the same bits as beside them, also in rows of a wider tensor."""
+    say("in place", call, hq, window)
+    b = Batch(qb, "bf16", 64, hq, hk, lengths, news, seed=50 + window)
+    want = attend(qb, call, b, window, 4)
+    q = b.q().clone()
+    assert torch.equal(attend(qb, call, b, window, 4, q=q, out=q), want)
+    wide = torch.zeros(q.shape[0], q.shape[1] + 64, dtype=q.dtype, device="cuda")
+    wide[:, :q.shape[1]] = b.q()
+    view = wide[:, :q.shape[1]]
+    assert torch.equal(attend(qb, call, b, window, 4, q=view, out=view), want) and not wide[:, q.shape[1]:].any()
+
+
+@pytest.mark.parametrize("call", CALLS)
 def test_a_captured_call_follows_the_lengths(qb, call):
     """One graph over lengths and row counts that change, with eager calls on the same cache between the replays."""
     say("captured", call)
