@@ -167,15 +167,25 @@ bool step_shape(int64_t max_new, int64_t Hq, int64_t Hkv, int64_t n_seqs, StepSh
     return true;
 }
 
-template <auto Kernel, class Params>
+template <auto Kernel, int WAVES = kPromptWaves, class Params>
 int launch_attention(unsigned int workgroups_x, unsigned int workgroups_y, int lds, hipStream_t st, const Params &p) {
     if (!large_lds<Kernel>()) return QUASAR_ERR_HIP;
-    hipLaunchKernelGGL(Kernel, dim3(workgroups_x, workgroups_y), dim3(kPromptWaves * 64), lds, st, p);
+    hipLaunchKernelGGL(Kernel, dim3(workgroups_x, workgroups_y), dim3(WAVES * 64), lds, st, p);
     return launched();
 }
+// Workgroups that each have a compute unit to themselves, a sequence each: eight waves (in bf16 and two tiles of rows those have too few registers).
+bool lone_step(int kv, int NQT, int64_t n_seqs, int64_t Hkv) { return n_seqs * Hkv <= compute_units() && (kv == KV_E4M3 || NQT == 1); }
 template <int KV, bool WINDOW>
 int launch_step(const PagedAttnParams &p, int NQT, hipStream_t st) {
-    const int lds = kPagedWaves * NQT * (8 * 64 * 16 + 16 * 2 * 4) + (kPagedWaves + 4 * (p.c.n_seqs + 1)) * 4;
+    auto lds_of = [&](int waves) { return waves * NQT * (8 * 64 * 16 + 16 * 2 * 4) + (waves + 4 * (p.c.n_seqs + 1)) * 4; };
+    if constexpr (WINDOW) {
+        constexpr int NW = kLoneWaves;
+        if (p.each && lone_step(KV, NQT, p.c.n_seqs, p.c.Hkv)) {
+            if (NQT == 1) return launch_attention<paged_attention_kernel<KV, 1, true, NW>, NW>(p.workers, p.c.Hkv, lds_of(NW), st, p);
+            if constexpr (KV == KV_E4M3) return launch_attention<paged_attention_kernel<KV, 2, true, NW>, NW>(p.workers, p.c.Hkv, lds_of(NW), st, p);
+        }
+    }
+    const int lds = lds_of(kPagedWaves);
     const int e = NQT == 1 ? launch_attention<paged_attention_kernel<KV, 1, WINDOW>>(p.workers, p.c.Hkv, lds, st, p)
                            : launch_attention<paged_attention_kernel<KV, 2, WINDOW>>(p.workers, p.c.Hkv, lds, st, p);
     if (e || p.workers == 1 || p.each) return e;                             // (one worker finishes every sequence)
@@ -248,8 +258,10 @@ bool hides(const Window *w, const CacheArgs &a) {
 
 // Steps of windows: a sequence (a tile of it) to a worker, where the longest then has at most `more` blocks beyond an even share of all; else they are shared as
 // without a window, and joined by a second launch.  Windows are short and nearly even, so that the join mostly costs more than it gives.  One token of 64 sequences,
-// 32 / 8 heads, windows of 128, 512 and 2048 positions: 12.6, 27.8 and 84.9 us, shared 20.8, 35.5 and 97.0; of 4 sequences 7.2, 9.7 and 25.4, and 12.6, 12.9 and 15.3 (which
-// is why there is a limit); 8 tokens of 16 sequences, 64 / 8 heads, 14.3, 20.6 and 58, and 22.8, 28.7 and 39.7.  A single sequence's join is short: half the limit.
+// 32 / 8 heads, windows of 128, 512 and 2048 positions: 12.6, 27.8 and 84.9 us, shared 20.8, 35.5 and 97.0; of 4 sequences, eight waves each, 7.1, 8.6 and 24.8 (with four
+// 7.2, 9.6 and 25.4), and 12.6, 12.9 and 15.3, in 8-bit pages of 1024 10.3 and 13.1, of 2048 14.7 and 14.1 (which is why there is a limit); in bf16 of
+// 1024 10.6 and 12.9 for 2 sequences, 16.8 and 16.0 for 8; 8 tokens of 16 sequences, 64 / 8
+// heads, 14.3, 20.6 and 58, and 22.8, 28.7 and 39.7.  A single sequence's join is short: a limit of its own.
 bool stays_whole(int64_t tiles, int64_t longest, int64_t workers, int64_t more) { return tiles >= workers || longest * (workers - tiles) <= more * workers; }
 
 int step_attention(const CacheArgs &a, const AttentionArgs &t, int64_t max_new, const Window *window) {
@@ -265,10 +277,10 @@ int step_attention(const CacheArgs &a, const AttentionArgs &t, int64_t max_new, 
     c.max_new = (int)max_new;
     hipStream_t st = static_cast<hipStream_t>(t.stream);
     const bool bf16 = kv_type(a.kv_dtype) == KV_BF16, windowed = hides(window, a);
-    auto each = [&](int64_t more, int64_t workers, int64_t tiles) {
+    auto each = [&](int64_t workers, int64_t more, int64_t more_of_one, int64_t tiles) {         // (the tiles of a sequence)
         if (!windowed) return false;
         const int64_t reach = a.max_pages * a.page_len, seen = window->size + max_new - 1, blocks = (seen + kKvBlock - 2) / kKvBlock + 1 + (window->sinks + kKvBlock - 1) / kKvBlock;
-        return stays_whole(a.n_seqs * tiles * a.Hkv, blocks < reach / kKvBlock ? blocks : reach / kKvBlock, workers, a.n_seqs > 1 ? more : more / 2);
+        return stays_whole(a.n_seqs * tiles * a.Hkv, blocks < reach / kKvBlock ? blocks : reach / kKvBlock, workers, a.n_seqs > 1 ? more : more_of_one);
     };
     if (shape.NQT) {
         PagedAttnParams p{};
@@ -279,7 +291,9 @@ int step_attention(const CacheArgs &a, const AttentionArgs &t, int64_t max_new, 
         if (windowed) {
             p.window = *window;
             // (two tiles of rows a worker, one workgroup a compute unit: of many rounds the starts cost more, 256 sequences 90.5 us, shared 81.8)
-            p.each = each(28, (3 - shape.NQT) * compute_units(), 1) && (shape.NQT == 1 || a.n_seqs * a.Hkv <= 4 * compute_units());
+            const int64_t cus = compute_units(), tiles = a.n_seqs * a.Hkv;
+            p.each = lone_step(bf16 ? KV_BF16 : KV_E4M3, shape.NQT, a.n_seqs, a.Hkv) ? each(cus, !bf16 ? 50 : tiles <= cus / 16 ? 34 : 24, 24, 1)
+                                                                                     : each((3 - shape.NQT) * cus, 28, 14, 1) && (shape.NQT == 1 || tiles <= 4 * cus);
             if (p.each) p.workers = (int)a.n_seqs;
             return bf16 ? launch_step<KV_BF16, true>(p, shape.NQT, st) : launch_step<KV_E4M3, true>(p, shape.NQT, st);
         }
@@ -290,7 +304,7 @@ int step_attention(const CacheArgs &a, const AttentionArgs &t, int64_t max_new, 
     p.q = t.q; p.out = t.out; p.ldq = t.ldq; p.ldo = t.ldo;
     p.scale_log2 = kScaleLog2;
     p.whole_more = -(1 << 30);                                                   // (a step's tiles are shared always: minus more than any share)
-    if (shape.flat.workers && !each(8 * kPromptStep / kKvBlock, 2 * compute_units(), (max_new * (a.Hq / a.Hkv) + 127) / 128)) lay_out(p, shape.flat, t.workspace);
+    if (shape.flat.workers && !each(2 * compute_units(), 16, 8, (max_new * (a.Hq / a.Hkv) + 127) / 128)) lay_out(p, shape.flat, t.workspace);
     if (windowed) {
         p.window = *window;
         return bf16 ? launch_prompt<KV_BF16, true>(p, shape.flat.tiles, shape.PW, st) : launch_prompt<KV_E4M3, true>(p, shape.flat.tiles, shape.PW, st);

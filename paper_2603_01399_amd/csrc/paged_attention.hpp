@@ -35,15 +35,15 @@ struct PagedAttnParams {
     bool each;                // WINDOW: a worker has a sequence, nothing is shared
 };
 
-constexpr int kPagedWaves = 4;
+constexpr int kPagedWaves = 4, kLoneWaves = 8;           // of a workgroup; where it has a compute unit and a sequence to itself
 constexpr int kMaxWorkers = 512;             // of a kv head
 
 // WINDOW: a sequence's blocks are those that its rows see some position of; those between the first tokens and the window have no place in
 // the line, whatever the context's length.  64 sequences of one token over up to 16000 positions in 8-bit pages, 32 / 8 heads, windows of 4096 (518 MB): 81.5 us,
 // 6.4 TB/s.
-template <int KV, int NQT, bool WINDOW>
-__global__ __launch_bounds__(kPagedWaves * 64, NQT == 1 ? 2 : 1) void paged_attention_kernel(const PagedAttnParams p) {
-    constexpr int NW = kPagedWaves, BB = kv_block_bytes<KV>, NL = BB / 1024;     // 16-byte loads of a lane per block
+template <int KV, int NQT, bool WINDOW, int NW = kPagedWaves>
+__global__ __launch_bounds__(NW * 64, NQT == 1 ? 2 : 1) void paged_attention_kernel(const PagedAttnParams p) {
+    constexpr int BB = kv_block_bytes<KV>, NL = BB / 1024;     // 16-byte loads of a lane per block
     extern __shared__ __align__(16) unsigned char lds[];
     f32x4 *lo = reinterpret_cast<f32x4 *>(lds);                                  // [NW][NQT][8][64]
     float *lml = reinterpret_cast<float *>(lds + NW * NQT * 8 * 64 * 16);        // [NW][NQT][16][2]

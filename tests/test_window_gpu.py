@@ -106,6 +106,19 @@ def test_windows_that_workers_share(qb, kv, group, new):
         close(bf16_to_host(attend(qb, "paged", b, window, sinks)), b, window, sinks)
 
 
+@pytest.mark.parametrize("kv", ["bf16", "e4m3"])
+@pytest.mark.parametrize("group,new,heads", [(1, 1, 2), (4, 4, 2), (4, 7, 2), (16, 2, 1), (8, 1, 1)])
+def test_windows_of_few_sequences(qb, kv, group, new, heads):
+    """A sequence a workgroup of eight waves, of fewer blocks than waves, and of many more."""
+    say("few sequences", kv, group, new, heads)
+    b = Batch(qb, kv, 64, heads * group, heads, [3000, 31, 1400, 0, 400], [new, 1, max(new - 1, 0), new, new], seed=500 + group + new)
+    for window, sinks in ((1, 0), (200, 3), (600, 40), (700, 0)):
+        close(bf16_to_host(attend(qb, "paged", b, window, sinks)), b, window, sinks)
+    one = Batch(qb, kv, 64, heads * group, heads, [2000], [new], seed=600 + group + new)
+    for window, sinks in ((300, 1), (600, 0), (900, 0)):
+        close(bf16_to_host(attend(qb, "paged", one, window, sinks)), one, window, sinks)
+
+
 @pytest.mark.parametrize("group,new,seqs", [(2, 1, 1000), (2, 4, 1000), (16, 2, 600), (16, 2, 500), (32, 2, 300)])
 def test_windows_of_many_sequences(qb, group, new, seqs):
     say("many sequences", group, new, seqs)
