@@ -154,17 +154,18 @@ __device__ __forceinline__ float wave_max(float v) {             // in every lan
 }
 template <class N> __device__ __forceinline__ N wave_sum(N v) { return of_lane(lane_sums_through(v), 63); }
 
-// How a row is drawn.  ALL: nothing is filtered.  FEW: top-k of at most kFew, so that all that is left can be gathered.  MANY: a cut anywhere.
-enum { DRAW_ALL = 0, DRAW_FEW = 1, DRAW_MANY = 2 };
+// How a row is drawn.  FIRST: the first token is all that is left.  ALL: nothing is filtered.  FEW: top-k of at most kFew, so that all that is left can be gathered.  MANY: a cut anywhere.
+enum { DRAW_ALL = 0, DRAW_FEW = 1, DRAW_MANY = 2, DRAW_FIRST = 3 };
 constexpr int kFew = 2048;
 __device__ __forceinline__ int draw_mode(const Filters &f) {
+    if (f.k == 1) return DRAW_FIRST;
     if (f.k && f.k <= kFew) return DRAW_FEW;
     return f.k || f.p < 1.0f || f.min_p > 0.0f ? DRAW_MANY : DRAW_ALL;
 }
 
 // Grid (parts, rows).  A part's 16 tokens a thread stay in registers between its largest logit and the buckets.  What the row asks for is counted and nothing
-// else: the whole part's mass (ALL), counts (FEW), masses, and counts where there is a top-k (MANY).  Bound by instructions: a compute unit does one for 64 tokens a
-// cycle, 0.25 us for each that is done for every token of 64 rows of 152 K; vector instructions fill 75 % of the cycles.  64 rows more of fp32 logits take 7.5 us
+// else: nothing (FIRST), the whole part's mass (ALL), counts (FEW), masses, and counts where there is a top-k (MANY).  Bound by instructions: a compute unit does one for 64 tokens a
+// cycle, 0.25 us for each that is done for every token of 64 rows of 152 K; vector instructions fill 80 to 88 % of the cycles.  64 rows more of fp32 logits take 7.5 us
 // (FEW: 39 MB, 5.2 TB/s), 11 (ALL) and 15.5 (MANY).  Tried: two, four or eight copies of the buckets in LDS for the lanes of a wave, fewer workgroups a compute unit,
 // so that some load while others compute: the same; 256 threads of 32 tokens 2 to 4 us more, 1024 of 8 up to 4 more where there are many rows.
 template <int DT>
@@ -208,6 +209,7 @@ __global__ __launch_bounds__(kPartThreads) void token_parts_kernel(const TokenPa
 #pragma unroll
     for (int i = 0; i < kPartWaves; ++i) largest = fmaxf(largest, wave_largest[i]);
     if (tid == 0) p.part_max[(long long)r * p.nb + b] = largest;
+    if (mode == DRAW_FIRST) return;
     const float top = bucket_line(largest, f.scale);
     const long long to = ((long long)r * p.nb + b) * kBuckets;
     // (a token that min_p keeps from being left in its part cannot be left in the row; where top-p counts it for the whole all the same, it is taken)
@@ -322,7 +324,7 @@ __device__ __forceinline__ uint32_t least_ordered_of_bucket(int j, float scale, 
 // A workgroup a row.  Two things bound it.  It is a chain of steps that each wait for the one before (a trip to memory 1 us, a barrier of sixteen waves 0.2): requests are made
 // together and ahead, and no step is one thread's.  And a compute unit does one instruction for 64 tokens a cycle, 1 us for each that is done for every token of
 // 152 K: what chunks hold is compared with the ends of the gathered buckets, two instructions, and only what lies between is worked on.  One row of 152 K tokens takes
-// 7 us without filters, 13 to 16 with top-k, and 34 with a top-p whose cut lies in a bucket of thousands, where every chunk is read: buckets 7, chunks 10, their keys and the
+// 7 us without filters (where the first is all that is left a call takes 6.6), 13 to 16 with top-k, and 34 with a top-p whose cut lies in a bucket of thousands, where every chunk is read: buckets 7, chunks 10, their keys and the
 // digits 8, the rest 9.  Tried: two to eight workgroups that read such a row's chunks together and the last of which goes on: what each has to make visible to the others
 // costs more than it reads (64 rows with top-p 52 us, 61 by two, 69 by four).
 template <int DT>
@@ -408,6 +410,28 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
     if (!(most > -__builtin_inff())) {                           // nothing to draw from
         if (tid == 0 && p.p) p.p[row_at] = 0.0f;
         finish(-1, false);
+        return;
+    }
+    if (mode == DRAW_FIRST) {                                    // of the first chunk that has the largest logit the first place that has it
+        int chunk = 0;
+#pragma unroll 1
+        for (int i = 0; i * kDrawThreads < maxima; ++i) {
+            int first, last;
+            talk.ends((i == 0 ? chunk_max[0] : chunk_max_at(i)) == most, false, first, last);
+            if (first == kDrawThreads) continue;
+            chunk = first + i * kDrawThreads;
+            break;
+        }
+        const int unit = chunk * 16 + (lane & 15);
+        float x[N];
+        row.values(unit, row.request(unit), x, [](float z) { return logit_weighed(z); });
+        int place = N;
+#pragma unroll
+        for (int e = N - 1; e >= 0; --e) place = x[e] == most ? e : place;
+        const int l = __builtin_ctzll(__builtin_amdgcn_ballot_w64(place < N)), token = (chunk * 16 + l) * N + __builtin_amdgcn_readlane(place, l) - row.skew;
+        const bool all = draft == token;                         // the draft has all mass
+        if (tid == 0 && p.p) p.p[row_at] = !p.draft || all ? 1.0f : 0.0f;
+        finish(all && !last_row ? -1 : token, all && !last_row && u_accept < 1.0f);
         return;
     }
     const float top = bucket_line(most, f.scale);

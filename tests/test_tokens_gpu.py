@@ -125,6 +125,35 @@ def test_equal_logits(qb, V):
             assert np.allclose(p.cpu(), 1 / left, rtol=2.0 ** -23)
 
 
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V,off", [(1, 0), (5, 3), (130, 1), (8190, 7), (30000, 2), (151936, 5), (1 << 20, 0)])
+def test_the_first_of_equal_ones_wherever_it_is(qb, dtype, V, off):
+    """Temperature 0, top_k 1, top_p 0: the largest logit's first place, of ties at the row's ends and at borders of what is read together, among what is no number."""
+    say("first", dtype, V, off)
+    r = np.random.Generator(np.random.Philox(V))
+    ends = sorted({v for v in (0, 1, 6, 7, 8, 63, 64, 127, 128, 8185, 8191, 8192, 16383, V // 2, V - 2, V - 1) if 0 <= v < V})
+    wide = torch.full((len(ends), V + off), float("nan"), dtype=dtype, device="cuda")
+    z = wide[:, off:]
+    z.copy_(dev(np.where(r.random(V) < 0.02, np.nan, np.where(r.random(V) < 0.02, -np.inf, -np.abs(r.standard_normal(V)) - 1)), torch.float32))
+    top = (0.0, 3.5, np.inf, -0.5)
+    for i, v in enumerate(ends):
+        z[i, v] = -0.0 if top[i % 4] == 0 else top[i % 4]
+        for w in ends[i + 1:]:
+            z[i, w] = top[i % 4]
+    n = len(ends)
+    u = dev(r.random(n), torch.float32)
+    for f in (dict(temperature=dev([0.0] * n, torch.float32)), dict(top_k=dev([1] * n, torch.int32), top_p=dev([0.5] * n, torch.float32)), dict(top_p=dev([0.0] * n, torch.float32))):
+        token, p = qb.sample_tokens(z, u, **f)
+        assert token.tolist() == ends and (p == 1).all()
+    starts, one = dev([0, n], torch.int32), dev([1], torch.int32)
+    accepted, token, p = qb.verify_tokens(z, starts, dev(ends, torch.int32), u * 0 + 0.999, u, top_k=one)
+    assert (accepted.tolist(), token.tolist()) == ([n - 1], [ends[-1]]) and (p == 1).all()
+    if n > 1:
+        wrong = dev([ends[0], *[v + 1 for v in ends[1:]]], torch.int32)
+        accepted, token, p = qb.verify_tokens(z, starts, wrong, u * 0, u, top_k=one)
+        assert (accepted.tolist(), token.tolist()) == ([min(1, n - 1)], [ends[1]]) and p.tolist() == [1.0] + [0.0] * (n - 1)
+
+
 @pytest.mark.parametrize("spread", [1e-6, 1e-3, 0.05])
 def test_a_bucket_of_more_than_fit(qb, spread):
     """Continuous logits so near that they share a bucket or a few: the cut is found in tokens that are read again."""
