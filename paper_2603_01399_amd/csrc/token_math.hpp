@@ -109,19 +109,23 @@ template <int DT> QUASAR_BOTH u64 first_key(uint32_t most) {
     return (u64)(~most >> (DT == 1 ? 16 : 0)) << kIndexBits;
 }
 
-// A logit's place on the line of buckets: whole, falls with z never, and the same for every part of a vocabulary.  (fmax takes what is not a number,
-// -inf times a scale of 0, for the smallest.)
-QUASAR_BOTH float bucket_line(float z, float scale) { return __builtin_floorf(__builtin_fminf(__builtin_fmaxf(z * scale, -kLargest), kLargest)); }
-// Bucket of a logit, 0 for those nearest the largest one (line_top: its place, of a finite logit); kBuckets: beyond them all, as -inf is.
-QUASAR_BOTH int bucket_of(float z, float scale, float line_top) {
-    const float d = line_top - bucket_line(z, scale);
-    return z == -__builtin_inff() ? kBuckets : (int)__builtin_fminf(d, (float)kBuckets);
+// A logit's place on the line of buckets, plus 1.5 2^52: to the nearest whole number, falls with z never, and the same for every part of a vocabulary.  In 64 bits:
+// a logit may be 2^24 buckets and more away from 0 (2^20 temperatures), and the few between it and another one have to be exact all the same.  (Beyond 2^51, where
+// places are no longer every whole number, different logits are 2^26 buckets apart.)
+QUASAR_BOTH double bucket_line(float z, double scale) { return __builtin_fma((double)z, scale, 0x1.8p52); }
+// Bucket of a logit, 0 for those nearest the largest one (line_top: its place, of a finite logit); kBuckets: beyond them all, as -inf is (whose place is no
+// number at a scale of 0: fmin takes the other one).
+QUASAR_BOTH int bucket_of(float z, double scale, double line_top) { return (int)__builtin_fmin(line_top - bucket_line(z, scale), (double)kBuckets); }
+// The last bucket that a logit can lie in whose weight is at least this: D = 16 ln(1 / min_p) buckets below the largest, two roundings of at most half a bucket each.
+QUASAR_BOTH int last_bucket(float log2_min_p) {
+    const int last = (int)(-0.6931472f * kBucketsPerUnit * log2_min_p) + 2;
+    return last < kBuckets - 1 ? last : kBuckets - 1;
 }
-
 // What a row's filters come to.
 struct Filters {
     double rate;              // log2(e) / temperature
-    float scale;              // kBucketsPerUnit / temperature
+    double scale;             // kBucketsPerUnit / temperature
+    float temperature;        // above 0
     int k;                    // 0: no limit
     float p;                  // 1: no limit
     float min_p;              // 0: no limit
@@ -132,12 +136,44 @@ QUASAR_BOTH Filters filters_of(float temperature, int top_k, float top_p, float 
     f.p = top_p < 1.0f ? top_p : 1.0f;                       // (not a number: no limit)
     f.min_p = min_p > 0x1p-50f ? (min_p < 1.0f ? min_p : 1.0f) : 0.0f;   // (what weighs less is beyond the buckets)
     if (!(temperature > 0.0f)) temperature = 1.0f, f.k = 1;
+    f.temperature = temperature;
     if (f.p <= 0.0f) f.p = 1.0f, f.k = 1;                    // (the first is always left)
-    f.rate = 1.4426950408889634 / (double)temperature;
-    const float scale = (float)kBucketsPerUnit / temperature;
-    f.scale = scale < kLargest ? scale : kLargest;
+    const double scale = (double)kBucketsPerUnit / (double)temperature;
+    f.rate = scale * (1.4426950408889634 / kBucketsPerUnit);
+    f.scale = scale < (double)kLargest ? scale : (double)kLargest;
     return f;
 }
+// The smallest logit of buckets 0 .. j, as ordered bits, found by 64 at a time: around where the line says, else anywhere.  `ballot` asks whether a number holds
+// for lanes 0 .. 63, `most` is the largest logit.  What a bucket holds is asked of bucket_of, so that an interval of logits is the bucket's exactly.  (Zero in the
+// form that orders ahead of the other.)
+template <class Ballot>
+QUASAR_BOTH uint32_t least_of_buckets(int j, const Filters &f, double line_top, float most, Ballot ballot) {
+    const uint32_t least = ordered_bits(-kLargest), largest = ordered_bits(most);
+    auto holds = [&](uint32_t at) { return bucket_of(value_of_ordered(at), f.scale, line_top) <= j; };
+    const double place = (line_top - 0x1.8p52 - (double)j - 0.5) * (1.0 / kBucketsPerUnit * (double)f.temperature);
+    const float guess = (float)__builtin_fmin(__builtin_fmax(place, -(double)kLargest), (double)most);
+    const long long first = (long long)ordered_bits(guess) - 32;
+    auto around = [&](int i) { return (uint32_t)(first + i < (long long)least ? least : first + i > (long long)largest ? largest : first + i); };
+    u64 held = ballot([&](int i) { return holds(around(i)); });
+    uint32_t found;
+    if (held && (!(held & 1) || around(0) == least)) {
+        found = around(__builtin_ctzll(held));
+    } else {
+        uint32_t lo = least, hi = largest;                       // (it holds for the largest)
+        while (lo < hi) {
+            const uint32_t step = (hi - lo) / 64 + 1;
+            auto here = [&](int i) { return (uint32_t)((u64)lo + (u64)step * (u64)i < hi ? (u64)lo + (u64)step * (u64)i : hi); };
+            held = ballot([&](int i) { return holds(here(i)); });
+            const int l = held ? __builtin_ctzll(held) : 64;     // (none: it is behind the last one asked)
+            const uint32_t behind = l ? here(l - 1) + 1 : lo;
+            if (held) hi = here(l);
+            lo = behind;
+        }
+        found = hi;
+    }
+    return found == ordered_bits(0.0f) ? found - 1 : found;
+}
+
 // The smallest logit whose weight is at least min_p (> 0); most: the largest logit.
 QUASAR_BOTH float least_logit(float most, double rate, float min_p) {
     const double at = (double)most + log2((double)min_p) / rate;

@@ -21,7 +21,7 @@ namespace quasar {
 constexpr int kPartTokens = 8192, kPartThreads = 512, kPartWaves = kPartThreads / 64, kPartLane = kPartTokens / kPartThreads;
 constexpr int kMaxTokenParts = ((1 << kIndexBits) + 7 + kPartTokens - 1) / kPartTokens;
 constexpr int kDrawThreads = 1024, kDrawWaves = kDrawThreads / 64;
-constexpr int kChunkTurn = 24;               // chunks that a wave reads at a time, at most
+constexpr int kChunkTurn = 16;               // chunks that a wave reads at a time
 constexpr int kListed = 3584;                // tokens of a bucket that are kept in LDS; more are read again where they are asked for
 
 struct TokenParams {
@@ -210,11 +210,11 @@ __global__ __launch_bounds__(kPartThreads) void token_parts_kernel(const TokenPa
     for (int i = 0; i < kPartWaves; ++i) largest = fmaxf(largest, wave_largest[i]);
     if (tid == 0) p.part_max[(long long)r * p.nb + b] = largest;
     if (mode == DRAW_FIRST) return;
-    const float top = bucket_line(largest, f.scale);
+    const double top = bucket_line(largest, f.scale);
     const long long to = ((long long)r * p.nb + b) * kBuckets;
     // (a token that min_p keeps from being left in its part cannot be left in the row; where top-p counts it for the whole all the same, it is taken)
     int last = kBuckets - 1;
-    if (mode == DRAW_MANY && !counts && f.p >= 1.0f) last = min(last, (int)(-0.6931472f * kBucketsPerUnit * __log2f(f.min_p)) + 2);
+    if (mode == DRAW_MANY && !counts && f.p >= 1.0f) last = last_bucket(__log2f(f.min_p));
     if (mode == DRAW_ALL) {
         u64 whole = 0;
 #pragma unroll
@@ -287,38 +287,9 @@ struct WaveTalk {
     }
 };
 
-// The smallest logit of buckets 0 .. j, found by the lanes of a wave side by side: around where the line says, else anywhere.  (Zero in the form that
-// orders ahead of the other.)
-__device__ __forceinline__ uint32_t least_ordered_of_bucket(int j, float scale, float top, float most) {
+__device__ __forceinline__ uint32_t least_ordered_of_bucket(int j, const Filters &f, double top, float most) {
     const int lane = threadIdx.x & 63;
-    const float place = top - (float)j;
-    const uint32_t least = ordered_bits(-kLargest), largest = ordered_bits(most);
-    auto holds = [&](uint32_t at) { return bucket_line(value_of_ordered(at), scale) >= place; };
-    const float guess = __builtin_fminf(__builtin_fmaxf(place / scale, -kLargest), most);
-    const long long around = (long long)ordered_bits(guess) - 32 + lane;
-    const uint32_t at = around < (long long)least ? least : around > (long long)largest ? largest : (uint32_t)around;
-    unsigned long long mask = __builtin_amdgcn_ballot_w64(holds(at));
-    uint32_t found;
-    if (mask && (!(mask & 1) || (uint32_t)of_lane((int)at, 0) == least)) {
-        found = (uint32_t)of_lane((int)at, __builtin_ctzll(mask));
-    } else {
-        uint32_t lo = least, hi = largest;                       // (it holds for the largest)
-        while (lo < hi) {
-            const uint32_t step = (hi - lo) / 64 + 1;
-            const unsigned long long to = (unsigned long long)lo + (unsigned long long)step * lane;
-            const uint32_t here = to > hi ? hi : (uint32_t)to;
-            mask = __builtin_amdgcn_ballot_w64(holds(here));
-            if (!mask) {
-                lo = (uint32_t)of_lane((int)here, 63) + 1;
-                continue;
-            }
-            const int l = __builtin_ctzll(mask);
-            hi = (uint32_t)of_lane((int)here, l);
-            if (l) lo = (uint32_t)of_lane((int)here, l - 1) + 1;
-        }
-        found = hi;
-    }
-    return found == ordered_bits(0.0f) ? found - 1 : found;
+    return least_of_buckets(j, f, top, most, [&](auto holds) { return (u64)__builtin_amdgcn_ballot_w64(holds(lane)); });
 }
 
 // A workgroup a row.  Two things bound it.  It is a chain of steps that each wait for the one before (a trip to memory 1 us, a barrier of sixteen waves 0.2): requests are made
@@ -331,7 +302,9 @@ template <int DT>
 __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenParams p) {
     constexpr int N = lane_tokens<DT>, CHUNKS = part_chunks<DT>;
     constexpr int AHEAD = 4;                                     // chunks' largest logits of a thread that are requested at the start: of vocabularies up to 2^18 or 2^19 all
-    constexpr int DEPTH = DT == 1 ? 4 : 6;                       // loads of a turn of a wave that reads chunks (a bit a token: 32 at most); two turns are under way
+    // Loads of a turn of a wave that reads chunks (a bit a token: 32 at most); two turns are under way.  (fp32 logits with six: 18 vector registers spilled, one row with top-k
+    // 20.3 us, 64 with top-k 37.5 and with top-p 59.6; with four none, 19.4, 34.7 and 56.9.)
+    constexpr int DEPTH = 4;
     constexpr u64 ALL = ~0ull;
     constexpr int kPairs = 128;                                  // tokens up to which each is compared with each (of 16 bytes from LDS a pair: 512 tokens take 15 us, a digit 3)
     extern __shared__ unsigned short chunks[];                   // that may hold some of the gathered buckets
@@ -370,7 +343,8 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
     const RowOf of = row_of(p, row_at);
     if (of.who < 0) return;
     const bool last_row = of.last(row_at);
-    const Filters f = filters_at(p, of.who);
+    Filters f = filters_at(p, of.who);
+    f.scale = of_lane(f.scale, 0);                               // (into scalar registers, as the place below)
     const int mode = draw_mode(f);
     WaveTalk talk{talk_places, 0};
 
@@ -434,12 +408,12 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
         finish(all && !last_row ? -1 : token, all && !last_row && u_accept < 1.0f);
         return;
     }
-    const float top = bucket_line(most, f.scale);
+    const double top = of_lane(bucket_line(most, f.scale), 0);
     const float draft_logit = draft >= 0 && draft < p.V ? row.one(draft) : -__builtin_inff();    // (one address for the workgroup)
     static_assert(kMaxTokenParts <= kDrawThreads, "a part a thread");
     if (tid < nb) {
         part_max[tid] = mine_max;
-        shift[tid] = bucket_of(mine_max, f.scale, top);
+        if (mode != DRAW_ALL) shift[tid] = bucket_of(mine_max, f.scale, top);
         factor[tid] = mine_max > -__builtin_inff() ? weight_of(mine_max, most, f.rate) : 0.0;
         part_mass[tid] = mode == DRAW_ALL ? mine_mass : 0;
     }
@@ -542,11 +516,11 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
             if (mode == DRAW_FEW || border == kBuckets) break;
             from = to = border;
         }
-        const uint32_t least = least_ordered_of_bucket(to, f.scale, top, most);
+        const uint32_t least = least_ordered_of_bucket(to, f, top, most);
         if (gathered != (from << 16 | to)) {
             gathered = from << 16 | to;
             gathered_from = value_of_ordered(least);
-            gathered_to = from ? value_of_ordered(least_ordered_of_bucket(from - 1, f.scale, top, most) - 1) : __builtin_inff();
+            gathered_to = from ? value_of_ordered(least_ordered_of_bucket(from - 1, f, top, most) - 1) : __builtin_inff();
             if (tid == 0) n_chunks = 0, n_listed = 0;
             __syncthreads();
 #pragma unroll 1
@@ -644,7 +618,7 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
         // Among the keys lo .. hi, `inside` of them, the first `want` (tokens, or units of mass: those ahead of which less lies).  Masses are relative to the largest
         // logit there may be among them.
         const bool by_mass = step == BY_MASS, one = !by_mass || from;            // (one bucket's)
-        const uint32_t largest = one && to ? least_ordered_of_bucket(to - 1, f.scale, top, most) - 1 : ordered_bits(most);
+        const uint32_t largest = one && to ? least_ordered_of_bucket(to - 1, f, top, most) - 1 : ordered_bits(most);
         const float ref = value_of_ordered(largest);
         const double to_row = weight_of(ref, most, f.rate) * (1.0 / (double)(1ull << kListBits));
         u64 lo = first_key<DT>(largest), hi = last_key<DT>(least), before = 0;
@@ -721,7 +695,11 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
             total = (double)talk.sum(mass) * (1.0 / (double)(1ull << kListBits)) + (from ? through_mass[from - 1] : 0.0);
         }
     }
-    auto kept = [&](float z, int v) { return rank_key<DT>(z, v) <= cut && (mode != DRAW_MANY || bucket_of(z, f.scale, top) < kBuckets); };
+    if (mode == DRAW_MANY && border == kBuckets) {               // (what lies beyond the buckets is not counted)
+        const u64 key = last_key<DT>(least_ordered_of_bucket(kBuckets - 1, f, top, most));
+        cut = key < cut ? key : cut;
+    }
+    auto kept = [&](float z, int v) { return rank_key<DT>(z, v) <= cut; };
 
     // ---- what is left of each part
     __syncthreads();

@@ -1,0 +1,69 @@
+"""GPU parity of drawing tokens where logits are many times the temperature, so that a place on the line of buckets is far from 0.  Tolerances as derived in
+test_tokens_gpu.py; weights are of a few values here, whose running masses do not meet a share of the whole."""
+import numpy as np
+import pytest
+import torch
+
+import test_tokens_gpu as base
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def qb():
+    assert torch.cuda.is_available(), "these tests need the MI355X"
+    from paper_2603_01399_amd import binding
+    return binding
+
+
+NEAR = [dict(top_k=3), dict(top_k=100), dict(top_k=2500), dict(top_p=0.5), dict(top_p=0.9), dict(top_p=0.999), dict(min_p=0.1654), dict(min_p=1.95e-5), dict(top_k=100, top_p=0.8),
+        dict(top_k=4000, top_p=0.7, min_p=1e-3), dict()]
+
+
+def check(qb, z, filters, us=(0.0, 0.37, 0.8, 0.999, 1 - 2.0 ** -24)):
+    """Every row with every one of the filters, at every one of the numbers."""
+    T, V = z.shape
+    rows = [f for _ in range(T) for f in filters for _ in us]
+    many = z.repeat_interleave(len(filters) * len(us), 0)
+    u = np.array(list(us) * (T * len(filters)), np.float32)
+    token, p = qb.sample_tokens(many, base.dev(u, torch.float32), **base.params(rows))
+    token, p, host = token.tolist(), p.tolist(), base.seen(z)
+    for i, f in enumerate(rows):
+        base.check_draw(host[i // (len(filters) * len(us))], u[i], token[i], p[i], V, **base.as_seen(f))
+
+
+def test_ten_equal_ones_a_bucket_below_the_largest(qb):
+    """exp(-1/4) each: of 1 + 7.788 the first six hold a half."""
+    base.say("ten equal ones")
+    z = torch.full((1, 3000), 2.0 ** 21 - 40, device="cuda")
+    z[0, 700], z[0, 1000:2000:100] = 2.0 ** 21 + 0.25, 2.0 ** 21
+    check(qb, z, [dict(top_p=0.5), dict(top_k=4), dict(min_p=0.5), dict(top_k=6, top_p=0.6)])
+    u = torch.ones(1, device="cuda")
+    assert int(qb.sample_tokens(z, u, top_p=u * 0.5)[0]) == 1400 and int(qb.sample_tokens(z, u, top_k=u.int() * 4)[0]) == 1200
+
+
+@pytest.mark.parametrize("most,t", [(2097152.25, 1.0), (200.000015, 1e-4), (20.0000019, 1e-5), (413.573486, 3.93e-5), (30.7390366, 8.96e-7), (3.9999998, 1.4901161e-8), (1e9, 100.0), (-2097152.25, 1.0),
+                                    (-20.0000019, 1e-5), (-3.9999998, 1.4901161e-8), (1e30, 1e22), (7.5, 1.0)])
+def test_logits_of_many_temperatures(qb, most, t):
+    """Logits a few temperatures below the largest, on what grid fp32 has there: within a part, in several, in a row that is not aligned."""
+    base.say("many temperatures", most, t)
+    r = np.random.Generator(np.random.Philox(3))
+    for V, off in ((1000, 0), (20011, 1)):
+        z = torch.full((3, V + off), float(most), device="cuda")[:, off:]
+        away = np.stack([r.exponential(2.0, V), r.exponential(6.0, V), r.random(V) * 40])
+        away[0, V // 2:] += 3                                     # (a part's largest is not the row's)
+        z.copy_(base.dev(np.minimum(np.float64(np.float32(most)) - away * t, most), torch.float32))
+        check(qb, z, [f | dict(temperature=t) for f in NEAR], us=(0.0, 0.37, 0.999))
+
+
+def test_min_p_alone_far_from_zero(qb):
+    """Logits, temperatures and bounds of every size: what min_p keeps is counted, in whatever bucket it lies."""
+    base.say("min_p far from zero")
+    r = np.random.Generator(np.random.Philox(4))
+    for _ in range(60):
+        most, t, m = np.float32(16 * 64 ** r.random()), float(np.float32(10 ** r.uniform(-8, -2))), float(np.float32(10 ** r.uniform(-6, -0.3)))
+        V = 2000
+        steps = np.floor(r.exponential(2.0 + 8 * r.random(), V))
+        step = max(float(np.spacing(most)), t / 3)
+        z = base.dev(np.float64(most) - steps * step, torch.float32)[None]
+        check(qb, z, [dict(min_p=m, temperature=t)], us=(0.0, 0.5, 0.9, 0.999))
