@@ -208,7 +208,7 @@ __global__ __launch_bounds__(kPartThreads) void token_parts_kernel(const TokenPa
     __syncthreads();
 #pragma unroll
     for (int i = 0; i < kPartWaves; ++i) largest = fmaxf(largest, wave_largest[i]);
-    if (tid == 0) p.part_max[(long long)r * p.nb + b] = largest;
+    if (tid == 0) p.part_max[(long long)r * p.nb + b] = largest + 0.0f;      // (as it is ordered: one zero)
     if (mode == DRAW_FIRST) return;
     const double top = bucket_line(largest, f.scale);
     const long long to = ((long long)r * p.nb + b) * kBuckets;

@@ -67,3 +67,28 @@ def test_min_p_alone_far_from_zero(qb):
         step = max(float(np.spacing(most)), t / 3)
         z = base.dev(np.float64(most) - steps * step, torch.float32)[None]
         check(qb, z, [dict(min_p=m, temperature=t)], us=(0.0, 0.5, 0.9, 0.999))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_zeros_that_are_the_largest(qb, dtype):
+    """Of either sign, alone or with others below them: both count as the same number, also where all have the sign."""
+    base.say("zeros", dtype)
+    r = np.random.Generator(np.random.Philox(5))
+    for V in (100, 5000, 20011):
+        z = torch.full((6, V), -0.0, dtype=dtype, device="cuda")
+        z[1] = 0.0
+        z[2, 1::2] = 0.0
+        z[3] = base.dev(-np.abs(r.standard_normal(V)) * 0.05, torch.float32).to(dtype)
+        z[3, r.permutation(V)[:40]] = -0.0
+        z[4] = base.dev(-np.abs(r.standard_normal(V)) - 0.2, torch.float32).to(dtype)
+        z[4, r.permutation(V)[:40]] = -0.0
+        z[5, V // 2:] = -1.0
+        assert bool((torch.signbit(z[0])).all()) and bool(torch.signbit(z[3]).all())
+        us = (0.0, 0.4, 0.999)
+        check(qb, z, [dict(top_k=5), dict(top_k=30), dict(top_k=V // 2), dict(min_p=1.0), dict(min_p=0.97), dict(top_k=7, top_p=0.5), dict(top_k=3000, top_p=0.3), dict(temperature=0.0), dict()], us)
+        # (a half of V equal ones is the first V / 2 of them, or one more)
+        u = torch.full((6,), 1.0, device="cuda")
+        token, _ = qb.sample_tokens(z, u, top_k=u.int() * 5)
+        assert token.tolist()[:3] == [4, 4, 4]
+        token, _ = qb.sample_tokens(z[:3].contiguous(), u[:3], top_p=u[:3] * 0.5)
+        assert token.tolist() == [-(-V // 2) - 1] * 3
