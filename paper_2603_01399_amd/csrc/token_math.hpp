@@ -17,7 +17,8 @@ typedef unsigned long long u64;
 
 constexpr int kBuckets = 512, kBucketsPerUnit = 16;          // of (largest - z) / temperature: the first 32 units; what lies behind weighs less than 2^-46
 constexpr int kPartBits = 48;                                // a part of the vocabulary has at most 2^13 tokens
-constexpr int kListBits = 42;                                // a whole vocabulary has at most 2^20
+constexpr int kListBits = 43;                                // a whole vocabulary has at most 2^20
+constexpr int kFewBits = 51;                                 // of at most 2^11 tokens
 constexpr int kIndexBits = 20;
 constexpr float kLargest = 3.4028234663852886e38f;
 

@@ -615,17 +615,19 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
         }
         if (step == OF_BORDER) break;
         border = to;
-        // Among the keys lo .. hi, `inside` of them, the first `want` (tokens, or units of mass: those ahead of which less lies).  Masses are relative to the largest
-        // logit there may be among them.
+        // Among the keys lo .. hi, `inside` of them, the first `want` (tokens, or units of mass: those ahead of which less lies).  Masses are multiples of 2^-43 of the largest
+        // logit's weight that there may be in the one bucket that is gathered: off by 2^-43.9 of the bucket's at most, however little that is of the row's.  Where all that is
+        // left is gathered, up to kFew tokens of many buckets, they are multiples of 2^-51 of the row's largest.
         const bool by_mass = step == BY_MASS, one = !by_mass || from;            // (one bucket's)
         const uint32_t largest = one && to ? least_ordered_of_bucket(to - 1, f, top, most) - 1 : ordered_bits(most);
-        const float ref = value_of_ordered(largest);
-        const double to_row = weight_of(ref, most, f.rate) * (1.0 / (double)(1ull << kListBits));
+        const int bits = mode == DRAW_FEW ? kFewBits : kListBits;
+        const float ref = mode == DRAW_FEW ? most : value_of_ordered(largest);
+        const double to_row = of_lane(weight_of(ref, most, f.rate) * (mode == DRAW_FEW ? 1.0 / (1ull << kFewBits) : 1.0 / (1ull << kListBits)), 0);
         u64 lo = first_key<DT>(largest), hi = last_key<DT>(least), before = 0;
         hi = cut < hi ? cut : hi;
         int inside = from || by_mass ? n_listed : (int)(through_count[to] - (to ? through_count[to - 1] : 0u));
         const double units = by_mass ? __builtin_ceil(limit / to_row) : (double)need;
-        const u64 want = units < 1.0 ? 1ull : units < 0x1p62 ? (u64)units : 1ull << 62;
+        const u64 want = units < 1.0 ? 1ull : units < 0x1p63 ? (u64)units : 1ull << 63;
         if (by_mass || need < (unsigned int)inside) {
 #pragma unroll 1
             while (inside > kPairs && lo < hi) {                 // a digit of ten bits at a time
@@ -638,7 +640,7 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
                     if (key < lo || key > hi) return;
                     const int at = (int)((key - lo) >> digit);
                     atomicAdd(&bin_count[at], 1u);
-                    if (by_mass) atomicAdd(&bin_mass[at], weight_units(key_value<DT>(key), ref, f.rate, kListBits));
+                    if (by_mass) atomicAdd(&bin_mass[at], weight_units(key_value<DT>(key), ref, f.rate, bits));
                 });
                 __syncthreads();
                 const unsigned int count = bin_count[tid];
@@ -664,7 +666,7 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
                 });
                 __syncthreads();
                 const int n = min(n_edge, kPairs), mine = tid / 4, part = tid % 4;
-                if (tid < n) bin_mass[tid] = by_mass ? weight_units(key_value<DT>(edge[tid]), ref, f.rate, kListBits) : 1;
+                if (tid < n) bin_mass[tid] = by_mass ? weight_units(key_value<DT>(edge[tid]), ref, f.rate, bits) : 1;
                 else if (tid < n + 16) edge[tid] = ALL;          // (ahead of none)
                 __syncthreads();
                 if (4 * n > (tid & ~63)) {                       // (whole waves)
@@ -690,9 +692,9 @@ __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenPar
         if (!by_mass && f.p < 1.0f) {                            // the mass up to the cut
             u64 mass = 0;
             each([&](u64 key) {
-                if (key <= cut) mass += weight_units(key_value<DT>(key), most, f.rate, kListBits);
+                if (key <= cut) mass += weight_units(key_value<DT>(key), ref, f.rate, bits);
             });
-            total = (double)talk.sum(mass) * (1.0 / (double)(1ull << kListBits)) + (from ? through_mass[from - 1] : 0.0);
+            total = (double)talk.sum(mass) * to_row + (from ? through_mass[from - 1] : 0.0);
         }
     }
     if (mode == DRAW_MANY && border == kBuckets) {               // (what lies beyond the buckets is not counted)

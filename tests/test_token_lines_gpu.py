@@ -92,3 +92,23 @@ def test_zeros_that_are_the_largest(qb, dtype):
         assert token.tolist()[:3] == [4, 4, 4]
         token, _ = qb.sample_tokens(z[:3].contiguous(), u[:3], top_p=u[:3] * 0.5)
         assert token.tolist() == [-(-V // 2) - 1] * 3
+
+
+# One token of weight 1, n equal ones of about 2^-30, whose units are no whole numbers; the last one left (a number of 1 draws it) says where top-p cuts.  Running masses and the
+# share of the whole are off by at most V 2^-45 + 2^-44 of the whole each (test_tokens_gpu.py), which is less than the weight of a token, or of two.
+@pytest.mark.parametrize("V,k,steps", [(1900, 1899, 14), (1900, 1899, 25), (60000, 50000, 300), (60000, 50000, 9), (2049, 2048, 20)])
+def test_where_top_p_cuts_among_small_equal_weights(qb, V, k, steps):
+    base.say("small equal weights", V, k, steps)
+    T = 400
+    small = -20.7944 - np.arange(T) * 2.0 ** -17
+    z = torch.full((T, V), float("-inf"), device="cuda")
+    z[:, 1:] = base.dev(small, torch.float32)[:, None]
+    z[:, 0] = 0.0
+    p = 1 - steps * 2.0 ** -24
+    ones = torch.ones(T, device="cuda")
+    token, _ = qb.sample_tokens(z, ones, top_k=ones.int() * k, top_p=base.dev([p] * T, torch.float32))
+    w = np.exp(base.seen(z[:, 1]))
+    whole, n = 1 + (k - 1) * w, token.cpu().numpy()               # (tokens behind the first one that are left)
+    tol = base.tol_of(V) * whole
+    assert (1 + (n - 1) * w < p * whole + 2 * tol).all() and (1 + n * w >= p * whole - 2 * tol).all()
+    assert (n > 0).all() and (n < k - 1).all()
