@@ -959,7 +959,8 @@ def _window_arg(window, sinks):
 def paged_attention(q: torch.Tensor, n_q_heads: int, cache: PagedKvCache, layer: int, row_start: torch.Tensor, max_new: int,
                     workspace: torch.Tensor = None, out: torch.Tensor = None, *, window: int = None, sinks: int = 0) -> torch.Tensor:
     """Attention of the new tokens of a step, at most max_new (1 .. 32) a sequence, over their sequences' pages.
-    window: a row sees its own and the window - 1 positions ahead of it, and the first `sinks` of the sequence (None: all ahead of it)."""
+    window: a row sees its own and the window - 1 positions ahead of it, and the first `sinks` of the sequence (None: all ahead of it).  For windows that most
+    sequences fill: where one sees far more positions than the others, and the window is long, the call takes as long as that one takes alone."""
     if window is None:
         if sinks:
             raise ValueError("sinks belong to a window")

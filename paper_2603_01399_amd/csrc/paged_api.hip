@@ -261,7 +261,14 @@ bool hides(const Window *w, const CacheArgs &a) {
 // 32 / 8 heads, windows of 128, 512 and 2048 positions: 12.6, 27.8 and 84.9 us, shared 20.8, 35.5 and 97.0; of 4 sequences, eight waves each, 7.1, 8.6 and 24.8 (with four
 // 7.2, 9.6 and 25.4), and 12.6, 12.9 and 15.3, in 8-bit pages of 1024 10.3 and 13.1, of 2048 14.7 and 14.1 (which is why there is a limit); in bf16 of
 // 1024 10.6 and 12.9 for 2 sequences, 16.8 and 16.0 for 8; 8 tokens of 16 sequences, 64 / 8
-// heads, 14.3, 20.6 and 58, and 22.8, 28.7 and 39.7.  A single sequence's join is short: a limit of its own.
+// heads, 14.3, 20.6 and 58, and 22.8, 28.7 and 39.7.
+// The limits are what the join and its launch cost, 4 to 8 us, in blocks of a worker: an e4m3 block is half a bf16 one, a workgroup that has a compute unit to itself reads
+// faster than two that share one and faster still where few are under way, a tile of 64 or 128 rows computes longer on a block, and one sequence's join is short.  Over 2112 forms
+// (1 to 128 sequences of 1 to 32 tokens, windows of 128 to 4096 that are full, 8 / 8, 12 / 4, 16 / 2, 32 / 8, 40 / 8 and 64 / 8 heads, both types) both ways take the same at 34 to 50 blocks beyond an even
+// share (bf16, alone; limits 24 and 34), 50 to 70 (e4m3, alone; 50), 16 to 30 (bf16, two a unit; 28), 34 to 50 (e4m3, two a unit; 28), 24 to 34 (tiles; 16) and, of one sequence, 24 to 28 (24), 8 to 16 (14; tiles
+// 8); the rule takes the slower way by more than 10 % in 8 % of the forms, by half at most.
+// It goes by the window alone: the host does not know the lengths.  Where sequences fill the slots and one of them sees far more than the others, it is one worker's: one token of 64
+// sequences, one of 32000 positions and 63 of 500, a window of 32768, 543 us, shared 54; 65 even ones of 2048, which are a round more than 64, 98 and 93.
 bool stays_whole(int64_t tiles, int64_t longest, int64_t workers, int64_t more) { return tiles >= workers || longest * (workers - tiles) <= more * workers; }
 
 int step_attention(const CacheArgs &a, const AttentionArgs &t, int64_t max_new, const Window *window) {

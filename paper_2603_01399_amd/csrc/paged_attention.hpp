@@ -39,7 +39,7 @@ constexpr int kPagedWaves = 4, kLoneWaves = 8;           // of a workgroup; wher
 constexpr int kMaxWorkers = 512;             // of a kv head
 
 // WINDOW: a sequence's blocks are those that its rows see some position of; those between the first tokens and the window have no place in
-// the line, whatever the context's length.  64 sequences of one token over up to 16000 positions in 8-bit pages, 32 / 8 heads, windows of 4096 (518 MB): 81.5 us,
+// the line, whatever the context's length.  64 sequences of one token over up to 16000 positions in 8-bit pages, 64 / 8 heads, windows of 4096 (518 MB): 81.5 us,
 // 6.4 TB/s.
 template <int KV, int NQT, bool WINDOW, int NW = kPagedWaves>
 __global__ __launch_bounds__(NW * 64, NQT == 1 ? 2 : 1) void paged_attention_kernel(const PagedAttnParams p) {

@@ -154,8 +154,8 @@ constexpr int kPromptStepBytes = kPromptStep / kKvBlock * 2 * kKvBlockBytes;   /
 // widened by each wave that reads them, 2 x 8 tokens of 64 / 8 heads over 100003 positions take 75.7 us, and 76.6 so.)
 // WINDOW: a tile's steps are those that its rows see some position of, the ones that every row sees whole first (the order is free), so that the two
 // loops over them are the same.  (Steps of any two blocks of 32, which leave no half of a step unused at the first tokens and the window's ends, are 5 % fewer and
-// took longer: 9 prompts of up to 1531 rows, a window of 333 and 4 first tokens 93.5 us, and 88.1; a draft's shared tiles 33.8 and 31.3.)  8192 rows of 64 / 8 heads,
-// windows of 1024: 322 us, 0.8 PFLOP/s of what the rows see; of the 17 or 18 steps of a tile's 16 positions two or three are seen in part.
+// took 6 to 8 % longer, for prompts as for a draft's shared tiles.)  9 prompts of up to 1531 rows of 32 / 8 heads, a window of 333 and 4 first tokens: 92 us, 97 in 8-bit pages.  8192 rows of 64 / 8 heads,
+// windows of 1024: 314 us, 0.82 PFLOP/s of what the rows see; of the 17 or 18 steps of a tile's 16 positions two or three are seen in part.
 template <int KV, bool FLAT, int PW, bool WINDOW>
 __global__ __launch_bounds__(kPromptWaves * 64, 2) void prompt_attention_kernel(const PromptParams p) {
     constexpr int NW = kPromptWaves, RW = NW / PW, ROWS = 32 * RW, NB = 2 / PW;  // row groups; blocks of a step for a wave

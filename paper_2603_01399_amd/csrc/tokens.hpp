@@ -165,8 +165,8 @@ __device__ __forceinline__ int draw_mode(const Filters &f) {
 
 // Grid (parts, rows).  A part's 16 tokens a thread stay in registers between its largest logit and the buckets.  What the row asks for is counted and nothing
 // else: nothing (FIRST), the whole part's mass (ALL), counts (FEW), masses, and counts where there is a top-k (MANY).  Bound by instructions: a compute unit does one for 64 tokens a
-// cycle, 0.25 us for each that is done for every token of 64 rows of 152 K; vector instructions fill 80 to 88 % of the cycles.  64 rows more of fp32 logits take 7.5 us
-// (FEW: 39 MB, 5.2 TB/s), 11 (ALL) and 15.5 (MANY).  Tried: two, four or eight copies of the buckets in LDS for the lanes of a wave, fewer workgroups a compute unit,
+// cycle, 0.25 us for each that is done for every token of 64 rows of 152 K; vector instructions fill 79 to 88 % of the cycles.  64 rows more of fp32 logits take 7.0 us
+// (FEW: 39 MB, 5.6 TB/s), 10.8 (ALL) and 13.9 (MANY).  Tried: two, four or eight copies of the buckets in LDS for the lanes of a wave, fewer workgroups a compute unit,
 // so that some load while others compute: the same; 256 threads of 32 tokens 2 to 4 us more, 1024 of 8 up to 4 more where there are many rows.
 template <int DT>
 __global__ __launch_bounds__(kPartThreads) void token_parts_kernel(const TokenParams p) {
@@ -297,7 +297,8 @@ __device__ __forceinline__ uint32_t least_ordered_of_bucket(int j, const Filters
 // 152 K: what chunks hold is compared with the ends of the gathered buckets, two instructions, and only what lies between is worked on.  One row of 152 K tokens takes
 // 7 us without filters (where the first is all that is left a call takes 6.6), 13 to 16 with top-k, and 34 with a top-p whose cut lies in a bucket of thousands, where every chunk is read: buckets 7, chunks 10, their keys and the
 // digits 8, the rest 9.  Tried: two to eight workgroups that read such a row's chunks together and the last of which goes on: what each has to make visible to the others
-// costs more than it reads (64 rows with top-p 52 us, 61 by two, 69 by four).
+// costs more than it reads (64 rows with top-p 52 us, 61 by two, 69 by four).  A thread has 128 vector registers: of bf16 logits three are spilled, of fp32 ones one, and 41 to 43 scalar
+// ones lie in lanes of vector ones.
 template <int DT>
 __global__ __launch_bounds__(kDrawThreads) void token_draw_kernel(const TokenParams p) {
     constexpr int N = lane_tokens<DT>, CHUNKS = part_chunks<DT>;

@@ -112,3 +112,22 @@ def test_where_top_p_cuts_among_small_equal_weights(qb, V, k, steps):
     tol = base.tol_of(V) * whole
     assert (1 + (n - 1) * w < p * whole + 2 * tol).all() and (1 + n * w >= p * whole - 2 * tol).all()
     assert (n > 0).all() and (n < k - 1).all()
+
+
+@pytest.mark.parametrize("most,t", [(2097152.25, 1.0), (20.0000019, 1e-5), (-0.0, 0.3)])
+def test_drafts_far_from_zero(qb, most, t):
+    """Candidates that are kept, cut, or nobody's, of rows as above."""
+    base.say("drafts far from zero", most, t)
+    r = np.random.Generator(np.random.Philox(6))
+    V, news = 9001, [4, 1, 7, 3, 5, 2, 6]
+    starts = np.concatenate([[0], np.cumsum(news)])
+    T = int(starts[-1])
+    away = r.exponential(4.0, (T, V)) * t
+    away[:, 77] = 0.0
+    z = base.dev(np.float64(np.float32(most)) - away, torch.float32)
+    z[:, 77] = most
+    seqs = [NEAR[i] | dict(temperature=t) for i in (1, 3, 4, 6, 8, 9, 10)]
+    drafts = np.where(r.random(T) < 0.6, 77, np.argsort(away, 1)[:, 3])
+    ua, us = r.random(T).astype(np.float32) * np.float32(1e-3), r.random(T).astype(np.float32)
+    some = base.check_verify(qb, z, starts, drafts, ua, us, [base.as_seen(f) for f in seqs], base.params(seqs))
+    assert max(some) > 0
